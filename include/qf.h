@@ -50,7 +50,8 @@ typedef enum {
   QF_ERR_TOO_LARGE = 10 /* the problem needs more scratch than the built-in buffer of qf_fq_linear_fwd_noalloc */
 } qf_status_t;
 
-typedef enum { QF_DT_BF16 = 0, QF_DT_F32 = 1 } qf_dtype_t;
+/* The integer types are for expert ids only (qf_moe_sort, qf_fq_grouped_matvec). */
+typedef enum { QF_DT_BF16 = 0, QF_DT_F32 = 1, QF_DT_I32 = 2, QF_DT_I64 = 3 } qf_dtype_t;
 
 typedef enum {
   QF_OP_QDQ = 0,
@@ -274,6 +275,95 @@ qf_status_t qf_unpack(qf_layout_t layout, qf_format_t fmt, const void* packed, i
 qf_status_t qf_fp4_matmul_native(qf_format_t fmt, const void* a_codes, const void* a_scales, const float* a_tscale,
                                  const void* b_codes, const void* b_scales, const float* b_tscale, int64_t M, int64_t N,
                                  int64_t K, float* Y, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- mixture-of-experts routing: tokens into expert order and back ---------------------------------------------
+ *
+ * What stands around the grouped linear layer (Section 3.3 "Mixture-of-experts adaptation"): a router gives every one
+ * of T tokens top_k experts and weights; the P = T * top_k (token, expert) pairs become rows of a buffer sorted by
+ * expert, in segments padded to 128 rows, which is what qf_fq_grouped_linear_fwd / _bwd take.
+ *
+ *   forward   qf_moe_sort -> qf_moe_dispatch -> grouped linear calls -> qf_moe_combine
+ *   backward  qf_moe_combine_bwd -> grouped backward calls -> qf_moe_dispatch_bwd
+ *
+ * The routing table of one batch is three device int32 arrays:
+ *   row_of [T, top_k]        row of the sorted buffer that holds pair (t, j), or -1 if the pair is dropped
+ *   group_offsets [G+1]      segment starts (multiples of 128); rows past group_offsets[G] belong to no segment
+ *   counts [G]               real rows of every segment; the rest of the segment is padding
+ * rows_padded is the number of rows of the sorted buffer, a multiple of 128 chosen by the caller. With
+ * rows_padded >= qf_moe_rows_bound() every routing fits, and nothing has to be read back from the device.
+ * G is at most QF_MOE_MAX_EXPERTS. hidden is a multiple of 8. The tables are device memory, so the host cannot
+ * check them: the kernels treat a row_of entry outside [0, rows_padded) as a dropped pair and force offsets and
+ * counts into the buffer, so that a table that breaks the contract gives meaningless results, never an access out of
+ * range. Unlike elsewhere in this interface, infinities and NaN in data pass through as IEEE arithmetic has them; rows
+ * that no pair owns (padding) are never read. */
+#define QF_MOE_MAX_EXPERTS 1024
+
+/* Rows that hold any routing of tokens * top_k pairs to G experts: a multiple of 128; -1 for arguments that
+ * qf_moe_sort would refuse. */
+int64_t qf_moe_rows_bound(int64_t tokens, int top_k, int G);
+
+/* Builds the routing table. Pair p = t * top_k + j goes to expert e = expert_ids[p]; rows of one expert are in the order
+ * of p (a stable sort): row_of[p] = group_offsets[e] + #{q < p : expert_ids[q] = e}.
+ *   expert_ids   device [tokens, top_k], ids_dtype QF_DT_I32 or QF_DT_I64. An id outside [0, G) drops the pair
+ *                (row_of = -1). The same expert may occur twice for a token.
+ * A pair whose row would be at or past rows_padded is dropped as well, and group_offsets and counts are cut at rows_padded. */
+qf_status_t qf_moe_sort(const void* expert_ids, qf_dtype_t ids_dtype, int64_t tokens, int top_k, int G, int64_t rows_padded,
+                        int32_t* row_of, int32_t* group_offsets, int32_t* counts, void* stream);
+
+/* xs[row_of[t,j], :] = x[t, :]; every other row of xs [rows_padded, hidden] is set to zero. x, xs BF16. */
+qf_status_t qf_moe_dispatch(const void* x, int64_t tokens, int top_k, int64_t hidden, const int32_t* row_of,
+                            const int32_t* group_offsets, const int32_t* counts, int G, int64_t rows_padded, void* xs, void* stream);
+
+/* Gradient of qf_moe_dispatch: dx[t, :] = sum over j of dxs[row_of[t,j], :], added in FP32 in the order of j and rounded
+ * once. dxs BF16 or FP32 [rows_padded, hidden]; dx BF16 or FP32 [tokens, hidden]. */
+qf_status_t qf_moe_dispatch_bwd(const void* dxs, qf_dtype_t dxs_dtype, int64_t tokens, int top_k, int64_t hidden,
+                                const int32_t* row_of, int64_t rows_padded, void* dx, qf_dtype_t dx_dtype, void* stream);
+
+/* out[t, :] = sum over j of weights[t,j] * ys[row_of[t,j], :] (FP32 fused multiply-adds in the order of j, rounded once;
+ * dropped pairs are left out). ys BF16 or FP32 [rows_padded, hidden], weights FP32 [tokens, top_k], out BF16 or FP32.
+ * row_of may be NULL: pair (t, j) is then row t * top_k + j of ys (what qf_fq_grouped_matvec writes), and rows_padded may be
+ * any number >= tokens * top_k. */
+qf_status_t qf_moe_combine(const void* ys, qf_dtype_t ys_dtype, const float* weights, int64_t tokens, int top_k, int64_t hidden,
+                           const int32_t* row_of, int64_t rows_padded, void* out, qf_dtype_t out_dtype, void* stream);
+
+/* Gradients of qf_moe_combine with respect to ys and to the weights:
+ *     dys[row_of[t,j], :] = weights[t,j] * dout[t, :]    (one FP32 product, rounded once to BF16: the type that
+ *                                                         qf_fq_grouped_linear_bwd takes as dY)
+ *     dweights[t,j] = sum over h of dout[t,h] * ys[row_of[t,j], h]    (FP32, in an order that depends on the shape alone)
+ * Rows of dys [rows_padded, hidden] that no pair owns are set to zero, dweights of dropped pairs too.
+ * dout BF16 or FP32 [tokens, hidden]; ys as in the forward; dys BF16; dweights FP32 [tokens, top_k]. dweights may be
+ * NULL (weights that are not trained): ys is then not read and may be NULL. */
+qf_status_t qf_moe_combine_bwd(const void* dout, qf_dtype_t dout_dtype, const void* ys, qf_dtype_t ys_dtype, const float* weights,
+                               int64_t tokens, int top_k, int64_t hidden, const int32_t* row_of, const int32_t* group_offsets,
+                               const int32_t* counts, int G, int64_t rows_padded, void* dys, float* dweights, void* stream);
+
+/* ---- products with a few tokens, from the 4-bit codes -------------------------------------------------------------
+ *
+ * Y[M,N] = X[M,K] . W[N,K]^T with W read as the codes and scales that qf_qdq emitted (layouts there): what a rollout or
+ * serving step does with the quantized weights (Section 3.4). FP32 accumulation. The dequantized weights are not rounded to
+ * BF16: for MXFP4 they are exact in BF16 anyway (Eq. mxfp4-dequant), for NVFP4 the tensor scale multiplies the finished sum
+ * (like qf_fp4_matmul_native), for Q4_K the sums are sum over sub-blocks of (d*s6) * sum(C*x) - (dmin*m6) * sum(x).
+ * The result therefore differs from qf_fq_linear_fwd(X, W, fmt, QF_FMT_NONE) by FP32 summation order and, for NVFP4 and
+ * Q4_K, by that rounding. For quantized activations pass X_hat (qf_qdq). Results do not depend on what else runs, and the
+ * rows of X do not influence one another.
+ *   X       BF16 [M, K], K a multiple of the format's block; Y BF16 or FP32 [M, N], any N
+ *   tensor_scale  NVFP4: device float*; otherwise ignored
+ * The weights are read once per QF_MATVEC_TOKENS rows of X: meant for M up to about that; a larger M is right but slower
+ * than qf_fq_linear_fwd on the dequantized weight. */
+#define QF_MATVEC_TOKENS 32
+qf_status_t qf_fq_matvec(qf_format_t fmt, const void* X, int64_t M, const void* codes, const void* scales, const float* tensor_scale,
+                         int64_t N, int64_t K, void* Y, qf_dtype_t y_dtype, void* stream);
+
+/* The same per expert, without sorting: Y[p, :] = X[p / (pairs / x_rows), :] . W[expert_ids[p]]^T for p in [0, pairs).
+ * W [G,N,K] as codes [G, N, K/2] with scales [G, N, ...] and, for NVFP4, tensor_scales [G].
+ *   x_rows       rows of X: a divisor of pairs. pairs / top_k (every token's row serves its top_k pairs: gate and up
+ *                projections) or pairs (a row per pair: down projection)
+ *   expert_ids   device [pairs], ids_dtype QF_DT_I32 or QF_DT_I64; an id outside [0, G) gives a row of zeros
+ * The codes of an expert are read once per QF_MATVEC_TOKENS of its pairs; experts that no pair names are not read. G at most
+ * QF_MOE_MAX_EXPERTS. */
+qf_status_t qf_fq_grouped_matvec(qf_format_t fmt, const void* X, int64_t x_rows, const void* expert_ids, qf_dtype_t ids_dtype,
+                                 int64_t pairs, int G, const void* codes, const void* scales, const float* tensor_scales, int64_t N,
+                                 int64_t K, void* Y, qf_dtype_t y_dtype, void* stream);
 
 /* Allocation-free forward of the quantization-aware linear layer. (The paper has no counterpart:
  * this is a packaging variant of qf_fq_linear_fwd for hosts that cannot hand the library a workspace.)

@@ -9,11 +9,12 @@ from __future__ import annotations
 import ctypes
 from ctypes import c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 from pathlib import Path
+from typing import NamedTuple
 
 import torch
 
 FMT_NONE, FMT_NVFP4, FMT_MXFP4, FMT_Q4_K = 0, 1, 2, 3
-DT_BF16, DT_F32 = 0, 1
+DT_BF16, DT_F32, DT_I32, DT_I64 = 0, 1, 2, 3
 OP_QDQ, OP_LINEAR_FWD, OP_LINEAR_BWD, OP_GROUPED_FWD, OP_GROUPED_BWD, OP_QDQ_BATCHED = 0, 1, 2, 3, 4, 5
 TENSOR_SCALE_GIVEN = 0x1
 W_TSCALE_GIVEN, A_TSCALE_GIVEN, ACCUMULATE_DW, FUSED_QDQ, AMAX_RUNNING = 0x1, 0x2, 0x4, 0x8, 0x10
@@ -30,10 +31,12 @@ EXPORTS = [
     "qf_status_string", "qf_version", "qf_workspace_bytes", "qf_read_status", "qf_qdq", "qf_dequant", "qf_amax",
     "qf_fq_linear_fwd", "qf_fq_linear_bwd", "qf_fq_grouped_linear_fwd", "qf_fq_grouped_linear_bwd", "qf_selftest_cvt",
     "qf_selftest_div", "qf_fq_linear_fwd_noalloc", "qf_selftest_mxfp4_bf16", "qf_selftest_timeout", "qf_pack_bytes", "qf_pack", "qf_unpack", "qf_nvfp4_tensor_scale", "qf_qdq_lora",
-    "qf_fp4_matmul_native", "qf_qdq_batched",
+    "qf_fp4_matmul_native", "qf_qdq_batched", "qf_moe_rows_bound", "qf_moe_sort", "qf_moe_dispatch", "qf_moe_dispatch_bwd",
+    "qf_moe_combine", "qf_moe_combine_bwd", "qf_fq_matvec", "qf_fq_grouped_matvec",
 ]
 NOALLOC_SCRATCH_BYTES = 32 << 20
 LAYOUT_GGUF_Q4_K, LAYOUT_FP4_SWIZZLED_SCALES = 1, 2
+MOE_MAX_EXPERTS, MATVEC_TOKENS = 1024, 32
 
 
 class QfError(RuntimeError):
@@ -108,6 +111,24 @@ def lib() -> ctypes.CDLL:
         L.qf_selftest_mxfp4_bf16.argtypes = [c_void_p, c_void_p]
         L.qf_selftest_div.restype = c_int
         L.qf_selftest_div.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p]
+        L.qf_moe_rows_bound.restype = c_int64
+        L.qf_moe_rows_bound.argtypes = [c_int64, c_int, c_int]
+        L.qf_moe_sort.restype = c_int
+        L.qf_moe_sort.argtypes = [c_void_p, c_int, c_int64, c_int, c_int, c_int64, c_void_p, c_void_p, c_void_p, c_void_p]
+        L.qf_moe_dispatch.restype = c_int
+        L.qf_moe_dispatch.argtypes = [c_void_p, c_int64, c_int, c_int64, c_void_p, c_void_p, c_void_p, c_int, c_int64, c_void_p, c_void_p]
+        L.qf_moe_dispatch_bwd.restype = c_int
+        L.qf_moe_dispatch_bwd.argtypes = [c_void_p, c_int, c_int64, c_int, c_int64, c_void_p, c_int64, c_void_p, c_int, c_void_p]
+        L.qf_moe_combine.restype = c_int
+        L.qf_moe_combine.argtypes = [c_void_p, c_int, c_void_p, c_int64, c_int, c_int64, c_void_p, c_int64, c_void_p, c_int, c_void_p]
+        L.qf_moe_combine_bwd.restype = c_int
+        L.qf_moe_combine_bwd.argtypes = [c_void_p, c_int, c_void_p, c_int, c_void_p, c_int64, c_int, c_int64, c_void_p, c_void_p,
+                                         c_void_p, c_int, c_int64, c_void_p, c_void_p, c_void_p]
+        L.qf_fq_matvec.restype = c_int
+        L.qf_fq_matvec.argtypes = [c_int, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_int, c_void_p]
+        L.qf_fq_grouped_matvec.restype = c_int
+        L.qf_fq_grouped_matvec.argtypes = [c_int, c_void_p, c_int64, c_void_p, c_int, c_int64, c_int, c_void_p, c_void_p, c_void_p,
+                                           c_int64, c_int64, c_void_p, c_int, c_void_p]
         _lib = L
     return _lib
 
@@ -401,6 +422,155 @@ def qf_qdq_lora(fmt: int, W: torch.Tensor, B: torch.Tensor, A: torch.Tensor, lor
     _check(lib().qf_qdq_lora(fmt, _ptr(W), _ptr(B), _ptr(A), rank, float(lora_scale), rows, cols, _ptr(out), _ptr(codes),
                              _ptr(scales), _ptr(ts), flags, _ptr(ws), ws.numel(), _stream()), "qf_qdq_lora")
     return {"out": out, "codes": codes, "scales": scales, "tensor_scale": ts}
+
+
+class MoePlan(NamedTuple):
+    """The routing table of one batch (see qf_moe_sort in qf.h); the tensors are int32 on the GPU."""
+    row_of: torch.Tensor           # [tokens, top_k]: row of the sorted buffer, -1 for a dropped pair
+    group_offsets: torch.Tensor    # [experts + 1]: segment starts, multiples of 128 (what the grouped linear calls take)
+    counts: torch.Tensor           # [experts]: real rows per segment
+    rows_padded: int               # rows of the sorted buffer
+
+
+_IDS_DTYPE = {torch.int32: DT_I32, torch.int64: DT_I64}
+_DATA_DTYPE = {torch.bfloat16: DT_BF16, torch.float32: DT_F32}
+
+
+def _tensor(t: torch.Tensor, name: str, dtypes, shape) -> int:
+    """Address of a contiguous CUDA tensor of one of ``dtypes`` and the given shape."""
+    if t.dtype not in dtypes or not t.is_cuda or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous CUDA tensor of type {' or '.join(map(str, dtypes))}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return t.data_ptr()
+
+
+_BF16, _F32, _I32, _U8 = (torch.bfloat16,), (torch.float32,), (torch.int32,), (torch.uint8,)
+
+
+def qf_moe_rows_bound(tokens: int, top_k: int, experts: int) -> int:
+    """Rows of a sorted buffer that holds any routing of tokens * top_k pairs: a multiple of 128."""
+    rows = int(lib().qf_moe_rows_bound(tokens, top_k, experts))
+    if rows < 0:
+        raise QfError(2, "qf_moe_rows_bound")
+    return rows
+
+
+def qf_moe_sort(expert_ids: torch.Tensor, experts: int, *, rows_padded: int | None = None) -> MoePlan:
+    """Routing table of ``expert_ids`` [tokens, top_k] (int32 or int64; an id outside [0, experts) drops the pair). The default
+    ``rows_padded`` holds any routing."""
+    tokens, top_k = expert_ids.shape
+    if rows_padded is None:
+        rows_padded = qf_moe_rows_bound(tokens, top_k, experts)
+    ids = _tensor(expert_ids, "expert_ids", _IDS_DTYPE, expert_ids.shape)
+    dev = expert_ids.device
+    row_of = torch.empty((tokens, top_k), dtype=torch.int32, device=dev)
+    offs = torch.empty(experts + 1, dtype=torch.int32, device=dev)
+    counts = torch.empty(experts, dtype=torch.int32, device=dev)
+    _check(lib().qf_moe_sort(ids, _IDS_DTYPE[expert_ids.dtype], tokens, top_k, experts, rows_padded, row_of.data_ptr(),
+                             offs.data_ptr(), counts.data_ptr(), _stream()), "qf_moe_sort")
+    return MoePlan(row_of, offs, counts, rows_padded)
+
+
+def _plan_ptrs(plan: MoePlan):
+    experts = plan.counts.shape[0]
+    return (_tensor(plan.row_of, "plan.row_of", _I32, plan.row_of.shape), _tensor(plan.group_offsets, "plan.group_offsets", _I32, (experts + 1,)),
+            _tensor(plan.counts, "plan.counts", _I32, (experts,)), experts)
+
+
+def qf_moe_dispatch(x: torch.Tensor, plan: MoePlan, *, xs: torch.Tensor | None = None) -> torch.Tensor:
+    """xs [rows_padded, hidden]: row plan.row_of[t, j] holds x[t], every other row is zero."""
+    (tokens, top_k), rows = plan.row_of.shape, plan.rows_padded
+    hidden = x.shape[-1]
+    px = _tensor(x, "x", _BF16, (tokens, hidden))
+    row_of, offs, counts, experts = _plan_ptrs(plan)
+    if xs is None:
+        xs = torch.empty((rows, hidden), dtype=torch.bfloat16, device=x.device)
+    _check(lib().qf_moe_dispatch(px, tokens, top_k, hidden, row_of, offs, counts, experts, rows, _tensor(xs, "xs", _BF16, (rows, hidden)),
+                                 _stream()), "qf_moe_dispatch")
+    return xs
+
+
+def qf_moe_dispatch_bwd(dxs: torch.Tensor, plan: MoePlan, *, dx_dtype=torch.bfloat16, dx: torch.Tensor | None = None) -> torch.Tensor:
+    """dx[t] = sum over j of dxs[plan.row_of[t, j]]."""
+    (tokens, top_k), rows = plan.row_of.shape, plan.rows_padded
+    hidden = dxs.shape[-1]
+    pd = _tensor(dxs, "dxs", _DATA_DTYPE, (rows, hidden))
+    if dx is None:
+        dx = torch.empty((tokens, hidden), dtype=dx_dtype, device=dxs.device)
+    _check(lib().qf_moe_dispatch_bwd(pd, _DATA_DTYPE[dxs.dtype], tokens, top_k, hidden, _tensor(plan.row_of, "plan.row_of", _I32, (tokens, top_k)),
+                                     rows, _tensor(dx, "dx", _DATA_DTYPE, (tokens, hidden)), _DATA_DTYPE[dx.dtype], _stream()), "qf_moe_dispatch_bwd")
+    return dx
+
+
+def qf_moe_combine(ys: torch.Tensor, weights: torch.Tensor, plan: MoePlan | None = None, *, out_dtype=torch.bfloat16,
+                   out: torch.Tensor | None = None) -> torch.Tensor:
+    """out[t] = sum over j of weights[t, j] * ys[plan.row_of[t, j]]; without a plan, ys holds pair (t, j) in row t * top_k + j."""
+    tokens, top_k = weights.shape
+    hidden = ys.shape[-1]
+    rows = tokens * top_k if plan is None else plan.rows_padded
+    py = _tensor(ys, "ys", _DATA_DTYPE, (rows, hidden))
+    if out is None:
+        out = torch.empty((tokens, hidden), dtype=out_dtype, device=ys.device)
+    row_of = None if plan is None else _tensor(plan.row_of, "plan.row_of", _I32, (tokens, top_k))
+    _check(lib().qf_moe_combine(py, _DATA_DTYPE[ys.dtype], _tensor(weights, "weights", _F32, (tokens, top_k)), tokens, top_k, hidden, row_of, rows,
+                                _tensor(out, "out", _DATA_DTYPE, (tokens, hidden)), _DATA_DTYPE[out.dtype], _stream()), "qf_moe_combine")
+    return out
+
+
+def qf_moe_combine_bwd(dout: torch.Tensor, ys: torch.Tensor | None, weights: torch.Tensor, plan: MoePlan, *, want_dweights: bool = True,
+                       dys: torch.Tensor | None = None, dweights: torch.Tensor | None = None):
+    """(dys, dweights): dys[plan.row_of[t, j]] = weights[t, j] * dout[t] in BF16, every other row zero; dweights[t, j] =
+    <dout[t], ys[plan.row_of[t, j]]>, zero for dropped pairs (None if not wanted; ys is then not needed)."""
+    (tokens, top_k), rows = plan.row_of.shape, plan.rows_padded
+    hidden = dout.shape[-1]
+    pd = _tensor(dout, "dout", _DATA_DTYPE, (tokens, hidden))
+    py = _tensor(ys, "ys", _DATA_DTYPE, (rows, hidden)) if want_dweights or ys is not None else None
+    row_of, offs, counts, experts = _plan_ptrs(plan)
+    if dys is None:
+        dys = torch.empty((rows, hidden), dtype=torch.bfloat16, device=dout.device)
+    if want_dweights and dweights is None:
+        dweights = torch.empty((tokens, top_k), dtype=torch.float32, device=dout.device)
+    pw = _tensor(dweights, "dweights", _F32, (tokens, top_k)) if want_dweights else None
+    _check(lib().qf_moe_combine_bwd(pd, _DATA_DTYPE[dout.dtype], py, _DATA_DTYPE[ys.dtype] if ys is not None else DT_BF16,
+                                    _tensor(weights, "weights", _F32, (tokens, top_k)), tokens, top_k, hidden, row_of, offs, counts, experts,
+                                    rows, _tensor(dys, "dys", _BF16, (rows, hidden)), pw, _stream()), "qf_moe_combine_bwd")
+    return dys, dweights if want_dweights else None
+
+
+def qf_fq_matvec(fmt: int, X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, tensor_scale: torch.Tensor | None = None, *,
+                 y_dtype=torch.bfloat16, Y: torch.Tensor | None = None) -> torch.Tensor:
+    """Y [M, N] = X [M, K] . deq(codes, scales)[N, K]^T for a few rows of X, from what qf_qdq emitted for the weight."""
+    M, K = X.shape
+    N = codes.shape[0]
+    if fmt not in BLOCK or K % BLOCK[fmt]:
+        raise QfError(2 if fmt in BLOCK else 4, "qf_fq_matvec")
+    if Y is None:
+        Y = torch.empty((M, N), dtype=y_dtype, device=X.device)
+    ts = _tensor(tensor_scale, "tensor_scale", _F32, (1,)) if fmt == FMT_NVFP4 else None
+    _check(lib().qf_fq_matvec(fmt, _tensor(X, "X", _BF16, (M, K)), M, _tensor(codes, "codes", _U8, (N, K // 2)),
+                              _tensor(scales, "scales", _U8, scales_shape(fmt, N, K)), ts, N, K, _tensor(Y, "Y", _DATA_DTYPE, (M, N)),
+                              _DATA_DTYPE[Y.dtype], _stream()), "qf_fq_matvec")
+    return Y
+
+
+def qf_fq_grouped_matvec(fmt: int, X: torch.Tensor, expert_ids: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor,
+                         tensor_scales: torch.Tensor | None = None, *, y_dtype=torch.bfloat16, Y: torch.Tensor | None = None) -> torch.Tensor:
+    """Y [pairs, N]: row p is X[p // (pairs / rows of X)] . deq(W[expert_ids[p]])^T, from codes [G, N, K/2], scales [G, N, ...] and
+    (NVFP4) tensor_scales [G]. ``expert_ids`` of any shape with ``pairs`` elements; an id outside [0, G) gives zeros."""
+    x_rows, K = X.shape
+    G, N, _ = codes.shape
+    pairs = expert_ids.numel()
+    if fmt not in BLOCK or K % BLOCK[fmt]:
+        raise QfError(2 if fmt in BLOCK else 4, "qf_fq_grouped_matvec")
+    if Y is None:
+        Y = torch.empty((pairs, N), dtype=y_dtype, device=X.device)
+    ts = _tensor(tensor_scales, "tensor_scales", _F32, (G,)) if fmt == FMT_NVFP4 else None
+    _check(lib().qf_fq_grouped_matvec(fmt, _tensor(X, "X", _BF16, (x_rows, K)), x_rows, _tensor(expert_ids, "expert_ids", _IDS_DTYPE, expert_ids.shape),
+                                      _IDS_DTYPE[expert_ids.dtype], pairs, G, _tensor(codes, "codes", _U8, (G, N, K // 2)),
+                                      _tensor(scales, "scales", _U8, (G, *scales_shape(fmt, N, K))), ts, N, K, _tensor(Y, "Y", _DATA_DTYPE, (pairs, N)),
+                                      _DATA_DTYPE[Y.dtype], _stream()), "qf_fq_grouped_matvec")
+    return Y
 
 
 def qf_fp4_matmul_native(fmt: int, a: dict, b: dict, K: int, *, flags: int = 0, ws=None) -> torch.Tensor:

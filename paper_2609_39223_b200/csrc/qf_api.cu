@@ -611,6 +611,150 @@ qf_status_t qf_fq_linear_fwd_noalloc(const void* X, const void* W, void* Y, qf_d
                          QF_NOALLOC_SCRATCH_BYTES, static_cast<cudaStream_t>(stream));
 }
 
+// ---- mixture-of-experts routing, products with a few tokens ---------------------------------------------
+
+// More pairs, or rows of the sorted buffer, than 32-bit row numbers can name are refused with the other shapes.
+static bool moe_shape_ok(int64_t tokens, int top_k, int G) {
+  return tokens >= 0 && top_k >= 1 && G >= 1 && G <= QF_MOE_MAX_EXPERTS && tokens <= (INT32_MAX - 128 * QF_MOE_MAX_EXPERTS) / top_k;
+}
+static bool moe_rows_ok(int64_t rows_padded) { return rows_padded >= 0 && rows_padded % 128 == 0 && rows_padded <= INT32_MAX; }
+
+int64_t qf_moe_rows_bound(int64_t tokens, int top_k, int G) {
+  if (!moe_shape_ok(tokens, top_k, G)) return -1;
+  const int64_t pairs = tokens * top_k;
+  return (pairs + 127 * (pairs < G ? pairs : G)) / 128 * 128;
+}
+
+qf_status_t qf_moe_sort(const void* expert_ids, qf_dtype_t ids_dtype, int64_t tokens, int top_k, int G, int64_t rows_padded,
+                        int32_t* row_of, int32_t* group_offsets, int32_t* counts, void* stream) {
+  if (!moe_shape_ok(tokens, top_k, G) || !moe_rows_ok(rows_padded)) return QF_ERR_SHAPE;
+  if (ids_dtype != QF_DT_I32 && ids_dtype != QF_DT_I64) return QF_ERR_DTYPE;
+  if (!group_offsets || !counts || (tokens > 0 && (!expert_ids || !row_of))) return QF_ERR_NULL;
+  if (!aligned16(expert_ids) || !aligned16(row_of) || !aligned16(group_offsets) || !aligned16(counts)) return QF_ERR_ALIGN;
+  if (qf_status_t s = check_arch()) return s;
+  return cu(launch_moe_sort(expert_ids, ids_dtype == QF_DT_I64, tokens * top_k, G, rows_padded, row_of, group_offsets, counts,
+                            static_cast<cudaStream_t>(stream)));
+}
+
+// The checks that the dispatch and combine calls share. Bytes of either buffer stay far below 2^63: rows and tokens are
+// 32-bit numbers and hidden is bounded here.
+static qf_status_t check_moe(int64_t tokens, int top_k, int64_t hidden, int64_t rows_padded) {
+  if (!moe_shape_ok(tokens, top_k, 1) || rows_padded < 0 || rows_padded > INT32_MAX) return QF_ERR_SHAPE;
+  if (hidden < 0 || hidden % 8 || hidden > (1ll << 28)) return QF_ERR_SHAPE;
+  return QF_OK;
+}
+static MoeTable moe_table(const int32_t* row_of, const int32_t* offs, const int32_t* counts, int G, int64_t rows, int64_t tokens,
+                          int64_t hidden, int top_k) {
+  MoeTable t{};
+  t.row_of = row_of; t.offs = offs; t.counts = counts; t.G = G; t.rows = rows; t.tokens = tokens; t.hidden = hidden; t.top_k = top_k;
+  return t;
+}
+
+qf_status_t qf_moe_dispatch(const void* x, int64_t tokens, int top_k, int64_t hidden, const int32_t* row_of,
+                            const int32_t* group_offsets, const int32_t* counts, int G, int64_t rows_padded, void* xs, void* stream) {
+  if (qf_status_t s = check_moe(tokens, top_k, hidden, rows_padded)) return s;
+  if (G < 1 || G > QF_MOE_MAX_EXPERTS || !moe_rows_ok(rows_padded)) return QF_ERR_SHAPE;
+  const bool rows_any = rows_padded > 0 && hidden > 0, tokens_any = tokens > 0 && hidden > 0;
+  if (!group_offsets || !counts || (rows_any && !xs) || (tokens_any && (!x || !row_of))) return QF_ERR_NULL;
+  if (!aligned16(x) || !aligned16(xs) || !aligned16(row_of) || !aligned16(group_offsets) || !aligned16(counts)) return QF_ERR_ALIGN;
+  if (qf_status_t s = check_arch()) return s;
+  if (!rows_any) return QF_OK;
+  return cu(launch_moe_dispatch(moe_table(row_of, group_offsets, counts, G, rows_padded, tokens, hidden, top_k), x, xs,
+                                static_cast<cudaStream_t>(stream)));
+}
+
+qf_status_t qf_moe_dispatch_bwd(const void* dxs, qf_dtype_t dxs_dtype, int64_t tokens, int top_k, int64_t hidden,
+                                const int32_t* row_of, int64_t rows_padded, void* dx, qf_dtype_t dx_dtype, void* stream) {
+  if (qf_status_t s = check_moe(tokens, top_k, hidden, rows_padded)) return s;
+  if (!moe_rows_ok(rows_padded)) return QF_ERR_SHAPE;
+  if (!valid_dtype(dxs_dtype) || !valid_dtype(dx_dtype)) return QF_ERR_DTYPE;
+  const bool any = tokens > 0 && hidden > 0;
+  if (any && ((rows_padded > 0 && !dxs) || !row_of || !dx)) return QF_ERR_NULL;
+  if (!aligned16(dxs) || !aligned16(row_of) || !aligned16(dx)) return QF_ERR_ALIGN;
+  if (qf_status_t s = check_arch()) return s;
+  if (!any) return QF_OK;
+  return cu(launch_moe_combine(moe_table(row_of, nullptr, nullptr, 0, rows_padded, tokens, hidden, top_k), dxs, dxs_dtype, nullptr, dx,
+                               dx_dtype, static_cast<cudaStream_t>(stream)));
+}
+
+qf_status_t qf_moe_combine(const void* ys, qf_dtype_t ys_dtype, const float* weights, int64_t tokens, int top_k, int64_t hidden,
+                           const int32_t* row_of, int64_t rows_padded, void* out, qf_dtype_t out_dtype, void* stream) {
+  if (qf_status_t s = check_moe(tokens, top_k, hidden, rows_padded)) return s;
+  if (row_of ? !moe_rows_ok(rows_padded) : rows_padded < tokens * top_k) return QF_ERR_SHAPE;
+  if (!valid_dtype(ys_dtype) || !valid_dtype(out_dtype)) return QF_ERR_DTYPE;
+  const bool any = tokens > 0 && hidden > 0;
+  if (any && ((rows_padded > 0 && !ys) || !weights || !out)) return QF_ERR_NULL;
+  if (!aligned16(ys) || !aligned16(weights) || !aligned16(row_of) || !aligned16(out)) return QF_ERR_ALIGN;
+  if (qf_status_t s = check_arch()) return s;
+  if (!any) return QF_OK;
+  return cu(launch_moe_combine(moe_table(row_of, nullptr, nullptr, 0, rows_padded, tokens, hidden, top_k), ys, ys_dtype, weights, out,
+                               out_dtype, static_cast<cudaStream_t>(stream)));
+}
+
+qf_status_t qf_moe_combine_bwd(const void* dout, qf_dtype_t dout_dtype, const void* ys, qf_dtype_t ys_dtype, const float* weights,
+                               int64_t tokens, int top_k, int64_t hidden, const int32_t* row_of, const int32_t* group_offsets,
+                               const int32_t* counts, int G, int64_t rows_padded, void* dys, float* dweights, void* stream) {
+  if (qf_status_t s = check_moe(tokens, top_k, hidden, rows_padded)) return s;
+  if (G < 1 || G > QF_MOE_MAX_EXPERTS || !moe_rows_ok(rows_padded)) return QF_ERR_SHAPE;
+  if (!valid_dtype(dout_dtype) || !valid_dtype(ys_dtype)) return QF_ERR_DTYPE;
+  const bool rows_any = rows_padded > 0 && hidden > 0;
+  if (!group_offsets || !counts || (rows_any && !dys)) return QF_ERR_NULL;
+  if (tokens > 0 && (!row_of || !weights || (hidden > 0 && !dout) || (dweights && rows_any && !ys))) return QF_ERR_NULL;
+  if (!aligned16(dout) || !aligned16(ys) || !aligned16(weights) || !aligned16(row_of) || !aligned16(group_offsets) ||
+      !aligned16(counts) || !aligned16(dys) || !aligned16(dweights))
+    return QF_ERR_ALIGN;
+  if (qf_status_t s = check_arch()) return s;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (!rows_any)      // no row holds anything: every pair is dropped, or a sum over nothing
+    return dweights && tokens > 0 ? cu(cudaMemsetAsync(dweights, 0, static_cast<size_t>(tokens) * top_k * 4, st)) : QF_OK;
+  return cu(launch_moe_combine_bwd(moe_table(row_of, group_offsets, counts, G, rows_padded, tokens, hidden, top_k), dout, dout_dtype,
+                                   ys, ys_dtype, weights, dys, dweights, st));
+}
+
+static qf_status_t matvec_impl(int fmt, const void* X, int64_t M, int64_t x_rows, const void* ids, int ids_dtype, int G, const void* codes,
+                               const void* scales, const float* tscale, int64_t N, int64_t K, void* Y, int y_dtype, void* stream) {
+  if (!valid_fmt(fmt, false)) return QF_ERR_FORMAT;
+  if (!valid_dtype(y_dtype)) return QF_ERR_DTYPE;
+  // rows and tiles are numbered in 32 bits; byte offsets in 64
+  if (M < 0 || N < 0 || K < 0 || K % block_of(fmt) || M > INT32_MAX - 256 || N > INT32_MAX - 256 || K > INT32_MAX - 256) return QF_ERR_SHAPE;
+  if (x_rows < 0 || (M > 0 && (x_rows < 1 || M % x_rows))) return QF_ERR_SHAPE;
+  const bool any = M > 0 && N > 0;
+  if (any && (!Y || (K > 0 && (!X || !codes || !scales || (fmt == QF_FMT_NVFP4 && !tscale))))) return QF_ERR_NULL;
+  if (!aligned16(X) || !aligned16(codes) || !aligned16(scales) || !aligned16(Y) || !aligned16(ids)) return QF_ERR_ALIGN;
+  if (reinterpret_cast<uintptr_t>(tscale) & 3u) return QF_ERR_ALIGN;
+  if (qf_status_t s = check_arch()) return s;
+  if (!any) return QF_OK;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (K == 0)        // an empty contraction still defines the output: zeros
+    return cu(cudaMemsetAsync(Y, 0, static_cast<size_t>(M) * N * (y_dtype == QF_DT_F32 ? 4 : 2), st));
+  MatvecArgs a{};
+  a.fmt = fmt;
+  a.X = X;
+  a.M = M; a.N = N; a.K = K;
+  a.x_div = M / x_rows;
+  a.ids = ids;
+  a.ids64 = ids_dtype == QF_DT_I64;
+  a.G = G;
+  a.codes = codes; a.scales = scales; a.tscale = tscale;
+  a.Y = Y;
+  a.y_dtype = y_dtype;
+  return cu(launch_matvec(a, st));
+}
+
+qf_status_t qf_fq_matvec(qf_format_t fmt, const void* X, int64_t M, const void* codes, const void* scales, const float* tensor_scale,
+                         int64_t N, int64_t K, void* Y, qf_dtype_t y_dtype, void* stream) {
+  return matvec_impl(fmt, X, M, M, nullptr, QF_DT_I32, 1, codes, scales, tensor_scale, N, K, Y, y_dtype, stream);
+}
+
+qf_status_t qf_fq_grouped_matvec(qf_format_t fmt, const void* X, int64_t x_rows, const void* expert_ids, qf_dtype_t ids_dtype,
+                                 int64_t pairs, int G, const void* codes, const void* scales, const float* tensor_scales, int64_t N,
+                                 int64_t K, void* Y, qf_dtype_t y_dtype, void* stream) {
+  if (G < 1 || G > QF_MOE_MAX_EXPERTS) return QF_ERR_SHAPE;
+  if (ids_dtype != QF_DT_I32 && ids_dtype != QF_DT_I64) return QF_ERR_DTYPE;
+  if (pairs > 0 && !expert_ids) return QF_ERR_NULL;
+  return matvec_impl(fmt, X, pairs, x_rows, expert_ids, ids_dtype, G, codes, scales, tensor_scales, N, K, Y, y_dtype, stream);
+}
+
 static qf_status_t check_pack(int layout, int fmt, int64_t rows, int64_t cols) {
   if (layout == QF_LAYOUT_GGUF_Q4_K) { if (fmt != QF_FMT_Q4_K) return QF_ERR_FORMAT; }
   else if (layout == QF_LAYOUT_FP4_SWIZZLED_SCALES) { if (fmt != QF_FMT_NVFP4 && fmt != QF_FMT_MXFP4) return QF_ERR_FORMAT; }

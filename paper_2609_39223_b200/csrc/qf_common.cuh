@@ -346,6 +346,44 @@ struct Fp4GemmArgs {
 };
 cudaError_t launch_fp4_native(const Fp4GemmArgs& a, cudaStream_t st);
 bool gemm_can_fuse(const GemmArgs& a);
+
+// Mixture-of-experts routing (qf_moe.cu). The tables are device memory; see qf.h for their meaning.
+struct MoeTable {
+  const int32_t* row_of;             // [tokens, top_k]; null (combine only): pair p is row p
+  const int32_t* offs;               // [G+1]
+  const int32_t* counts;             // [G]
+  int G;
+  int64_t rows;                      // rows of the sorted buffer
+  int64_t tokens, hidden;
+  int top_k;
+};
+cudaError_t launch_moe_sort(const void* ids, bool ids64, int64_t pairs, int G, int64_t rows, int32_t* row_of, int32_t* offs,
+                            int32_t* counts, cudaStream_t st);
+cudaError_t launch_moe_dispatch(const MoeTable& t, const void* x, void* xs, cudaStream_t st);
+// weights null: plain sums (the gradient of dispatch)
+cudaError_t launch_moe_combine(const MoeTable& t, const void* ys, int ys_dtype, const float* weights, void* out, int out_dtype,
+                               cudaStream_t st);
+cudaError_t launch_moe_combine_bwd(const MoeTable& t, const void* dout, int dout_dtype, const void* ys, int ys_dtype,
+                                   const float* weights, void* dys, float* dweights, cudaStream_t st);
+
+// Products with a few tokens from 4-bit codes (qf_matvec.cu).
+struct MatvecArgs {
+  int fmt;
+  const void* X;
+  int64_t M;                         // rows of Y: tokens, or (token, expert) pairs
+  int64_t x_div;                     // row m of Y uses row m / x_div of X
+  const void* ids;                   // expert of every row (null: one weight for all)
+  bool ids64;
+  int G;
+  const void* codes;
+  const void* scales;
+  const float* tscale;               // NVFP4: one per expert
+  int64_t N, K;
+  void* Y;
+  int y_dtype;
+};
+cudaError_t launch_matvec(const MatvecArgs& a, cudaStream_t st);
+
 cudaError_t launch_selftest_timeout(uint32_t* status, long long limit_cycles, int* gave_up, cudaStream_t st);
 
 }  // namespace qf
