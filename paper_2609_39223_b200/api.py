@@ -445,6 +445,15 @@ def _tensor(t: torch.Tensor, name: str, dtypes, shape) -> int:
     return t.data_ptr()
 
 
+def _stream_of(t: torch.Tensor) -> int:
+    """Current stream of the current device, which has to be the tensor's. (The calls below take a few microseconds on the GPU;
+    torch.cuda.current_stream() builds an object and takes three by itself.)"""
+    device = t.get_device()
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors are on cuda:{device}, the current device is cuda:{torch._C._cuda_getDevice()}")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 _BF16, _F32, _I32, _U8 = (torch.bfloat16,), (torch.float32,), (torch.int32,), (torch.uint8,)
 
 
@@ -463,12 +472,11 @@ def qf_moe_sort(expert_ids: torch.Tensor, experts: int, *, rows_padded: int | No
     if rows_padded is None:
         rows_padded = qf_moe_rows_bound(tokens, top_k, experts)
     ids = _tensor(expert_ids, "expert_ids", _IDS_DTYPE, expert_ids.shape)
-    dev = expert_ids.device
-    row_of = torch.empty((tokens, top_k), dtype=torch.int32, device=dev)
-    offs = torch.empty(experts + 1, dtype=torch.int32, device=dev)
-    counts = torch.empty(experts, dtype=torch.int32, device=dev)
+    row_of = expert_ids.new_empty((tokens, top_k), dtype=torch.int32)
+    offs = expert_ids.new_empty(experts + 1, dtype=torch.int32)
+    counts = expert_ids.new_empty(experts, dtype=torch.int32)
     _check(lib().qf_moe_sort(ids, _IDS_DTYPE[expert_ids.dtype], tokens, top_k, experts, rows_padded, row_of.data_ptr(),
-                             offs.data_ptr(), counts.data_ptr(), _stream()), "qf_moe_sort")
+                             offs.data_ptr(), counts.data_ptr(), _stream_of(expert_ids)), "qf_moe_sort")
     return MoePlan(row_of, offs, counts, rows_padded)
 
 
@@ -485,9 +493,9 @@ def qf_moe_dispatch(x: torch.Tensor, plan: MoePlan, *, xs: torch.Tensor | None =
     px = _tensor(x, "x", _BF16, (tokens, hidden))
     row_of, offs, counts, experts = _plan_ptrs(plan)
     if xs is None:
-        xs = torch.empty((rows, hidden), dtype=torch.bfloat16, device=x.device)
+        xs = x.new_empty((rows, hidden), dtype=torch.bfloat16)
     _check(lib().qf_moe_dispatch(px, tokens, top_k, hidden, row_of, offs, counts, experts, rows, _tensor(xs, "xs", _BF16, (rows, hidden)),
-                                 _stream()), "qf_moe_dispatch")
+                                 _stream_of(x)), "qf_moe_dispatch")
     return xs
 
 
@@ -497,9 +505,9 @@ def qf_moe_dispatch_bwd(dxs: torch.Tensor, plan: MoePlan, *, dx_dtype=torch.bflo
     hidden = dxs.shape[-1]
     pd = _tensor(dxs, "dxs", _DATA_DTYPE, (rows, hidden))
     if dx is None:
-        dx = torch.empty((tokens, hidden), dtype=dx_dtype, device=dxs.device)
+        dx = dxs.new_empty((tokens, hidden), dtype=dx_dtype)
     _check(lib().qf_moe_dispatch_bwd(pd, _DATA_DTYPE[dxs.dtype], tokens, top_k, hidden, _tensor(plan.row_of, "plan.row_of", _I32, (tokens, top_k)),
-                                     rows, _tensor(dx, "dx", _DATA_DTYPE, (tokens, hidden)), _DATA_DTYPE[dx.dtype], _stream()), "qf_moe_dispatch_bwd")
+                                     rows, _tensor(dx, "dx", _DATA_DTYPE, (tokens, hidden)), _DATA_DTYPE[dx.dtype], _stream_of(dxs)), "qf_moe_dispatch_bwd")
     return dx
 
 
@@ -511,10 +519,10 @@ def qf_moe_combine(ys: torch.Tensor, weights: torch.Tensor, plan: MoePlan | None
     rows = tokens * top_k if plan is None else plan.rows_padded
     py = _tensor(ys, "ys", _DATA_DTYPE, (rows, hidden))
     if out is None:
-        out = torch.empty((tokens, hidden), dtype=out_dtype, device=ys.device)
+        out = ys.new_empty((tokens, hidden), dtype=out_dtype)
     row_of = None if plan is None else _tensor(plan.row_of, "plan.row_of", _I32, (tokens, top_k))
     _check(lib().qf_moe_combine(py, _DATA_DTYPE[ys.dtype], _tensor(weights, "weights", _F32, (tokens, top_k)), tokens, top_k, hidden, row_of, rows,
-                                _tensor(out, "out", _DATA_DTYPE, (tokens, hidden)), _DATA_DTYPE[out.dtype], _stream()), "qf_moe_combine")
+                                _tensor(out, "out", _DATA_DTYPE, (tokens, hidden)), _DATA_DTYPE[out.dtype], _stream_of(ys)), "qf_moe_combine")
     return out
 
 
@@ -528,13 +536,13 @@ def qf_moe_combine_bwd(dout: torch.Tensor, ys: torch.Tensor | None, weights: tor
     py = _tensor(ys, "ys", _DATA_DTYPE, (rows, hidden)) if want_dweights or ys is not None else None
     row_of, offs, counts, experts = _plan_ptrs(plan)
     if dys is None:
-        dys = torch.empty((rows, hidden), dtype=torch.bfloat16, device=dout.device)
+        dys = dout.new_empty((rows, hidden), dtype=torch.bfloat16)
     if want_dweights and dweights is None:
-        dweights = torch.empty((tokens, top_k), dtype=torch.float32, device=dout.device)
+        dweights = dout.new_empty((tokens, top_k), dtype=torch.float32)
     pw = _tensor(dweights, "dweights", _F32, (tokens, top_k)) if want_dweights else None
     _check(lib().qf_moe_combine_bwd(pd, _DATA_DTYPE[dout.dtype], py, _DATA_DTYPE[ys.dtype] if ys is not None else DT_BF16,
                                     _tensor(weights, "weights", _F32, (tokens, top_k)), tokens, top_k, hidden, row_of, offs, counts, experts,
-                                    rows, _tensor(dys, "dys", _BF16, (rows, hidden)), pw, _stream()), "qf_moe_combine_bwd")
+                                    rows, _tensor(dys, "dys", _BF16, (rows, hidden)), pw, _stream_of(dout)), "qf_moe_combine_bwd")
     return dys, dweights if want_dweights else None
 
 
@@ -546,11 +554,11 @@ def qf_fq_matvec(fmt: int, X: torch.Tensor, codes: torch.Tensor, scales: torch.T
     if fmt not in BLOCK or K % BLOCK[fmt]:
         raise QfError(2 if fmt in BLOCK else 4, "qf_fq_matvec")
     if Y is None:
-        Y = torch.empty((M, N), dtype=y_dtype, device=X.device)
+        Y = X.new_empty((M, N), dtype=y_dtype)
     ts = _tensor(tensor_scale, "tensor_scale", _F32, (1,)) if fmt == FMT_NVFP4 else None
     _check(lib().qf_fq_matvec(fmt, _tensor(X, "X", _BF16, (M, K)), M, _tensor(codes, "codes", _U8, (N, K // 2)),
                               _tensor(scales, "scales", _U8, scales_shape(fmt, N, K)), ts, N, K, _tensor(Y, "Y", _DATA_DTYPE, (M, N)),
-                              _DATA_DTYPE[Y.dtype], _stream()), "qf_fq_matvec")
+                              _DATA_DTYPE[Y.dtype], _stream_of(X)), "qf_fq_matvec")
     return Y
 
 
@@ -564,12 +572,12 @@ def qf_fq_grouped_matvec(fmt: int, X: torch.Tensor, expert_ids: torch.Tensor, co
     if fmt not in BLOCK or K % BLOCK[fmt]:
         raise QfError(2 if fmt in BLOCK else 4, "qf_fq_grouped_matvec")
     if Y is None:
-        Y = torch.empty((pairs, N), dtype=y_dtype, device=X.device)
+        Y = X.new_empty((pairs, N), dtype=y_dtype)
     ts = _tensor(tensor_scales, "tensor_scales", _F32, (G,)) if fmt == FMT_NVFP4 else None
     _check(lib().qf_fq_grouped_matvec(fmt, _tensor(X, "X", _BF16, (x_rows, K)), x_rows, _tensor(expert_ids, "expert_ids", _IDS_DTYPE, expert_ids.shape),
                                       _IDS_DTYPE[expert_ids.dtype], pairs, G, _tensor(codes, "codes", _U8, (G, N, K // 2)),
                                       _tensor(scales, "scales", _U8, (G, *scales_shape(fmt, N, K))), ts, N, K, _tensor(Y, "Y", _DATA_DTYPE, (pairs, N)),
-                                      _DATA_DTYPE[Y.dtype], _stream()), "qf_fq_grouped_matvec")
+                                      _DATA_DTYPE[Y.dtype], _stream_of(X)), "qf_fq_grouped_matvec")
     return Y
 
 

@@ -1,20 +1,29 @@
 // Products with a few tokens straight from 4-bit codes and block scales: Y = X . deq(W)^T, plain and per expert.
 //
-// The weights are the only large operand, so the bound is the read of codes and scales (0.53-0.56 bytes per weight). One
-// FP32 multiply-add per weight and token would cost more issue slots than that read leaves (about 2.8 instructions per weight
-// at the copy rate), and the decode alone takes two. So the multiply-adds go to mma.sync m16n8k16 (16 weight rows x 8
-// tokens): a tcgen05 tile needs 128 rows of an operand in shared memory, which would mean writing every decoded weight there
-// first; here the decoded weights never leave registers.
+// The weights are the only large operand, so the floor is the read of codes and scales (0.53-0.56 bytes per weight). At the
+// copy rate that leaves about 2.8 instructions per weight, decode included: too few for one FP32 multiply-add per weight and
+// token. So the multiply-adds go to mma.sync m16n8k16 (16 weight rows x 8 tokens): a tcgen05 tile needs 128 rows of an operand
+// in shared memory, which would mean writing every decoded weight there first; here decoded weights never leave registers.
 //
-//  * A fragments: a lane loads 32 (or 8) consecutive bytes of codes of one weight row and decodes them in place. Which k a
-//    lane's elements stand for is free as long as both operands agree, so no code is ever moved between lanes.
-//  * B fragments: the CTA stages its slice of X in shared memory once, already in the order the lanes read it.
-//  * FP4 codes become BF16 by one multiplication: a nibble times 0x1040 puts its sign at bit 15 and its three other bits
-//    at bits 8..6, which is the value as a BF16 number scaled by 2^-126 (subnormals included); one packed BF16 product
-//    with the block scale times a power of two gives value * scale, exactly (two and four significant bits).
-//  * Q4_K codes are whole numbers below 16; a sub-block's sum of C*x is finished in FP32 with its scale and offset.
-//  * Rows are cut into tiles of 16 for a warp; the contraction is split over the warps of a CTA and over the CTAs of a cluster
-//    where there are too few tiles to keep every SM loading; the parts meet in (distributed) shared memory in a fixed order.
+//  * A fragments: a lane decodes up to 32 consecutive bytes of codes of one weight row in place. Which k a lane's elements stand
+//    for is free as long as both operands agree, so no code is ever moved between lanes.
+//  * Every decoded weight is exact in FP16 up to a factor that a row or a step shares: E2M1 value times E4M3 scale has six
+//    significant bits; E2M1 value times 2^p is exact while p lies in [-21, 5]; a Q4_K code C times its 6-bit scale s6 is a whole
+//    number below 1024, kept as that multiple of 2^-24 (an FP16 subnormal is its own bit pattern, so C needs no conversion).
+//    One conversion and one packed product decode two FP4 weights, one mask and one product two Q4_K weights.
+//  * B fragments: the CTA stages its slice of X in shared memory once, in the order the lanes read it, as FP16 of 2^6 x. That is
+//    exact for zeros and 2^-23 <= |x| < 1023. A token that has another x in a step of the contraction (or a tile with another p)
+//    takes that step with BF16 fragments, weights and X read again: a sum of exact products either way, so the choice
+//    costs time only (of N(0, 1) values one in ten million falls below). It goes by token: rows of X do not influence one another.
+//  * BF16 fragments from FP4 codes: a nibble times 0x1040 puts its sign at bit 15 and its three other bits at bits 8..6, which is
+//    the value as a BF16 number scaled by 2^-126 (subnormals included); a packed product with the scale gives value * scale.
+//    This takes 15 instructions for eight weights where the FP16 route takes 8, which is why it is not the only route.
+//  * Q4_K offsets: sum over sub-blocks of m6 * sum(x) is a product of its own, 8 sub-blocks deep, with the sums of x split into
+//    three BF16 parts (24 bits); one FP32 multiply-add per super-block applies d and dmin.
+//  * The tensor core truncates as it accumulates: it adds up one step (64 to 256 elements) at a time, the steps are added in FP32.
+//  * Codes arrive through a ring of kStages steps per warp in shared memory (cp.async), so that loads in flight cost no registers.
+//  * Rows are cut into tiles of 16 or 32 for a warp; the contraction is split over the warps of a CTA and over the CTAs of a
+//    cluster where there are too few tiles to keep every SM loading; the parts meet in (distributed) shared memory in a fixed order.
 #include <cooperative_groups.h>
 
 #include "qf_common.cuh"
@@ -24,10 +33,11 @@ namespace cg = cooperative_groups;
 namespace qf {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
+constexpr int kWarpsMost = 16;                       // of a CTA; 128 registers a thread, so 16 warps fill an SM
+constexpr int kStages = 2;                           // turns of codes a warp has in shared memory or on the way
+constexpr int kSmemMost = 232448 - 128;              // dynamic shared memory of a CTA
+constexpr float kXScale = 64.0f;                     // X is staged as FP16 of this times x
 constexpr int kListCap = 1024;                       // pairs looked at in one go by a CTA of the grouped product
-constexpr int kXBytes = 64 * 1024;                   // shared memory for the staged slice of X
 
 struct MvParams {
   const __nv_bfloat16* X;
@@ -36,12 +46,13 @@ struct MvParams {
   const float* tscale;
   const void* ids;
   void* Y;
-  int64_t x_div;
+  int x_div;
   int M, N, K, G;
-  int kw;                                            // warps of a CTA that share a row tile (1, 2, 4 or 8)
-  int kz;                                            // contraction length of a CTA (a multiple of 256)
-  int kc;                                            // contraction length staged at a time (a multiple of 256)
-  int x_words;                                       // 32-bit words of shared memory for X
+  int blocks;                                        // row blocks of a weight; CTA x takes blocks x, x + gridDim.x, ...
+  int kw;                                            // warps of a CTA that share a row tile
+  int kz;                                            // contraction length of a CTA (a multiple of 512)
+  int kc;                                            // contraction length staged at a time (a multiple of 512)
+  int sx_at, flags_at, list_at, red_at, ring_at;     // bytes from the start of dynamic shared memory (X comes first)
   bool ids64, by_pair, y_f32;
 };
 
@@ -54,17 +65,45 @@ __device__ __forceinline__ int expert_id(const MvParams& p, int i) {
   return e >= 0 && e < p.G ? e : -1;
 }
 
-// D += A . B, A 16x16 and B 16x8 in BF16, FP32 accumulators
-__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+__device__ __forceinline__ void store_y(const MvParams& p, int64_t row, int n, float v) {
+  if (p.y_f32) static_cast<float*>(p.Y)[row * p.N + n] = v;
+  else static_cast<__nv_bfloat16*>(p.Y)[row * p.N + n] = __float2bfloat16_rn(v);
+}
+
+// D = A . B (+ D), A 16x16 and B 16x8, FP32 accumulators; a0/a1: rows g / g + 8, first k pair, a2/a3: second k pair
+template <bool F16>
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (F16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) { return bf2_bits(__hmul2(bits_bf2(a), bits_bf2(b))); }
+__device__ __forceinline__ __half2 bits_h2(uint32_t v) { return *reinterpret_cast<__half2*>(&v); }
+__device__ __forceinline__ uint32_t h2_bits(__half2 v) { return *reinterpret_cast<uint32_t*>(&v); }
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) { return h2_bits(__hmul2(bits_h2(a), bits_h2(b))); }
 
-// Eight E2M1 codes -> four BF16 pairs (elements i and i + 4), each the code's value times 2^-126.
-__device__ __forceinline__ void e2m1_words(uint32_t q, uint32_t (&w)[4]) {
+// Eight E2M1 codes -> four FP16 pairs (2i, 2i + 1)
+__device__ __forceinline__ void e2m1_f16(uint32_t q, uint32_t (&w)[4]) {
+  asm("{\n.reg .b8 a, b, c, d;\nmov.b32 {a, b, c, d}, %4;\n"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\ncvt.rn.f16x2.e2m1x2 %1, b;\ncvt.rn.f16x2.e2m1x2 %2, c;\ncvt.rn.f16x2.e2m1x2 %3, d;\n}"
+      : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+      : "r"(q));
+}
+// Two E4M3 codes -> FP16 pair
+__device__ __forceinline__ uint32_t e4m3_f16(uint32_t two) {
+  uint32_t r;
+  asm("{\n.reg .b16 h;\ncvt.u16.u32 h, %1;\ncvt.rn.f16x2.e4m3x2 %0, h;\n}" : "=r"(r) : "r"(two));
+  return r;
+}
+
+// Eight E2M1 codes -> four BF16 pairs (i, i + 4), each the code's value times 2^-126.
+__device__ __forceinline__ void e2m1_bf16(uint32_t q, uint32_t (&w)[4]) {
   const uint32_t h = q >> 8;
   w[0] = ((q & 0x000F000Fu) * 0x1040u) & 0x81C081C0u;
   w[1] = ((q & 0x00F000F0u) * 0x0104u) & 0x81C081C0u;
@@ -72,66 +111,178 @@ __device__ __forceinline__ void e2m1_words(uint32_t q, uint32_t (&w)[4]) {
   w[3] = ((h & 0x00F000F0u) * 0x0104u) & 0x81C081C0u;
 }
 
-// 16 elements of X in the order the A words have: FP4 pairs (i, i + 4), Q4_K pairs (i, i + 2)
-template <int FMT>
-__device__ __forceinline__ uint4 x_unit(uint4 v) {
-  if constexpr (FMT == QF_FMT_Q4_K)
-    return make_uint4(__byte_perm(v.x, v.y, 0x5410), __byte_perm(v.x, v.y, 0x7632), __byte_perm(v.z, v.w, 0x5410), __byte_perm(v.z, v.w, 0x7632));
-  else
-    return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+// Packed 6-bit scales (first two words) and offsets (last two) of a Q4_K super-block, a byte per sub-block.
+__device__ __forceinline__ void q4k_unpack(const uint32_t (&m)[4], uint32_t (&v)[4]) {
+  v[0] = m[1] & 0x3F3F3F3Fu;
+  v[1] = (m[3] & 0x0F0F0F0Fu) | ((m[1] >> 2) & 0x30303030u);
+  v[2] = m[2] & 0x3F3F3F3Fu;
+  v[3] = ((m[3] >> 4) & 0x0F0F0F0Fu) | ((m[2] >> 2) & 0x30303030u);
 }
 
-__device__ __forceinline__ void load32(const uint8_t* p, uint32_t (&q)[8]) {
-  asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]), "=r"(q[4]), "=r"(q[5]), "=r"(q[6]), "=r"(q[7])
-               : "l"(p));
-}
-
-// What a lane holds of one weight row for one step of the contraction: FP4 wide 64 weights (a step is 256), FP4 narrow 16
-// weights (a step is 64), Q4_K 64 weights of a super-block (8 bytes of each of its four chunks).
-template <int FMT, bool WIDE>
+// What a lane holds of one weight row for one step of the contraction: LB bytes of codes. FP4: consecutive ones (a step is
+// 8 * LB weights). Q4_K (LB = 32): 8 bytes of each of the four chunks of a super-block (a step is a super-block).
+template <int FMT, int LB>
 struct RowPart {
-  static constexpr int kWords = FMT == QF_FMT_Q4_K || WIDE ? 8 : 2;
-  uint32_t q[kWords];
+  uint32_t q[LB / 4];
   uint32_t s[FMT == QF_FMT_Q4_K ? 4 : 1];            // block scales as stored
 };
 
-template <int FMT, bool WIDE>
-__device__ __forceinline__ void load_part(RowPart<FMT, WIDE>& r, const uint8_t* codes, const uint8_t* scales, int k_step, int K, int t) {
-  if constexpr (FMT == QF_FMT_Q4_K) {
-    const uint8_t* c = codes + k_step / 2 + t * 8;
+// Weights per block scale, and bytes of block scales of a lane's part of a row (half a block counts as one).
+template <int FMT>
+constexpr int kBlock = FMT == QF_FMT_MXFP4 ? 32 : 16;
+template <int FMT, int LB>
+constexpr int kPartScales = 2 * LB / kBlock<FMT> ? 2 * LB / kBlock<FMT> : 1;
+
+// The same straight from global memory, 8 bytes at a time.
+template <int FMT, int LB>
+__device__ __forceinline__ void load_part(RowPart<FMT, LB>& r, const uint8_t* codes, const uint8_t* scales, int k_step, int K, int t) {
+  const int k = FMT == QF_FMT_Q4_K ? k_step + t * 16 : k_step + t * 2 * LB;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint2 v = __ldg(reinterpret_cast<const uint2*>(c + 32 * i));
-      r.q[2 * i] = v.x;
-      r.q[2 * i + 1] = v.y;
-    }
+  for (int i = 0; i < LB / 8; ++i) {
+    uint2 v = make_uint2(0u, 0u);
+    if (k < K) v = __ldg(reinterpret_cast<const uint2*>(codes + k / 2 + i * (FMT == QF_FMT_Q4_K ? 32 : 8)));
+    r.q[2 * i] = v.x;
+    r.q[2 * i + 1] = v.y;
+  }
+  if constexpr (FMT == QF_FMT_Q4_K) {
     const uint4 m = __ldg(reinterpret_cast<const uint4*>(scales + k_step / 16));
     r.s[0] = m.x; r.s[1] = m.y; r.s[2] = m.z; r.s[3] = m.w;
   } else {
-    const int k = k_step + t * (WIDE ? 64 : 16);
+    r.s[0] = FMT == QF_FMT_MXFP4 ? 0x7F7F7F7Fu : 0u;   // zeros with a scale in range past the end
     if (k < K) {
-      if constexpr (WIDE) {
-        load32(codes + k / 2, r.q);
-        if constexpr (FMT == QF_FMT_NVFP4) r.s[0] = __ldg(reinterpret_cast<const uint32_t*>(scales + k / 16));
-        else r.s[0] = __ldg(reinterpret_cast<const uint16_t*>(scales + k / 32));
-      } else {
-        const uint2 v = __ldg(reinterpret_cast<const uint2*>(codes + k / 2));
-        r.q[0] = v.x;
-        r.q[1] = v.y;
-        r.s[0] = __ldg(scales + k / (FMT == QF_FMT_NVFP4 ? 16 : 32));
+      r.s[0] = 0u;
+#pragma unroll
+      for (int i = 0; i < kPartScales<FMT, LB>; ++i) r.s[0] |= static_cast<uint32_t>(__ldg(scales + k / (FMT == QF_FMT_NVFP4 ? 16 : 32) + i)) << (8 * i);
+    }
+  }
+}
+
+// ---- a warp's ring of steps in shared memory, filled by asynchronous copies -----------------------------------------------
+// LB = 32 (K a multiple of 128; a step is 256 weights of 16 rows): rows of 128 bytes, each copied by eight lanes at a time. (Four
+// lanes a row, 64 bytes of eight rows at a time, took 81 us for the copies of a 128256 x 4096 weight where this takes 49.)
+// 16-byte pieces are permuted inside a row so that the lanes that read together meet different banks. Then the scales: 16 bytes
+// (NVFP4, Q4_K) or 8 (MXFP4) of every row.
+// LB = 8 (any K; a step is 64 weights): every lane copies its own 8 bytes of two rows, scales go to registers.
+
+template <int FMT>
+constexpr int kStepScales = FMT == QF_FMT_MXFP4 ? 8 : 16;
+template <int FMT, int LB>
+constexpr int kStepBytes = LB == 8 ? 512 : 16 * (128 + kStepScales<FMT>);
+// Steps a warp takes in a turn of its loop: two where the products of a step are few, so that addresses and bookkeeping are shared.
+template <int NT, int LB>
+constexpr int kTurn = NT == 1 && LB == 32 ? 2 : 1;
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+// place of 16-byte piece `piece` of row r: FP4 lanes read pieces 2t (then 2t + 1) of two rows together, Q4_K lanes halves of
+// pieces 2c and 2c + 1 of four rows
+template <int FMT>
+__device__ __forceinline__ uint32_t piece_at(int r, int piece) {
+  return r * 128 + ((piece ^ (FMT == QF_FMT_Q4_K ? (r & 3) * 2 : r & 1)) * 16);
+}
+
+// Where a warp's next step of codes and scales lies: this lane's address in the first row it copies, and the distance of its
+// other rows. The addresses advance from turn to turn; they are set up anew for every tile. A lane whose part lies past the end
+// of the contraction copies an earlier part of its row: any finite weight will do, X is zero there.
+template <int FMT, int LB>
+struct Source {
+  static constexpr int kRows = LB == 8 ? 2 : 4;      // rows a lane copies codes of
+  static constexpr int SHIFT = FMT == QF_FMT_MXFP4 ? 4 : 3;            // bytes of codes to bytes of scales
+  static constexpr int SCALE_LANES = FMT == QF_FMT_Q4_K ? 1 : 2;       // lanes that copy a row's scales
+  const uint8_t* codes;
+  const uint8_t* scales;
+  uint32_t row[kRows - 1];                           // bytes of codes to the other rows
+  int k;                                             // of the step (LB = 8: of this lane's first code)
+
+  __device__ __forceinline__ void tile(const MvParams& p, int64_t row0, int n0, int k_step, int lane) {
+    const int first = n0 + (LB == 8 ? lane >> 2 : lane >> 3), gap = LB == 8 ? 8 : 4;
+    const int n = min(first, p.N - 1);
+    const uint32_t pitch = static_cast<uint32_t>(p.K) / 2;
+    k = LB == 8 ? k_step + (lane & 3) * 16 : k_step;
+    const int64_t at = (row0 + n) * pitch + k / 2;
+    codes = p.codes + at + (LB == 8 ? 0 : (lane & 7) * 16);
+#pragma unroll
+    for (int i = 1; i < kRows; ++i) row[i - 1] = static_cast<uint32_t>(min(first + gap * i, p.N - 1) - n) * pitch;
+    if constexpr (LB == 8) {
+      scales = p.scales + (at >> SHIFT);
+    } else {
+      const int r = lane / SCALE_LANES & 15;
+      scales = p.scales + (((row0 + min(n0 + r, p.N - 1)) * pitch + k / 2) >> SHIFT) + lane % SCALE_LANES * (kStepScales<FMT> / SCALE_LANES);
+    }
+  }
+  __device__ __forceinline__ void advance(int dk) {
+    k += dk;
+    codes += dk / 2;
+    scales += dk / kBlock<FMT>;
+  }
+  // Starts the copies of the first `steps` steps of a turn.
+  template <int TURN>
+  __device__ __forceinline__ void start(const MvParams& p, uint32_t stage, int steps, int lane, uint32_t (&sc)[2]) const {
+    if constexpr (LB == 8) {
+      const int back = k < p.K ? 0 : k;              // past the end: the row's first part
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t off = i ? row[i - 1] : 0u;
+        copy_async<8>(stage + i * 256 + lane * 8, codes + off - back / 2);
+        sc[i] = __ldg(scales + (off >> SHIFT) - back / kBlock<FMT>);
       }
     } else {
+      const uint32_t to = stage + piece_at<FMT>(lane >> 3, lane & 7), to_sc = stage + 16 * 128 + lane * (kStepScales<FMT> / SCALE_LANES);
 #pragma unroll
-      for (int i = 0; i < RowPart<FMT, WIDE>::kWords; ++i) r.q[i] = 0u;
-      r.s[0] = 0u;
+      for (int u = 0; u < TURN; ++u) {
+        if (u >= steps) break;
+        // the second half of a step may lie past the end, K being a multiple of 128: those lanes step back to the first
+        const bool past = FMT != QF_FMT_Q4_K && k + u * 256 + 128 >= p.K;
+        const uint8_t* c = codes + u * 128 - (past && (lane & 4) ? 64 : 0);
+        const uint8_t* s = scales + u * (256 / kBlock<FMT>) - (past && (lane & 1) ? 128 / kBlock<FMT> : 0);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) copy_async<16>(to + u * kStepBytes<FMT, LB> + h * 512, c + (h ? row[h - 1] : 0u));
+        if (SCALE_LANES == 2 || lane < 16) copy_async<kStepScales<FMT> / SCALE_LANES>(to_sc + u * kStepBytes<FMT, LB>, s);
+      }
+    }
+  }
+};
+
+// A step back from the ring; sc: LB = 8, the scales that came with it.
+template <int FMT, int LB>
+__device__ __forceinline__ void read_step(RowPart<FMT, LB> (&r)[2], const uint8_t* stage, int lane, const uint32_t (&sc)[2]) {
+  const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = g + 8 * i;
+    if constexpr (LB == 8) {
+      const uint2 v = *reinterpret_cast<const uint2*>(stage + i * 256 + lane * 8);
+      r[i].q[0] = v.x;
+      r[i].q[1] = v.y;
+      r[i].s[0] = sc[i];
+    } else if constexpr (FMT == QF_FMT_Q4_K) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint2 v = *reinterpret_cast<const uint2*>(stage + piece_at<FMT>(row, 2 * c) + t * 8);
+        r[i].q[2 * c] = v.x;
+        r[i].q[2 * c + 1] = v.y;
+      }
+      const uint4 m = *reinterpret_cast<const uint4*>(stage + 16 * 128 + row * 16);
+      r[i].s[0] = m.x; r[i].s[1] = m.y; r[i].s[2] = m.z; r[i].s[3] = m.w;
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint4 v = *reinterpret_cast<const uint4*>(stage + piece_at<FMT>(row, 2 * t + h));
+        r[i].q[4 * h] = v.x; r[i].q[4 * h + 1] = v.y; r[i].q[4 * h + 2] = v.z; r[i].q[4 * h + 3] = v.w;
+      }
+      const uint8_t* s = stage + 16 * 128 + row * kStepScales<FMT> + t * kPartScales<FMT, LB>;
+      r[i].s[0] = FMT == QF_FMT_NVFP4 ? *reinterpret_cast<const uint32_t*>(s) : *reinterpret_cast<const uint16_t*>(s);
     }
   }
 }
 
 // The packed BF16 factor that turns value * 2^-126 into value * scale (NVFP4: times 2^-7, put right at the end).
 template <int FMT>
-__device__ __forceinline__ uint32_t fp4_factor(uint32_t code) {
+__device__ __forceinline__ uint32_t bf16_factor(uint32_t code) {
   if constexpr (FMT == QF_FMT_NVFP4) {
     // code << 20 is the scale times 2^-120 as FP32
     const uint32_t f = __float_as_uint(__fmul_rn(__fmul_rn(__uint_as_float(code << 20), 0x1p127f), 0x1p112f));
@@ -141,24 +292,305 @@ __device__ __forceinline__ uint32_t fp4_factor(uint32_t code) {
   }
 }
 
-template <int FMT, int NT, bool WIDE>
-__global__ void __launch_bounds__(kThreads, 2) matvec_kernel(const __grid_constant__ MvParams p) {
+// MXFP4 scale codes for which value * 2^p, kept as value * 2^(p + 7), is exact in FP16: p in [-21, 5]
+constexpr uint32_t kMxLow = 106, kMxHigh = 132;
+
+// whether that holds for all scales of the warp's step
+template <int LB>
+__device__ __forceinline__ bool mx_exact(const RowPart<QF_FMT_MXFP4, LB> (&r)[2]) {
+  constexpr int NS = LB == 32 ? 2 : 1;
+  bool in = true;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < NS; ++j) in = in && ((r[i].s[0] >> (8 * j)) & 0xFFu) - kMxLow <= kMxHigh - kMxLow;
+  return __all_sync(0xFFFFFFFFu, in);
+}
+
+// ---- one step of the contraction, FP16 fragments from shared memory: c[nt] += A . B ------------------------------------
+// x: the step's X in shared memory, `at` this lane's place in each token tile. Returns false if a scale is out of range (c is then
+// worthless). c is the sum times 2^6 (from X) and times 1 (NVFP4), 2^7 (MXFP4) or 2^-24 / d (Q4_K).
+
+// This lane's 16 bytes of X for one word of codes (Q4_K: one sub-block). A single token tile stands lane by lane, 16 bytes of
+// padding after each lane's words, so that a lane's words have fixed distances; lanes without a token read nothing (columns of
+// the product do not meet, whatever is in their registers). Several tiles stand word by word.
+template <int NT, int LB>
+__device__ __forceinline__ uint4 x_word(uint32_t x, int w, uint32_t at, bool live) {
+  uint4 v;
+  if constexpr (NT == 1)
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %5, 0;\n@p ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n}"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "r"(x + at + w * 16), "r"(static_cast<int>(live)));
+  else
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(x + at + w * (8 * NT * 64)));
+  return v;
+}
+
+template <int FMT, int NT, int LB>
+__device__ __forceinline__ bool step_f16(const RowPart<FMT, LB> (&r)[2], uint32_t x, const uint32_t (&at)[NT], bool live, float (&c)[NT][4]) {
+  constexpr int LW = LB / 4;
+  bool in = true;
+  if constexpr (FMT == QF_FMT_Q4_K) {
+    uint32_t v[2][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) q4k_unpack(r[i].s, v[i]);
+#pragma unroll
+    for (int chunk = 0; chunk < 4; ++chunk) {
+      __half2 f[2];                               // s6 of the chunk's two sub-blocks; the odd one's codes come out 16 times as large
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        f[i] = __hfma2(bits_h2(__byte_perm(v[i][chunk >> 1], 0x64646464u, chunk & 1 ? 0x4342 : 0x4140)), bits_h2(0x2C003C00u), bits_h2(0xD400E400u));
+#pragma unroll
+      for (int odd = 0; odd < 2; ++odd) {
+        uint4 xv[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) xv[nt] = x_word<NT, LB>(x, 2 * chunk + odd, at[nt], live);
+        {
+          uint32_t w[2][4];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t mask = odd ? 0x00F000F0u : 0x000F000Fu;
+            const __half2 fac = odd ? __high2half2(f[i]) : __low2half2(f[i]);
+            const uint32_t q0 = r[i].q[2 * chunk], q1 = r[i].q[2 * chunk + 1];
+            w[i][0] = h2_bits(__hmul2(bits_h2(q0 & mask), fac));
+            w[i][1] = h2_bits(__hmul2(bits_h2((q0 >> 8) & mask), fac));
+            w[i][2] = h2_bits(__hmul2(bits_h2(q1 & mask), fac));
+            w[i][3] = h2_bits(__hmul2(bits_h2((q1 >> 8) & mask), fac));
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            mma16816<true>(c[nt], w[0][0], w[1][0], w[0][1], w[1][1], xv[nt].x, xv[nt].y);
+            mma16816<true>(c[nt], w[0][2], w[1][2], w[0][3], w[1][3], xv[nt].z, xv[nt].w);
+          }
+        }
+      }
+    }
+  } else {
+    constexpr int PER = FMT == QF_FMT_NVFP4 ? 2 : 4;   // words of codes per scale
+    uint32_t f[2];
+    __half2 pair[2];                              // NVFP4: two scales as FP16
+#pragma unroll
+    for (int w = 0; w < LW; ++w) {
+      if (w % PER == 0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if constexpr (FMT == QF_FMT_NVFP4) {
+            if (w % 4 == 0) pair[i] = bits_h2(e4m3_f16((w ? r[i].s[0] >> 16 : r[i].s[0]) & 0xFFFFu));
+            f[i] = h2_bits(w % 4 ? __high2half2(pair[i]) : __low2half2(pair[i]));
+          } else {
+            const uint32_t u = ((r[i].s[0] >> (8 * (w / PER))) & 0xFFu) - kMxLow;
+            in = in && u <= kMxHigh - kMxLow;
+            f[i] = u * 0x04000400u + 0x04000400u;      // 2^(p + 7): exponent field p + 22 = code - 105
+          }
+        }
+      }
+      uint4 xv[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) xv[nt] = x_word<NT, LB>(x, w, at[nt], live);
+      {
+        uint32_t wa[4], wb[4];
+        e2m1_f16(r[0].q[w], wa);
+        e2m1_f16(r[1].q[w], wb);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          wa[h] = mul_f16x2(wa[h], f[0]);
+          wb[h] = mul_f16x2(wb[h], f[1]);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          mma16816<true>(c[nt], wa[0], wb[0], wa[1], wb[1], xv[nt].x, xv[nt].y);
+          mma16816<true>(c[nt], wa[2], wb[2], wa[3], wb[3], xv[nt].z, xv[nt].w);
+        }
+      }
+    }
+  }
+  return in;
+}
+
+// ---- the same step with BF16 fragments for the tokens in `bad` (all of them if a scale of the tile is out of the FP16 range),
+// weights and X read again from global memory: their sums in the final units (NVFP4: without the tensor scale), zero for the
+// other tokens. Rare, and out of line so that it costs the fast path no registers.
+
+template <int NT>
+struct Sums { float c[NT][4]; };
+
+template <int FMT, int NT, int LB>
+__device__ __noinline__ Sums<NT> step_bf16(const MvParams& p, const int* list, int first, int mt, int64_t row0, int n0, int k_step, uint32_t bad) {
+  constexpr int LW = LB / 4;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int64_t scale_pitch = FMT == QF_FMT_Q4_K ? p.K / 16 : p.K / (FMT == QF_FMT_NVFP4 ? 16 : 32);
+  Sums<NT> sum = {};
+  RowPart<FMT, LB> r[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int64_t row = row0 + min(n0 + g + 8 * i, p.N - 1);
+    load_part<FMT, LB>(r[i], p.codes + row * (p.K / 2), p.scales + row * scale_pitch, k_step, p.K, t);
+  }
+  if constexpr (FMT == QF_FMT_MXFP4)
+    if (!mx_exact<LB>(r)) bad = 0xFFFFFFFFu;
+  if (bad == 0u) return sum;
+  const __nv_bfloat16* xrow[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int m = first + min(nt * 8 + g, mt - 1);
+    xrow[nt] = p.X + static_cast<int64_t>((p.ids ? list[m] : m) / p.x_div) * p.K;
+  }
+  if constexpr (FMT == QF_FMT_Q4_K) {
+#pragma unroll
+    for (int blk = 0; blk < 8; ++blk) {
+      const int k = k_step + blk * 32 + t * 8;
+      {
+        uint32_t w[2][4];
+        float es[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const RowPart<FMT, LB>& part = r[i];
+          uint32_t v[4];
+          q4k_unpack(part.s, v);
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {                // 128 + C as BF16, minus 128: elements (0, 2), (1, 3), (4, 6), (5, 7)
+            const uint32_t n = (part.q[blk / 2 * 2 + h / 2] >> (4 * (blk & 1) + 8 * (h & 1))) & 0x000F000Fu;
+            w[i][h] = bf2_bits(__hsub2(bits_bf2(n | 0x43004300u), bits_bf2(0x43004300u)));
+          }
+          const float d = __half2float(__ushort_as_half(static_cast<unsigned short>(part.s[0] & 0xFFFFu)));
+          es[i] = d * static_cast<float>((v[blk / 4] >> (8 * (blk & 3))) & 63u);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const uint4 x = __ldg(reinterpret_cast<const uint4*>(xrow[nt] + k));
+          float c[4] = {};
+          mma16816<false>(c, w[0][0], w[1][0], w[0][1], w[1][1], __byte_perm(x.x, x.y, 0x5410), __byte_perm(x.x, x.y, 0x7632));
+          mma16816<false>(c, w[0][2], w[1][2], w[0][3], w[1][3], __byte_perm(x.z, x.w, 0x5410), __byte_perm(x.z, x.w, 0x7632));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sum.c[nt][j] = fmaf(es[j >> 1], c[j], sum.c[nt][j]);
+        }
+      }
+    }
+  } else {
+    constexpr int PER = FMT == QF_FMT_NVFP4 ? 2 : 4;
+#pragma unroll
+    for (int word = 0; word < LW; ++word) {
+      const int k = k_step + t * 2 * LB + word * 8;
+      {
+        uint32_t w[2][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t code = (r[i].s[0] >> (8 * (word / PER))) & 0xFFu, f = bf16_factor<FMT>(code);
+          e2m1_bf16(r[i].q[word], w[i]);
+          const uint32_t rest = FMT == QF_FMT_MXFP4 ? (max(code, 128u) - 1u) * 0x00800080u : 0x3F803F80u;
+#pragma unroll
+          for (int h = 0; h < 4; ++h) w[i][h] = mul_bf16x2(mul_bf16x2(w[i][h], f), rest);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          uint4 x = make_uint4(0u, 0u, 0u, 0u);
+          if (k < p.K) x = __ldg(reinterpret_cast<const uint4*>(xrow[nt] + k));
+          mma16816<false>(sum.c[nt], w[0][0], w[1][0], w[0][1], w[1][1], __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632));
+          mma16816<false>(sum.c[nt], w[0][2], w[1][2], w[0][3], w[1][3], __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
+        }
+      }
+    }
+  }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        sum.c[nt][j] = (bad >> (nt * 8 + 2 * t + (j & 1))) & 1u ? sum.c[nt][j] * (FMT == QF_FMT_NVFP4 ? 0x1p7f : 1.0f) : 0.0f;
+  return sum;
+}
+
+// Stages 8 elements: FP16 of 2^6 x. False if that is not exact for one of them (or it is a NaN).
+__device__ __forceinline__ bool stage_f16(const uint4& v, uint32_t (&h)[4]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  bool exact = true;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float lo = bf16_lo(w[i]) * kXScale, hi = bf16_hi(w[i]) * kXScale;
+    const __half2 r = __floats2half2_rn(lo, hi);
+    const float2 back = __half22float2(r);
+    exact = exact && back.x == lo && back.y == hi;
+    h[i] = h2_bits(r);
+  }
+  return exact;
+}
+
+// One step with FP16 fragments into acc; the tokens in `bad` are left out. Returns bad, or all ones if a scale of the tile is out of
+// the FP16 range.
+template <int FMT, int NT, int LB>
+__device__ __forceinline__ uint32_t add_step(const RowPart<FMT, LB> (&r)[2], uint32_t x, uint32_t sx, const uint32_t (&at)[NT], const uint32_t (&sx_at)[NT],
+                                             bool live, int t, uint32_t bad, float (&acc)[NT][4]) {
+  float c[NT][4] = {};
+  const bool in = step_f16<FMT, NT, LB>(r, x, at, live, c);
+  if constexpr (FMT == QF_FMT_MXFP4)
+    if (!__all_sync(0xFFFFFFFFu, in)) bad = 0xFFFFFFFFu;
+  if (__builtin_expect(bad != 0u, 0)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c[nt][j] = (bad >> (nt * 8 + 2 * t + (j & 1))) & 1u ? 0.0f : c[nt][j];
+  }
+  {
+    float f[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      f[i] = FMT == QF_FMT_NVFP4 ? 1.0f / kXScale : 1.0f / (kXScale * 128.0f);
+      if constexpr (FMT == QF_FMT_Q4_K) f[i] = __half2float(__ushort_as_half(static_cast<unsigned short>(r[i].s[0] & 0xFFFFu))) * (0x1p24f / kXScale);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[nt][j] = fmaf(f[j >> 1], c[nt][j], acc[nt][j]);
+  }
+  if constexpr (FMT == QF_FMT_Q4_K) {
+    // offsets: m6 [16 rows x 8 sub-blocks] times the three parts of the sums of X
+    {
+      uint32_t m6[2];
+      float dmin[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        uint32_t v[4];
+        q4k_unpack(r[i].s, v);
+        m6[i] = bf2_bits(__hsub2(bits_bf2(__byte_perm(t & 2 ? v[3] : v[2], 0x43434343u, 0x4140u + (t & 1) * 0x0202u)), bits_bf2(0x43004300u)));
+        dmin[i] = __half2float(__ushort_as_half(static_cast<unsigned short>(r[i].s[0] >> 16)));
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        uint4 b;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(sx + sx_at[nt]));
+        float m[4] = {};
+        mma16816<false>(m, m6[0], m6[1], m6[0], m6[1], b.x, b.y);
+        mma16816<false>(m, m6[0], m6[1], 0u, 0u, b.z, 0u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[nt][j] = fmaf(-dmin[j >> 1], m[j], acc[nt][j]);
+      }
+    }
+  }
+  return bad;
+}
+
+template <int FMT, int NT, int LB>
+__global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid_constant__ MvParams p) {
   constexpr int MT = 8 * NT;                           // tokens of a pass
   constexpr bool Q4K = FMT == QF_FMT_Q4_K;
-  constexpr int STEP = Q4K || WIDE ? 256 : 64;
-  constexpr int LW = Q4K || WIDE ? 8 : 2;              // 16-byte units of X per lane and step
-  extern __shared__ uint4 smem[];                      // X slice | Q4_K: sums of X per sub-block | partial sums
-  uint4* xs = smem;
-  float* sx = reinterpret_cast<float*>(smem) + p.x_words;                          // [kc / 32][MT]
-  float* red = sx + (Q4K ? p.kc / 32 * MT : 0);                                    // [kw][rows of the CTA][MT]
-  __shared__ int list[kListCap];
-  __shared__ int warp_count[kWarps];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-  const int rows_cta = kWarps / p.kw * 16;
+  constexpr int STEP = 8 * LB, TURN = kTurn<NT, LB>;
+  constexpr int LW = LB / 4;                           // 16-byte units of X per lane and step
+  constexpr int XL = LW * 16 + 16;                     // a lane's bytes of X for a step (a single token tile)
+  extern __shared__ __align__(16) uint8_t smem[];                                  // X: [kc / STEP][tokens][4 lanes][XL], or [kc / STEP][LW][MT][4 lanes][16]
+  uint4* sx = reinterpret_cast<uint4*>(smem + p.sx_at);                            // Q4_K: [kc / 256][MT][4]: sums over two sub-blocks in three BF16 parts
+  uint32_t* inexact = reinterpret_cast<uint32_t*>(smem + p.flags_at);              // [kc / STEP]: tokens whose X is not exact as staged
+  int* list = reinterpret_cast<int*>(smem + p.list_at);                            // grouped: rows of Y served
+  float* red = reinterpret_cast<float*>(smem + p.red_at);                          // split contraction: [kw][MT][rows of the CTA + 4]
+  __shared__ int warp_count[kWarpsMost];
+  const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5, g = lane >> 2, t = lane & 3;
+  constexpr int SB = TURN * kStepBytes<FMT, LB>;
+  const int ring = p.ring_at + warp * kStages * SB;    // in bytes from the start
+  const uint32_t smem0 = smem_addr(smem);
+  const int rows_cta = warps / p.kw * 16, red_pitch = rows_cta + 4;
   const int rw = warp / p.kw, kw = warp - rw * p.kw;
-  const int n_cta = blockIdx.x * rows_cta, n_warp = n_cta + rw * 16;
   const int z = blockIdx.z, nz = gridDim.z;
   const int k_begin = z * p.kz, k_end = min(p.K, k_begin + p.kz);
+  const bool whole = p.kc >= p.kz;                     // the slice of X is staged once for all row blocks
+  const bool split = p.kw > 1 || nz > 1;
 
   int e = 0;
   if (p.ids) {
@@ -166,236 +598,308 @@ __global__ void __launch_bounds__(kThreads, 2) matvec_kernel(const __grid_consta
       // slot = pair: the first pair that names an expert takes all pairs that do
       e = expert_id(p, blockIdx.y);
       bool seen = false;
-      for (int i = tid; i < static_cast<int>(blockIdx.y); i += kThreads) seen |= expert_id(p, i) == e;
+      for (int i = tid; i < static_cast<int>(blockIdx.y); i += threads) seen |= expert_id(p, i) == e;
       if (__syncthreads_or(seen) && e >= 0) return;
       if (e < 0) {
         if (z == 0)
-          for (int i = tid; i < min(rows_cta, p.N - n_cta); i += kThreads) {
-            const int64_t at = static_cast<int64_t>(blockIdx.y) * p.N + n_cta + i;
-            if (p.y_f32) static_cast<float*>(p.Y)[at] = 0.0f;
-            else static_cast<__nv_bfloat16*>(p.Y)[at] = __float2bfloat16_rn(0.0f);
-          }
+          for (int n = blockIdx.x * threads + tid; n < p.N; n += gridDim.x * threads) store_y(p, blockIdx.y, n, 0.0f);
         return;
       }
     } else {
       e = blockIdx.y;
     }
   }
-  const float tscale = FMT == QF_FMT_NVFP4 ? p.tscale[e] * 0x1p7f : 1.0f;
+  const float unit = FMT == QF_FMT_NVFP4 ? p.tscale[e] : 1.0f;
   const int64_t row0 = static_cast<int64_t>(e) * p.N;
-  const int64_t ra = row0 + min(n_warp + g, p.N - 1), rb = row0 + min(n_warp + g + 8, p.N - 1);
-  const int64_t scale_pitch = Q4K ? p.K / 16 : p.K / (FMT == QF_FMT_NVFP4 ? 16 : 32);
-  const uint8_t* ca = p.codes + ra * (p.K / 2);
-  const uint8_t* cb = p.codes + rb * (p.K / 2);
-  const uint8_t* sa = p.scales + ra * scale_pitch;
-  const uint8_t* sb = p.scales + rb * scale_pitch;
 
   for (int w0 = 0; w0 < p.M; w0 += kListCap) {
-    // the rows of Y that this CTA's weights serve
+    // the rows of Y that this CTA's weight serves
     const int w1 = min(p.M, w0 + kListCap);
     int count = w1 - w0;
     if (p.ids) {
       count = 0;
-      for (int i0 = w0; i0 < w1; i0 += kThreads) {
+      for (int i0 = w0; i0 < w1; i0 += threads) {
         const int i = i0 + tid;
         const int id = i < w1 ? expert_id(p, i) : -2;
         const bool mine = id == e;
         if (!p.by_pair && e == 0 && id == -1 && z == 0)
-          for (int n = n_cta; n < min(n_cta + rows_cta, p.N); ++n) {
-            const int64_t at = static_cast<int64_t>(i) * p.N + n;
-            if (p.y_f32) static_cast<float*>(p.Y)[at] = 0.0f;
-            else static_cast<__nv_bfloat16*>(p.Y)[at] = __float2bfloat16_rn(0.0f);
-          }
+          for (int n = blockIdx.x; n < p.N; n += gridDim.x) store_y(p, i, n, 0.0f);
         const uint32_t vote = __ballot_sync(0xFFFFFFFFu, mine);
         __syncthreads();
         if (lane == 0) warp_count[warp] = __popc(vote);
         __syncthreads();
-        int at = count + __popc(vote & ((1u << lane) - 1u));
-        for (int w = 0; w < kWarps; ++w) {
-          if (w < warp) at += warp_count[w];
+        int to = count + __popc(vote & ((1u << lane) - 1u));
+        for (int w = 0; w < warps; ++w) {
+          if (w < warp) to += warp_count[w];
           count += warp_count[w];
         }
-        if (mine) list[at] = i;
+        if (mine) list[to] = i;
       }
       __syncthreads();
     }
     for (int c0 = 0; c0 < count; c0 += MT) {
-      const int mt = min(MT, count - c0);
+      const int mt = min(MT, count - c0), first_row = p.ids ? c0 : w0 + c0;
+      // columns of the product do not meet: a lane whose token does not exist reads the last one's X instead
+      const bool live = g < mt;
+      uint32_t at[NT], sx_at[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int m = min(nt * 8 + g, mt - 1);
+        at[nt] = NT == 1 ? (m * 4 + t) * XL : (m * 4 + t) * 16;
+        sx_at[nt] = (m * 4 + t) * 16;
+      }
+      const uint32_t x_step = NT == 1 ? mt * 4 * XL : LW * MT * 64;      // bytes of X of a step
       float acc[NT][4] = {};
-      for (int kc0 = k_begin; kc0 < k_end; kc0 += p.kc) {
-        const int kc1 = min(kc0 + p.kc, k_end), steps = (kc1 - kc0 + STEP - 1) / STEP;
-        RowPart<FMT, WIDE> a[2], b[2];
-        if (kw < steps) {
-          load_part(a[0], ca, sa, kc0 + kw * STEP, p.K, t);
-          load_part(b[0], cb, sb, kc0 + kw * STEP, p.K, t);
-        }
-        __syncthreads();
-        // X slice: unit u of 8 elements of token m; zeros past the end of the contraction
-        const int units = steps * (STEP / 8);
-        for (int i = tid; i < mt * units; i += kThreads) {
-          const int m = i / units, u = i - m * units, k = kc0 + u * 8;
-          const int64_t row = p.ids ? list[c0 + m] : w0 + c0 + m;
-          uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (k < p.K) v = __ldg(reinterpret_cast<const uint4*>(p.X + row / p.x_div * p.K + k));
-          if constexpr (Q4K) {
-            xs[((u >> 2) * mt + m) * 4 + (u & 3)] = x_unit<FMT>(v);
-            const float s = bf16_lo(v.x) + bf16_hi(v.x) + bf16_lo(v.y) + bf16_hi(v.y) + (bf16_lo(v.z) + bf16_hi(v.z) + bf16_lo(v.w) + bf16_hi(v.w));
-            // units is a multiple of 32, so the four lanes of a sub-block are here together
-            const float s2 = s + __shfl_xor_sync(0xFFFFFFFFu, s, 1);
-            const float s4 = s2 + __shfl_xor_sync(0xFFFFFFFFu, s2, 2);
-            if ((u & 3) == 0) sx[(u >> 2) * MT + m] = s4;
-          } else {
-            xs[((u / (4 * LW) * LW + u % LW) * mt + m) * 4 + u / LW % 4] = x_unit<FMT>(v);
-          }
-        }
-        __syncthreads();
-        for (int s0 = kw, i = 0; s0 < steps; s0 += 2 * p.kw, i += 2) {
-#pragma unroll
-          for (int d = 0; d < 2; ++d) {
-            const int s = s0 + d * p.kw;
-            if (s < steps) {
-              if (s + p.kw < steps) {
-                load_part(a[1 - d], ca, sa, kc0 + (s + p.kw) * STEP, p.K, t);
-                load_part(b[1 - d], cb, sb, kc0 + (s + p.kw) * STEP, p.K, t);
+
+      for (int b0 = blockIdx.x; b0 < p.blocks; b0 += whole ? p.blocks : gridDim.x) {
+        for (int kc0 = k_begin; kc0 < k_end; kc0 += p.kc) {
+          const int kc1 = min(kc0 + p.kc, k_end), steps = (kc1 - kc0 + STEP - 1) / STEP;
+          const int turns = (steps + TURN - 1) / TURN;
+          const int per_tile = kw < turns ? (turns - kw + p.kw - 1) / p.kw : 0;      // turns of this warp in a tile
+          const int tiles = whole ? (p.blocks - b0 + gridDim.x - 1) / gridDim.x : 1;
+          // the first codes are under way while X is staged
+          int next_n = (b0 * (warps / p.kw) + rw) * 16, next = 0, tiles_left = per_tile ? tiles : 0;
+          Source<FMT, LB> src;
+          if (tiles_left) src.tile(p, row0, next_n, kc0 + kw * TURN * STEP, lane);
+          uint32_t sc[2];                           // LB = 8: scales of the step that is read next
+          auto start = [&](int stage) {
+            if (tiles_left > 0) {
+              src.template start<TURN>(p, smem0 + stage, TURN == 1 ? 1 : steps - (next * p.kw + kw) * TURN, lane, sc);
+              if (++next < per_tile) {
+                src.advance(p.kw * TURN * STEP);
+              } else if (--tiles_left > 0) {
+                next = 0;
+                next_n += gridDim.x * rows_cta;
+                src.tile(p, row0, next_n, kc0 + kw * TURN * STEP, lane);
               }
-              if constexpr (Q4K) {
-                const uint4 ma = make_uint4(a[d].s[0], a[d].s[1], a[d].s[2], a[d].s[3]), mb = make_uint4(b[d].s[0], b[d].s[1], b[d].s[2], b[d].s[3]);
-                const uint32_t s6a[2] = {ma.y & 0x3F3F3F3Fu, (ma.w & 0x0F0F0F0Fu) | ((ma.y >> 2) & 0x30303030u)};
-                const uint32_t m6a[2] = {ma.z & 0x3F3F3F3Fu, ((ma.w >> 4) & 0x0F0F0F0Fu) | ((ma.z >> 2) & 0x30303030u)};
-                const uint32_t s6b[2] = {mb.y & 0x3F3F3F3Fu, (mb.w & 0x0F0F0F0Fu) | ((mb.y >> 2) & 0x30303030u)};
-                const uint32_t m6b[2] = {mb.z & 0x3F3F3F3Fu, ((mb.w >> 4) & 0x0F0F0F0Fu) | ((mb.z >> 2) & 0x30303030u)};
-                const float2 fa = __half22float2(*reinterpret_cast<const __half2*>(&ma.x)), fb = __half22float2(*reinterpret_cast<const __half2*>(&mb.x));
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+          };
+          start(ring);
+          if (LB != 8) start(ring + SB);                 // LB = 8 keeps one step under way, so that its scales can wait in registers
+          for (int i = tid; i < steps; i += threads) inexact[i] = 0u;
+          __syncthreads();
+          bool exact = true;
+          // X slice: a warp takes 32 units of 8 elements of a token, four times over before it waits
+          const int units = steps * (STEP / 8), groups = (units + 31) / 32;
+          for (int task0 = warp; task0 < mt * groups; task0 += 4 * warps) {
+            uint4 q[4];
+            int m[4], v[4];
 #pragma unroll
-                for (int blk = 0; blk < 8; ++blk) {
-                  const uint32_t qa[2] = {a[d].q[blk / 2 * 2] >> (4 * (blk & 1)), a[d].q[blk / 2 * 2 + 1] >> (4 * (blk & 1))};
-                  const uint32_t qb[2] = {b[d].q[blk / 2 * 2] >> (4 * (blk & 1)), b[d].q[blk / 2 * 2 + 1] >> (4 * (blk & 1))};
-                  uint32_t wa[4], wb[4];
+            for (int i = 0; i < 4; ++i) {
+              const int task = task0 + i * warps;
+              m[i] = task / groups;
+              v[i] = (task - m[i] * groups) * 32 + lane;
+              q[i] = make_uint4(0u, 0u, 0u, 0u);
+              if (m[i] < mt && v[i] < units) {
+                const int s = v[i] / (STEP / 8), w = v[i] / 4 % LW;                  // step, word of codes, and lane v % 4
+                const int k = kc0 + 8 * (Q4K ? v[i] : s * (STEP / 8) + (v[i] & 3) * LW + w);
+                const int row = p.ids ? list[c0 + m[i]] : w0 + c0 + m[i];
+                if (k < p.K) q[i] = __ldg(reinterpret_cast<const uint4*>(p.X + static_cast<int64_t>(row / p.x_div) * p.K + k));
+              }
+            }
 #pragma unroll
-                  for (int h = 0; h < 4; ++h) {       // 128 + C as BF16, minus 128
-                    const __nv_bfloat162 off = bits_bf2(0x43004300u);
-                    wa[h] = bf2_bits(__hsub2(bits_bf2(((qa[h / 2] >> (8 * (h & 1))) & 0x000F000Fu) | 0x43004300u), off));
-                    wb[h] = bf2_bits(__hsub2(bits_bf2(((qb[h / 2] >> (8 * (h & 1))) & 0x000F000Fu) | 0x43004300u), off));
-                  }
-                  const float esa = fa.x * static_cast<float>((s6a[blk / 4] >> (8 * (blk & 3))) & 63u);
-                  const float ema = fa.y * static_cast<float>((m6a[blk / 4] >> (8 * (blk & 3))) & 63u);
-                  const float esb = fb.x * static_cast<float>((s6b[blk / 4] >> (8 * (blk & 3))) & 63u);
-                  const float emb = fb.y * static_cast<float>((m6b[blk / 4] >> (8 * (blk & 3))) & 63u);
-                  const uint32_t f0[4] = {wa[0], wb[0], wa[1], wb[1]}, f1[4] = {wa[2], wb[2], wa[3], wb[3]};
-                  const int sub = s * 8 + blk;
-#pragma unroll
-                  for (int nt = 0; nt < NT; ++nt) {
-                    uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                    if (nt * 8 + g < mt) x = xs[(sub * mt + nt * 8 + g) * 4 + t];
-                    float c[4] = {};
-                    mma16816(c, f0, x.x, x.y);
-                    mma16816(c, f1, x.z, x.w);
-                    const float2 sum = *reinterpret_cast<const float2*>(sx + sub * MT + nt * 8 + 2 * t);
-                    acc[nt][0] = fmaf(esa, c[0], fmaf(-ema, sum.x, acc[nt][0]));
-                    acc[nt][1] = fmaf(esa, c[1], fmaf(-ema, sum.y, acc[nt][1]));
-                    acc[nt][2] = fmaf(esb, c[2], fmaf(-emb, sum.x, acc[nt][2]));
-                    acc[nt][3] = fmaf(esb, c[3], fmaf(-emb, sum.y, acc[nt][3]));
-                  }
+            for (int i = 0; i < 4; ++i) {
+              if (m[i] >= mt || v[i] >= units) continue;           // for Q4_K a whole warp or none of it
+              const int s = v[i] / (STEP / 8), w = v[i] / 4 % LW;
+              uint32_t h[4];
+              if (!stage_f16(q[i], h)) {
+                exact = false;
+                atomicOr(inexact + s, 1u << m[i]);
+              }
+              uint4* to = reinterpret_cast<uint4*>(smem + s * x_step + (NT == 1 ? (m[i] * 4 + (v[i] & 3)) * XL + w * 16 : (w * MT + m[i]) * 64 + (v[i] & 3) * 16));
+              if constexpr (Q4K) {                     // elements (0, 2), (1, 3), (4, 6), (5, 7): the order of the decoded words
+                *to = make_uint4(__byte_perm(h[0], h[1], 0x5410), __byte_perm(h[0], h[1], 0x7632), __byte_perm(h[2], h[3], 0x5410), __byte_perm(h[2], h[3], 0x7632));
+                float sum = bf16_lo(q[i].x) + bf16_hi(q[i].x) + bf16_lo(q[i].y) + bf16_hi(q[i].y) +
+                            (bf16_lo(q[i].z) + bf16_hi(q[i].z) + bf16_lo(q[i].w) + bf16_hi(q[i].w));
+                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+                if ((v[i] & 3) < 3) {
+                  const __nv_bfloat16 p1 = __float2bfloat16_rn(sum), p2 = __float2bfloat16_rn(sum - __bfloat162float(p1));
+                  const __nv_bfloat16 p3 = __float2bfloat16_rn(sum - __bfloat162float(p1) - __bfloat162float(p2));
+                  reinterpret_cast<__nv_bfloat16*>(sx + (s * MT + m[i]) * 4 + w / 2)[2 * (v[i] & 3) + (w & 1)] = (v[i] & 3) == 0 ? p1 : (v[i] & 3) == 1 ? p2 : p3;
                 }
               } else {
-                constexpr int PER = FMT == QF_FMT_NVFP4 ? 2 : 4;         // words of codes per scale
-                float c[NT][4] = {};
-#pragma unroll
-                for (int w = 0; w < LW; ++w) {
-                  const uint32_t ea = (a[d].s[0] >> (8 * (w / PER))) & 0xFFu, eb = (b[d].s[0] >> (8 * (w / PER))) & 0xFFu;
-                  const uint32_t fa = fp4_factor<FMT>(ea), fb = fp4_factor<FMT>(eb);
-                  uint32_t wa[4], wb[4];
-                  e2m1_words(a[d].q[w], wa);
-                  e2m1_words(b[d].q[w], wb);
-#pragma unroll
-                  for (int h = 0; h < 4; ++h) {
-                    wa[h] = mul_bf16x2(wa[h], fa);
-                    wb[h] = mul_bf16x2(wb[h], fb);
-                  }
-                  if constexpr (FMT == QF_FMT_MXFP4) {
-                    // scales above 2^1 (weights of 8 and more): the rest of the power
-                    if (__any_sync(0xFFFFFFFFu, max(ea, eb) > 128u)) {
-                      const uint32_t ga = (max(ea, 128u) - 1u) * 0x00800080u, gb = (max(eb, 128u) - 1u) * 0x00800080u;
-#pragma unroll
-                      for (int h = 0; h < 4; ++h) {
-                        wa[h] = mul_bf16x2(wa[h], ga);
-                        wb[h] = mul_bf16x2(wb[h], gb);
-                      }
-                    }
-                  }
-                  const uint32_t f0[4] = {wa[0], wb[0], wa[1], wb[1]}, f1[4] = {wa[2], wb[2], wa[3], wb[3]};
-#pragma unroll
-                  for (int nt = 0; nt < NT; ++nt) {
-                    uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                    if (nt * 8 + g < mt) x = xs[((s * LW + w) * mt + nt * 8 + g) * 4 + t];
-                    mma16816(c[nt], f0, x.x, x.y);
-                    mma16816(c[nt], f1, x.z, x.w);
-                  }
-                }
-                // the tensor core truncates as it accumulates: a step at a time, the steps in FP32 adds
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                  for (int j = 0; j < 4; ++j) acc[nt][j] += c[nt][j];
+                *to = make_uint4(h[0], h[1], h[2], h[3]);
               }
             }
           }
+          const bool any_inexact = __syncthreads_or(!exact);
+
+          int stage = ring;
+#pragma unroll 1
+          for (int tile = 0; tile < tiles; ++tile) {
+            const int block = b0 + tile * gridDim.x;
+            uint32_t any_bad = 0u;
+            int s = kw * TURN;
+#pragma unroll 1
+            for (int j = 0; j < per_tile; ++j) {
+              // the older turn's copies are complete
+              if (LB == 8) asm volatile("cp.async.wait_group 0;" ::: "memory");
+              else asm volatile("cp.async.wait_group 1;" ::: "memory");
+              if constexpr (Q4K || LB == 32) __syncwarp();
+              const int in_turn = TURN == 1 ? 1 : min(TURN, steps - s);
+#pragma unroll 1
+              for (int u = 0; u < in_turn; ++u) {
+                RowPart<FMT, LB> r[2];
+                read_step<FMT, LB>(r, smem + stage + u * kStepBytes<FMT, LB>, lane, sc);
+                if constexpr (LB == 8) start(stage == ring ? ring + SB : ring);
+                uint32_t bad = 0u;
+                if (any_inexact) bad = inexact[s + u];
+                any_bad |= add_step<FMT, NT, LB>(r, smem0 + (s + u) * x_step, smem0 + p.sx_at + (s + u) * MT * 64, at, sx_at, live, t, bad, acc);
+              }
+              if constexpr (Q4K || LB == 32) __syncwarp();
+              if constexpr (LB != 8) start(stage);
+              stage = stage == ring ? ring + SB : ring;
+              s += p.kw * TURN;
+            }
+            // end of the tile; a warp without a turn in a split contraction meets the others here all the same
+              const int n_warp = (block * (warps / p.kw) + rw) * 16;
+              if (any_bad) {
+                for (int s = 0; s < steps; ++s) {
+                  if (s / TURN % p.kw != kw) continue;
+                  const Sums<NT> sum = step_bf16<FMT, NT, LB>(p, list, first_row, mt, row0, n_warp, kc0 + s * STEP, inexact[s]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                      for (int j = 0; j < 4; ++j) acc[nt][j] += sum.c[nt][j];
+                }
+              }
+              if (kc1 == k_end) {
+                const int n_cta = block * rows_cta;
+                if (!split) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                      for (int j = 0; j < 4; ++j) {
+                        const int n = n_warp + g + (j >> 1) * 8, m = nt * 8 + 2 * t + (j & 1);
+                        if (n < p.N && m < mt) store_y(p, p.ids ? list[c0 + m] : w0 + c0 + m, n, acc[nt][j] * unit);
+                      }
+                } else {
+                  float* mine = red + kw * MT * red_pitch + rw * 16 + g;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                      for (int j = 0; j < 4; ++j) mine[(nt * 8 + 2 * t + (j & 1)) * red_pitch + (j >> 1) * 8] = acc[nt][j];
+                  if (nz > 1) cg::this_cluster().sync();
+                  else __syncthreads();
+                  // CTA z of the cluster finishes every nz-th part of the outputs
+                  for (int m = 0; m < mt; ++m) {
+                    const int64_t row = p.ids ? list[c0 + m] : w0 + c0 + m;
+                    for (int i = tid + z * threads; i < rows_cta && n_cta + i < p.N; i += threads * nz) {
+                      float sum = 0.0f;
+                      for (int zz = 0; zz < nz; ++zz) {
+                        const float* part = (nz > 1 ? cg::this_cluster().map_shared_rank(red, zz) : red) + m * red_pitch + i;
+                        for (int k = 0; k < p.kw; ++k) sum += part[k * MT * red_pitch];
+                      }
+                      store_y(p, row, n_cta + i, sum * unit);
+                    }
+                  }
+                  if (nz > 1) cg::this_cluster().sync();
+                  else __syncthreads();
+                }
+#pragma unroll
+                  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[nt][j] = 0.0f;
+              }
+          }
+          __syncthreads();                               // the slice is read; its memory is free
         }
       }
-      // partial sums: [kw][row][token]
-      float* mine = red + (kw * rows_cta + rw * 16) * MT;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) mine[(g + (j >> 1) * 8) * MT + nt * 8 + 2 * t + (j & 1)] = acc[nt][j];
-      if (nz > 1) cg::this_cluster().sync();
-      else __syncthreads();
-      // CTA z of the cluster finishes every nz-th part of the outputs
-      for (int i = tid + z * kThreads; i < rows_cta * mt; i += kThreads * nz) {
-        const int m = i / rows_cta, r = i - m * rows_cta, n = n_cta + r;
-        if (n >= p.N) continue;
-        float sum = 0.0f;
-        for (int zz = 0; zz < nz; ++zz) {
-          const float* part = nz > 1 ? cg::this_cluster().map_shared_rank(red, zz) : red;
-          for (int k = 0; k < p.kw; ++k) sum += part[(k * rows_cta + r) * MT + m];
-        }
-        const int64_t row = p.ids ? list[c0 + m] : w0 + c0 + m;
-        if (FMT == QF_FMT_NVFP4) sum *= tscale;
-        if (p.y_f32) static_cast<float*>(p.Y)[row * p.N + n] = sum;
-        else static_cast<__nv_bfloat16*>(p.Y)[row * p.N + n] = __float2bfloat16_rn(sum);
-      }
-      if (nz > 1) cg::this_cluster().sync();
-      else __syncthreads();
     }
   }
 }
 
-template <int FMT, int NT, bool WIDE>
-cudaError_t launch(const MvParams& p, dim3 grid, size_t smem, cudaStream_t st) {
-  auto kernel = matvec_kernel<FMT, NT, WIDE>;
-  if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024)) return e;
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// How a product is cut: warps of a CTA, warps that share a tile, CTAs of a cluster that share the contraction, row blocks.
+struct Cut {
+  int warps, kw, nz;
+  int64_t kz, kc, blocks, grid_x;
+  size_t smem;
+};
+
+// Picks the cut with the least estimated time (microseconds; the constants are measured costs on this part): every SM streams
+// one step of 16 warps (32 KB of codes) in 0.75, meeting costs 0.4 in a CTA and 1.2 in a cluster, a slice of X 1 and 1 per 80 KB.
+Cut choose_cut(int64_t N, int64_t K, int slots, int mt, int nt, int stage_bytes, int x_bytes, int step, bool q4k, bool grouped, MvParams& p) {
+  Cut best{};
+  double best_time = 1e30;
+  const int64_t turns = ceil_div(K, 512);
+  for (int warps = 4; warps <= kWarpsMost; warps *= 2)
+    for (int kw = 1; kw <= warps; kw *= 2)
+      for (int nz = 1; nz <= 8; ++nz) {
+        if ((kw > 1 || nz > 1) && kw * nz > turns) continue;
+        Cut c{};
+        c.warps = warps; c.kw = kw;
+        c.kz = ceil_div(turns, nz) * 512;
+        c.nz = static_cast<int>(ceil_div(K, c.kz));
+        if (c.nz != nz) continue;
+        const int rows_cta = warps / kw * 16;
+        c.blocks = ceil_div(N, rows_cta);
+        const size_t ring = static_cast<size_t>(warps) * kStages * stage_bytes;
+        const size_t red = kw > 1 || nz > 1 ? static_cast<size_t>(kw) * 8 * nt * (rows_cta + 4) * 4 : 0;
+        const size_t fixed = ring + red + (grouped ? kListCap * 4 : 0) + 64;
+        const int64_t per_k = 512 / step * (x_bytes + 4) + (q4k ? 2 * 8 * nt * 64 : 0);           // bytes per 512 of the contraction
+        if (fixed + per_k > kSmemMost) continue;
+        const int64_t most = (kSmemMost - fixed) / per_k * 512;
+        c.kc = c.kz < most ? c.kz : most;
+        c.smem = fixed + c.kc / 512 * per_k;
+        int per_sm = kWarpsMost / warps;
+        if (per_sm > static_cast<int>(kSmemMost / (c.smem + 1024))) per_sm = static_cast<int>(kSmemMost / (c.smem + 1024));
+        if (per_sm < 1) per_sm = 1;
+        const int64_t room = static_cast<int64_t>(kNumSMs / nz) * per_sm;                       // clusters that run at a time
+        int64_t gx = room / slots;
+        if (gx < 1) gx = 1;
+        if (gx > c.blocks) gx = c.blocks;
+        c.grid_x = gx;
+        const int64_t waves = ceil_div(gx * slots, room), tiles = ceil_div(c.blocks, gx);
+        const int64_t resident = ceil_div(gx * slots * nz, kNumSMs) < per_sm ? ceil_div(gx * slots * nz, kNumSMs) : per_sm;
+        const bool whole = c.kc >= c.kz;
+        const double stage_x = 1.0 + static_cast<double>(mt) * c.kz * 2 / 8e4;
+        const double tile = ceil_div(c.kz / 512, kw) * 1.5 * warps * resident / 16 * (resident * warps < 16 ? 16.0 / (resident * warps) * (resident * warps < 8 ? 0.85 : 0.75) : 1.0) +
+                            (nz > 1 ? 1.2 : kw > 1 ? 0.4 : 0.05);
+        const double time = waves * ((whole ? stage_x : tiles * stage_x * ceil_div(c.kz, c.kc)) + tiles * tile);
+        if (time < best_time) { best_time = time; best = c; }
+      }
+  p.blocks = static_cast<int>(best.blocks);
+  p.kw = best.kw;
+  p.kz = static_cast<int>(best.kz);
+  p.kc = static_cast<int>(best.kc);
+  p.sx_at = static_cast<int>(best.kc / step * x_bytes);
+  p.flags_at = p.sx_at + (q4k ? static_cast<int>(best.kc / 256 * 8 * nt * 64) : 0);
+  p.list_at = static_cast<int>(ceil_div(p.flags_at + best.kc / step * 4, 16) * 16);
+  p.red_at = p.list_at + (grouped ? kListCap * 4 : 0);
+  const int rows_cta = best.warps / best.kw * 16;
+  p.ring_at = static_cast<int>(ceil_div(p.red_at + (best.kw > 1 || best.nz > 1 ? best.kw * 8 * nt * (rows_cta + 4) * 4 : 0), 16) * 16);
+  return best;
+}
+
+template <int FMT, int NT, int LB>
+cudaError_t launch(MvParams& p, int slots, int mt, cudaStream_t st) {
+  const Cut c = choose_cut(p.N, p.K, slots, mt, NT, kTurn<NT, LB> * kStepBytes<FMT, LB>, NT == 1 ? mt * 4 * (LB * 4 + 16) : LB * 16 * 8 * NT, 8 * LB, FMT == QF_FMT_Q4_K, p.ids != nullptr, p);
+  auto kernel = matvec_kernel<FMT, NT, LB>;
+  static bool ready[64] = {};                          // per device
+  int dev = 0;
+  if (cudaError_t e = cudaGetDevice(&dev)) return e;
+  if (dev >= 64 || !ready[dev]) {
+    if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost)) return e;
+    if (dev < 64) ready[dev] = true;
+  }
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.gridDim = dim3(static_cast<unsigned>(c.grid_x), static_cast<unsigned>(slots), static_cast<unsigned>(c.nz));
+  cfg.blockDim = dim3(32 * c.warps);
+  cfg.dynamicSmemBytes = c.smem;
   cfg.stream = st;
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = 1;
   attr.val.clusterDim.y = 1;
-  attr.val.clusterDim.z = grid.z;
+  attr.val.clusterDim.z = c.nz;
   cfg.attrs = &attr;
-  cfg.numAttrs = grid.z > 1 ? 1 : 0;
+  cfg.numAttrs = c.nz > 1 ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
-
-template <int FMT, bool WIDE>
-cudaError_t launch_nt(int nt, const MvParams& p, dim3 grid, size_t smem, cudaStream_t st) {
-  if (nt == 1) return launch<FMT, 1, WIDE>(p, grid, smem, st);
-  if (nt == 2) return launch<FMT, 2, WIDE>(p, grid, smem, st);
-  return launch<FMT, 4, WIDE>(p, grid, smem, st);
-}
-
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace
 
@@ -408,7 +912,7 @@ cudaError_t launch_matvec(const MatvecArgs& a, cudaStream_t st) {
   p.ids = a.ids;
   p.ids64 = a.ids64;
   p.Y = a.Y;
-  p.x_div = a.x_div;
+  p.x_div = static_cast<int>(a.x_div);
   p.M = static_cast<int>(a.M); p.N = static_cast<int>(a.N); p.K = static_cast<int>(a.K); p.G = a.G;
   p.y_f32 = a.y_dtype == QF_DT_F32;
   p.by_pair = a.ids && a.M <= a.G;
@@ -416,30 +920,19 @@ cudaError_t launch_matvec(const MatvecArgs& a, cudaStream_t st) {
   // tokens of a pass: few pairs per expert are the rule in the grouped product
   const int nt = a.ids ? (a.M <= 4ll * a.G || a.M <= 8 ? 1 : 4) : a.M <= 8 ? 1 : a.M <= 16 ? 2 : 4;
   const int mt = static_cast<int>(a.M < 8 * nt ? a.M : 8 * nt);
-  // Split of the contraction: enough warps for 16 on each SM, no warp with less than one step of 256. Within a CTA the warps
-  // that share a row tile multiply the traffic for X (every CTA stages its slice), so with many tokens the cluster splits.
-  const int64_t tiles = ceil_div(a.N, 16) * slots;
-  int split = 1;
-  while (split < 64 && tiles * split < 16 * kNumSMs && a.K > 256 * split) split *= 2;
-  const int kw_most = mt <= 2 ? 8 : mt <= 4 ? 4 : 2;
-  p.kw = split < kw_most ? split : kw_most;
-  int nz = split / p.kw;
-  if (nz > 8) nz = 8;
-  p.kz = static_cast<int>(ceil_div(ceil_div(a.K, nz), 256) * 256);
-  nz = static_cast<int>(ceil_div(a.K, p.kz));
-  const int kc_most = kXBytes / (2 * mt) / 256 * 256;
-  p.kc = p.kz < kc_most ? p.kz : kc_most;
-  p.x_words = mt * p.kc / 2;
-  const int rows_cta = kWarps / p.kw * 16;
-  const size_t smem = 4 * (static_cast<size_t>(p.x_words) + (a.fmt == QF_FMT_Q4_K ? p.kc / 32 * 8 * nt : 0) + kWarps * 16 * 8 * nt);
-  const dim3 grid(static_cast<unsigned>(ceil_div(a.N, rows_cta)), static_cast<unsigned>(slots), static_cast<unsigned>(nz));
-  // 32-byte loads of codes need rows that start on 32 bytes
-  const bool wide = a.K % 64 == 0 && (reinterpret_cast<uintptr_t>(a.codes) & 31u) == 0;
-  switch (a.fmt) {
-    case QF_FMT_NVFP4: return wide ? launch_nt<QF_FMT_NVFP4, true>(nt, p, grid, smem, st) : launch_nt<QF_FMT_NVFP4, false>(nt, p, grid, smem, st);
-    case QF_FMT_MXFP4: return wide ? launch_nt<QF_FMT_MXFP4, true>(nt, p, grid, smem, st) : launch_nt<QF_FMT_MXFP4, false>(nt, p, grid, smem, st);
-    default: return launch_nt<QF_FMT_Q4_K, true>(nt, p, grid, smem, st);
+  // With a contraction that is a multiple of 128, a lane takes 32 bytes of a row at a time (16 of two tiles' rows); any other one
+  // is taken 8 bytes at a time.
+  const bool wide = a.K % 128 == 0;
+  constexpr int NV = QF_FMT_NVFP4, MX = QF_FMT_MXFP4, Q4 = QF_FMT_Q4_K;
+  if (a.fmt == Q4) return nt == 1 ? launch<Q4, 1, 32>(p, slots, mt, st) : nt == 2 ? launch<Q4, 2, 32>(p, slots, mt, st) : launch<Q4, 4, 32>(p, slots, mt, st);
+  if (a.fmt == NV) {
+    if (nt == 1) return wide ? launch<NV, 1, 32>(p, slots, mt, st) : launch<NV, 1, 8>(p, slots, mt, st);
+    if (nt == 2) return wide ? launch<NV, 2, 32>(p, slots, mt, st) : launch<NV, 2, 8>(p, slots, mt, st);
+    return wide ? launch<NV, 4, 32>(p, slots, mt, st) : launch<NV, 4, 8>(p, slots, mt, st);
   }
+  if (nt == 1) return wide ? launch<MX, 1, 32>(p, slots, mt, st) : launch<MX, 1, 8>(p, slots, mt, st);
+  if (nt == 2) return wide ? launch<MX, 2, 32>(p, slots, mt, st) : launch<MX, 2, 8>(p, slots, mt, st);
+  return wide ? launch<MX, 4, 32>(p, slots, mt, st) : launch<MX, 4, 8>(p, slots, mt, st);
 }
 
 }  // namespace qf

@@ -199,6 +199,7 @@ cudaError_t launch_moe_sort(const void* ids, bool ids64, int64_t pairs, int G, i
                             int32_t* counts, cudaStream_t st) {
   const size_t smem = static_cast<size_t>(kSortWarps) * G * 4;
   auto go = [&](auto kernel, auto* p) -> cudaError_t {
+    if (smem > 48 * 1024)
     if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortWarps * QF_MOE_MAX_EXPERTS * 4)) return e;
     kernel<<<1, kSortThreads, smem, st>>>(p, pairs, G, rows, row_of, offs, counts);
     return cudaGetLastError();

@@ -118,7 +118,7 @@ def test_combine_gradient_refusals():
 def test_matvec_refusals():
     f = _call(api.lib().qf_fq_matvec, "fmt X M codes scales ts N K Y dt".split(),
               dict(fmt=api.FMT_NVFP4, X=P, M=3, codes=P, scales=P, ts=P, N=10, K=512, Y=P, dt=BF))
-    for kw in (dict(M=-1), dict(N=-1), dict(K=-16), dict(K=500), dict(fmt=api.FMT_MXFP4, K=528), dict(fmt=api.FMT_Q4_K, K=384), dict(N=1 << 31),
+    for kw in (dict(M=-1), dict(N=-1), dict(K=-16), dict(K=500), dict(fmt=api.FMT_MXFP4, K=528), dict(fmt=api.FMT_Q4_K, K=384), dict(N=1 << 31), dict(K=(1 << 26) + 256),
                dict(M=1 << 31)):
         assert f(**kw) == SHAPE, kw
     for fmt in (api.FMT_NONE, 4, -1):
