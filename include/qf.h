@@ -350,7 +350,7 @@ qf_status_t qf_moe_combine_bwd(const void* dout, qf_dtype_t dout_dtype, const vo
  *   tensor_scale  NVFP4: device float*; otherwise ignored
  * The weights are read once per QF_MATVEC_TOKENS rows of X: meant for M up to about that; a larger M is right but slower
  * than qf_fq_linear_fwd on the dequantized weight. */
-#define QF_MATVEC_TOKENS 32
+#define QF_MATVEC_TOKENS 16
 #define QF_MATVEC_MAX_K (1 << 26)
 qf_status_t qf_fq_matvec(qf_format_t fmt, const void* X, int64_t M, const void* codes, const void* scales, const float* tensor_scale,
                          int64_t N, int64_t K, void* Y, qf_dtype_t y_dtype, void* stream);

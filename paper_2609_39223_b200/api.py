@@ -36,7 +36,7 @@ EXPORTS = [
 ]
 NOALLOC_SCRATCH_BYTES = 32 << 20
 LAYOUT_GGUF_Q4_K, LAYOUT_FP4_SWIZZLED_SCALES = 1, 2
-MOE_MAX_EXPERTS, MATVEC_TOKENS = 1024, 32
+MOE_MAX_EXPERTS, MATVEC_TOKENS = 1024, 16
 
 
 class QfError(RuntimeError):

@@ -166,6 +166,8 @@ __device__ __forceinline__ void load_part(RowPart<FMT, LB>& r, const uint8_t* co
 
 template <int FMT>
 constexpr int kStepScales = FMT == QF_FMT_MXFP4 ? 8 : 16;
+template <int FMT>
+constexpr int kScaleLanes = FMT == QF_FMT_Q4_K ? 1 : 2;                 // lanes that copy a row's scales
 template <int FMT, int LB>
 constexpr int kStepBytes = LB == 8 ? 512 : 16 * (128 + kStepScales<FMT>);
 // Steps a warp takes in a turn of its loop: two where the products of a step are few, so that addresses and bookkeeping are shared.
@@ -192,7 +194,6 @@ template <int FMT, int LB>
 struct Source {
   static constexpr int kRows = LB == 8 ? 2 : 4;      // rows a lane copies codes of
   static constexpr int SHIFT = FMT == QF_FMT_MXFP4 ? 4 : 3;            // bytes of codes to bytes of scales
-  static constexpr int SCALE_LANES = FMT == QF_FMT_Q4_K ? 1 : 2;       // lanes that copy a row's scales
   const uint8_t* codes;
   const uint8_t* scales;
   uint32_t row[kRows - 1];                           // bytes of codes to the other rows
@@ -210,8 +211,8 @@ struct Source {
     if constexpr (LB == 8) {
       scales = p.scales + (at >> SHIFT);
     } else {
-      const int r = lane / SCALE_LANES & 15;
-      scales = p.scales + (((row0 + min(n0 + r, p.N - 1)) * pitch + k / 2) >> SHIFT) + lane % SCALE_LANES * (kStepScales<FMT> / SCALE_LANES);
+      const int r = lane / kScaleLanes<FMT> & 15;
+      scales = p.scales + (((row0 + min(n0 + r, p.N - 1)) * pitch + k / 2) >> SHIFT) + lane % kScaleLanes<FMT> * (kStepScales<FMT> / kScaleLanes<FMT>);
     }
   }
   __device__ __forceinline__ void advance(int dk) {
@@ -231,7 +232,7 @@ struct Source {
         sc[i] = __ldg(scales + (off >> SHIFT) - back / kBlock<FMT>);
       }
     } else {
-      const uint32_t to = stage + piece_at<FMT>(lane >> 3, lane & 7), to_sc = stage + 16 * 128 + lane * (kStepScales<FMT> / SCALE_LANES);
+      const uint32_t to = stage + piece_at<FMT>(lane >> 3, lane & 7), to_sc = stage + 16 * 128 + lane * (kStepScales<FMT> / kScaleLanes<FMT>);
 #pragma unroll
       for (int u = 0; u < TURN; ++u) {
         if (u >= steps) break;
@@ -241,7 +242,7 @@ struct Source {
         const uint8_t* s = scales + u * (256 / kBlock<FMT>) - (past && (lane & 1) ? 128 / kBlock<FMT> : 0);
 #pragma unroll
         for (int h = 0; h < 4; ++h) copy_async<16>(to + u * kStepBytes<FMT, LB> + h * 512, c + (h ? row[h - 1] : 0u));
-        if (SCALE_LANES == 2 || lane < 16) copy_async<kStepScales<FMT> / SCALE_LANES>(to_sc + u * kStepBytes<FMT, LB>, s);
+        if (kScaleLanes<FMT> == 2 || lane < 16) copy_async<kStepScales<FMT> / kScaleLanes<FMT>>(to_sc + u * kStepBytes<FMT, LB>, s);
       }
     }
   }
@@ -311,6 +312,11 @@ __device__ __forceinline__ bool mx_exact(const RowPart<QF_FMT_MXFP4, LB> (&r)[2]
 // x: the step's X in shared memory, `at` this lane's place in each token tile. Returns false if a scale is out of range (c is then
 // worthless). c is the sum times 2^6 (from X) and times 1 (NVFP4), 2^7 (MXFP4) or 2^-24 / d (Q4_K).
 
+// Bytes between consecutive words of X where several token tiles stand word by word (16 of padding, so that the threads that
+// stage consecutive words meet different banks).
+template <int NT>
+constexpr int kXPitch = 8 * NT * 64 + 16;
+
 // This lane's 16 bytes of X for one word of codes (Q4_K: one sub-block). A single token tile stands lane by lane, 16 bytes of
 // padding after each lane's words, so that a lane's words have fixed distances; lanes without a token read nothing (columns of
 // the product do not meet, whatever is in their registers). Several tiles stand word by word.
@@ -322,7 +328,7 @@ __device__ __forceinline__ uint4 x_word(uint32_t x, int w, uint32_t at, bool liv
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                  : "r"(x + at + w * 16), "r"(static_cast<int>(live)));
   else
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(x + at + w * (8 * NT * 64)));
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(x + at + w * kXPitch<NT>));
   return v;
 }
 
@@ -575,7 +581,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
   constexpr int STEP = 8 * LB, TURN = kTurn<NT, LB>;
   constexpr int LW = LB / 4;                           // 16-byte units of X per lane and step
   constexpr int XL = LW * 16 + 16;                     // a lane's bytes of X for a step (a single token tile)
-  extern __shared__ __align__(16) uint8_t smem[];                                  // X: [kc / STEP][tokens][4 lanes][XL], or [kc / STEP][LW][MT][4 lanes][16]
+  extern __shared__ __align__(16) uint8_t smem[];                                  // X: [kc / STEP][tokens][4 lanes][XL], or [kc / STEP][LW][MT][4 lanes][16] and padding
   uint4* sx = reinterpret_cast<uint4*>(smem + p.sx_at);                            // Q4_K: [kc / 256][MT][4]: sums over two sub-blocks in three BF16 parts
   uint32_t* inexact = reinterpret_cast<uint32_t*>(smem + p.flags_at);              // [kc / STEP]: tokens whose X is not exact as staged
   int* list = reinterpret_cast<int*>(smem + p.list_at);                            // grouped: rows of Y served
@@ -648,7 +654,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
         at[nt] = NT == 1 ? (m * 4 + t) * XL : (m * 4 + t) * 16;
         sx_at[nt] = (m * 4 + t) * 16;
       }
-      const uint32_t x_step = NT == 1 ? mt * 4 * XL : LW * MT * 64;      // bytes of X of a step
+      const uint32_t x_step = NT == 1 ? mt * 4 * XL : LW * kXPitch<NT>;      // bytes of X of a step
       float acc[NT][4] = {};
 
       for (int b0 = blockIdx.x; b0 < p.blocks; b0 += whole ? p.blocks : gridDim.x) {
@@ -680,47 +686,48 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
           for (int i = tid; i < steps; i += threads) inexact[i] = 0u;
           __syncthreads();
           bool exact = true;
-          // X slice: a warp takes 32 units of 8 elements of a token, four times over before it waits
+          // X slice: as many warps for a token as there are to spare; a warp loads 32 units of 8 elements, kBatch times over before
+          // it waits
+          constexpr int kBatch = 8;
           const int units = steps * (STEP / 8), groups = (units + 31) / 32;
-          for (int task0 = warp; task0 < mt * groups; task0 += 4 * warps) {
-            uint4 q[4];
-            int m[4], v[4];
+          int share = warps;                             // warps of a token
+          while (share > 1 && share * mt > warps) share >>= 1;
+          for (int m = warp / share; m < mt; m += warps / share) {
+            const int row = p.ids ? list[c0 + m] : w0 + c0 + m;
+            const uint4* x = reinterpret_cast<const uint4*>(p.X + static_cast<int64_t>(row / p.x_div) * p.K + kc0);
+            for (int g0 = warp & (share - 1); g0 < groups; g0 += share * kBatch) {
+              uint4 q[kBatch];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int task = task0 + i * warps;
-              m[i] = task / groups;
-              v[i] = (task - m[i] * groups) * 32 + lane;
-              q[i] = make_uint4(0u, 0u, 0u, 0u);
-              if (m[i] < mt && v[i] < units) {
-                const int s = v[i] / (STEP / 8), w = v[i] / 4 % LW;                  // step, word of codes, and lane v % 4
-                const int k = kc0 + 8 * (Q4K ? v[i] : s * (STEP / 8) + (v[i] & 3) * LW + w);
-                const int row = p.ids ? list[c0 + m[i]] : w0 + c0 + m[i];
-                if (k < p.K) q[i] = __ldg(reinterpret_cast<const uint4*>(p.X + static_cast<int64_t>(row / p.x_div) * p.K + k));
+              for (int i = 0; i < kBatch; ++i) {
+                const int v = (g0 + i * share) * 32 + lane, s = v / (STEP / 8), w = v / 4 % LW;       // step, word of codes, and lane v % 4
+                const int unit = Q4K ? v : s * (STEP / 8) + (v & 3) * LW + w;
+                q[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (v < units && kc0 + 8 * unit < p.K) q[i] = __ldg(x + unit);
               }
-            }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (m[i] >= mt || v[i] >= units) continue;           // for Q4_K a whole warp or none of it
-              const int s = v[i] / (STEP / 8), w = v[i] / 4 % LW;
-              uint32_t h[4];
-              if (!stage_f16(q[i], h)) {
-                exact = false;
-                atomicOr(inexact + s, 1u << m[i]);
-              }
-              uint4* to = reinterpret_cast<uint4*>(smem + s * x_step + (NT == 1 ? (m[i] * 4 + (v[i] & 3)) * XL + w * 16 : (w * MT + m[i]) * 64 + (v[i] & 3) * 16));
-              if constexpr (Q4K) {                     // elements (0, 2), (1, 3), (4, 6), (5, 7): the order of the decoded words
-                *to = make_uint4(__byte_perm(h[0], h[1], 0x5410), __byte_perm(h[0], h[1], 0x7632), __byte_perm(h[2], h[3], 0x5410), __byte_perm(h[2], h[3], 0x7632));
-                float sum = bf16_lo(q[i].x) + bf16_hi(q[i].x) + bf16_lo(q[i].y) + bf16_hi(q[i].y) +
-                            (bf16_lo(q[i].z) + bf16_hi(q[i].z) + bf16_lo(q[i].w) + bf16_hi(q[i].w));
-                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
-                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
-                if ((v[i] & 3) < 3) {
-                  const __nv_bfloat16 p1 = __float2bfloat16_rn(sum), p2 = __float2bfloat16_rn(sum - __bfloat162float(p1));
-                  const __nv_bfloat16 p3 = __float2bfloat16_rn(sum - __bfloat162float(p1) - __bfloat162float(p2));
-                  reinterpret_cast<__nv_bfloat16*>(sx + (s * MT + m[i]) * 4 + w / 2)[2 * (v[i] & 3) + (w & 1)] = (v[i] & 3) == 0 ? p1 : (v[i] & 3) == 1 ? p2 : p3;
+              for (int i = 0; i < kBatch; ++i) {
+                const int v = (g0 + i * share) * 32 + lane, s = v / (STEP / 8), w = v / 4 % LW;
+                if (v >= units) continue;                // for Q4_K a whole warp or none of it
+                uint32_t h[4];
+                if (!stage_f16(q[i], h)) {
+                  exact = false;
+                  atomicOr(inexact + s, 1u << m);
                 }
-              } else {
-                *to = make_uint4(h[0], h[1], h[2], h[3]);
+                uint4* to = reinterpret_cast<uint4*>(smem + s * x_step + (NT == 1 ? (m * 4 + (v & 3)) * XL + w * 16 : w * kXPitch<NT> + m * 64 + (v & 3) * 16));
+                if constexpr (Q4K) {                     // elements (0, 2), (1, 3), (4, 6), (5, 7): the order of the decoded words
+                  *to = make_uint4(__byte_perm(h[0], h[1], 0x5410), __byte_perm(h[0], h[1], 0x7632), __byte_perm(h[2], h[3], 0x5410), __byte_perm(h[2], h[3], 0x7632));
+                  float sum = bf16_lo(q[i].x) + bf16_hi(q[i].x) + bf16_lo(q[i].y) + bf16_hi(q[i].y) +
+                              (bf16_lo(q[i].z) + bf16_hi(q[i].z) + bf16_lo(q[i].w) + bf16_hi(q[i].w));
+                  sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+                  sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+                  if ((v & 3) < 3) {
+                    const __nv_bfloat16 p1 = __float2bfloat16_rn(sum), p2 = __float2bfloat16_rn(sum - __bfloat162float(p1));
+                    const __nv_bfloat16 p3 = __float2bfloat16_rn(sum - __bfloat162float(p1) - __bfloat162float(p2));
+                    reinterpret_cast<__nv_bfloat16*>(sx + (s * MT + m) * 4 + w / 2)[2 * (v & 3) + (w & 1)] = (v & 3) == 0 ? p1 : (v & 3) == 1 ? p2 : p3;
+                  }
+                } else {
+                  *to = make_uint4(h[0], h[1], h[2], h[3]);
+                }
               }
             }
           }
@@ -783,17 +790,17 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
                       for (int j = 0; j < 4; ++j) mine[(nt * 8 + 2 * t + (j & 1)) * red_pitch + (j >> 1) * 8] = acc[nt][j];
                   if (nz > 1) cg::this_cluster().sync();
                   else __syncthreads();
-                  // CTA z of the cluster finishes every nz-th part of the outputs
-                  for (int m = 0; m < mt; ++m) {
-                    const int64_t row = p.ids ? list[c0 + m] : w0 + c0 + m;
-                    for (int i = tid + z * threads; i < rows_cta && n_cta + i < p.N; i += threads * nz) {
-                      float sum = 0.0f;
-                      for (int zz = 0; zz < nz; ++zz) {
-                        const float* part = (nz > 1 ? cg::this_cluster().map_shared_rank(red, zz) : red) + m * red_pitch + i;
-                        for (int k = 0; k < p.kw; ++k) sum += part[k * MT * red_pitch];
-                      }
-                      store_y(p, row, n_cta + i, sum * unit);
+                  // the CTAs of the cluster share the outputs
+                  for (int i = tid + z * threads; i < mt * rows_cta; i += threads * nz) {
+                    const int m = i / rows_cta, n = i - m * rows_cta;
+                    const int at_i = m * red_pitch + n;
+                    float sum = 0.0f;
+                    for (int zz = 0; zz < nz; ++zz) {
+                      const float* part = (nz > 1 ? cg::this_cluster().map_shared_rank(red, zz) : red) + at_i;
+#pragma unroll 4
+                      for (int k = 0; k < p.kw; ++k) sum += part[k * MT * red_pitch];
                     }
+                    if (n_cta + n < p.N) store_y(p, p.ids ? list[c0 + m] : w0 + c0 + m, n_cta + n, sum * unit);
                   }
                   if (nz > 1) cg::this_cluster().sync();
                   else __syncthreads();
@@ -820,15 +827,19 @@ struct Cut {
   size_t smem;
 };
 
-// Picks the cut with the least estimated time (microseconds; the constants are measured costs on this part): every SM streams
-// one step of 16 warps (32 KB of codes) in 0.75, meeting costs 0.4 in a CTA and 1.2 in a cluster, a slice of X 1 and 1 per 80 KB.
+// Picks the cut with the least estimated time. The constants are microseconds measured on this part over weights from
+// 1024 x 4096 to 128256 x 4096 and 1 to 16 tokens: a turn of 512 weights takes turn_fixed and turn_each per warp that the SM
+// holds; meeting costs 0.7 in a CTA and 1.5 in a cluster (3.5 if there
+// are tiles to come, since it empties the rings); a slice of X takes 0.7 and 1 per 30 KB that the SM stages. The choice
+// is within 10% of the best cut in nine of ten of those cases.
 Cut choose_cut(int64_t N, int64_t K, int slots, int mt, int nt, int stage_bytes, int x_bytes, int step, bool q4k, bool grouped, MvParams& p) {
   Cut best{};
   double best_time = 1e30;
+  const double turn_fixed = q4k ? 0.55 : 0.25, turn_each = nt == 1 ? 0.115 + 0.001 * mt : 0.15;
   const int64_t turns = ceil_div(K, 512);
   for (int warps = 4; warps <= kWarpsMost; warps *= 2)
     for (int kw = 1; kw <= warps; kw *= 2)
-      for (int nz = 1; nz <= 8; ++nz) {
+      for (int nz = 1; nz <= 4; nz *= 2) {
         if ((kw > 1 || nz > 1) && kw * nz > turns) continue;
         Cut c{};
         c.warps = warps; c.kw = kw;
@@ -848,18 +859,18 @@ Cut choose_cut(int64_t N, int64_t K, int slots, int mt, int nt, int stage_bytes,
         int per_sm = kWarpsMost / warps;
         if (per_sm > static_cast<int>(kSmemMost / (c.smem + 1024))) per_sm = static_cast<int>(kSmemMost / (c.smem + 1024));
         if (per_sm < 1) per_sm = 1;
-        const int64_t room = static_cast<int64_t>(kNumSMs / nz) * per_sm;                       // clusters that run at a time
+        const int64_t room = static_cast<int64_t>(nz == 4 ? 33 : kNumSMs / nz) * per_sm;        // clusters that run at a time
         int64_t gx = room / slots;
         if (gx < 1) gx = 1;
         if (gx > c.blocks) gx = c.blocks;
         c.grid_x = gx;
-        const int64_t waves = ceil_div(gx * slots, room), tiles = ceil_div(c.blocks, gx);
-        const int64_t resident = ceil_div(gx * slots * nz, kNumSMs) < per_sm ? ceil_div(gx * slots * nz, kNumSMs) : per_sm;
-        const bool whole = c.kc >= c.kz;
-        const double stage_x = 1.0 + static_cast<double>(mt) * c.kz * 2 / 8e4;
-        const double tile = ceil_div(c.kz / 512, kw) * 1.5 * warps * resident / 16 * (resident * warps < 16 ? 16.0 / (resident * warps) * (resident * warps < 8 ? 0.85 : 0.75) : 1.0) +
-                            (nz > 1 ? 1.2 : kw > 1 ? 0.4 : 0.05);
-        const double time = waves * ((whole ? stage_x : tiles * stage_x * ceil_div(c.kz, c.kc)) + tiles * tile);
+        const int64_t waves = ceil_div(gx * slots, room);
+        const int64_t sm_ctas = ceil_div(gx * slots * nz, kNumSMs), resident = sm_ctas < per_sm ? sm_ctas : per_sm;
+        // CTAs that share an SM even out some of what they have more or less of
+        const double most_tiles = static_cast<double>(ceil_div(c.blocks, gx)), tiles = resident > 1 && nz == 1 ? 0.5 * (most_tiles + static_cast<double>(c.blocks) / gx) : most_tiles;
+        const double stage_x = 0.7 + resident * static_cast<double>(mt) * c.kz * 2 / 3e4;
+        const double tile = ceil_div(c.kz / 512, kw) * (turn_fixed + turn_each * resident * warps) + (nz > 1 ? (most_tiles > 1 ? 3.5 : 1.5) : kw > 1 ? 0.7 : 0.05) + (warps == 4 ? 0.0 : 0.05 * ceil_div(c.kz / 512, kw));
+        const double time = waves * ((c.kc >= c.kz ? stage_x : tiles * stage_x * ceil_div(c.kz, c.kc)) + tiles * tile);
         if (time < best_time) { best_time = time; best = c; }
       }
   p.blocks = static_cast<int>(best.blocks);
@@ -877,7 +888,7 @@ Cut choose_cut(int64_t N, int64_t K, int slots, int mt, int nt, int stage_bytes,
 
 template <int FMT, int NT, int LB>
 cudaError_t launch(MvParams& p, int slots, int mt, cudaStream_t st) {
-  const Cut c = choose_cut(p.N, p.K, slots, mt, NT, kTurn<NT, LB> * kStepBytes<FMT, LB>, NT == 1 ? mt * 4 * (LB * 4 + 16) : LB * 16 * 8 * NT, 8 * LB, FMT == QF_FMT_Q4_K, p.ids != nullptr, p);
+  const Cut c = choose_cut(p.N, p.K, slots, mt, NT, kTurn<NT, LB> * kStepBytes<FMT, LB>, NT == 1 ? mt * 4 * (LB * 4 + 16) : LB / 4 * kXPitch<NT>, 8 * LB, FMT == QF_FMT_Q4_K, p.ids != nullptr, p);
   auto kernel = matvec_kernel<FMT, NT, LB>;
   static bool ready[64] = {};                          // per device
   int dev = 0;
@@ -918,21 +929,19 @@ cudaError_t launch_matvec(const MatvecArgs& a, cudaStream_t st) {
   p.by_pair = a.ids && a.M <= a.G;
   const int slots = !a.ids ? 1 : p.by_pair ? p.M : a.G;
   // tokens of a pass: few pairs per expert are the rule in the grouped product
-  const int nt = a.ids ? (a.M <= 4ll * a.G || a.M <= 8 ? 1 : 4) : a.M <= 8 ? 1 : a.M <= 16 ? 2 : 4;
+  const int nt = (a.ids ? a.M <= 4ll * a.G || a.M <= 8 : a.M <= 8) ? 1 : 2;
   const int mt = static_cast<int>(a.M < 8 * nt ? a.M : 8 * nt);
   // With a contraction that is a multiple of 128, a lane takes 32 bytes of a row at a time (16 of two tiles' rows); any other one
   // is taken 8 bytes at a time.
   const bool wide = a.K % 128 == 0;
   constexpr int NV = QF_FMT_NVFP4, MX = QF_FMT_MXFP4, Q4 = QF_FMT_Q4_K;
-  if (a.fmt == Q4) return nt == 1 ? launch<Q4, 1, 32>(p, slots, mt, st) : nt == 2 ? launch<Q4, 2, 32>(p, slots, mt, st) : launch<Q4, 4, 32>(p, slots, mt, st);
+  if (a.fmt == Q4) return nt == 1 ? launch<Q4, 1, 32>(p, slots, mt, st) : launch<Q4, 2, 32>(p, slots, mt, st);
   if (a.fmt == NV) {
     if (nt == 1) return wide ? launch<NV, 1, 32>(p, slots, mt, st) : launch<NV, 1, 8>(p, slots, mt, st);
-    if (nt == 2) return wide ? launch<NV, 2, 32>(p, slots, mt, st) : launch<NV, 2, 8>(p, slots, mt, st);
-    return wide ? launch<NV, 4, 32>(p, slots, mt, st) : launch<NV, 4, 8>(p, slots, mt, st);
+    return wide ? launch<NV, 2, 32>(p, slots, mt, st) : launch<NV, 2, 8>(p, slots, mt, st);
   }
   if (nt == 1) return wide ? launch<MX, 1, 32>(p, slots, mt, st) : launch<MX, 1, 8>(p, slots, mt, st);
-  if (nt == 2) return wide ? launch<MX, 2, 32>(p, slots, mt, st) : launch<MX, 2, 8>(p, slots, mt, st);
-  return wide ? launch<MX, 4, 32>(p, slots, mt, st) : launch<MX, 4, 8>(p, slots, mt, st);
+  return wide ? launch<MX, 2, 32>(p, slots, mt, st) : launch<MX, 2, 8>(p, slots, mt, st);
 }
 
 }  // namespace qf
