@@ -641,6 +641,7 @@ qf_status_t qf_moe_sort(const void* expert_ids, qf_dtype_t ids_dtype, int64_t to
 static qf_status_t check_moe(int64_t tokens, int top_k, int64_t hidden, int64_t rows_padded) {
   if (!moe_shape_ok(tokens, top_k, 1) || rows_padded < 0 || rows_padded > INT32_MAX) return QF_ERR_SHAPE;
   if (hidden < 0 || hidden % 8 || hidden > (1ll << 28)) return QF_ERR_SHAPE;
+  if (tokens * hidden > (1ll << 40)) return QF_ERR_SHAPE;          // CTAs of the token kernels are numbered in 31 bits
   return QF_OK;
 }
 static MoeTable moe_table(const int32_t* row_of, const int32_t* offs, const int32_t* counts, int G, int64_t rows, int64_t tokens,

@@ -62,7 +62,7 @@ def test_sort_refusals():
 def test_dispatch_refusals():
     f = _call(api.lib().qf_moe_dispatch, "x tokens k H row_of offs counts G rows xs".split(),
               dict(x=P, tokens=10, k=2, H=64, row_of=P, offs=P, counts=P, G=4, rows=512, xs=P))
-    for kw in (dict(tokens=-1), dict(k=0), dict(H=-8), dict(H=12), dict(H=1 << 29), dict(G=0), dict(G=2000), dict(rows=130), dict(rows=-128)):
+    for kw in (dict(tokens=-1), dict(k=0), dict(H=-8), dict(H=12), dict(H=1 << 29), dict(tokens=1 << 24, k=1, H=1 << 20), dict(G=0), dict(G=2000), dict(rows=130), dict(rows=-128)):
         assert f(**kw) == SHAPE, kw
     for name in ("x", "row_of", "offs", "counts", "xs"):
         assert f(**{name: None}) == NULL, name
