@@ -25,6 +25,7 @@
 //  * Rows are cut into tiles of 16 or 32 for a warp; the contraction is split over the warps of a CTA and over the CTAs of a
 //    cluster where there are too few tiles to keep every SM loading; the parts meet in (distributed) shared memory in a fixed order.
 #include <cooperative_groups.h>
+#include <math.h>
 
 #include "qf_common.cuh"
 
@@ -421,7 +422,7 @@ template <int NT>
 struct Sums { float c[NT][4]; };
 
 template <int FMT, int NT, int LB>
-__device__ __noinline__ Sums<NT> step_bf16(const MvParams& p, const int* list, int first, int mt, int64_t row0, int n0, int k_step, uint32_t bad) {
+__device__ __noinline__ Sums<NT> step_bf16(const MvParams& p, const uint16_t* list, int w0, int c0, int mt, int64_t row0, int n0, int k_step, uint32_t bad) {
   constexpr int LW = LB / 4;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int64_t scale_pitch = FMT == QF_FMT_Q4_K ? p.K / 16 : p.K / (FMT == QF_FMT_NVFP4 ? 16 : 32);
@@ -438,8 +439,8 @@ __device__ __noinline__ Sums<NT> step_bf16(const MvParams& p, const int* list, i
   const __nv_bfloat16* xrow[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int m = first + min(nt * 8 + g, mt - 1);
-    xrow[nt] = p.X + static_cast<int64_t>((p.ids ? list[m] : m) / p.x_div) * p.K;
+    const int m = c0 + min(nt * 8 + g, mt - 1);
+    xrow[nt] = p.X + static_cast<int64_t>((w0 + (p.ids ? list[m] : m)) / p.x_div) * p.K;
   }
   if constexpr (FMT == QF_FMT_Q4_K) {
 #pragma unroll
@@ -584,7 +585,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
   extern __shared__ __align__(16) uint8_t smem[];                                  // X: [kc / STEP][tokens][4 lanes][XL], or [kc / STEP][LW][MT][4 lanes][16] and padding
   uint4* sx = reinterpret_cast<uint4*>(smem + p.sx_at);                            // Q4_K: [kc / 256][MT][4]: sums over two sub-blocks in three BF16 parts
   uint32_t* inexact = reinterpret_cast<uint32_t*>(smem + p.flags_at);              // [kc / STEP]: tokens whose X is not exact as staged
-  int* list = reinterpret_cast<int*>(smem + p.list_at);                            // grouped: rows of Y served
+  uint16_t* list = reinterpret_cast<uint16_t*>(smem + p.list_at);                  // grouped: rows of Y served, from w0
   float* red = reinterpret_cast<float*>(smem + p.red_at);                          // split contraction: [kw][MT][rows of the CTA + 4]
   __shared__ int warp_count[kWarpsMost];
   const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5, g = lane >> 2, t = lane & 3;
@@ -639,12 +640,12 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
           if (w < warp) to += warp_count[w];
           count += warp_count[w];
         }
-        if (mine) list[to] = i;
+        if (mine) list[to] = static_cast<uint16_t>(i - w0);
       }
       __syncthreads();
     }
     for (int c0 = 0; c0 < count; c0 += MT) {
-      const int mt = min(MT, count - c0), first_row = p.ids ? c0 : w0 + c0;
+      const int mt = min(MT, count - c0);
       // columns of the product do not meet: a lane whose token does not exist reads the last one's X instead
       const bool live = g < mt;
       uint32_t at[NT], sx_at[NT];
@@ -693,7 +694,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
           int share = warps;                             // warps of a token
           while (share > 1 && share * mt > warps) share >>= 1;
           for (int m = warp / share; m < mt; m += warps / share) {
-            const int row = p.ids ? list[c0 + m] : w0 + c0 + m;
+            const int row = w0 + (p.ids ? list[c0 + m] : c0 + m);
             const uint4* x = reinterpret_cast<const uint4*>(p.X + static_cast<int64_t>(row / p.x_div) * p.K + kc0);
             for (int g0 = warp & (share - 1); g0 < groups; g0 += share * kBatch) {
               uint4 q[kBatch];
@@ -765,7 +766,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
               if (any_bad) {
                 for (int s = 0; s < steps; ++s) {
                   if (s / TURN % p.kw != kw) continue;
-                  const Sums<NT> sum = step_bf16<FMT, NT, LB>(p, list, first_row, mt, row0, n_warp, kc0 + s * STEP, inexact[s]);
+                  const Sums<NT> sum = step_bf16<FMT, NT, LB>(p, list, w0, c0, mt, row0, n_warp, kc0 + s * STEP, inexact[s]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -780,7 +781,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
 #pragma unroll
                       for (int j = 0; j < 4; ++j) {
                         const int n = n_warp + g + (j >> 1) * 8, m = nt * 8 + 2 * t + (j & 1);
-                        if (n < p.N && m < mt) store_y(p, p.ids ? list[c0 + m] : w0 + c0 + m, n, acc[nt][j] * unit);
+                        if (n < p.N && m < mt) store_y(p, w0 + (p.ids ? list[c0 + m] : c0 + m), n, acc[nt][j] * unit);
                       }
                 } else {
                   float* mine = red + kw * MT * red_pitch + rw * 16 + g;
@@ -800,7 +801,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
 #pragma unroll 4
                       for (int k = 0; k < p.kw; ++k) sum += part[k * MT * red_pitch];
                     }
-                    if (n_cta + n < p.N) store_y(p, p.ids ? list[c0 + m] : w0 + c0 + m, n_cta + n, sum * unit);
+                    if (n_cta + n < p.N) store_y(p, w0 + (p.ids ? list[c0 + m] : c0 + m), n_cta + n, sum * unit);
                   }
                   if (nz > 1) cg::this_cluster().sync();
                   else __syncthreads();
@@ -832,7 +833,7 @@ struct Cut {
 // holds; meeting costs 0.7 in a CTA and 1.5 in a cluster (3.5 if there
 // are tiles to come, since it empties the rings); a slice of X takes 0.7 and 1 per 30 KB that the SM stages. The choice
 // is within 10% of the best cut in nine of ten of those cases.
-Cut choose_cut(int64_t N, int64_t K, int slots, int mt, int nt, int stage_bytes, int x_bytes, int step, bool q4k, bool grouped, MvParams& p) {
+Cut choose_cut(int64_t N, int64_t K, double slots, int mt, int nt, int stage_bytes, int x_bytes, int step, bool q4k, bool grouped, MvParams& p) {
   Cut best{};
   double best_time = 1e30;
   const double turn_fixed = q4k ? 0.55 : 0.25, turn_each = nt == 1 ? 0.115 + 0.001 * mt : 0.15;
@@ -850,7 +851,7 @@ Cut choose_cut(int64_t N, int64_t K, int slots, int mt, int nt, int stage_bytes,
         c.blocks = ceil_div(N, rows_cta);
         const size_t ring = static_cast<size_t>(warps) * kStages * stage_bytes;
         const size_t red = kw > 1 || nz > 1 ? static_cast<size_t>(kw) * 8 * nt * (rows_cta + 4) * 4 : 0;
-        const size_t fixed = ring + red + (grouped ? kListCap * 4 : 0) + 64;
+        const size_t fixed = ring + red + (grouped ? kListCap * 2 : 0) + 64;
         const int64_t per_k = 512 / step * (x_bytes + 4) + (q4k ? 2 * 8 * nt * 64 : 0);           // bytes per 512 of the contraction
         if (fixed + per_k > kSmemMost) continue;
         const int64_t most = (kSmemMost - fixed) / per_k * 512;
@@ -860,12 +861,12 @@ Cut choose_cut(int64_t N, int64_t K, int slots, int mt, int nt, int stage_bytes,
         if (per_sm > static_cast<int>(kSmemMost / (c.smem + 1024))) per_sm = static_cast<int>(kSmemMost / (c.smem + 1024));
         if (per_sm < 1) per_sm = 1;
         const int64_t room = static_cast<int64_t>(nz == 4 ? 33 : kNumSMs / nz) * per_sm;        // clusters that run at a time
-        int64_t gx = room / slots;
+        int64_t gx = static_cast<int64_t>(room / slots);
         if (gx < 1) gx = 1;
         if (gx > c.blocks) gx = c.blocks;
         c.grid_x = gx;
-        const int64_t waves = ceil_div(gx * slots, room);
-        const int64_t sm_ctas = ceil_div(gx * slots * nz, kNumSMs), resident = sm_ctas < per_sm ? sm_ctas : per_sm;
+        const int64_t grid = static_cast<int64_t>(gx * slots + 0.5), waves = ceil_div(grid, room);
+        const int64_t sm_ctas = ceil_div(grid * nz, kNumSMs), resident = sm_ctas < per_sm ? sm_ctas : per_sm;
         // CTAs that share an SM even out some of what they have more or less of
         const double most_tiles = static_cast<double>(ceil_div(c.blocks, gx)), tiles = resident > 1 && nz == 1 ? 0.5 * (most_tiles + static_cast<double>(c.blocks) / gx) : most_tiles;
         const double stage_x = 0.7 + resident * static_cast<double>(mt) * c.kz * 2 / 3e4;
@@ -880,7 +881,7 @@ Cut choose_cut(int64_t N, int64_t K, int slots, int mt, int nt, int stage_bytes,
   p.sx_at = static_cast<int>(best.kc / step * x_bytes);
   p.flags_at = p.sx_at + (q4k ? static_cast<int>(best.kc / 256 * 8 * nt * 64) : 0);
   p.list_at = static_cast<int>(ceil_div(p.flags_at + best.kc / step * 4, 16) * 16);
-  p.red_at = p.list_at + (grouped ? kListCap * 4 : 0);
+  p.red_at = p.list_at + (grouped ? kListCap * 2 : 0);
   const int rows_cta = best.warps / best.kw * 16;
   p.ring_at = static_cast<int>(ceil_div(p.red_at + (best.kw > 1 || best.nz > 1 ? best.kw * 8 * nt * (rows_cta + 4) * 4 : 0), 16) * 16);
   return best;
@@ -888,7 +889,9 @@ Cut choose_cut(int64_t N, int64_t K, int slots, int mt, int nt, int stage_bytes,
 
 template <int FMT, int NT, int LB>
 cudaError_t launch(MvParams& p, int slots, int mt, cudaStream_t st) {
-  const Cut c = choose_cut(p.N, p.K, slots, mt, NT, kTurn<NT, LB> * kStepBytes<FMT, LB>, NT == 1 ? mt * 4 * (LB * 4 + 16) : LB / 4 * kXPitch<NT>, 8 * LB, FMT == QF_FMT_Q4_K, p.ids != nullptr, p);
+  // experts that even routing is expected to meet; the others' CTAs leave at once
+  const double busy = p.ids ? p.G * (1.0 - pow(1.0 - 1.0 / p.G, p.M)) : 1.0;
+  const Cut c = choose_cut(p.N, p.K, busy, mt, NT, kTurn<NT, LB> * kStepBytes<FMT, LB>, NT == 1 ? mt * 4 * (LB * 4 + 16) : LB / 4 * kXPitch<NT>, 8 * LB, FMT == QF_FMT_Q4_K, p.ids != nullptr, p);
   auto kernel = matvec_kernel<FMT, NT, LB>;
   static bool ready[64] = {};                          // per device
   int dev = 0;
