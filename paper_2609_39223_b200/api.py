@@ -445,6 +445,16 @@ def _tensor(t: torch.Tensor, name: str, dtypes, shape) -> int:
     return t.data_ptr()
 
 
+def _out(like: torch.Tensor, given: torch.Tensor | None, name: str, dtypes, shape, dtype):
+    """The caller's output, checked, or a new one on the device of ``like``; with its address."""
+    if given is not None:
+        return given, _tensor(given, name, dtypes, shape)
+    if dtype not in dtypes:
+        raise TypeError(f"{name} cannot be {dtype}")
+    new = like.new_empty(shape, dtype=dtype)
+    return new, new.data_ptr()
+
+
 def _stream_of(t: torch.Tensor) -> int:
     """Current stream of the current device, which has to be the tensor's. (The calls below take a few microseconds on the GPU;
     torch.cuda.current_stream() builds an object and takes three by itself.)"""
@@ -492,10 +502,8 @@ def qf_moe_dispatch(x: torch.Tensor, plan: MoePlan, *, xs: torch.Tensor | None =
     hidden = x.shape[-1]
     px = _tensor(x, "x", _BF16, (tokens, hidden))
     row_of, offs, counts, experts = _plan_ptrs(plan)
-    if xs is None:
-        xs = x.new_empty((rows, hidden), dtype=torch.bfloat16)
-    _check(lib().qf_moe_dispatch(px, tokens, top_k, hidden, row_of, offs, counts, experts, rows, _tensor(xs, "xs", _BF16, (rows, hidden)),
-                                 _stream_of(x)), "qf_moe_dispatch")
+    xs, po = _out(x, xs, "xs", _BF16, (rows, hidden), torch.bfloat16)
+    _check(lib().qf_moe_dispatch(px, tokens, top_k, hidden, row_of, offs, counts, experts, rows, po, _stream_of(x)), "qf_moe_dispatch")
     return xs
 
 
@@ -504,10 +512,9 @@ def qf_moe_dispatch_bwd(dxs: torch.Tensor, plan: MoePlan, *, dx_dtype=torch.bflo
     (tokens, top_k), rows = plan.row_of.shape, plan.rows_padded
     hidden = dxs.shape[-1]
     pd = _tensor(dxs, "dxs", _DATA_DTYPE, (rows, hidden))
-    if dx is None:
-        dx = dxs.new_empty((tokens, hidden), dtype=dx_dtype)
+    dx, po = _out(dxs, dx, "dx", _DATA_DTYPE, (tokens, hidden), dx_dtype)
     _check(lib().qf_moe_dispatch_bwd(pd, _DATA_DTYPE[dxs.dtype], tokens, top_k, hidden, _tensor(plan.row_of, "plan.row_of", _I32, (tokens, top_k)),
-                                     rows, _tensor(dx, "dx", _DATA_DTYPE, (tokens, hidden)), _DATA_DTYPE[dx.dtype], _stream_of(dxs)), "qf_moe_dispatch_bwd")
+                                     rows, po, _DATA_DTYPE[dx.dtype], _stream_of(dxs)), "qf_moe_dispatch_bwd")
     return dx
 
 
@@ -518,11 +525,10 @@ def qf_moe_combine(ys: torch.Tensor, weights: torch.Tensor, plan: MoePlan | None
     hidden = ys.shape[-1]
     rows = tokens * top_k if plan is None else plan.rows_padded
     py = _tensor(ys, "ys", _DATA_DTYPE, (rows, hidden))
-    if out is None:
-        out = ys.new_empty((tokens, hidden), dtype=out_dtype)
+    out, po = _out(ys, out, "out", _DATA_DTYPE, (tokens, hidden), out_dtype)
     row_of = None if plan is None else _tensor(plan.row_of, "plan.row_of", _I32, (tokens, top_k))
     _check(lib().qf_moe_combine(py, _DATA_DTYPE[ys.dtype], _tensor(weights, "weights", _F32, (tokens, top_k)), tokens, top_k, hidden, row_of, rows,
-                                _tensor(out, "out", _DATA_DTYPE, (tokens, hidden)), _DATA_DTYPE[out.dtype], _stream_of(ys)), "qf_moe_combine")
+                                po, _DATA_DTYPE[out.dtype], _stream_of(ys)), "qf_moe_combine")
     return out
 
 
@@ -535,15 +541,12 @@ def qf_moe_combine_bwd(dout: torch.Tensor, ys: torch.Tensor | None, weights: tor
     pd = _tensor(dout, "dout", _DATA_DTYPE, (tokens, hidden))
     py = _tensor(ys, "ys", _DATA_DTYPE, (rows, hidden)) if want_dweights or ys is not None else None
     row_of, offs, counts, experts = _plan_ptrs(plan)
-    if dys is None:
-        dys = dout.new_empty((rows, hidden), dtype=torch.bfloat16)
-    if want_dweights and dweights is None:
-        dweights = dout.new_empty((tokens, top_k), dtype=torch.float32)
-    pw = _tensor(dweights, "dweights", _F32, (tokens, top_k)) if want_dweights else None
+    dys, po = _out(dout, dys, "dys", _BF16, (rows, hidden), torch.bfloat16)
+    dweights, pw = _out(dout, dweights, "dweights", _F32, (tokens, top_k), torch.float32) if want_dweights else (None, None)
     _check(lib().qf_moe_combine_bwd(pd, _DATA_DTYPE[dout.dtype], py, _DATA_DTYPE[ys.dtype] if ys is not None else DT_BF16,
                                     _tensor(weights, "weights", _F32, (tokens, top_k)), tokens, top_k, hidden, row_of, offs, counts, experts,
-                                    rows, _tensor(dys, "dys", _BF16, (rows, hidden)), pw, _stream_of(dout)), "qf_moe_combine_bwd")
-    return dys, dweights if want_dweights else None
+                                    rows, po, pw, _stream_of(dout)), "qf_moe_combine_bwd")
+    return dys, dweights
 
 
 def qf_fq_matvec(fmt: int, X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, tensor_scale: torch.Tensor | None = None, *,
@@ -553,12 +556,12 @@ def qf_fq_matvec(fmt: int, X: torch.Tensor, codes: torch.Tensor, scales: torch.T
     N = codes.shape[0]
     if fmt not in BLOCK or K % BLOCK[fmt]:
         raise QfError(2 if fmt in BLOCK else 4, "qf_fq_matvec")
-    if Y is None:
-        Y = X.new_empty((M, N), dtype=y_dtype)
+    px = _tensor(X, "X", _BF16, (M, K))
+    Y, po = _out(X, Y, "Y", _DATA_DTYPE, (M, N), y_dtype)
     ts = _tensor(tensor_scale, "tensor_scale", _F32, (1,)) if fmt == FMT_NVFP4 else None
-    _check(lib().qf_fq_matvec(fmt, _tensor(X, "X", _BF16, (M, K)), M, _tensor(codes, "codes", _U8, (N, K // 2)),
-                              _tensor(scales, "scales", _U8, scales_shape(fmt, N, K)), ts, N, K, _tensor(Y, "Y", _DATA_DTYPE, (M, N)),
-                              _DATA_DTYPE[Y.dtype], _stream_of(X)), "qf_fq_matvec")
+    _check(lib().qf_fq_matvec(fmt, px, M, _tensor(codes, "codes", _U8, (N, K // 2)),
+                              _tensor(scales, "scales", _U8, scales_shape(fmt, N, K)), ts, N, K, po, _DATA_DTYPE[Y.dtype],
+                              _stream_of(X)), "qf_fq_matvec")
     return Y
 
 
@@ -571,12 +574,12 @@ def qf_fq_grouped_matvec(fmt: int, X: torch.Tensor, expert_ids: torch.Tensor, co
     pairs = expert_ids.numel()
     if fmt not in BLOCK or K % BLOCK[fmt]:
         raise QfError(2 if fmt in BLOCK else 4, "qf_fq_grouped_matvec")
-    if Y is None:
-        Y = X.new_empty((pairs, N), dtype=y_dtype)
+    px = _tensor(X, "X", _BF16, (x_rows, K))
+    Y, po = _out(X, Y, "Y", _DATA_DTYPE, (pairs, N), y_dtype)
     ts = _tensor(tensor_scales, "tensor_scales", _F32, (G,)) if fmt == FMT_NVFP4 else None
-    _check(lib().qf_fq_grouped_matvec(fmt, _tensor(X, "X", _BF16, (x_rows, K)), x_rows, _tensor(expert_ids, "expert_ids", _IDS_DTYPE, expert_ids.shape),
+    _check(lib().qf_fq_grouped_matvec(fmt, px, x_rows, _tensor(expert_ids, "expert_ids", _IDS_DTYPE, expert_ids.shape),
                                       _IDS_DTYPE[expert_ids.dtype], pairs, G, _tensor(codes, "codes", _U8, (G, N, K // 2)),
-                                      _tensor(scales, "scales", _U8, (G, *scales_shape(fmt, N, K))), ts, N, K, _tensor(Y, "Y", _DATA_DTYPE, (pairs, N)),
+                                      _tensor(scales, "scales", _U8, (G, *scales_shape(fmt, N, K))), ts, N, K, po,
                                       _DATA_DTYPE[Y.dtype], _stream_of(X)), "qf_fq_grouped_matvec")
     return Y
 
