@@ -5,7 +5,7 @@
 // token. So the multiply-adds go to mma.sync m16n8k16 (16 weight rows x 8 tokens): a tcgen05 tile needs 128 rows of an operand
 // in shared memory, which would mean writing every decoded weight there first; here decoded weights never leave registers.
 //
-//  * A fragments: a lane decodes up to 32 consecutive bytes of codes of one weight row in place. Which k a lane's elements stand
+//  * A fragments: a lane decodes 32 consecutive bytes of codes of one weight row in place. Which k a lane's elements stand
 //    for is free as long as both operands agree, so no code is ever moved between lanes.
 //  * Every decoded weight is exact in FP16 up to a factor that a row or a step shares: E2M1 value times E4M3 scale has six
 //    significant bits; E2M1 value times 2^p is exact while p lies in [-21, 5]; a Q4_K code C times its 6-bit scale s6 is a whole
@@ -20,7 +20,7 @@
 //    This takes 15 instructions for eight weights where the FP16 route takes 8, which is why it is not the only route.
 //  * Q4_K offsets: sum over sub-blocks of m6 * sum(x) is a product of its own, 8 sub-blocks deep, with the sums of x split into
 //    three BF16 parts (24 bits); one FP32 multiply-add per super-block applies d and dmin.
-//  * The tensor core truncates as it accumulates: it adds up one step (64 to 256 elements) at a time, the steps are added in FP32.
+//  * The tensor core truncates as it accumulates: it adds up one step of 256 elements at a time, the steps are added in FP32.
 //  * Codes arrive through a ring of kStages steps per warp in shared memory (cp.async), so that loads in flight cost no registers.
 //  * Rows are cut into tiles of 16 or 32 for a warp; the contraction is split over the warps of a CTA and over the CTAs of a
 //    cluster where there are too few tiles to keep every SM loading; the parts meet in (distributed) shared memory in a fixed order.
@@ -44,6 +44,7 @@ struct MvParams {
   const __nv_bfloat16* X;
   const uint8_t* codes;
   const uint8_t* scales;
+  const uint8_t* scales_end;
   const float* tscale;
   const void* ids;
   void* Y;
@@ -120,28 +121,27 @@ __device__ __forceinline__ void q4k_unpack(const uint32_t (&m)[4], uint32_t (&v)
   v[3] = ((m[3] >> 4) & 0x0F0F0F0Fu) | ((m[2] >> 2) & 0x30303030u);
 }
 
-// What a lane holds of one weight row for one step of the contraction: LB bytes of codes. FP4: consecutive ones (a step is
-// 8 * LB weights). Q4_K (LB = 32): 8 bytes of each of the four chunks of a super-block (a step is a super-block).
-template <int FMT, int LB>
+constexpr int kStep = 256;                            // weights of a row that a warp takes at a time
+
+// What a lane holds of one weight row for one step of the contraction: 32 bytes of codes. FP4: 64 consecutive weights. Q4_K: 8
+// bytes of each of the four chunks of a super-block.
+template <int FMT>
 struct RowPart {
-  uint32_t q[LB / 4];
+  uint32_t q[8];
   uint32_t s[FMT == QF_FMT_Q4_K ? 4 : 1];            // block scales as stored
 };
 
-// Weights per block scale, and bytes of block scales of a lane's part of a row (half a block counts as one).
 template <int FMT>
-constexpr int kBlock = FMT == QF_FMT_MXFP4 ? 32 : 16;
-template <int FMT, int LB>
-constexpr int kPartScales = 2 * LB / kBlock<FMT> ? 2 * LB / kBlock<FMT> : 1;
+constexpr int kBlock = FMT == QF_FMT_MXFP4 ? 32 : 16;                   // weights per block scale (Q4_K: per byte of metadata)
 
-// The same straight from global memory, 8 bytes at a time.
-template <int FMT, int LB>
-__device__ __forceinline__ void load_part(RowPart<FMT, LB>& r, const uint8_t* codes, const uint8_t* scales, int k_step, int K, int t) {
-  const int k = FMT == QF_FMT_Q4_K ? k_step + t * 16 : k_step + t * 2 * LB;
+// The same straight from global memory, piece by piece; zeros (with a scale in range) past the end of the contraction.
+template <int FMT>
+__device__ __forceinline__ void load_part(RowPart<FMT>& r, const uint8_t* codes, const uint8_t* scales, int k_step, int K, int t) {
+  const int k = FMT == QF_FMT_Q4_K ? k_step + t * 16 : k_step + t * 64;
 #pragma unroll
-  for (int i = 0; i < LB / 8; ++i) {
+  for (int i = 0; i < 4; ++i) {
     uint2 v = make_uint2(0u, 0u);
-    if (k < K) v = __ldg(reinterpret_cast<const uint2*>(codes + k / 2 + i * (FMT == QF_FMT_Q4_K ? 32 : 8)));
+    if (FMT == QF_FMT_Q4_K || k + 16 * i < K) v = __ldg(reinterpret_cast<const uint2*>(codes + k / 2 + i * (FMT == QF_FMT_Q4_K ? 32 : 8)));
     r.q[2 * i] = v.x;
     r.q[2 * i + 1] = v.y;
   }
@@ -149,37 +149,37 @@ __device__ __forceinline__ void load_part(RowPart<FMT, LB>& r, const uint8_t* co
     const uint4 m = __ldg(reinterpret_cast<const uint4*>(scales + k_step / 16));
     r.s[0] = m.x; r.s[1] = m.y; r.s[2] = m.z; r.s[3] = m.w;
   } else {
-    r.s[0] = FMT == QF_FMT_MXFP4 ? 0x7F7F7F7Fu : 0u;   // zeros with a scale in range past the end
-    if (k < K) {
-      r.s[0] = 0u;
+    r.s[0] = 0u;
 #pragma unroll
-      for (int i = 0; i < kPartScales<FMT, LB>; ++i) r.s[0] |= static_cast<uint32_t>(__ldg(scales + k / (FMT == QF_FMT_NVFP4 ? 16 : 32) + i)) << (8 * i);
-    }
+    for (int i = 0; i < 64 / kBlock<FMT>; ++i)
+      r.s[0] |= (k + i * kBlock<FMT> < K ? static_cast<uint32_t>(__ldg(scales + k / kBlock<FMT> + i)) : FMT == QF_FMT_MXFP4 ? 127u : 0u) << (8 * i);
   }
 }
 
 // ---- a warp's ring of steps in shared memory, filled by asynchronous copies -----------------------------------------------
-// LB = 32 (K a multiple of 128; a step is 256 weights of 16 rows): rows of 128 bytes, each copied by eight lanes at a time. (Four
-// lanes a row, 64 bytes of eight rows at a time, took 81 us for the copies of a 128256 x 4096 weight where this takes 49.)
-// 16-byte pieces are permuted inside a row so that the lanes that read together meet different banks. Then the scales: 16 bytes
-// (NVFP4, Q4_K) or 8 (MXFP4) of every row.
-// LB = 8 (any K; a step is 64 weights): every lane copies its own 8 bytes of two rows, scales go to registers.
+// The codes of 16 rows, 128 bytes each, in pieces of 16 bytes that eight lanes copy for a row at a time. (Four lanes a row, 64 bytes
+// of eight rows at a time, took 81 us for the copies of a 128256 x 4096 weight where this takes 49.) Pieces are permuted
+// inside a row so that the lanes that read together meet different banks. Then the scales of every row.
+// LOOSE: rows that do not start on 16 bytes, or scales that do not start on words (K not a multiple of 128): pieces of 8 bytes,
+// 16 lanes a row, and for the scales the aligned words around them (NVFP4, one token, 32768 x 4112: 33 us, where 4096 takes 21; with lanes that copied their own 8 bytes of two rows it was 49).
 
-template <int FMT>
-constexpr int kStepScales = FMT == QF_FMT_MXFP4 ? 8 : 16;
-template <int FMT>
-constexpr int kScaleLanes = FMT == QF_FMT_Q4_K ? 1 : 2;                 // lanes that copy a row's scales
-template <int FMT, int LB>
-constexpr int kStepBytes = LB == 8 ? 512 : 16 * (128 + kStepScales<FMT>);
+template <int FMT, bool LOOSE>
+constexpr int kStepScales = LOOSE ? (FMT == QF_FMT_MXFP4 ? 16 : 24) : FMT == QF_FMT_MXFP4 ? 8 : 16;       // bytes a row
+template <int FMT, bool LOOSE>
+constexpr int kStepBytes = 16 * (128 + kStepScales<FMT, LOOSE>);
 // Steps a warp takes in a turn of its loop: two where the products of a step are few, so that addresses and bookkeeping are shared.
-template <int NT, int LB>
-constexpr int kTurn = NT == 1 && LB == 32 ? 2 : 1;
+template <int NT>
+constexpr int kTurn = NT == 1 ? 2 : 1;
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 template <int BYTES>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
   if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
   else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+// four bytes, of which the first `bytes` exist; zeros for the others
+__device__ __forceinline__ void copy_word(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 // place of 16-byte piece `piece` of row r: FP4 lanes read pieces 2t (then 2t + 1) of two rows together, Q4_K lanes halves of
 // pieces 2c and 2c + 1 of four rows
@@ -188,33 +188,27 @@ __device__ __forceinline__ uint32_t piece_at(int r, int piece) {
   return r * 128 + ((piece ^ (FMT == QF_FMT_Q4_K ? (r & 3) * 2 : r & 1)) * 16);
 }
 
-// Where a warp's next step of codes and scales lies: this lane's address in the first row it copies, and the distance of its
-// other rows. The addresses advance from turn to turn; they are set up anew for every tile. A lane whose part lies past the end
-// of the contraction copies an earlier part of its row: any finite weight will do, X is zero there.
-template <int FMT, int LB>
+// Where a warp's next step of codes and scales lies. The addresses advance from turn to turn; they are set up anew for every tile.
+// A lane whose piece lies past the end of the contraction copies an earlier one of its row: any finite weight will do, X is
+// zero there.
+template <int FMT, bool LOOSE>
 struct Source {
-  static constexpr int kRows = LB == 8 ? 2 : 4;      // rows a lane copies codes of
   static constexpr int SHIFT = FMT == QF_FMT_MXFP4 ? 4 : 3;            // bytes of codes to bytes of scales
-  const uint8_t* codes;
+  const uint8_t* codes;                              // this lane's piece in the first row it copies
   const uint8_t* scales;
-  uint32_t row[kRows - 1];                           // bytes of codes to the other rows
-  int k;                                             // of the step (LB = 8: of this lane's first code)
+  int k;                                             // of the step
+  int more;                                          // rows of the weight after that first one
 
   __device__ __forceinline__ void tile(const MvParams& p, int64_t row0, int n0, int k_step, int lane) {
-    const int first = n0 + (LB == 8 ? lane >> 2 : lane >> 3), gap = LB == 8 ? 8 : 4;
-    const int n = min(first, p.N - 1);
+    const int first = n0 + (LOOSE ? lane >> 4 : lane >> 3), n = min(first, p.N - 1);
     const uint32_t pitch = static_cast<uint32_t>(p.K) / 2;
-    k = LB == 8 ? k_step + (lane & 3) * 16 : k_step;
-    const int64_t at = (row0 + n) * pitch + k / 2;
-    codes = p.codes + at + (LB == 8 ? 0 : (lane & 7) * 16);
-#pragma unroll
-    for (int i = 1; i < kRows; ++i) row[i - 1] = static_cast<uint32_t>(min(first + gap * i, p.N - 1) - n) * pitch;
-    if constexpr (LB == 8) {
-      scales = p.scales + (at >> SHIFT);
-    } else {
-      const int r = lane / kScaleLanes<FMT> & 15;
-      scales = p.scales + (((row0 + min(n0 + r, p.N - 1)) * pitch + k / 2) >> SHIFT) + lane % kScaleLanes<FMT> * (kStepScales<FMT> / kScaleLanes<FMT>);
-    }
+    k = k_step;
+    more = p.N - 1 - n;
+    codes = p.codes + (row0 + n) * pitch + k / 2 + (LOOSE ? (lane & 15) * 8 : (lane & 7) * 16);
+    const int row = FMT == QF_FMT_Q4_K ? lane & 15 : lane >> 1;         // Q4_K: one lane for a row's scales, otherwise two
+    const int64_t at = ((row0 + min(n0 + row, p.N - 1)) * pitch + k / 2) >> SHIFT;
+    if constexpr (LOOSE) scales = p.scales + (at & ~static_cast<int64_t>(3)) + (lane & 1) * (kStepScales<FMT, LOOSE> / 2);
+    else scales = p.scales + at + (FMT == QF_FMT_Q4_K ? 0 : (lane & 1) * (kStepScales<FMT, LOOSE> / 2));
   }
   __device__ __forceinline__ void advance(int dk) {
     k += dk;
@@ -223,52 +217,55 @@ struct Source {
   }
   // Starts the copies of the first `steps` steps of a turn.
   template <int TURN>
-  __device__ __forceinline__ void start(const MvParams& p, uint32_t stage, int steps, int lane, uint32_t (&sc)[2]) const {
-    if constexpr (LB == 8) {
-      const int back = k < p.K ? 0 : k;              // past the end: the row's first part
+  __device__ __forceinline__ void start(const MvParams& p, uint32_t stage, int steps, int lane) const {
+    constexpr int ROWS = LOOSE ? 8 : 4, GAP = 16 / ROWS, PIECE = LOOSE ? 8 : 16, SB = kStepBytes<FMT, LOOSE>, HALF = kStepScales<FMT, LOOSE> / 2;
+    const int piece = LOOSE ? lane & 15 : lane & 7;
+    const uint32_t pitch = static_cast<uint32_t>(p.K) / 2;
+    const uint32_t to = stage + (LOOSE ? piece_at<FMT>(lane >> 4, piece >> 1) + (piece & 1) * 8 : piece_at<FMT>(lane >> 3, piece));
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint32_t off = i ? row[i - 1] : 0u;
-        copy_async<8>(stage + i * 256 + lane * 8, codes + off - back / 2);
-        sc[i] = __ldg(scales + (off >> SHIFT) - back / kBlock<FMT>);
+    for (int u = 0; u < TURN; ++u) {
+      if (u >= steps) break;
+      const bool past = k + u * kStep + piece * (2 * PIECE) >= p.K;
+      const uint8_t* c = codes + u * (kStep / 2) - (past ? piece * PIECE : 0);
+#pragma unroll
+      for (int h = 0; h < ROWS; ++h) {
+        const uint32_t off = static_cast<uint32_t>(min(h * GAP, more)) * pitch;
+        copy_async<PIECE>(to + u * SB + h * GAP * 128, c + off);       // a gap keeps the bits of the row that permute pieces
       }
-    } else {
-      const uint32_t to = stage + piece_at<FMT>(lane >> 3, lane & 7), to_sc = stage + 16 * 128 + lane * (kStepScales<FMT> / kScaleLanes<FMT>);
+      const uint8_t* s = scales + u * (kStep / kBlock<FMT>);
+      const uint32_t to_sc = stage + u * SB + 16 * 128;
+      if constexpr (FMT == QF_FMT_Q4_K) {
+        if (lane < 16) copy_async<16>(to_sc + lane * 16, s);
+      } else if constexpr (!LOOSE) {
+        copy_async<HALF>(to_sc + lane * HALF, s - (k + u * kStep + 128 >= p.K && (lane & 1) ? HALF : 0));
+      } else {
+        const int64_t room = p.scales_end - s;         // the last words may lie past the end of the tensor
 #pragma unroll
-      for (int u = 0; u < TURN; ++u) {
-        if (u >= steps) break;
-        // the second half of a step may lie past the end, K being a multiple of 128: those lanes step back to the first
-        const bool past = FMT != QF_FMT_Q4_K && k + u * 256 + 128 >= p.K;
-        const uint8_t* c = codes + u * 128 - (past && (lane & 4) ? 64 : 0);
-        const uint8_t* s = scales + u * (256 / kBlock<FMT>) - (past && (lane & 1) ? 128 / kBlock<FMT> : 0);
-#pragma unroll
-        for (int h = 0; h < 4; ++h) copy_async<16>(to + u * kStepBytes<FMT, LB> + h * 512, c + (h ? row[h - 1] : 0u));
-        if (kScaleLanes<FMT> == 2 || lane < 16) copy_async<kStepScales<FMT> / kScaleLanes<FMT>>(to_sc + u * kStepBytes<FMT, LB>, s);
+        for (int i = 0; i < HALF / 4; ++i) {
+          const int64_t rest = room - 4 * i;
+          copy_word(to_sc + lane * HALF + 4 * i, rest > 0 ? s + 4 * i : p.scales, rest >= 4 ? 4 : rest > 0 ? static_cast<int>(rest) : 0);
+        }
       }
     }
   }
 };
 
-// A step back from the ring; sc: LB = 8, the scales that came with it.
-template <int FMT, int LB>
-__device__ __forceinline__ void read_step(RowPart<FMT, LB> (&r)[2], const uint8_t* stage, int lane, const uint32_t (&sc)[2]) {
+// A step back from the ring; skew: LOOSE, where in its first word each row's scales begin.
+template <int FMT, bool LOOSE>
+__device__ __forceinline__ void read_step(RowPart<FMT> (&r)[2], const uint8_t* stage, int lane, const uint32_t (&skew)[2]) {
   const int g = lane >> 2, t = lane & 3;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int row = g + 8 * i;
-    if constexpr (LB == 8) {
-      const uint2 v = *reinterpret_cast<const uint2*>(stage + i * 256 + lane * 8);
-      r[i].q[0] = v.x;
-      r[i].q[1] = v.y;
-      r[i].s[0] = sc[i];
-    } else if constexpr (FMT == QF_FMT_Q4_K) {
+    const uint8_t* sc = stage + 16 * 128 + row * kStepScales<FMT, LOOSE>;
+    if constexpr (FMT == QF_FMT_Q4_K) {
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         const uint2 v = *reinterpret_cast<const uint2*>(stage + piece_at<FMT>(row, 2 * c) + t * 8);
         r[i].q[2 * c] = v.x;
         r[i].q[2 * c + 1] = v.y;
       }
-      const uint4 m = *reinterpret_cast<const uint4*>(stage + 16 * 128 + row * 16);
+      const uint4 m = *reinterpret_cast<const uint4*>(sc);
       r[i].s[0] = m.x; r[i].s[1] = m.y; r[i].s[2] = m.z; r[i].s[3] = m.w;
     } else {
 #pragma unroll
@@ -276,8 +273,15 @@ __device__ __forceinline__ void read_step(RowPart<FMT, LB> (&r)[2], const uint8_
         const uint4 v = *reinterpret_cast<const uint4*>(stage + piece_at<FMT>(row, 2 * t + h));
         r[i].q[4 * h] = v.x; r[i].q[4 * h + 1] = v.y; r[i].q[4 * h + 2] = v.z; r[i].q[4 * h + 3] = v.w;
       }
-      const uint8_t* s = stage + 16 * 128 + row * kStepScales<FMT> + t * kPartScales<FMT, LB>;
-      r[i].s[0] = FMT == QF_FMT_NVFP4 ? *reinterpret_cast<const uint32_t*>(s) : *reinterpret_cast<const uint16_t*>(s);
+      if constexpr (!LOOSE) {
+        r[i].s[0] = FMT == QF_FMT_NVFP4 ? reinterpret_cast<const uint32_t*>(sc)[t] : reinterpret_cast<const uint16_t*>(sc)[t];
+      } else if constexpr (FMT == QF_FMT_NVFP4) {
+        const uint8_t* b = sc + skew[i] + t * 4;
+        r[i].s[0] = b[0] | b[1] << 8 | b[2] << 16 | static_cast<uint32_t>(b[3]) << 24;
+      } else {
+        const uint8_t* b = sc + skew[i] + t * 2;
+        r[i].s[0] = b[0] | b[1] << 8;
+      }
     }
   }
 }
@@ -298,9 +302,8 @@ __device__ __forceinline__ uint32_t bf16_factor(uint32_t code) {
 constexpr uint32_t kMxLow = 106, kMxHigh = 132;
 
 // whether that holds for all scales of the warp's step
-template <int LB>
-__device__ __forceinline__ bool mx_exact(const RowPart<QF_FMT_MXFP4, LB> (&r)[2]) {
-  constexpr int NS = LB == 32 ? 2 : 1;
+__device__ __forceinline__ bool mx_exact(const RowPart<QF_FMT_MXFP4> (&r)[2]) {
+  constexpr int NS = 2;
   bool in = true;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
@@ -321,7 +324,7 @@ constexpr int kXPitch = 8 * NT * 64 + 16;
 // This lane's 16 bytes of X for one word of codes (Q4_K: one sub-block). A single token tile stands lane by lane, 16 bytes of
 // padding after each lane's words, so that a lane's words have fixed distances; lanes without a token read nothing (columns of
 // the product do not meet, whatever is in their registers). Several tiles stand word by word.
-template <int NT, int LB>
+template <int NT>
 __device__ __forceinline__ uint4 x_word(uint32_t x, int w, uint32_t at, bool live) {
   uint4 v;
   if constexpr (NT == 1)
@@ -333,9 +336,9 @@ __device__ __forceinline__ uint4 x_word(uint32_t x, int w, uint32_t at, bool liv
   return v;
 }
 
-template <int FMT, int NT, int LB>
-__device__ __forceinline__ bool step_f16(const RowPart<FMT, LB> (&r)[2], uint32_t x, const uint32_t (&at)[NT], bool live, float (&c)[NT][4]) {
-  constexpr int LW = LB / 4;
+template <int FMT, int NT>
+__device__ __forceinline__ bool step_f16(const RowPart<FMT> (&r)[2], uint32_t x, const uint32_t (&at)[NT], bool live, float (&c)[NT][4]) {
+  constexpr int LW = 8;
   bool in = true;
   if constexpr (FMT == QF_FMT_Q4_K) {
     uint32_t v[2][4];
@@ -351,7 +354,7 @@ __device__ __forceinline__ bool step_f16(const RowPart<FMT, LB> (&r)[2], uint32_
       for (int odd = 0; odd < 2; ++odd) {
         uint4 xv[NT];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) xv[nt] = x_word<NT, LB>(x, 2 * chunk + odd, at[nt], live);
+        for (int nt = 0; nt < NT; ++nt) xv[nt] = x_word<NT>(x, 2 * chunk + odd, at[nt], live);
         {
           uint32_t w[2][4];
 #pragma unroll
@@ -393,7 +396,7 @@ __device__ __forceinline__ bool step_f16(const RowPart<FMT, LB> (&r)[2], uint32_
       }
       uint4 xv[NT];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) xv[nt] = x_word<NT, LB>(x, w, at[nt], live);
+      for (int nt = 0; nt < NT; ++nt) xv[nt] = x_word<NT>(x, w, at[nt], live);
       {
         uint32_t wa[4], wb[4];
         e2m1_f16(r[0].q[w], wa);
@@ -421,20 +424,20 @@ __device__ __forceinline__ bool step_f16(const RowPart<FMT, LB> (&r)[2], uint32_
 template <int NT>
 struct Sums { float c[NT][4]; };
 
-template <int FMT, int NT, int LB>
+template <int FMT, int NT>
 __device__ __noinline__ Sums<NT> step_bf16(const MvParams& p, const uint16_t* list, int w0, int c0, int mt, int64_t row0, int n0, int k_step, uint32_t bad) {
-  constexpr int LW = LB / 4;
+  constexpr int LW = 8;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int64_t scale_pitch = FMT == QF_FMT_Q4_K ? p.K / 16 : p.K / (FMT == QF_FMT_NVFP4 ? 16 : 32);
   Sums<NT> sum = {};
-  RowPart<FMT, LB> r[2];
+  RowPart<FMT> r[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int64_t row = row0 + min(n0 + g + 8 * i, p.N - 1);
-    load_part<FMT, LB>(r[i], p.codes + row * (p.K / 2), p.scales + row * scale_pitch, k_step, p.K, t);
+    load_part<FMT>(r[i], p.codes + row * (p.K / 2), p.scales + row * scale_pitch, k_step, p.K, t);
   }
   if constexpr (FMT == QF_FMT_MXFP4)
-    if (!mx_exact<LB>(r)) bad = 0xFFFFFFFFu;
+    if (!mx_exact(r)) bad = 0xFFFFFFFFu;
   if (bad == 0u) return sum;
   const __nv_bfloat16* xrow[NT];
 #pragma unroll
@@ -451,7 +454,7 @@ __device__ __noinline__ Sums<NT> step_bf16(const MvParams& p, const uint16_t* li
         float es[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const RowPart<FMT, LB>& part = r[i];
+          const RowPart<FMT>& part = r[i];
           uint32_t v[4];
           q4k_unpack(part.s, v);
 #pragma unroll
@@ -477,7 +480,7 @@ __device__ __noinline__ Sums<NT> step_bf16(const MvParams& p, const uint16_t* li
     constexpr int PER = FMT == QF_FMT_NVFP4 ? 2 : 4;
 #pragma unroll
     for (int word = 0; word < LW; ++word) {
-      const int k = k_step + t * 2 * LB + word * 8;
+      const int k = k_step + t * 64 + word * 8;
       {
         uint32_t w[2][4];
 #pragma unroll
@@ -523,11 +526,11 @@ __device__ __forceinline__ bool stage_f16(const uint4& v, uint32_t (&h)[4]) {
 
 // One step with FP16 fragments into acc; the tokens in `bad` are left out. Returns bad, or all ones if a scale of the tile is out of
 // the FP16 range.
-template <int FMT, int NT, int LB>
-__device__ __forceinline__ uint32_t add_step(const RowPart<FMT, LB> (&r)[2], uint32_t x, uint32_t sx, const uint32_t (&at)[NT], const uint32_t (&sx_at)[NT],
+template <int FMT, int NT>
+__device__ __forceinline__ uint32_t add_step(const RowPart<FMT> (&r)[2], uint32_t x, uint32_t sx, const uint32_t (&at)[NT], const uint32_t (&sx_at)[NT],
                                              bool live, int t, uint32_t bad, float (&acc)[NT][4]) {
   float c[NT][4] = {};
-  const bool in = step_f16<FMT, NT, LB>(r, x, at, live, c);
+  const bool in = step_f16<FMT, NT>(r, x, at, live, c);
   if constexpr (FMT == QF_FMT_MXFP4)
     if (!__all_sync(0xFFFFFFFFu, in)) bad = 0xFFFFFFFFu;
   if (__builtin_expect(bad != 0u, 0)) {
@@ -575,12 +578,12 @@ __device__ __forceinline__ uint32_t add_step(const RowPart<FMT, LB> (&r)[2], uin
   return bad;
 }
 
-template <int FMT, int NT, int LB>
+template <int FMT, int NT, bool LOOSE>
 __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid_constant__ MvParams p) {
   constexpr int MT = 8 * NT;                           // tokens of a pass
   constexpr bool Q4K = FMT == QF_FMT_Q4_K;
-  constexpr int STEP = 8 * LB, TURN = kTurn<NT, LB>;
-  constexpr int LW = LB / 4;                           // 16-byte units of X per lane and step
+  constexpr int STEP = kStep, TURN = kTurn<NT>;
+  constexpr int LW = 8;                                // 16-byte units of X per lane and step
   constexpr int XL = LW * 16 + 16;                     // a lane's bytes of X for a step (a single token tile)
   extern __shared__ __align__(16) uint8_t smem[];                                  // X: [kc / STEP][tokens][4 lanes][XL], or [kc / STEP][LW][MT][4 lanes][16] and padding
   uint4* sx = reinterpret_cast<uint4*>(smem + p.sx_at);                            // Q4_K: [kc / 256][MT][4]: sums over two sub-blocks in three BF16 parts
@@ -589,7 +592,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
   float* red = reinterpret_cast<float*>(smem + p.red_at);                          // split contraction: [kw][MT][rows of the CTA + 4]
   __shared__ int warp_count[kWarpsMost];
   const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5, g = lane >> 2, t = lane & 3;
-  constexpr int SB = TURN * kStepBytes<FMT, LB>;
+  constexpr int SB = TURN * kStepBytes<FMT, LOOSE>;
   const int ring = p.ring_at + warp * kStages * SB;    // in bytes from the start
   const uint32_t smem0 = smem_addr(smem);
   const int rows_cta = warps / p.kw * 16, red_pitch = rows_cta + 4;
@@ -666,12 +669,11 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
           const int tiles = whole ? (p.blocks - b0 + gridDim.x - 1) / gridDim.x : 1;
           // the first codes are under way while X is staged
           int next_n = (b0 * (warps / p.kw) + rw) * 16, next = 0, tiles_left = per_tile ? tiles : 0;
-          Source<FMT, LB> src;
+          Source<FMT, LOOSE> src;
           if (tiles_left) src.tile(p, row0, next_n, kc0 + kw * TURN * STEP, lane);
-          uint32_t sc[2];                           // LB = 8: scales of the step that is read next
           auto start = [&](int stage) {
             if (tiles_left > 0) {
-              src.template start<TURN>(p, smem0 + stage, TURN == 1 ? 1 : steps - (next * p.kw + kw) * TURN, lane, sc);
+              src.template start<TURN>(p, smem0 + stage, TURN == 1 ? 1 : steps - (next * p.kw + kw) * TURN, lane);
               if (++next < per_tile) {
                 src.advance(p.kw * TURN * STEP);
               } else if (--tiles_left > 0) {
@@ -683,7 +685,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
             asm volatile("cp.async.commit_group;" ::: "memory");
           };
           start(ring);
-          if (LB != 8) start(ring + SB);                 // LB = 8 keeps one step under way, so that its scales can wait in registers
+          start(ring + SB);
           for (int i = tid; i < steps; i += threads) inexact[i] = 0u;
           __syncthreads();
           bool exact = true;
@@ -739,25 +741,37 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
           for (int tile = 0; tile < tiles; ++tile) {
             const int block = b0 + tile * gridDim.x;
             uint32_t any_bad = 0u;
+            uint32_t skew[2] = {0u, 0u};
+            if constexpr (LOOSE) {
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+                skew[i] = (static_cast<uint32_t>(row0) + min((block * (warps / p.kw) + rw) * 16 + g + 8 * i, p.N - 1)) * static_cast<uint32_t>(p.K / kBlock<FMT>) & 3u;
+            }
             int s = kw * TURN;
 #pragma unroll 1
             for (int j = 0; j < per_tile; ++j) {
               // the older turn's copies are complete
-              if (LB == 8) asm volatile("cp.async.wait_group 0;" ::: "memory");
-              else asm volatile("cp.async.wait_group 1;" ::: "memory");
-              if constexpr (Q4K || LB == 32) __syncwarp();
+              asm volatile("cp.async.wait_group 1;" ::: "memory");
+              __syncwarp();
               const int in_turn = TURN == 1 ? 1 : min(TURN, steps - s);
 #pragma unroll 1
               for (int u = 0; u < in_turn; ++u) {
-                RowPart<FMT, LB> r[2];
-                read_step<FMT, LB>(r, smem + stage + u * kStepBytes<FMT, LB>, lane, sc);
-                if constexpr (LB == 8) start(stage == ring ? ring + SB : ring);
+                RowPart<FMT> r[2];
+                read_step<FMT, LOOSE>(r, smem + stage + u * kStepBytes<FMT, LOOSE>, lane, skew);
+                if constexpr (FMT == QF_FMT_MXFP4 && LOOSE) {
+                  // what stands past the end of the row is no scale of it: one in range instead
+                  const int left = p.K - (kc0 + (s + u) * STEP + t * 64);
+                  if (left < 64) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) r[i].s[0] = left <= 0 ? 0x7F7Fu : (r[i].s[0] & 0xFFu) | (left <= 32 ? 0x7F00u : r[i].s[0] & 0xFF00u);
+                  }
+                }
                 uint32_t bad = 0u;
                 if (any_inexact) bad = inexact[s + u];
-                any_bad |= add_step<FMT, NT, LB>(r, smem0 + (s + u) * x_step, smem0 + p.sx_at + (s + u) * MT * 64, at, sx_at, live, t, bad, acc);
+                any_bad |= add_step<FMT, NT>(r, smem0 + (s + u) * x_step, smem0 + p.sx_at + (s + u) * MT * 64, at, sx_at, live, t, bad, acc);
               }
-              if constexpr (Q4K || LB == 32) __syncwarp();
-              if constexpr (LB != 8) start(stage);
+              __syncwarp();
+              start(stage);
               stage = stage == ring ? ring + SB : ring;
               s += p.kw * TURN;
             }
@@ -766,7 +780,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
               if (any_bad) {
                 for (int s = 0; s < steps; ++s) {
                   if (s / TURN % p.kw != kw) continue;
-                  const Sums<NT> sum = step_bf16<FMT, NT, LB>(p, list, w0, c0, mt, row0, n_warp, kc0 + s * STEP, inexact[s]);
+                  const Sums<NT> sum = step_bf16<FMT, NT>(p, list, w0, c0, mt, row0, n_warp, kc0 + s * STEP, inexact[s]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -833,11 +847,13 @@ struct Cut {
 // holds; meeting costs 0.7 in a CTA and 1.5 in a cluster (3.5 if there
 // are tiles to come, since it empties the rings); a slice of X takes 0.7 and 1 per 30 KB that the SM stages. The choice
 // is within 10% of the best cut in nine of ten of those cases.
-Cut choose_cut(int64_t N, int64_t K, double slots, int mt, int nt, int stage_bytes, int x_bytes, int step, bool q4k, bool grouped, MvParams& p) {
+Cut choose_cut(int64_t N, int64_t K, double slots, int mt, int nt, int stage_bytes, int x_bytes, int step, bool q4k, bool loose, bool grouped, MvParams& p) {
   Cut best{};
   double best_time = 1e30;
   const double turn_fixed = q4k ? 0.55 : 0.25, turn_each = nt == 1 ? 0.115 + 0.001 * mt : 0.15;
   const int64_t turns = ceil_div(K, 512);
+  // the small copies of loose rows go through L1, which has to be left some room (32768 x 4128, 8 tokens: 52 us at 230 KB, 34 at 160)
+  const size_t smem_most = loose ? 200 * 1024 : kSmemMost;
   for (int warps = 4; warps <= kWarpsMost; warps *= 2)
     for (int kw = 1; kw <= warps; kw *= 2)
       for (int nz = 1; nz <= 4; nz *= 2) {
@@ -853,8 +869,8 @@ Cut choose_cut(int64_t N, int64_t K, double slots, int mt, int nt, int stage_byt
         const size_t red = kw > 1 || nz > 1 ? static_cast<size_t>(kw) * 8 * nt * (rows_cta + 4) * 4 : 0;
         const size_t fixed = ring + red + (grouped ? kListCap * 2 : 0) + 64;
         const int64_t per_k = 512 / step * (x_bytes + 4) + (q4k ? 2 * 8 * nt * 64 : 0);           // bytes per 512 of the contraction
-        if (fixed + per_k > kSmemMost) continue;
-        const int64_t most = (kSmemMost - fixed) / per_k * 512;
+        if (fixed + per_k > smem_most) continue;
+        const int64_t most = (smem_most - fixed) / per_k * 512;
         c.kc = c.kz < most ? c.kz : most;
         c.smem = fixed + c.kc / 512 * per_k;
         int per_sm = kWarpsMost / warps;
@@ -871,7 +887,7 @@ Cut choose_cut(int64_t N, int64_t K, double slots, int mt, int nt, int stage_byt
         const double most_tiles = static_cast<double>(ceil_div(c.blocks, gx)), tiles = resident > 1 && nz == 1 ? 0.5 * (most_tiles + static_cast<double>(c.blocks) / gx) : most_tiles;
         const double stage_x = 0.7 + resident * static_cast<double>(mt) * c.kz * 2 / 3e4;
         const double tile = ceil_div(c.kz / 512, kw) * (turn_fixed + turn_each * resident * warps) + (nz > 1 ? (most_tiles > 1 ? 3.5 : 1.5) : kw > 1 ? 0.7 : 0.05) + (warps == 4 ? 0.0 : 0.05 * ceil_div(c.kz / 512, kw));
-        const double time = waves * ((c.kc >= c.kz ? stage_x : tiles * stage_x * ceil_div(c.kz, c.kc)) + tiles * tile);
+        const double time = waves * ((c.kc >= c.kz ? stage_x : tiles * (stage_x + 1.5 * ceil_div(c.kz, c.kc))) + tiles * tile);
         if (time < best_time) { best_time = time; best = c; }
       }
   p.blocks = static_cast<int>(best.blocks);
@@ -887,12 +903,12 @@ Cut choose_cut(int64_t N, int64_t K, double slots, int mt, int nt, int stage_byt
   return best;
 }
 
-template <int FMT, int NT, int LB>
+template <int FMT, int NT, bool LOOSE>
 cudaError_t launch(MvParams& p, int slots, int mt, cudaStream_t st) {
   // experts that even routing is expected to meet; the others' CTAs leave at once
   const double busy = p.ids ? p.G * (1.0 - pow(1.0 - 1.0 / p.G, p.M)) : 1.0;
-  const Cut c = choose_cut(p.N, p.K, busy, mt, NT, kTurn<NT, LB> * kStepBytes<FMT, LB>, NT == 1 ? mt * 4 * (LB * 4 + 16) : LB / 4 * kXPitch<NT>, 8 * LB, FMT == QF_FMT_Q4_K, p.ids != nullptr, p);
-  auto kernel = matvec_kernel<FMT, NT, LB>;
+  const Cut c = choose_cut(p.N, p.K, busy, mt, NT, kTurn<NT> * kStepBytes<FMT, LOOSE>, NT == 1 ? mt * 4 * 144 : 8 * kXPitch<NT>, kStep, FMT == QF_FMT_Q4_K, LOOSE, p.ids != nullptr, p);
+  auto kernel = matvec_kernel<FMT, NT, LOOSE>;
   static bool ready[64] = {};                          // per device
   int dev = 0;
   if (cudaError_t e = cudaGetDevice(&dev)) return e;
@@ -922,6 +938,7 @@ cudaError_t launch_matvec(const MatvecArgs& a, cudaStream_t st) {
   p.X = static_cast<const __nv_bfloat16*>(a.X);
   p.codes = static_cast<const uint8_t*>(a.codes);
   p.scales = static_cast<const uint8_t*>(a.scales);
+  p.scales_end = p.scales + (a.ids ? a.G : 1) * a.N * (a.K / (a.fmt == QF_FMT_MXFP4 ? 32 : 16));
   p.tscale = a.tscale;
   p.ids = a.ids;
   p.ids64 = a.ids64;
@@ -934,17 +951,15 @@ cudaError_t launch_matvec(const MatvecArgs& a, cudaStream_t st) {
   // tokens of a pass: few pairs per expert are the rule in the grouped product
   const int nt = (a.ids ? a.M <= 4ll * a.G || a.M <= 8 : a.M <= 8) ? 1 : 2;
   const int mt = static_cast<int>(a.M < 8 * nt ? a.M : 8 * nt);
-  // With a contraction that is a multiple of 128, a lane takes 32 bytes of a row at a time (16 of two tiles' rows); any other one
-  // is taken 8 bytes at a time.
-  const bool wide = a.K % 128 == 0;
+  const bool loose = a.K % 128 != 0;
   constexpr int NV = QF_FMT_NVFP4, MX = QF_FMT_MXFP4, Q4 = QF_FMT_Q4_K;
-  if (a.fmt == Q4) return nt == 1 ? launch<Q4, 1, 32>(p, slots, mt, st) : launch<Q4, 2, 32>(p, slots, mt, st);
+  if (a.fmt == Q4) return nt == 1 ? launch<Q4, 1, false>(p, slots, mt, st) : launch<Q4, 2, false>(p, slots, mt, st);
   if (a.fmt == NV) {
-    if (nt == 1) return wide ? launch<NV, 1, 32>(p, slots, mt, st) : launch<NV, 1, 8>(p, slots, mt, st);
-    return wide ? launch<NV, 2, 32>(p, slots, mt, st) : launch<NV, 2, 8>(p, slots, mt, st);
+    if (nt == 1) return loose ? launch<NV, 1, true>(p, slots, mt, st) : launch<NV, 1, false>(p, slots, mt, st);
+    return loose ? launch<NV, 2, true>(p, slots, mt, st) : launch<NV, 2, false>(p, slots, mt, st);
   }
-  if (nt == 1) return wide ? launch<MX, 1, 32>(p, slots, mt, st) : launch<MX, 1, 8>(p, slots, mt, st);
-  return wide ? launch<MX, 2, 32>(p, slots, mt, st) : launch<MX, 2, 8>(p, slots, mt, st);
+  if (nt == 1) return loose ? launch<MX, 1, true>(p, slots, mt, st) : launch<MX, 1, false>(p, slots, mt, st);
+  return loose ? launch<MX, 2, true>(p, slots, mt, st) : launch<MX, 2, false>(p, slots, mt, st);
 }
 
 }  // namespace qf

@@ -193,6 +193,34 @@ def test_grouped_matvec(fmt, T, k, G, N, blocks, kind):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+def test_grouped_matvec_with_more_pairs_than_a_cta_lists_at_once(fmt):
+    """1024 pairs are listed in one go: experts whose pairs lie on both sides, and a last one."""
+    T, k, G, N, K = 700, 3, 5, 40, 256
+    r = np.random.default_rng(3)
+    ids = r.integers(0, G, (T, k))
+    ids[:, 0] = np.where(np.arange(T) == T - 1, 4, ids[:, 0] % 4)
+    codes, scales, ts = draw(fmt, (G,), N, K, seed=1)
+    x = acts((T, K), 1)
+    got = api.qf_fq_grouped_matvec(fmt, x.cuda(), torch.tensor(ids, device="cuda"), *gpu(codes, scales, ts), y_dtype=F32)
+    for e in range(G):
+        at = np.nonzero(ids.reshape(-1) == e)[0]
+        w, a = decode(fmt, codes[e], scales[e], None if ts is None else ts[e])
+        check(got[torch.tensor(at).cuda()], x.double().numpy()[at // k], w, a, F32)
+
+
+@pytest.mark.parametrize("fmt,unit", [(api.FMT_NVFP4, 16), (api.FMT_MXFP4, 32)])
+@pytest.mark.parametrize("blocks", [1, 2, 3, 5, 7, 9, 15, 17, 31, 33, 65, 129])
+def test_contractions_of_any_number_of_blocks(fmt, unit, blocks):
+    """Rows that begin anywhere a block can, in tensors that end with their last block."""
+    K = unit * blocks
+    for M, N in ((1, 37), (3, 161), (11, 18)):
+        codes, scales, ts = draw(fmt, (), N, K, seed=blocks + M)
+        x = acts((M, K), M)
+        w, a = decode(fmt, codes, scales, None if ts is None else ts[0])
+        check(api.qf_fq_matvec(fmt, x.cuda(), *gpu(codes, scales, ts), y_dtype=F32), x.double().numpy(), w, a, F32)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 def test_rows_do_not_influence_one_another(fmt):
     """The same row of X gives the same bits, whatever stands beside it; NaN and infinities stay in their rows."""
     N, K = 70, 512
