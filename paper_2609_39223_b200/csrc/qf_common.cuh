@@ -221,6 +221,14 @@ __device__ __forceinline__ void nvfp4_block_words(const uint32_t (&w)[NW], float
   }
 }
 
+// For kernels of a few microseconds, launched so that their CTAs may be placed while the kernel before them in the stream still
+// runs: lets the next kernel's CTAs be placed, then waits until everything before this kernel is complete and visible. Every thread
+// calls it before it touches global memory, and no path leaves the kernel before it.
+__device__ __forceinline__ void launch_after_previous() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // ---- host-side launchers implemented in the .cu files ---------------------------------------
 
 // NVFP4 with a speculated tensor scale: the first pass quantizes with the caller's guess while it accumulates the true

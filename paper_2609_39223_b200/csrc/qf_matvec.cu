@@ -35,7 +35,9 @@ namespace qf {
 namespace {
 
 constexpr int kWarpsMost = 16;                       // of a CTA; 128 registers a thread, so 16 warps fill an SM
-constexpr int kStages = 2;                           // turns of codes a warp has in shared memory or on the way
+// Steps of codes that a warp has in shared memory or on the way: four (37 KB an SM of four warps' copies) where X leaves the room
+template <int NT>
+constexpr int kStages = NT == 1 ? 4 : 2;
 constexpr int kSmemMost = 232448 - 128;              // dynamic shared memory of a CTA
 constexpr float kXScale = 64.0f;                     // X is staged as FP16 of this times x
 constexpr int kListCap = 1024;                       // pairs looked at in one go by a CTA of the grouped product
@@ -52,8 +54,8 @@ struct MvParams {
   int M, N, K, G;
   int blocks;                                        // row blocks of a weight; CTA x takes blocks x, x + gridDim.x, ...
   int kw;                                            // warps of a CTA that share a row tile
-  int kz;                                            // contraction length of a CTA (a multiple of 512)
-  int kc;                                            // contraction length staged at a time (a multiple of 512)
+  int kz;                                            // contraction length of a CTA (a multiple of 256)
+  int kc;                                            // contraction length staged at a time (a multiple of 256)
   int sx_at, flags_at, list_at, red_at, ring_at;     // bytes from the start of dynamic shared memory (X comes first)
   bool ids64, by_pair, y_f32;
 };
@@ -167,9 +169,6 @@ template <int FMT, bool LOOSE>
 constexpr int kStepScales = LOOSE ? (FMT == QF_FMT_MXFP4 ? 16 : 24) : FMT == QF_FMT_MXFP4 ? 8 : 16;       // bytes a row
 template <int FMT, bool LOOSE>
 constexpr int kStepBytes = 16 * (128 + kStepScales<FMT, LOOSE>);
-// Steps a warp takes in a turn of its loop: two where the products of a step are few, so that addresses and bookkeeping are shared.
-template <int NT>
-constexpr int kTurn = NT == 1 ? 2 : 1;
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 template <int BYTES>
@@ -197,13 +196,18 @@ struct Source {
   const uint8_t* codes;                              // this lane's piece in the first row it copies
   const uint8_t* scales;
   int k;                                             // of the step
-  int more;                                          // rows of the weight after that first one
+  int more;                                          // LOOSE: rows of the weight after that first one
+  uint32_t row[3];                                   // otherwise: bytes of codes to the other rows
 
   __device__ __forceinline__ void tile(const MvParams& p, int64_t row0, int n0, int k_step, int lane) {
     const int first = n0 + (LOOSE ? lane >> 4 : lane >> 3), n = min(first, p.N - 1);
     const uint32_t pitch = static_cast<uint32_t>(p.K) / 2;
     k = k_step;
     more = p.N - 1 - n;
+    if constexpr (!LOOSE) {
+#pragma unroll
+      for (int h = 1; h < 4; ++h) row[h - 1] = static_cast<uint32_t>(min(4 * h, more)) * pitch;
+    }
     codes = p.codes + (row0 + n) * pitch + k / 2 + (LOOSE ? (lane & 15) * 8 : (lane & 7) * 16);
     const int row = FMT == QF_FMT_Q4_K ? lane & 15 : lane >> 1;         // Q4_K: one lane for a row's scales, otherwise two
     const int64_t at = ((row0 + min(n0 + row, p.N - 1)) * pitch + k / 2) >> SHIFT;
@@ -215,36 +219,28 @@ struct Source {
     codes += dk / 2;
     scales += dk / kBlock<FMT>;
   }
-  // Starts the copies of the first `steps` steps of a turn.
-  template <int TURN>
-  __device__ __forceinline__ void start(const MvParams& p, uint32_t stage, int steps, int lane) const {
-    constexpr int ROWS = LOOSE ? 8 : 4, GAP = 16 / ROWS, PIECE = LOOSE ? 8 : 16, SB = kStepBytes<FMT, LOOSE>, HALF = kStepScales<FMT, LOOSE> / 2;
+  // Starts the copies of the step.
+  __device__ __forceinline__ void start(const MvParams& p, uint32_t stage, int lane) const {
+    constexpr int ROWS = LOOSE ? 8 : 4, GAP = 16 / ROWS, PIECE = LOOSE ? 8 : 16, HALF = kStepScales<FMT, LOOSE> / 2;
     const int piece = LOOSE ? lane & 15 : lane & 7;
-    const uint32_t pitch = static_cast<uint32_t>(p.K) / 2;
     const uint32_t to = stage + (LOOSE ? piece_at<FMT>(lane >> 4, piece >> 1) + (piece & 1) * 8 : piece_at<FMT>(lane >> 3, piece));
+    const uint8_t* c = codes - (FMT != QF_FMT_Q4_K && k + piece * (2 * PIECE) >= p.K ? piece * PIECE : 0);
 #pragma unroll
-    for (int u = 0; u < TURN; ++u) {
-      if (u >= steps) break;
-      const bool past = k + u * kStep + piece * (2 * PIECE) >= p.K;
-      const uint8_t* c = codes + u * (kStep / 2) - (past ? piece * PIECE : 0);
+    for (int h = 0; h < ROWS; ++h) {                   // a gap keeps the bits of the row that permute pieces
+      const uint32_t off = h == 0 ? 0u : LOOSE ? static_cast<uint32_t>(min(h * GAP, more)) * (static_cast<uint32_t>(p.K) / 2) : row[(h - 1) & 3];
+      copy_async<PIECE>(to + h * GAP * 128, c + off);
+    }
+    const uint32_t to_sc = stage + 16 * 128;
+    if constexpr (FMT == QF_FMT_Q4_K) {
+      if (lane < 16) copy_async<16>(to_sc + lane * 16, scales);
+    } else if constexpr (!LOOSE) {
+      copy_async<HALF>(to_sc + lane * HALF, scales - (k + 128 >= p.K && (lane & 1) ? HALF : 0));
+    } else {
+      const int64_t room = p.scales_end - scales;      // the last words may lie past the end of the tensor
 #pragma unroll
-      for (int h = 0; h < ROWS; ++h) {
-        const uint32_t off = static_cast<uint32_t>(min(h * GAP, more)) * pitch;
-        copy_async<PIECE>(to + u * SB + h * GAP * 128, c + off);       // a gap keeps the bits of the row that permute pieces
-      }
-      const uint8_t* s = scales + u * (kStep / kBlock<FMT>);
-      const uint32_t to_sc = stage + u * SB + 16 * 128;
-      if constexpr (FMT == QF_FMT_Q4_K) {
-        if (lane < 16) copy_async<16>(to_sc + lane * 16, s);
-      } else if constexpr (!LOOSE) {
-        copy_async<HALF>(to_sc + lane * HALF, s - (k + u * kStep + 128 >= p.K && (lane & 1) ? HALF : 0));
-      } else {
-        const int64_t room = p.scales_end - s;         // the last words may lie past the end of the tensor
-#pragma unroll
-        for (int i = 0; i < HALF / 4; ++i) {
-          const int64_t rest = room - 4 * i;
-          copy_word(to_sc + lane * HALF + 4 * i, rest > 0 ? s + 4 * i : p.scales, rest >= 4 ? 4 : rest > 0 ? static_cast<int>(rest) : 0);
-        }
+      for (int i = 0; i < HALF / 4; ++i) {
+        const int64_t rest = room - 4 * i;
+        copy_word(to_sc + lane * HALF + 4 * i, rest > 0 ? scales + 4 * i : p.scales, rest >= 4 ? 4 : rest > 0 ? static_cast<int>(rest) : 0);
       }
     }
   }
@@ -582,7 +578,7 @@ template <int FMT, int NT, bool LOOSE>
 __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid_constant__ MvParams p) {
   constexpr int MT = 8 * NT;                           // tokens of a pass
   constexpr bool Q4K = FMT == QF_FMT_Q4_K;
-  constexpr int STEP = kStep, TURN = kTurn<NT>;
+  constexpr int STEP = kStep;
   constexpr int LW = 8;                                // 16-byte units of X per lane and step
   constexpr int XL = LW * 16 + 16;                     // a lane's bytes of X for a step (a single token tile)
   extern __shared__ __align__(16) uint8_t smem[];                                  // X: [kc / STEP][tokens][4 lanes][XL], or [kc / STEP][LW][MT][4 lanes][16] and padding
@@ -592,8 +588,8 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
   float* red = reinterpret_cast<float*>(smem + p.red_at);                          // split contraction: [kw][MT][rows of the CTA + 4]
   __shared__ int warp_count[kWarpsMost];
   const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5, g = lane >> 2, t = lane & 3;
-  constexpr int SB = TURN * kStepBytes<FMT, LOOSE>;
-  const int ring = p.ring_at + warp * kStages * SB;    // in bytes from the start
+  constexpr int SB = kStepBytes<FMT, LOOSE>;
+  const int ring = p.ring_at + warp * kStages<NT> * SB, ring_end = ring + kStages<NT> * SB;     // in bytes from the start
   const uint32_t smem0 = smem_addr(smem);
   const int rows_cta = warps / p.kw * 16, red_pitch = rows_cta + 4;
   const int rw = warp / p.kw, kw = warp - rw * p.kw;
@@ -602,6 +598,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
   const bool whole = p.kc >= p.kz;                     // the slice of X is staged once for all row blocks
   const bool split = p.kw > 1 || nz > 1;
 
+  launch_after_previous();
   int e = 0;
   if (p.ids) {
     if (p.by_pair) {
@@ -664,28 +661,27 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
       for (int b0 = blockIdx.x; b0 < p.blocks; b0 += whole ? p.blocks : gridDim.x) {
         for (int kc0 = k_begin; kc0 < k_end; kc0 += p.kc) {
           const int kc1 = min(kc0 + p.kc, k_end), steps = (kc1 - kc0 + STEP - 1) / STEP;
-          const int turns = (steps + TURN - 1) / TURN;
-          const int per_tile = kw < turns ? (turns - kw + p.kw - 1) / p.kw : 0;      // turns of this warp in a tile
+          const int per_tile = kw < steps ? (steps - kw + p.kw - 1) / p.kw : 0;      // steps of this warp in a tile
           const int tiles = whole ? (p.blocks - b0 + gridDim.x - 1) / gridDim.x : 1;
           // the first codes are under way while X is staged
           int next_n = (b0 * (warps / p.kw) + rw) * 16, next = 0, tiles_left = per_tile ? tiles : 0;
           Source<FMT, LOOSE> src;
-          if (tiles_left) src.tile(p, row0, next_n, kc0 + kw * TURN * STEP, lane);
+          if (tiles_left) src.tile(p, row0, next_n, kc0 + kw * STEP, lane);
           auto start = [&](int stage) {
             if (tiles_left > 0) {
-              src.template start<TURN>(p, smem0 + stage, TURN == 1 ? 1 : steps - (next * p.kw + kw) * TURN, lane);
+              src.start(p, smem0 + stage, lane);
               if (++next < per_tile) {
-                src.advance(p.kw * TURN * STEP);
+                src.advance(p.kw * STEP);
               } else if (--tiles_left > 0) {
                 next = 0;
                 next_n += gridDim.x * rows_cta;
-                src.tile(p, row0, next_n, kc0 + kw * TURN * STEP, lane);
+                src.tile(p, row0, next_n, kc0 + kw * STEP, lane);
               }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
           };
-          start(ring);
-          start(ring + SB);
+#pragma unroll 1
+          for (int d = 0; d < kStages<NT>; ++d) start(ring + d * SB);
           for (int i = tid; i < steps; i += threads) inexact[i] = 0u;
           __syncthreads();
           bool exact = true;
@@ -747,39 +743,35 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
               for (int i = 0; i < 2; ++i)
                 skew[i] = (static_cast<uint32_t>(row0) + min((block * (warps / p.kw) + rw) * 16 + g + 8 * i, p.N - 1)) * static_cast<uint32_t>(p.K / kBlock<FMT>) & 3u;
             }
-            int s = kw * TURN;
+            int s = kw;
 #pragma unroll 1
             for (int j = 0; j < per_tile; ++j) {
-              // the older turn's copies are complete
-              asm volatile("cp.async.wait_group 1;" ::: "memory");
+              // the oldest step's copies are complete
+              asm volatile("cp.async.wait_group %0;" ::"n"(kStages<NT> - 1) : "memory");
               __syncwarp();
-              const int in_turn = TURN == 1 ? 1 : min(TURN, steps - s);
-#pragma unroll 1
-              for (int u = 0; u < in_turn; ++u) {
-                RowPart<FMT> r[2];
-                read_step<FMT, LOOSE>(r, smem + stage + u * kStepBytes<FMT, LOOSE>, lane, skew);
-                if constexpr (FMT == QF_FMT_MXFP4 && LOOSE) {
-                  // what stands past the end of the row is no scale of it: one in range instead
-                  const int left = p.K - (kc0 + (s + u) * STEP + t * 64);
-                  if (left < 64) {
+              RowPart<FMT> r[2];
+              read_step<FMT, LOOSE>(r, smem + stage, lane, skew);
+              if constexpr (FMT == QF_FMT_MXFP4 && LOOSE) {
+                // what stands past the end of the row is no scale of it: one in range instead
+                const int left = p.K - (kc0 + s * STEP + t * 64);
+                if (left < 64) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) r[i].s[0] = left <= 0 ? 0x7F7Fu : (r[i].s[0] & 0xFFu) | (left <= 32 ? 0x7F00u : r[i].s[0] & 0xFF00u);
-                  }
+                  for (int i = 0; i < 2; ++i) r[i].s[0] = left <= 0 ? 0x7F7Fu : (r[i].s[0] & 0xFFu) | (left <= 32 ? 0x7F00u : r[i].s[0] & 0xFF00u);
                 }
-                uint32_t bad = 0u;
-                if (any_inexact) bad = inexact[s + u];
-                any_bad |= add_step<FMT, NT>(r, smem0 + (s + u) * x_step, smem0 + p.sx_at + (s + u) * MT * 64, at, sx_at, live, t, bad, acc);
               }
+              uint32_t bad = 0u;
+              if (any_inexact) bad = inexact[s];
+              any_bad |= add_step<FMT, NT>(r, smem0 + s * x_step, smem0 + p.sx_at + s * MT * 64, at, sx_at, live, t, bad, acc);
               __syncwarp();
               start(stage);
-              stage = stage == ring ? ring + SB : ring;
-              s += p.kw * TURN;
+              stage = stage + SB == ring_end ? ring : stage + SB;
+              s += p.kw;
             }
-            // end of the tile; a warp without a turn in a split contraction meets the others here all the same
+            // end of the tile; a warp without a step in a split contraction meets the others here all the same
               const int n_warp = (block * (warps / p.kw) + rw) * 16;
               if (any_bad) {
                 for (int s = 0; s < steps; ++s) {
-                  if (s / TURN % p.kw != kw) continue;
+                  if (s % p.kw != kw) continue;
                   const Sums<NT> sum = step_bf16<FMT, NT>(p, list, w0, c0, mt, row0, n_warp, kc0 + s * STEP, inexact[s]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
@@ -842,37 +834,36 @@ struct Cut {
   size_t smem;
 };
 
-// Picks the cut with the least estimated time. The constants are microseconds measured on this part over weights from
-// 1024 x 4096 to 128256 x 4096 and 1 to 16 tokens: a turn of 512 weights takes turn_fixed and turn_each per warp that the SM
-// holds; meeting costs 0.7 in a CTA and 1.5 in a cluster (3.5 if there
-// are tiles to come, since it empties the rings); a slice of X takes 0.7 and 1 per 30 KB that the SM stages. The choice
-// is within 10% of the best cut in nine of ten of those cases.
-Cut choose_cut(int64_t N, int64_t K, double slots, int mt, int nt, int stage_bytes, int x_bytes, int step, bool q4k, bool loose, bool grouped, MvParams& p) {
+// Picks the cut with the least estimated time. The constants are microseconds measured on this part: a step takes step_fixed and
+// step_each per warp that the SM holds, 0.5 at least; meeting costs 0.5 in a CTA and 2 in a cluster (3.5 if there are tiles to
+// come, since it empties the rings); a slice of X takes 0.7 and 1 per 30 KB that the SM stages. Over 68 products from
+// 1024 x 4096 to 128256 x 4096 with 1 to 16 tokens the choice took 1.02 times as long as the best cut in the mean, 1.19 at most.
+Cut choose_cut(int64_t N, int64_t K, double slots, double tokens, int mt, int nt, int ring_bytes, int x_bytes, bool q4k, bool loose, bool grouped, MvParams& p) {
   Cut best{};
   double best_time = 1e30;
-  const double turn_fixed = q4k ? 0.55 : 0.25, turn_each = nt == 1 ? 0.115 + 0.001 * mt : 0.15;
-  const int64_t turns = ceil_div(K, 512);
+  const double step_fixed = q4k ? 0.28 : 0.13, step_each = nt == 1 ? 0.055 + 0.0008 * tokens : 0.075;
+  const int64_t steps = ceil_div(K, kStep);
   // the small copies of loose rows go through L1, which has to be left some room (32768 x 4128, 8 tokens: 52 us at 230 KB, 34 at 160)
   const size_t smem_most = loose ? 200 * 1024 : kSmemMost;
   for (int warps = 4; warps <= kWarpsMost; warps *= 2)
     for (int kw = 1; kw <= warps; kw *= 2)
       for (int nz = 1; nz <= 4; nz *= 2) {
-        if ((kw > 1 || nz > 1) && kw * nz > turns) continue;
+        if ((kw > 1 || nz > 1) && kw * nz > steps) continue;
         Cut c{};
         c.warps = warps; c.kw = kw;
-        c.kz = ceil_div(turns, nz) * 512;
+        c.kz = ceil_div(steps, nz) * kStep;
         c.nz = static_cast<int>(ceil_div(K, c.kz));
         if (c.nz != nz) continue;
         const int rows_cta = warps / kw * 16;
         c.blocks = ceil_div(N, rows_cta);
-        const size_t ring = static_cast<size_t>(warps) * kStages * stage_bytes;
+        const size_t ring = static_cast<size_t>(warps) * ring_bytes;
         const size_t red = kw > 1 || nz > 1 ? static_cast<size_t>(kw) * 8 * nt * (rows_cta + 4) * 4 : 0;
         const size_t fixed = ring + red + (grouped ? kListCap * 2 : 0) + 64;
-        const int64_t per_k = 512 / step * (x_bytes + 4) + (q4k ? 2 * 8 * nt * 64 : 0);           // bytes per 512 of the contraction
+        const int64_t per_k = x_bytes + 4 + (q4k ? 8 * nt * 64 : 0);                            // bytes per step of the contraction
         if (fixed + per_k > smem_most) continue;
-        const int64_t most = (smem_most - fixed) / per_k * 512;
+        const int64_t most = (smem_most - fixed) / per_k * kStep;
         c.kc = c.kz < most ? c.kz : most;
-        c.smem = fixed + c.kc / 512 * per_k;
+        c.smem = fixed + c.kc / kStep * per_k;
         int per_sm = kWarpsMost / warps;
         if (per_sm > static_cast<int>(kSmemMost / (c.smem + 1024))) per_sm = static_cast<int>(kSmemMost / (c.smem + 1024));
         if (per_sm < 1) per_sm = 1;
@@ -884,9 +875,11 @@ Cut choose_cut(int64_t N, int64_t K, double slots, int mt, int nt, int stage_byt
         const int64_t grid = static_cast<int64_t>(gx * slots + 0.5), waves = ceil_div(grid, room);
         const int64_t sm_ctas = ceil_div(grid * nz, kNumSMs), resident = sm_ctas < per_sm ? sm_ctas : per_sm;
         // CTAs that share an SM even out some of what they have more or less of
-        const double most_tiles = static_cast<double>(ceil_div(c.blocks, gx)), tiles = resident > 1 && nz == 1 ? 0.5 * (most_tiles + static_cast<double>(c.blocks) / gx) : most_tiles;
-        const double stage_x = 0.7 + resident * static_cast<double>(mt) * c.kz * 2 / 3e4;
-        const double tile = ceil_div(c.kz / 512, kw) * (turn_fixed + turn_each * resident * warps) + (nz > 1 ? (most_tiles > 1 ? 3.5 : 1.5) : kw > 1 ? 0.7 : 0.05) + (warps == 4 ? 0.0 : 0.05 * ceil_div(c.kz / 512, kw));
+        const double most_tiles = static_cast<double>(ceil_div(c.blocks, gx)), tiles = resident > 1 && nz == 1 ? 0.75 * most_tiles + 0.25 * c.blocks / gx : most_tiles;
+        const double stage_x = 0.7 + resident * tokens * c.kz * 2 / 3e4;
+        const double step = fmax(0.5, step_fixed + step_each * resident * warps);
+        const double tile = ceil_div(c.kz / kStep, kw) * step + (nz > 1 ? (most_tiles > 1 ? 3.5 : 2.0) : kw > 1 ? 0.5 : 0.05) +
+                            (warps == 4 ? 0.0 : (warps == 8 && resident > 1 ? 0.09 : 0.025) * ceil_div(c.kz / kStep, kw));
         const double time = waves * ((c.kc >= c.kz ? stage_x : tiles * (stage_x + 1.5 * ceil_div(c.kz, c.kc))) + tiles * tile);
         if (time < best_time) { best_time = time; best = c; }
       }
@@ -894,9 +887,9 @@ Cut choose_cut(int64_t N, int64_t K, double slots, int mt, int nt, int stage_byt
   p.kw = best.kw;
   p.kz = static_cast<int>(best.kz);
   p.kc = static_cast<int>(best.kc);
-  p.sx_at = static_cast<int>(best.kc / step * x_bytes);
-  p.flags_at = p.sx_at + (q4k ? static_cast<int>(best.kc / 256 * 8 * nt * 64) : 0);
-  p.list_at = static_cast<int>(ceil_div(p.flags_at + best.kc / step * 4, 16) * 16);
+  p.sx_at = static_cast<int>(best.kc / kStep * x_bytes);
+  p.flags_at = p.sx_at + (q4k ? static_cast<int>(best.kc / kStep * 8 * nt * 64) : 0);
+  p.list_at = static_cast<int>(ceil_div(p.flags_at + best.kc / kStep * 4, 16) * 16);
   p.red_at = p.list_at + (grouped ? kListCap * 2 : 0);
   const int rows_cta = best.warps / best.kw * 16;
   p.ring_at = static_cast<int>(ceil_div(p.red_at + (best.kw > 1 || best.nz > 1 ? best.kw * 8 * nt * (rows_cta + 4) * 4 : 0), 16) * 16);
@@ -907,7 +900,7 @@ template <int FMT, int NT, bool LOOSE>
 cudaError_t launch(MvParams& p, int slots, int mt, cudaStream_t st) {
   // experts that even routing is expected to meet; the others' CTAs leave at once
   const double busy = p.ids ? p.G * (1.0 - pow(1.0 - 1.0 / p.G, p.M)) : 1.0;
-  const Cut c = choose_cut(p.N, p.K, busy, mt, NT, kTurn<NT> * kStepBytes<FMT, LOOSE>, NT == 1 ? mt * 4 * 144 : 8 * kXPitch<NT>, kStep, FMT == QF_FMT_Q4_K, LOOSE, p.ids != nullptr, p);
+  const Cut c = choose_cut(p.N, p.K, busy, p.ids ? fmin(mt, fmax(1.0, p.M / busy)) : mt, mt, NT, kStages<NT> * kStepBytes<FMT, LOOSE>, NT == 1 ? mt * 4 * 144 : 8 * kXPitch<NT>, FMT == QF_FMT_Q4_K, LOOSE, p.ids != nullptr, p);
   auto kernel = matvec_kernel<FMT, NT, LOOSE>;
   static bool ready[64] = {};                          // per device
   int dev = 0;
@@ -921,13 +914,15 @@ cudaError_t launch(MvParams& p, int slots, int mt, cudaStream_t st) {
   cfg.blockDim = dim3(32 * c.warps);
   cfg.dynamicSmemBytes = c.smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = 1;
-  attr.val.clusterDim.y = 1;
-  attr.val.clusterDim.z = c.nz;
-  cfg.attrs = &attr;
-  cfg.numAttrs = c.nz > 1 ? 1 : 0;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 1;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = c.nz;
+  cfg.attrs = attr;
+  cfg.numAttrs = c.nz > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 

@@ -288,3 +288,26 @@ def test_on_another_stream_and_in_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(held, both()))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_calls_one_after_another_see_what_the_last_one_wrote(fmt):
+    """A chain of short products in the same buffers, each reading what the one before wrote (their launches overlap), gives the bits of
+    the same chain with a wait after every call."""
+    N = K = 1024
+    codes, scales, ts = gpu(*draw(fmt, (), N, K, seed=3))
+    def chain(wait):
+        a, b = acts((3, K), 5).cuda(), torch.empty((3, N), dtype=BF, device="cuda")
+        for _ in range(60):
+            for src, dst in ((a, b), (b, a)):
+                api.qf_fq_matvec(fmt, src, codes, scales, ts, Y=dst)
+                if wait:
+                    torch.cuda.synchronize()
+                dst.div_(dst.abs().amax() / 4)
+                if wait:
+                    torch.cuda.synchronize()
+            api.qf_fq_matvec(fmt, a, codes, scales, ts, Y=b)          # two products of ours in a row
+            api.qf_fq_matvec(fmt, b.clamp_(-8, 8), codes, scales, ts, Y=a)
+            a.div_(a.abs().amax() / 4)
+        return a
+    assert torch.equal(chain(False), chain(True))
