@@ -35,7 +35,8 @@ namespace qf {
 namespace {
 
 constexpr int kWarpsMost = 16;                       // of a CTA; 128 registers a thread, so 16 warps fill an SM
-// Steps of codes that a warp has in shared memory or on the way: four (37 KB an SM of four warps' copies) where X leaves the room
+// Steps of codes that a warp has in shared memory or on the way: four (9 KB a warp), or two where the X of two token tiles takes the
+// room (five tokens, 4096 x 14336: 17.9 us with two, 15.3 with four and the contraction split at any step)
 template <int NT>
 constexpr int kStages = NT == 1 ? 4 : 2;
 constexpr int kSmemMost = 232448 - 128;              // dynamic shared memory of a CTA
@@ -124,6 +125,7 @@ __device__ __forceinline__ void q4k_unpack(const uint32_t (&m)[4], uint32_t (&v)
 }
 
 constexpr int kStep = 256;                            // weights of a row that a warp takes at a time
+constexpr int kWords = 8;                             // words of codes (FP4) or sub-blocks (Q4_K) that a lane holds of a row
 
 // What a lane holds of one weight row for one step of the contraction: 32 bytes of codes. FP4: 64 consecutive weights. Q4_K: 8
 // bytes of each of the four chunks of a super-block.
@@ -334,7 +336,6 @@ __device__ __forceinline__ uint4 x_word(uint32_t x, int w, uint32_t at, bool liv
 
 template <int FMT, int NT>
 __device__ __forceinline__ bool step_f16(const RowPart<FMT> (&r)[2], uint32_t x, const uint32_t (&at)[NT], bool live, float (&c)[NT][4]) {
-  constexpr int LW = 8;
   bool in = true;
   if constexpr (FMT == QF_FMT_Q4_K) {
     uint32_t v[2][4];
@@ -351,23 +352,21 @@ __device__ __forceinline__ bool step_f16(const RowPart<FMT> (&r)[2], uint32_t x,
         uint4 xv[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) xv[nt] = x_word<NT>(x, 2 * chunk + odd, at[nt], live);
-        {
-          uint32_t w[2][4];
+        uint32_t w[2][4];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t mask = odd ? 0x00F000F0u : 0x000F000Fu;
-            const __half2 fac = odd ? __high2half2(f[i]) : __low2half2(f[i]);
-            const uint32_t q0 = r[i].q[2 * chunk], q1 = r[i].q[2 * chunk + 1];
-            w[i][0] = h2_bits(__hmul2(bits_h2(q0 & mask), fac));
-            w[i][1] = h2_bits(__hmul2(bits_h2((q0 >> 8) & mask), fac));
-            w[i][2] = h2_bits(__hmul2(bits_h2(q1 & mask), fac));
-            w[i][3] = h2_bits(__hmul2(bits_h2((q1 >> 8) & mask), fac));
-          }
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t mask = odd ? 0x00F000F0u : 0x000F000Fu;
+          const __half2 fac = odd ? __high2half2(f[i]) : __low2half2(f[i]);
+          const uint32_t q0 = r[i].q[2 * chunk], q1 = r[i].q[2 * chunk + 1];
+          w[i][0] = h2_bits(__hmul2(bits_h2(q0 & mask), fac));
+          w[i][1] = h2_bits(__hmul2(bits_h2((q0 >> 8) & mask), fac));
+          w[i][2] = h2_bits(__hmul2(bits_h2(q1 & mask), fac));
+          w[i][3] = h2_bits(__hmul2(bits_h2((q1 >> 8) & mask), fac));
+        }
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            mma16816<true>(c[nt], w[0][0], w[1][0], w[0][1], w[1][1], xv[nt].x, xv[nt].y);
-            mma16816<true>(c[nt], w[0][2], w[1][2], w[0][3], w[1][3], xv[nt].z, xv[nt].w);
-          }
+        for (int nt = 0; nt < NT; ++nt) {
+          mma16816<true>(c[nt], w[0][0], w[1][0], w[0][1], w[1][1], xv[nt].x, xv[nt].y);
+          mma16816<true>(c[nt], w[0][2], w[1][2], w[0][3], w[1][3], xv[nt].z, xv[nt].w);
         }
       }
     }
@@ -376,7 +375,7 @@ __device__ __forceinline__ bool step_f16(const RowPart<FMT> (&r)[2], uint32_t x,
     uint32_t f[2];
     __half2 pair[2];                              // NVFP4: two scales as FP16
 #pragma unroll
-    for (int w = 0; w < LW; ++w) {
+    for (int w = 0; w < kWords; ++w) {
       if (w % PER == 0) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -393,20 +392,18 @@ __device__ __forceinline__ bool step_f16(const RowPart<FMT> (&r)[2], uint32_t x,
       uint4 xv[NT];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) xv[nt] = x_word<NT>(x, w, at[nt], live);
-      {
-        uint32_t wa[4], wb[4];
-        e2m1_f16(r[0].q[w], wa);
-        e2m1_f16(r[1].q[w], wb);
+      uint32_t wa[4], wb[4];
+      e2m1_f16(r[0].q[w], wa);
+      e2m1_f16(r[1].q[w], wb);
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          wa[h] = mul_f16x2(wa[h], f[0]);
-          wb[h] = mul_f16x2(wb[h], f[1]);
-        }
+      for (int h = 0; h < 4; ++h) {
+        wa[h] = mul_f16x2(wa[h], f[0]);
+        wb[h] = mul_f16x2(wb[h], f[1]);
+      }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          mma16816<true>(c[nt], wa[0], wb[0], wa[1], wb[1], xv[nt].x, xv[nt].y);
-          mma16816<true>(c[nt], wa[2], wb[2], wa[3], wb[3], xv[nt].z, xv[nt].w);
-        }
+      for (int nt = 0; nt < NT; ++nt) {
+        mma16816<true>(c[nt], wa[0], wb[0], wa[1], wb[1], xv[nt].x, xv[nt].y);
+        mma16816<true>(c[nt], wa[2], wb[2], wa[3], wb[3], xv[nt].z, xv[nt].w);
       }
     }
   }
@@ -422,7 +419,6 @@ struct Sums { float c[NT][4]; };
 
 template <int FMT, int NT>
 __device__ __noinline__ Sums<NT> step_bf16(const MvParams& p, const uint16_t* list, int w0, int c0, int mt, int64_t row0, int n0, int k_step, uint32_t bad) {
-  constexpr int LW = 8;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int64_t scale_pitch = FMT == QF_FMT_Q4_K ? p.K / 16 : p.K / (FMT == QF_FMT_NVFP4 ? 16 : 32);
   Sums<NT> sum = {};
@@ -445,63 +441,59 @@ __device__ __noinline__ Sums<NT> step_bf16(const MvParams& p, const uint16_t* li
 #pragma unroll
     for (int blk = 0; blk < 8; ++blk) {
       const int k = k_step + blk * 32 + t * 8;
-      {
-        uint32_t w[2][4];
-        float es[2];
+      uint32_t w[2][4];
+      float es[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const RowPart<FMT>& part = r[i];
-          uint32_t v[4];
-          q4k_unpack(part.s, v);
+      for (int i = 0; i < 2; ++i) {
+        const RowPart<FMT>& part = r[i];
+        uint32_t v[4];
+        q4k_unpack(part.s, v);
 #pragma unroll
-          for (int h = 0; h < 4; ++h) {                // 128 + C as BF16, minus 128: elements (0, 2), (1, 3), (4, 6), (5, 7)
-            const uint32_t n = (part.q[blk / 2 * 2 + h / 2] >> (4 * (blk & 1) + 8 * (h & 1))) & 0x000F000Fu;
-            w[i][h] = bf2_bits(__hsub2(bits_bf2(n | 0x43004300u), bits_bf2(0x43004300u)));
-          }
-          const float d = __half2float(__ushort_as_half(static_cast<unsigned short>(part.s[0] & 0xFFFFu)));
-          es[i] = d * static_cast<float>((v[blk / 4] >> (8 * (blk & 3))) & 63u);
+        for (int h = 0; h < 4; ++h) {                // 128 + C as BF16, minus 128: elements (0, 2), (1, 3), (4, 6), (5, 7)
+          const uint32_t n = (part.q[blk / 2 * 2 + h / 2] >> (4 * (blk & 1) + 8 * (h & 1))) & 0x000F000Fu;
+          w[i][h] = bf2_bits(__hsub2(bits_bf2(n | 0x43004300u), bits_bf2(0x43004300u)));
         }
+        const float d = __half2float(__ushort_as_half(static_cast<unsigned short>(part.s[0] & 0xFFFFu)));
+        es[i] = d * static_cast<float>((v[blk / 4] >> (8 * (blk & 3))) & 63u);
+      }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const uint4 x = __ldg(reinterpret_cast<const uint4*>(xrow[nt] + k));
-          float c[4] = {};
-          mma16816<false>(c, w[0][0], w[1][0], w[0][1], w[1][1], __byte_perm(x.x, x.y, 0x5410), __byte_perm(x.x, x.y, 0x7632));
-          mma16816<false>(c, w[0][2], w[1][2], w[0][3], w[1][3], __byte_perm(x.z, x.w, 0x5410), __byte_perm(x.z, x.w, 0x7632));
+      for (int nt = 0; nt < NT; ++nt) {
+        const uint4 x = __ldg(reinterpret_cast<const uint4*>(xrow[nt] + k));
+        float c[4] = {};
+        mma16816<false>(c, w[0][0], w[1][0], w[0][1], w[1][1], __byte_perm(x.x, x.y, 0x5410), __byte_perm(x.x, x.y, 0x7632));
+        mma16816<false>(c, w[0][2], w[1][2], w[0][3], w[1][3], __byte_perm(x.z, x.w, 0x5410), __byte_perm(x.z, x.w, 0x7632));
 #pragma unroll
-          for (int j = 0; j < 4; ++j) sum.c[nt][j] = fmaf(es[j >> 1], c[j], sum.c[nt][j]);
-        }
+        for (int j = 0; j < 4; ++j) sum.c[nt][j] = fmaf(es[j >> 1], c[j], sum.c[nt][j]);
       }
     }
   } else {
     constexpr int PER = FMT == QF_FMT_NVFP4 ? 2 : 4;
 #pragma unroll
-    for (int word = 0; word < LW; ++word) {
+    for (int word = 0; word < kWords; ++word) {
       const int k = k_step + t * 64 + word * 8;
-      {
-        uint32_t w[2][4];
+      uint32_t w[2][4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t code = (r[i].s[0] >> (8 * (word / PER))) & 0xFFu, f = bf16_factor<FMT>(code);
-          e2m1_bf16(r[i].q[word], w[i]);
-          const uint32_t rest = FMT == QF_FMT_MXFP4 ? (max(code, 128u) - 1u) * 0x00800080u : 0x3F803F80u;
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t code = (r[i].s[0] >> (8 * (word / PER))) & 0xFFu, f = bf16_factor<FMT>(code);
+        e2m1_bf16(r[i].q[word], w[i]);
+        const uint32_t rest = FMT == QF_FMT_MXFP4 ? (max(code, 128u) - 1u) * 0x00800080u : 0x3F803F80u;
 #pragma unroll
-          for (int h = 0; h < 4; ++h) w[i][h] = mul_bf16x2(mul_bf16x2(w[i][h], f), rest);
-        }
+        for (int h = 0; h < 4; ++h) w[i][h] = mul_bf16x2(mul_bf16x2(w[i][h], f), rest);
+      }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          uint4 x = make_uint4(0u, 0u, 0u, 0u);
-          if (k < p.K) x = __ldg(reinterpret_cast<const uint4*>(xrow[nt] + k));
-          mma16816<false>(sum.c[nt], w[0][0], w[1][0], w[0][1], w[1][1], __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632));
-          mma16816<false>(sum.c[nt], w[0][2], w[1][2], w[0][3], w[1][3], __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
-        }
+      for (int nt = 0; nt < NT; ++nt) {
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (k < p.K) x = __ldg(reinterpret_cast<const uint4*>(xrow[nt] + k));
+        mma16816<false>(sum.c[nt], w[0][0], w[1][0], w[0][1], w[1][1], __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632));
+        mma16816<false>(sum.c[nt], w[0][2], w[1][2], w[0][3], w[1][3], __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
       }
     }
   }
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+  for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        sum.c[nt][j] = (bad >> (nt * 8 + 2 * t + (j & 1))) & 1u ? sum.c[nt][j] * (FMT == QF_FMT_NVFP4 ? 0x1p7f : 1.0f) : 0.0f;
+    for (int j = 0; j < 4; ++j)
+      sum.c[nt][j] = (bad >> (nt * 8 + 2 * t + (j & 1))) & 1u ? sum.c[nt][j] * (FMT == QF_FMT_NVFP4 ? 0x1p7f : 1.0f) : 0.0f;
   return sum;
 }
 
@@ -531,44 +523,40 @@ __device__ __forceinline__ uint32_t add_step(const RowPart<FMT> (&r)[2], uint32_
     if (!__all_sync(0xFFFFFFFFu, in)) bad = 0xFFFFFFFFu;
   if (__builtin_expect(bad != 0u, 0)) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c[nt][j] = (bad >> (nt * 8 + 2 * t + (j & 1))) & 1u ? 0.0f : c[nt][j];
-  }
-  {
-    float f[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      f[i] = FMT == QF_FMT_NVFP4 ? 1.0f / kXScale : 1.0f / (kXScale * 128.0f);
-      if constexpr (FMT == QF_FMT_Q4_K) f[i] = __half2float(__ushort_as_half(static_cast<unsigned short>(r[i].s[0] & 0xFFFFu))) * (0x1p24f / kXScale);
-    }
-#pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[nt][j] = fmaf(f[j >> 1], c[nt][j], acc[nt][j]);
+      for (int j = 0; j < 4; ++j) c[nt][j] = (bad >> (nt * 8 + 2 * t + (j & 1))) & 1u ? 0.0f : c[nt][j];
   }
+  float f[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    f[i] = FMT == QF_FMT_NVFP4 ? 1.0f / kXScale : 1.0f / (kXScale * 128.0f);
+    if constexpr (FMT == QF_FMT_Q4_K) f[i] = __half2float(__ushort_as_half(static_cast<unsigned short>(r[i].s[0] & 0xFFFFu))) * (0x1p24f / kXScale);
+  }
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[nt][j] = fmaf(f[j >> 1], c[nt][j], acc[nt][j]);
   if constexpr (FMT == QF_FMT_Q4_K) {
     // offsets: m6 [16 rows x 8 sub-blocks] times the three parts of the sums of X
-    {
-      uint32_t m6[2];
-      float dmin[2];
+    uint32_t m6[2];
+    float dmin[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        uint32_t v[4];
-        q4k_unpack(r[i].s, v);
-        m6[i] = bf2_bits(__hsub2(bits_bf2(__byte_perm(t & 2 ? v[3] : v[2], 0x43434343u, 0x4140u + (t & 1) * 0x0202u)), bits_bf2(0x43004300u)));
-        dmin[i] = __half2float(__ushort_as_half(static_cast<unsigned short>(r[i].s[0] >> 16)));
-      }
+    for (int i = 0; i < 2; ++i) {
+      uint32_t v[4];
+      q4k_unpack(r[i].s, v);
+      m6[i] = bf2_bits(__hsub2(bits_bf2(__byte_perm(t & 2 ? v[3] : v[2], 0x43434343u, 0x4140u + (t & 1) * 0x0202u)), bits_bf2(0x43004300u)));
+      dmin[i] = __half2float(__ushort_as_half(static_cast<unsigned short>(r[i].s[0] >> 16)));
+    }
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        uint4 b;
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(sx + sx_at[nt]));
-        float m[4] = {};
-        mma16816<false>(m, m6[0], m6[1], m6[0], m6[1], b.x, b.y);
-        mma16816<false>(m, m6[0], m6[1], 0u, 0u, b.z, 0u);
+    for (int nt = 0; nt < NT; ++nt) {
+      uint4 b;
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(sx + sx_at[nt]));
+      float m[4] = {};
+      mma16816<false>(m, m6[0], m6[1], m6[0], m6[1], b.x, b.y);
+      mma16816<false>(m, m6[0], m6[1], 0u, 0u, b.z, 0u);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[nt][j] = fmaf(-dmin[j >> 1], m[j], acc[nt][j]);
-      }
+      for (int j = 0; j < 4; ++j) acc[nt][j] = fmaf(-dmin[j >> 1], m[j], acc[nt][j]);
     }
   }
   return bad;
@@ -578,12 +566,10 @@ template <int FMT, int NT, bool LOOSE>
 __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid_constant__ MvParams p) {
   constexpr int MT = 8 * NT;                           // tokens of a pass
   constexpr bool Q4K = FMT == QF_FMT_Q4_K;
-  constexpr int STEP = kStep;
-  constexpr int LW = 8;                                // 16-byte units of X per lane and step
-  constexpr int XL = LW * 16 + 16;                     // a lane's bytes of X for a step (a single token tile)
-  extern __shared__ __align__(16) uint8_t smem[];                                  // X: [kc / STEP][tokens][4 lanes][XL], or [kc / STEP][LW][MT][4 lanes][16] and padding
+  constexpr int XL = kWords * 16 + 16;                     // a lane's bytes of X for a step (a single token tile)
+  extern __shared__ __align__(16) uint8_t smem[];                                  // X: [kc / kStep][tokens][4 lanes][XL], or [kc / kStep][kWords][MT][4 lanes][16] and padding
   uint4* sx = reinterpret_cast<uint4*>(smem + p.sx_at);                            // Q4_K: [kc / 256][MT][4]: sums over two sub-blocks in three BF16 parts
-  uint32_t* inexact = reinterpret_cast<uint32_t*>(smem + p.flags_at);              // [kc / STEP]: tokens whose X is not exact as staged
+  uint32_t* inexact = reinterpret_cast<uint32_t*>(smem + p.flags_at);              // [kc / kStep]: tokens whose X is not exact as staged
   uint16_t* list = reinterpret_cast<uint16_t*>(smem + p.list_at);                  // grouped: rows of Y served, from w0
   float* red = reinterpret_cast<float*>(smem + p.red_at);                          // split contraction: [kw][MT][rows of the CTA + 4]
   __shared__ int warp_count[kWarpsMost];
@@ -655,27 +641,27 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
         at[nt] = NT == 1 ? (m * 4 + t) * XL : (m * 4 + t) * 16;
         sx_at[nt] = (m * 4 + t) * 16;
       }
-      const uint32_t x_step = NT == 1 ? mt * 4 * XL : LW * kXPitch<NT>;      // bytes of X of a step
+      const uint32_t x_step = NT == 1 ? mt * 4 * XL : kWords * kXPitch<NT>;      // bytes of X of a step
       float acc[NT][4] = {};
 
       for (int b0 = blockIdx.x; b0 < p.blocks; b0 += whole ? p.blocks : gridDim.x) {
         for (int kc0 = k_begin; kc0 < k_end; kc0 += p.kc) {
-          const int kc1 = min(kc0 + p.kc, k_end), steps = (kc1 - kc0 + STEP - 1) / STEP;
+          const int kc1 = min(kc0 + p.kc, k_end), steps = (kc1 - kc0 + kStep - 1) / kStep;
           const int per_tile = kw < steps ? (steps - kw + p.kw - 1) / p.kw : 0;      // steps of this warp in a tile
           const int tiles = whole ? (p.blocks - b0 + gridDim.x - 1) / gridDim.x : 1;
           // the first codes are under way while X is staged
           int next_n = (b0 * (warps / p.kw) + rw) * 16, next = 0, tiles_left = per_tile ? tiles : 0;
           Source<FMT, LOOSE> src;
-          if (tiles_left) src.tile(p, row0, next_n, kc0 + kw * STEP, lane);
+          if (tiles_left) src.tile(p, row0, next_n, kc0 + kw * kStep, lane);
           auto start = [&](int stage) {
             if (tiles_left > 0) {
               src.start(p, smem0 + stage, lane);
               if (++next < per_tile) {
-                src.advance(p.kw * STEP);
+                src.advance(p.kw * kStep);
               } else if (--tiles_left > 0) {
                 next = 0;
                 next_n += gridDim.x * rows_cta;
-                src.tile(p, row0, next_n, kc0 + kw * STEP, lane);
+                src.tile(p, row0, next_n, kc0 + kw * kStep, lane);
               }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
@@ -688,7 +674,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
           // X slice: as many warps for a token as there are to spare; a warp loads 32 units of 8 elements, kBatch times over before
           // it waits
           constexpr int kBatch = 8;
-          const int units = steps * (STEP / 8), groups = (units + 31) / 32;
+          const int units = steps * (kStep / 8), groups = (units + 31) / 32;
           int share = warps;                             // warps of a token
           while (share > 1 && share * mt > warps) share >>= 1;
           for (int m = warp / share; m < mt; m += warps / share) {
@@ -698,14 +684,14 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
               uint4 q[kBatch];
 #pragma unroll
               for (int i = 0; i < kBatch; ++i) {
-                const int v = (g0 + i * share) * 32 + lane, s = v / (STEP / 8), w = v / 4 % LW;       // step, word of codes, and lane v % 4
-                const int unit = Q4K ? v : s * (STEP / 8) + (v & 3) * LW + w;
+                const int v = (g0 + i * share) * 32 + lane, s = v / (kStep / 8), w = v / 4 % kWords;       // step, word of codes, and lane v % 4
+                const int unit = Q4K ? v : s * (kStep / 8) + (v & 3) * kWords + w;
                 q[i] = make_uint4(0u, 0u, 0u, 0u);
                 if (v < units && kc0 + 8 * unit < p.K) q[i] = __ldg(x + unit);
               }
 #pragma unroll
               for (int i = 0; i < kBatch; ++i) {
-                const int v = (g0 + i * share) * 32 + lane, s = v / (STEP / 8), w = v / 4 % LW;
+                const int v = (g0 + i * share) * 32 + lane, s = v / (kStep / 8), w = v / 4 % kWords;
                 if (v >= units) continue;                // for Q4_K a whole warp or none of it
                 uint32_t h[4];
                 if (!stage_f16(q[i], h)) {
@@ -753,7 +739,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
               read_step<FMT, LOOSE>(r, smem + stage, lane, skew);
               if constexpr (FMT == QF_FMT_MXFP4 && LOOSE) {
                 // what stands past the end of the row is no scale of it: one in range instead
-                const int left = p.K - (kc0 + s * STEP + t * 64);
+                const int left = p.K - (kc0 + s * kStep + t * 64);
                 if (left < 64) {
 #pragma unroll
                   for (int i = 0; i < 2; ++i) r[i].s[0] = left <= 0 ? 0x7F7Fu : (r[i].s[0] & 0xFFu) | (left <= 32 ? 0x7F00u : r[i].s[0] & 0xFF00u);
@@ -768,55 +754,55 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
               s += p.kw;
             }
             // end of the tile; a warp without a step in a split contraction meets the others here all the same
-              const int n_warp = (block * (warps / p.kw) + rw) * 16;
-              if (any_bad) {
-                for (int s = 0; s < steps; ++s) {
-                  if (s % p.kw != kw) continue;
-                  const Sums<NT> sum = step_bf16<FMT, NT>(p, list, w0, c0, mt, row0, n_warp, kc0 + s * STEP, inexact[s]);
+            const int n_warp = (block * (warps / p.kw) + rw) * 16;
+            if (any_bad) {
+              for (int s = 0; s < steps; ++s) {
+                if (s % p.kw != kw) continue;
+                const Sums<NT> sum = step_bf16<FMT, NT>(p, list, w0, c0, mt, row0, n_warp, kc0 + s * kStep, inexact[s]);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                      for (int j = 0; j < 4; ++j) acc[nt][j] += sum.c[nt][j];
-                }
+                  for (int j = 0; j < 4; ++j) acc[nt][j] += sum.c[nt][j];
               }
-              if (kc1 == k_end) {
-                const int n_cta = block * rows_cta;
-                if (!split) {
+            }
+            if (kc1 == k_end) {
+              const int n_cta = block * rows_cta;
+              if (!split) {
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                      for (int j = 0; j < 4; ++j) {
-                        const int n = n_warp + g + (j >> 1) * 8, m = nt * 8 + 2 * t + (j & 1);
-                        if (n < p.N && m < mt) store_y(p, w0 + (p.ids ? list[c0 + m] : c0 + m), n, acc[nt][j] * unit);
-                      }
-                } else {
-                  float* mine = red + kw * MT * red_pitch + rw * 16 + g;
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                      for (int j = 0; j < 4; ++j) mine[(nt * 8 + 2 * t + (j & 1)) * red_pitch + (j >> 1) * 8] = acc[nt][j];
-                  if (nz > 1) cg::this_cluster().sync();
-                  else __syncthreads();
-                  // the CTAs of the cluster share the outputs
-                  for (int i = tid + z * threads; i < mt * rows_cta; i += threads * nz) {
-                    const int m = i / rows_cta, n = i - m * rows_cta;
-                    const int at_i = m * red_pitch + n;
-                    float sum = 0.0f;
-                    for (int zz = 0; zz < nz; ++zz) {
-                      const float* part = (nz > 1 ? cg::this_cluster().map_shared_rank(red, zz) : red) + at_i;
-#pragma unroll 4
-                      for (int k = 0; k < p.kw; ++k) sum += part[k * MT * red_pitch];
-                    }
-                    if (n_cta + n < p.N) store_y(p, w0 + (p.ids ? list[c0 + m] : c0 + m), n_cta + n, sum * unit);
+                  for (int j = 0; j < 4; ++j) {
+                    const int n = n_warp + g + (j >> 1) * 8, m = nt * 8 + 2 * t + (j & 1);
+                    if (n < p.N && m < mt) store_y(p, w0 + (p.ids ? list[c0 + m] : c0 + m), n, acc[nt][j] * unit);
                   }
-                  if (nz > 1) cg::this_cluster().sync();
-                  else __syncthreads();
+              } else {
+                float* mine = red + kw * MT * red_pitch + rw * 16 + g;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                  for (int j = 0; j < 4; ++j) mine[(nt * 8 + 2 * t + (j & 1)) * red_pitch + (j >> 1) * 8] = acc[nt][j];
+                if (nz > 1) cg::this_cluster().sync();
+                else __syncthreads();
+                // the CTAs of the cluster share the outputs
+                for (int i = tid + z * threads; i < mt * rows_cta; i += threads * nz) {
+                  const int m = i / rows_cta, n = i - m * rows_cta;
+                  const int at_i = m * red_pitch + n;
+                  float sum = 0.0f;
+                  for (int zz = 0; zz < nz; ++zz) {
+                    const float* part = (nz > 1 ? cg::this_cluster().map_shared_rank(red, zz) : red) + at_i;
+#pragma unroll 4
+                    for (int k = 0; k < p.kw; ++k) sum += part[k * MT * red_pitch];
+                  }
+                  if (n_cta + n < p.N) store_y(p, w0 + (p.ids ? list[c0 + m] : c0 + m), n_cta + n, sum * unit);
                 }
-#pragma unroll
-                  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[nt][j] = 0.0f;
+                if (nz > 1) cg::this_cluster().sync();
+                else __syncthreads();
               }
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[nt][j] = 0.0f;
+            }
           }
           __syncthreads();                               // the slice is read; its memory is free
         }
