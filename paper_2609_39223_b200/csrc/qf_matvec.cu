@@ -566,6 +566,9 @@ template <int FMT, int NT, bool LOOSE>
 __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid_constant__ MvParams p) {
   constexpr int MT = 8 * NT;                           // tokens of a pass
   constexpr bool Q4K = FMT == QF_FMT_Q4_K;
+  // The next copies into a step's place start as soon as it is in registers for FP4 and one token tile (128256 x 4096, 8 tokens: 65 us,
+  // 74 when they start after the products), after the products otherwise (two tiles 82 us against 96, Q4_K with one token 70 against 72)
+  constexpr bool EARLY = NT == 1 && !Q4K;
   constexpr int XL = kWords * 16 + 16;                     // a lane's bytes of X for a step (a single token tile)
   extern __shared__ __align__(16) uint8_t smem[];                                  // X: [kc / kStep][tokens][4 lanes][XL], or [kc / kStep][kWords][MT][4 lanes][16] and padding
   uint4* sx = reinterpret_cast<uint4*>(smem + p.sx_at);                            // Q4_K: [kc / 256][MT][4]: sums over two sub-blocks in three BF16 parts
@@ -583,6 +586,9 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
   const int k_begin = z * p.kz, k_end = min(p.K, k_begin + p.kz);
   const bool whole = p.kc >= p.kz;                     // the slice of X is staged once for all row blocks
   const bool split = p.kw > 1 || nz > 1;
+  // split contraction: the row of a tile and the tokens out_m, out_m + out_step, ... that this thread finishes (rows_cta is a power of
+  // two and at most the number of threads)
+  const int out_n = (tid + z * threads) & (rows_cta - 1), out_m = (tid + z * threads) >> (31 - __clz(rows_cta)), out_step = threads * nz >> (31 - __clz(rows_cta));
 
   launch_after_previous();
   int e = 0;
@@ -650,7 +656,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
           const int per_tile = kw < steps ? (steps - kw + p.kw - 1) / p.kw : 0;      // steps of this warp in a tile
           const int tiles = whole ? (p.blocks - b0 + gridDim.x - 1) / gridDim.x : 1;
           // the first codes are under way while X is staged
-          int next_n = (b0 * (warps / p.kw) + rw) * 16, next = 0, tiles_left = per_tile ? tiles : 0;
+          int next_n = b0 * rows_cta + rw * 16, next = 0, tiles_left = per_tile ? tiles : 0;
           Source<FMT, LOOSE> src;
           if (tiles_left) src.tile(p, row0, next_n, kc0 + kw * kStep, lane);
           auto start = [&](int stage) {
@@ -727,7 +733,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
             if constexpr (LOOSE) {
 #pragma unroll
               for (int i = 0; i < 2; ++i)
-                skew[i] = (static_cast<uint32_t>(row0) + min((block * (warps / p.kw) + rw) * 16 + g + 8 * i, p.N - 1)) * static_cast<uint32_t>(p.K / kBlock<FMT>) & 3u;
+                skew[i] = (static_cast<uint32_t>(row0) + min(block * rows_cta + rw * 16 + g + 8 * i, p.N - 1)) * static_cast<uint32_t>(p.K / kBlock<FMT>) & 3u;
             }
             int s = kw;
 #pragma unroll 1
@@ -745,16 +751,23 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
                   for (int i = 0; i < 2; ++i) r[i].s[0] = left <= 0 ? 0x7F7Fu : (r[i].s[0] & 0xFFu) | (left <= 32 ? 0x7F00u : r[i].s[0] & 0xFF00u);
                 }
               }
+              if constexpr (EARLY) {
+                __syncwarp();
+                start(stage);
+                stage = stage + SB == ring_end ? ring : stage + SB;
+              }
               uint32_t bad = 0u;
               if (any_inexact) bad = inexact[s];
               any_bad |= add_step<FMT, NT>(r, smem0 + s * x_step, smem0 + p.sx_at + s * MT * 64, at, sx_at, live, t, bad, acc);
-              __syncwarp();
-              start(stage);
-              stage = stage + SB == ring_end ? ring : stage + SB;
+              if constexpr (!EARLY) {
+                __syncwarp();
+                start(stage);
+                stage = stage + SB == ring_end ? ring : stage + SB;
+              }
               s += p.kw;
             }
             // end of the tile; a warp without a step in a split contraction meets the others here all the same
-            const int n_warp = (block * (warps / p.kw) + rw) * 16;
+            const int n_cta = block * rows_cta, n_warp = n_cta + rw * 16;
             if (any_bad) {
               for (int s = 0; s < steps; ++s) {
                 if (s % p.kw != kw) continue;
@@ -766,7 +779,6 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
               }
             }
             if (kc1 == k_end) {
-              const int n_cta = block * rows_cta;
               if (!split) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -784,16 +796,22 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
                 if (nz > 1) cg::this_cluster().sync();
                 else __syncthreads();
                 // the CTAs of the cluster share the outputs
-                for (int i = tid + z * threads; i < mt * rows_cta; i += threads * nz) {
-                  const int m = i / rows_cta, n = i - m * rows_cta;
-                  const int at_i = m * red_pitch + n;
-                  float sum = 0.0f;
-                  for (int zz = 0; zz < nz; ++zz) {
-                    const float* part = (nz > 1 ? cg::this_cluster().map_shared_rank(red, zz) : red) + at_i;
-#pragma unroll 4
-                    for (int k = 0; k < p.kw; ++k) sum += part[k * MT * red_pitch];
+                if (n_cta + out_n < p.N) {
+                  for (int m = out_m; m < mt; m += out_step) {
+                    const int at_m = m * red_pitch + out_n;
+                    float sum = 0.0f;
+                    if (nz == 1) {
+#pragma unroll 2
+                      for (int k = 0; k < p.kw; ++k) sum += red[at_m + k * MT * red_pitch];
+                    } else {
+                      for (int zz = 0; zz < nz; ++zz) {
+                        const float* part = cg::this_cluster().map_shared_rank(red, zz) + at_m;
+#pragma unroll 2
+                        for (int k = 0; k < p.kw; ++k) sum += part[k * MT * red_pitch];
+                      }
+                    }
+                    store_y(p, w0 + (p.ids ? list[c0 + m] : c0 + m), n_cta + out_n, sum * unit);
                   }
-                  if (n_cta + n < p.N) store_y(p, w0 + (p.ids ? list[c0 + m] : c0 + m), n_cta + n, sum * unit);
                 }
                 if (nz > 1) cg::this_cluster().sync();
                 else __syncthreads();
