@@ -214,7 +214,8 @@ qf_status_t qf_fq_linear_bwd(const void* dY, const void* X, const void* W, void*
 /* Per-expert variant for mixture-of-experts layers (every expert's latent weights are trained with
  * the same quantization-aware layer). Rows of X are sorted by expert; group_offsets is a device
  * int32[G+1] of segment starts, each a multiple of 128 (the caller pads segments with zero rows;
- * a zero row quantizes to a zero row in every format); rows_padded = group_offsets[G]. The table is device
+ * a zero row quantizes to a zero row in every format); rows_padded >= group_offsets[G], where rows of X (and dY) past the
+ * last segment are zero too and those of Y and dX mean nothing. The table is device
  * memory, so the host cannot check it: the kernels force every entry to a multiple of 128 in [0, rows_padded],
  * and a table that breaks the contract gives meaningless but finite results, never an out-of-range access.
  * W is [G,N,K], Y is [rows_padded,N]:  Y[r,:] = X_hat[r,:] . W_hat[g(r)]^T.
@@ -347,6 +348,7 @@ qf_status_t qf_moe_combine_bwd(const void* dout, qf_dtype_t dout_dtype, const vo
  * Q4_K, by that rounding. For quantized activations pass X_hat (qf_qdq). Results do not depend on what else runs, and the
  * rows of X do not influence one another.
  *   X       BF16 [M, K], K a multiple of the format's block and at most QF_MATVEC_MAX_K; Y BF16 or FP32 [M, N], any N
+ *   scales       as qf_qdq writes them: E4M3 codes 0x00..0x7E, E8M0 codes 0x00..0xFE (the results of others are not defined)
  *   tensor_scale  NVFP4: device float*; otherwise ignored
  * The weights are read once per QF_MATVEC_TOKENS rows of X: meant for M up to about that; a larger M is right but slower
  * than qf_fq_linear_fwd on the dequantized weight. */

@@ -22,8 +22,16 @@
 //    three BF16 parts (24 bits); one FP32 multiply-add per super-block applies d and dmin.
 //  * The tensor core truncates as it accumulates: it adds up one step of 256 elements at a time, the steps are added in FP32.
 //  * Codes arrive through a ring of kStages steps per warp in shared memory (cp.async), so that loads in flight cost no registers.
-//  * Rows are cut into tiles of 16 or 32 for a warp; the contraction is split over the warps of a CTA and over the CTAs of a
+//  * Rows are cut into tiles of 16 for a warp; the contraction is split over the warps of a CTA and over the CTAs of a
 //    cluster where there are too few tiles to keep every SM loading; the parts meet in (distributed) shared memory in a fixed order.
+//
+// What bounds it. 128256 x 4096, NVFP4: 61 us with one token (4.85 TB/s, 0.74 of the copy rate), 65 with 8, 82 with 16; MXFP4 82 with 16;
+// Q4_K 70 with one (4.2 TB/s). A warp's step of 16 x 256 weights takes about 270 instructions: 165 to decode and multiply (Q4_K
+// 205), 58 for the ring, the rest for tile ends and X. Decode and products alone, from registers, take an SM's schedulers 286
+// cycles a step (440 with two token tiles, whose X also takes 0.6 of the shared memory bandwidth) where the copy rate allows 394: both
+// have to overlap with four warps a scheduler, which is all that 128 registers leave (at 96 registers the spills cost 1.7 times). Sums
+// kept in two chains of products, Q4_K scales applied after the products instead of before: no gain, 1.03 times as long.
+// Small weights are bound by the launch, one staging of X and one trip to memory: 1024 x 4096 takes 5.1 us.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -840,8 +848,9 @@ struct Cut {
 
 // Picks the cut with the least estimated time. The constants are microseconds measured on this part: a step takes step_fixed and
 // step_each per warp that the SM holds, 0.5 at least; meeting costs 0.5 in a CTA and 2 in a cluster (3.5 if there are tiles to
-// come, since it empties the rings); a slice of X takes 0.7 and 1 per 30 KB that the SM stages. Over 68 products from
-// 1024 x 4096 to 128256 x 4096 with 1 to 16 tokens the choice took 1.02 times as long as the best cut in the mean, 1.19 at most.
+// come, since it empties the rings); a slice of X takes 0.7 and 1 per 30 KB that the SM stages. Over 58 products from
+// 1024 x 4096 to 128256 x 4096 with 1 to 24 tokens the choice took 1.02 times as long as the best cut in the mean, 1.22 at most (128
+// experts of 2048 x 768, one token: 8.3 us, 6.8 with twice the CTAs of two warps a tile).
 Cut choose_cut(int64_t N, int64_t K, double slots, double tokens, int mt, int nt, int ring_bytes, int x_bytes, bool q4k, bool loose, bool grouped, MvParams& p) {
   Cut best{};
   double best_time = 1e30;
