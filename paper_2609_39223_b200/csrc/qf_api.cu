@@ -716,8 +716,9 @@ static qf_status_t matvec_impl(int fmt, const void* X, int64_t M, int64_t x_rows
                                const void* scales, const float* tscale, int64_t N, int64_t K, void* Y, int y_dtype, void* stream) {
   if (!valid_fmt(fmt, false)) return QF_ERR_FORMAT;
   if (!valid_dtype(y_dtype)) return QF_ERR_DTYPE;
-  // rows are numbered in 32 bits, and so are the bytes from the first to the last of a tile's 32 rows; other offsets in 64
-  if (M < 0 || N < 0 || K < 0 || K % block_of(fmt) || M > INT32_MAX - 256 || N > INT32_MAX - 1024 || K > QF_MATVEC_MAX_K) return QF_ERR_SHAPE;
+  // rows of X and of the weight are numbered in 32 bits, up to the end of a listing of 1024 and of a CTA's 512 rows, and so are the
+  // bytes from the first to the last row of a tile; other offsets in 64
+  if (M < 0 || N < 0 || K < 0 || K % block_of(fmt) || M > INT32_MAX - 1024 || N > INT32_MAX - 1024 || K > QF_MATVEC_MAX_K) return QF_ERR_SHAPE;
   if (x_rows < 0 || (M > 0 && (x_rows < 1 || M % x_rows))) return QF_ERR_SHAPE;
   const bool any = M > 0 && N > 0;
   if (any && (!Y || (K > 0 && (!X || !codes || !scales || (fmt == QF_FMT_NVFP4 && !tscale))))) return QF_ERR_NULL;

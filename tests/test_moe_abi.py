@@ -131,6 +131,18 @@ def test_matvec_refusals():
         assert f() == HERE and f(fmt=api.FMT_MXFP4, ts=None) == HERE and f(M=0) == HERE
 
 
+
+def test_matvec_row_numbers_fit_32_bits():
+    """Rows are walked 1024 at a time with 32-bit numbers: the last step must not pass 2^31 - 1."""
+    f = _call(api.lib().qf_fq_matvec, "fmt X M codes scales ts N K Y dt".split(),
+              dict(fmt=api.FMT_NVFP4, X=P, M=1, codes=P, scales=P, ts=P, N=1, K=16, Y=P, dt=BF))
+    for name in ("M", "N"):
+        for most in ((1 << 31) - 1024, (1 << 31) - 257, (1 << 31) - 1):
+            assert f(**{name: most}) == SHAPE, (name, most)
+        if HERE:
+            assert f(**{name: (1 << 31) - 1025}) == HERE, name
+
+
 def test_grouped_matvec_refusals():
     f = _call(api.lib().qf_fq_grouped_matvec, "fmt X xr ids idt pairs G codes scales ts N K Y dt".split(),
               dict(fmt=api.FMT_MXFP4, X=P, xr=3, ids=P, idt=I32, pairs=24, G=16, codes=P, scales=P, ts=None, N=10, K=512, Y=P, dt=BF))
