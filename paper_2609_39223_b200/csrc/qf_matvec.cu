@@ -25,9 +25,9 @@
 //  * Rows are cut into tiles of 16 for a warp; the contraction is split over the warps of a CTA and over the CTAs of a
 //    cluster where there are too few tiles to keep every SM loading; the parts meet in (distributed) shared memory in a fixed order.
 //
-// What bounds it. 128256 x 4096, NVFP4: 61 us with one token (4.85 TB/s, 0.74 of the copy rate), 65 with 8, 82 with 16; MXFP4 82 with 16;
-// Q4_K 70 with one (4.2 TB/s). A warp's step of 16 x 256 weights takes about 270 instructions: 165 to decode and multiply (Q4_K
-// 205), 58 for the ring, the rest for tile ends and X. Decode and products alone, from registers, take an SM's schedulers 286
+// What bounds it. 128256 x 4096, NVFP4: 59 us with one token (5.0 TB/s, 0.76 of the copy rate), 64 with 8, 80 with 16; MXFP4 81 with 16;
+// Q4_K 70 with one (4.2 TB/s). A warp's step of 16 x 256 weights takes about 250 instructions: 165 to decode and multiply (Q4_K
+// 205), 45 for the ring, the rest for tile ends and X. Decode and products alone, from registers, take an SM's schedulers 286
 // cycles a step (440 with two token tiles, whose X also takes 0.6 of the shared memory bandwidth) where the copy rate allows 394: both
 // have to overlap with four warps a scheduler, which is all that 128 registers leave (at 96 registers the spills cost 1.7 times). Sums
 // kept in two chains of products, Q4_K scales applied after the products instead of before: no gain, 1.03 times as long.
@@ -234,7 +234,11 @@ struct Source {
     constexpr int ROWS = LOOSE ? 8 : 4, GAP = 16 / ROWS, PIECE = LOOSE ? 8 : 16, HALF = kStepScales<FMT, LOOSE> / 2;
     const int piece = LOOSE ? lane & 15 : lane & 7;
     const uint32_t to = stage + (LOOSE ? piece_at<FMT>(lane >> 4, piece >> 1) + (piece & 1) * 8 : piece_at<FMT>(lane >> 3, piece));
-    const uint8_t* c = codes - (FMT != QF_FMT_Q4_K && k + piece * (2 * PIECE) >= p.K ? piece * PIECE : 0);
+    const uint8_t *c = codes, *sc = scales;
+    if (FMT != QF_FMT_Q4_K && p.K % kStep) {             // the same for all: rows of whole steps skip the comparisons
+      if (k + piece * (2 * PIECE) >= p.K) c -= piece * PIECE;
+      if (!LOOSE && k + 128 >= p.K && (lane & 1)) sc -= HALF;
+    }
 #pragma unroll
     for (int h = 0; h < ROWS; ++h) {                   // a gap keeps the bits of the row that permute pieces
       const uint32_t off = h == 0 ? 0u : LOOSE ? static_cast<uint32_t>(min(h * GAP, more)) * (static_cast<uint32_t>(p.K) / 2) : row[(h - 1) & 3];
@@ -244,7 +248,7 @@ struct Source {
     if constexpr (FMT == QF_FMT_Q4_K) {
       if (lane < 16) copy_async<16>(to_sc + lane * 16, scales);
     } else if constexpr (!LOOSE) {
-      copy_async<HALF>(to_sc + lane * HALF, scales - (k + 128 >= p.K && (lane & 1) ? HALF : 0));
+      copy_async<HALF>(to_sc + lane * HALF, sc);
     } else {
       const int64_t room = p.scales_end - scales;      // the last words may lie past the end of the tensor
 #pragma unroll
