@@ -173,7 +173,7 @@ __device__ __forceinline__ void load_part(RowPart<FMT>& r, const uint8_t* codes,
 // of eight rows at a time, took 81 us for the copies of a 128256 x 4096 weight where this takes 49.) Pieces are permuted
 // inside a row so that the lanes that read together meet different banks. Then the scales of every row.
 // LOOSE: rows that do not start on 16 bytes, or scales that do not start on words (K not a multiple of 128): pieces of 8 bytes,
-// 16 lanes a row, and for the scales the aligned words around them (NVFP4, one token, 32768 x 4112: 33 us, where 4096 takes 21; with lanes that copied their own 8 bytes of two rows it was 49).
+// 16 lanes a row, and for the scales the aligned words around them (NVFP4, one token, 32768 x 4112: 31 us, where 4096 takes 21; with lanes that copied their own 8 bytes of two rows it was 49).
 
 template <int FMT, bool LOOSE>
 constexpr int kStepScales = LOOSE ? (FMT == QF_FMT_MXFP4 ? 16 : 24) : FMT == QF_FMT_MXFP4 ? 8 : 16;       // bytes a row
