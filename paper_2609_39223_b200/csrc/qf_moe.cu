@@ -332,12 +332,13 @@ __global__ void __launch_bounds__(kThreads, 3) moe_combine_bwd_kernel(const MoeT
 
 }  // namespace
 
-// Largest cluster of the sort kernel that the current device can hold with the most shared memory it may ask for.
+// Readies the sort kernels on the current device, once: room for the largest table that a call may ask for (never lowered for a smaller
+// one: another host thread may be about to launch with a larger one) and clusters of 16. *ctas: the largest cluster that the device can hold.
 static cudaError_t sort_cluster(int* ctas) {
   static int known[64] = {};
   int dev = 0;
   if (cudaError_t e = cudaGetDevice(&dev)) return e;
-  if (dev < 64 && known[dev]) { *ctas = known[dev]; return cudaSuccess; }
+  if (dev < 64 && (*ctas = __atomic_load_n(&known[dev], __ATOMIC_ACQUIRE))) return cudaSuccess;
   constexpr int kMostSmem = (kSortWarps + 1) * QF_MOE_MAX_EXPERTS * 4;
   bool room = true;
   auto ask = [&](auto kernel) -> cudaError_t {
@@ -362,27 +363,23 @@ static cudaError_t sort_cluster(int* ctas) {
   if (cudaError_t e = ask(moe_sort_kernel<int32_t>)) return e;
   if (cudaError_t e = ask(moe_sort_kernel<int64_t>)) return e;
   *ctas = room ? 16 : 8;
-  if (dev < 64) known[dev] = *ctas;
+  if (dev < 64) __atomic_store_n(&known[dev], *ctas, __ATOMIC_RELEASE);
   return cudaSuccess;
 }
 
 cudaError_t launch_moe_sort(const void* ids, bool ids64, int64_t pairs, int G, int64_t rows, int32_t* row_of, int32_t* offs,
                             int32_t* counts, cudaStream_t st) {
-  const size_t smem = static_cast<size_t>(kSortWarps + 1) * G * 4;
   // one CTA of a cluster for every kSortPairs pairs: up to 16 (10.9 us for 131072 pairs to 128 experts, 17.0 with 8 CTAs), or
   // the portable 8 where the device has no room for 16
   constexpr int64_t kSortPairs = 4096;
   int most = 1, ctas = 1;
-  if (pairs > kSortPairs)
-    if (cudaError_t e = sort_cluster(&most)) return e;
+  if (cudaError_t e = sort_cluster(&most)) return e;
   while (ctas < most && pairs > ctas * kSortPairs) ctas *= 2;
   auto go = [&](auto kernel, auto* p) -> cudaError_t {
-    if (smem > 48 * 1024)
-      if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem))) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(ctas);
     cfg.blockDim = dim3(kSortThreads);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = static_cast<size_t>(kSortWarps + 1) * G * 4;
     cfg.stream = st;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;
