@@ -57,7 +57,7 @@ class MoeLayer:
         offs = plan.group_offsets
         xs = api.qf_moe_dispatch(x, plan)
         gate_up = api.qf_fq_grouped_linear_fwd(xs, self.w_gate_up, offs, self.fmt, api.FMT_NONE, w_tscale=self._scales())
-        # rows past the last segment are not written by the product; no pair owns them
+        # rows past the last segment are not written by the product; no pair owns them and the next product leaves them out
         h = self.swiglu(gate_up)
         ys = api.qf_fq_grouped_linear_fwd(h, self.w_down, offs, self.fmt, api.FMT_NONE, w_tscale=self._scales())
         return api.qf_moe_combine(ys, weights, plan), (plan, xs, gate_up, h, ys, weights)

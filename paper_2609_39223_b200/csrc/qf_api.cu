@@ -63,11 +63,13 @@ Workspace carve(void* ws, int64_t N, int64_t K, int64_t groups) {
 
 // Fake-quantize one operand into `dst` (BF16, same shape). NVFP4 derives or reads its tensor scale.
 // `groups` > 1 (NVFP4 weights of a grouped layer): every expert has its own tensor scale, tscale_user is an
-// array of `groups` floats (required).
+// array of `groups` floats (required). rows_end: activations of a grouped layer, see QdqArgs.
 qf_status_t quantize_operand(int fmt, const void* src, int64_t rows, int64_t cols, void* dst, float* tscale_user,
                              bool tscale_given, uint32_t* header, int amax_word, int scale_word, cudaStream_t st,
-                             int groups = 1, bool mxfp4_noclip = false, bool speculative = false, uint32_t* amax_accum = nullptr) {
+                             int groups = 1, bool mxfp4_noclip = false, bool speculative = false, uint32_t* amax_accum = nullptr,
+                             const int32_t* rows_end = nullptr) {
   QdqArgs q{};
+  q.rows_end = rows_end;
   q.mxfp4_noclip = mxfp4_noclip;
   q.spec.amax_accum = amax_accum;       // FP4 formats, single pass: also accumulate max|src| there (zeroed beforehand)
   q.fmt = fmt;
@@ -92,9 +94,10 @@ qf_status_t quantize_operand(int fmt, const void* src, int64_t rows, int64_t col
 // pointer to the final scale(s) - the caller's when given, otherwise derived now from the operand's maximum (and written
 // back to the caller's array when there is one), with the maximum left in header[amax_word] for single tensors.
 qf_status_t fused_nvfp4_scale(const void* src, int64_t rows, int64_t cols, float* tscale_user, bool given, uint32_t* header,
-                              int amax_word, int scale_word, int groups, cudaStream_t st, const float** out) {
+                              int amax_word, int scale_word, int groups, cudaStream_t st, const float** out, const int32_t* rows_end = nullptr) {
   if (given) { *out = tscale_user; return QF_OK; }
   QdqArgs q{};
+  q.rows_end = rows_end;
   q.fmt = QF_FMT_NVFP4;
   q.in = src;
   q.rows = rows;
@@ -148,6 +151,7 @@ qf_status_t linear_fwd_impl(const void* X, const void* W, void* Y, int y_dtype, 
     return cu(cudaMemsetAsync(Y, 0, static_cast<size_t>(M) * N * (y_dtype == QF_DT_F32 ? 4 : 2), st));
   Workspace w = carve(ws, N, K, groups);
   if (cudaError_t e = cudaMemsetAsync(w.header, 0, kWsHeader, st)) return cu(e);
+  const int32_t* rows_end = grouped ? offs + G : nullptr;      // of the rows that belong to a segment
   GemmArgs g{};
   g.C = Y;
   g.Mo = M; g.No = N; g.Kc = K;
@@ -185,10 +189,10 @@ qf_status_t linear_fwd_impl(const void* X, const void* W, void* Y, int y_dtype, 
   if (fuse_a) {
     g.fuse_a_fmt = aq;
     if (aq == QF_FMT_NVFP4)
-      if (qf_status_t s = fused_nvfp4_scale(X, M, K, a_ts, flags & QF_A_TSCALE_GIVEN, w.header, kWsAmaxA, kWsScaleA, 1, st, &g.fuse_a_tscale)) return s;
+      if (qf_status_t s = fused_nvfp4_scale(X, M, K, a_ts, flags & QF_A_TSCALE_GIVEN, w.header, kWsAmaxA, kWsScaleA, 1, st, &g.fuse_a_tscale, rows_end)) return s;
   } else if (aq != QF_FMT_NONE) {
     if (!(flags & QF_REUSE_X_HAT))
-      if (qf_status_t s = quantize_operand(aq, X, M, K, w.x_hat, a_ts, flags & QF_A_TSCALE_GIVEN, w.header, kWsAmaxA, kWsScaleA, st, 1, (flags & QF_MXFP4_NO_CLIP) != 0, false, (a_amax_out && x_accumulates) ? amax_word : nullptr)) return s;
+      if (qf_status_t s = quantize_operand(aq, X, M, K, w.x_hat, a_ts, flags & QF_A_TSCALE_GIVEN, w.header, kWsAmaxA, kWsScaleA, st, 1, (flags & QF_MXFP4_NO_CLIP) != 0, false, (a_amax_out && x_accumulates) ? amax_word : nullptr, rows_end)) return s;
     Xh = w.x_hat;
   }
   if (a_amax_out)
@@ -220,6 +224,7 @@ qf_status_t linear_bwd_impl(const void* dY, const void* X, const void* W, void* 
   }
   Workspace w = carve(ws, N, K, groups);
   if (cudaError_t e = cudaMemsetAsync(w.header, 0, kWsHeader, st)) return cu(e);
+  const int32_t* rows_end = grouped ? offs + G : nullptr;      // of the rows that belong to a segment
   bool x_hat_done = false;          // X_hat already produced by a side job of the dX launch
   if (dX) {
     // dX[M,K] = dY[M,N] . W_hat[N,K]: A = dY contraction-major, B = W_hat stored [contraction N, K]
@@ -277,10 +282,10 @@ qf_status_t linear_bwd_impl(const void* dY, const void* X, const void* W, void* 
     if (fuse_b) {
       g.fuse_b_fmt = aq;                 // the activations are this product's B operand; one scale for all of X
       if (aq == QF_FMT_NVFP4)
-        if (qf_status_t s = fused_nvfp4_scale(X, M, K, a_ts, flags & QF_A_TSCALE_GIVEN, w.header, kWsAmaxA, kWsScaleA, 1, st, &g.fuse_b_tscale)) return s;
+        if (qf_status_t s = fused_nvfp4_scale(X, M, K, a_ts, flags & QF_A_TSCALE_GIVEN, w.header, kWsAmaxA, kWsScaleA, 1, st, &g.fuse_b_tscale, rows_end)) return s;
     } else if (aq != QF_FMT_NONE) {
       if (!(flags & QF_REUSE_X_HAT) && !x_hat_done)
-        if (qf_status_t s = quantize_operand(aq, X, M, K, w.x_hat, a_ts, flags & QF_A_TSCALE_GIVEN, w.header, kWsAmaxA, kWsScaleA, st, 1, (flags & QF_MXFP4_NO_CLIP) != 0)) return s;
+        if (qf_status_t s = quantize_operand(aq, X, M, K, w.x_hat, a_ts, flags & QF_A_TSCALE_GIVEN, w.header, kWsAmaxA, kWsScaleA, st, 1, (flags & QF_MXFP4_NO_CLIP) != 0, false, nullptr, rows_end)) return s;
       Xh = w.x_hat;
     }
     g.B = Xh;

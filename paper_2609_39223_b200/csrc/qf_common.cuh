@@ -253,6 +253,8 @@ struct QdqArgs {
   bool reverse;                  // walk the tensor back to front (after an amax pass: L2 holds the tail)
   bool mxfp4_noclip;             // MXFP4: smallest block exponent without saturation (QF_MXFP4_NO_CLIP)
   int groups;                    // NVFP4: > 1 = that many equal tensors back to back, each with its own tensor scale
+  const int32_t* rows_end;       // NVFP4 activations of a grouped layer (else null): device word, the end of the last segment; a derived
+                                 // tensor scale looks at the rows before it alone
   Nvfp4Speculation spec;         // all null unless launch_qdq_nvfp4_speculative() fills it in
   // LoRA merge ahead of the quantizer (lora_rank > 0): the input is W + lora_scale * B A, formed on the fly
   const void* lora_B;            // [rows, rank] BF16
@@ -277,7 +279,8 @@ struct QdqBatchArgs {
 };
 cudaError_t launch_qdq_batched(const QdqBatchArgs& a, cudaStream_t st);
 
-cudaError_t launch_amax(const void* in, int64_t n, uint32_t* amax_bits, cudaStream_t st);
+// rows_end (nullable): the maximum of the first *rows_end rows of row_elems elements each (a multiple of 8, then n a multiple of it)
+cudaError_t launch_amax(const void* in, int64_t n, uint32_t* amax_bits, cudaStream_t st, const int32_t* rows_end = nullptr, int64_t row_elems = 0);
 cudaError_t launch_qdq_nvfp4_speculative(const QdqArgs& a, uint32_t* header, int amax_word, int guess_word, cudaStream_t st);
 cudaError_t launch_amax_to_float(const uint32_t* amax_bits, float* out, cudaStream_t st);
 cudaError_t launch_amax_to_scale(const uint32_t* amax_bits, float* scale, cudaStream_t st);

@@ -54,12 +54,14 @@ struct LoraLoader {
 // ---------------------------------------------------------------------------------------------
 
 template <typename Loader>
-__global__ void __launch_bounds__(kThreads) amax_kernel(Loader src, int64_t nchunks,
+__global__ void __launch_bounds__(kThreads) amax_kernel(Loader src, int64_t nchunks, const int32_t* __restrict__ rows_end, int64_t row_chunks,
                                                         const __nv_bfloat16* __restrict__ tail, int ntail,
                                                         uint32_t* __restrict__ amax_bits) {
   // gridDim.y > 1: one tensor per y-slice (the experts of a grouped layer), nchunks chunks each
   const Loader in = src.slice(static_cast<int64_t>(blockIdx.y) * nchunks);
   amax_bits += blockIdx.y;
+  // rows past the last segment of a grouped layer's buffer hold nothing; the entry is read as the products read it
+  if (rows_end) nchunks = min(nchunks, static_cast<int64_t>(max(__ldg(rows_end), 0) & ~127) * row_chunks);
   uint32_t m = 0;
   const int64_t stride = static_cast<int64_t>(gridDim.x) * kThreads;
   int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
@@ -674,14 +676,14 @@ cudaError_t launch_amax_grouped(const void* in, int64_t n, int G, uint32_t* amax
   int gx = grid_for(nchunks, 4);
   const int cap = (kNumSMs * 8 + G - 1) / G;
   if (gx > cap) gx = cap < 1 ? 1 : cap;
-  amax_kernel<PlainLoader><<<dim3(gx, G), kThreads, 0, st>>>(PlainLoader{static_cast<const uint4*>(in)}, nchunks, nullptr, 0, amax_bits);
+  amax_kernel<PlainLoader><<<dim3(gx, G), kThreads, 0, st>>>(PlainLoader{static_cast<const uint4*>(in)}, nchunks, nullptr, 0, nullptr, 0, amax_bits);
   return cudaGetLastError();
 }
 
-cudaError_t launch_amax(const void* in, int64_t n, uint32_t* amax_bits, cudaStream_t st) {
+cudaError_t launch_amax(const void* in, int64_t n, uint32_t* amax_bits, cudaStream_t st, const int32_t* rows_end, int64_t row_elems) {
   const int64_t nchunks = n / 8;
   const int ntail = static_cast<int>(n % 8);
-  amax_kernel<PlainLoader><<<grid_for(nchunks, 4), kThreads, 0, st>>>(PlainLoader{static_cast<const uint4*>(in)}, nchunks,
+  amax_kernel<PlainLoader><<<grid_for(nchunks, 4), kThreads, 0, st>>>(PlainLoader{static_cast<const uint4*>(in)}, nchunks, rows_end, row_elems / 8,
                                                                       static_cast<const __nv_bfloat16*>(in) + nchunks * 8, ntail,
                                                                       amax_bits);
   return cudaGetLastError();
@@ -884,10 +886,10 @@ cudaError_t launch_qdq_nvfp4_derive(const QdqArgs& a, uint32_t* header, int amax
   if (a.lora_rank > 0) {
     // the absolute maximum is that of the merged weight, so the amax pass merges on the fly as well
     const int64_t nchunks = a.rows * a.cols / 8;
-    if (nchunks > 0) amax_kernel<LoraLoader><<<grid_for(nchunks, 4), kThreads, 0, st>>>(lora_loader(a), nchunks, nullptr, 0, amax_bits);
+    if (nchunks > 0) amax_kernel<LoraLoader><<<grid_for(nchunks, 4), kThreads, 0, st>>>(lora_loader(a), nchunks, nullptr, 0, nullptr, 0, amax_bits);
     if (cudaError_t e = cudaGetLastError()) return e;
   } else {
-    if (cudaError_t e = launch_amax(a.in, a.rows * a.cols, amax_bits, st)) return e;
+    if (cudaError_t e = launch_amax(a.in, a.rows * a.cols, amax_bits, st, a.rows_end, a.cols)) return e;
     q.reverse = true;
   }
   q.amax_bits = amax_bits;
@@ -904,7 +906,7 @@ cudaError_t launch_nvfp4_scales_only(const QdqArgs& a, uint32_t* header, int ama
     amax_to_scale_inplace_kernel<<<(a.groups + kThreads - 1) / kThreads, kThreads, 0, st>>>(bits, a.groups);
     return cudaGetLastError();
   }
-  if (cudaError_t e = launch_amax(a.in, a.rows * a.cols, header + amax_word, st)) return e;
+  if (cudaError_t e = launch_amax(a.in, a.rows * a.cols, header + amax_word, st, a.rows_end, a.cols)) return e;
   return launch_amax_to_scale(header + amax_word, a.tscale_out, st);
 }
 
