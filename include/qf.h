@@ -416,6 +416,12 @@ qf_status_t qf_selftest_cvt(const float* in, int64_t n, uint8_t* e2m1_out, uint8
  * receives the number of differences. */
 qf_status_t qf_selftest_div(const float* xs, int64_t nx, const float* ys, int64_t ny, uint64_t* mismatches, void* stream);
 
+/* Self-test hook for how a product with a few tokens is cut (no GPU is touched): for M rows of Y, G experts or 0 for the plain
+ * product, cut (host) receives token tiles of 8 in a pass, whether rows start off 16 bytes, warps of a CTA, warps that share a row
+ * tile, CTAs that share a contraction, its length for one of them, the length staged at a time, row blocks and the CTAs
+ * that take turns at them. The cut is an estimate's choice, so that tests name the paths they want and see that they have them. */
+qf_status_t qf_selftest_matvec_cut(qf_format_t fmt, int64_t M, int64_t N, int64_t K, int G, int cut[9]);
+
 /* Self-test hook for the bounded device-side waits: launches one thread that waits, with the given limit
  * in SM clock cycles (at most 2^28), on a barrier nothing ever arrives at. The wait gives up, the kernel
  * returns normally, and the workspace then holds QF_ERR_TIMEOUT in its status word (qf_read_status)

@@ -32,7 +32,7 @@ EXPORTS = [
     "qf_fq_linear_fwd", "qf_fq_linear_bwd", "qf_fq_grouped_linear_fwd", "qf_fq_grouped_linear_bwd", "qf_selftest_cvt",
     "qf_selftest_div", "qf_fq_linear_fwd_noalloc", "qf_selftest_mxfp4_bf16", "qf_selftest_timeout", "qf_pack_bytes", "qf_pack", "qf_unpack", "qf_nvfp4_tensor_scale", "qf_qdq_lora",
     "qf_fp4_matmul_native", "qf_qdq_batched", "qf_moe_rows_bound", "qf_moe_sort", "qf_moe_dispatch", "qf_moe_dispatch_bwd",
-    "qf_moe_combine", "qf_moe_combine_bwd", "qf_fq_matvec", "qf_fq_grouped_matvec",
+    "qf_moe_combine", "qf_moe_combine_bwd", "qf_fq_matvec", "qf_fq_grouped_matvec", "qf_selftest_matvec_cut",
 ]
 NOALLOC_SCRATCH_BYTES = 32 << 20
 LAYOUT_GGUF_Q4_K, LAYOUT_FP4_SWIZZLED_SCALES = 1, 2
@@ -129,6 +129,8 @@ def lib() -> ctypes.CDLL:
         L.qf_fq_grouped_matvec.restype = c_int
         L.qf_fq_grouped_matvec.argtypes = [c_int, c_void_p, c_int64, c_void_p, c_int, c_int64, c_int, c_void_p, c_void_p, c_void_p,
                                            c_int64, c_int64, c_void_p, c_int, c_void_p]
+        L.qf_selftest_matvec_cut.restype = c_int
+        L.qf_selftest_matvec_cut.argtypes = [c_int, c_int64, c_int64, c_int64, c_int, c_void_p]
         _lib = L
     return _lib
 
@@ -354,6 +356,25 @@ def qf_fq_linear_fwd_noalloc(X, W, Y, wq_fmt: int, aq_fmt: int, *, w_tscale=None
     _check(lib().qf_fq_linear_fwd_noalloc(_ptr(X), _ptr(W), _ptr(Y), _dt(Y.dtype), M, N, K, wq_fmt, aq_fmt, _ptr(w_tscale),
                                           _ptr(a_tscale), flags, _stream()), "qf_fq_linear_fwd_noalloc")
     return Y
+
+
+class MatvecCut(NamedTuple):
+    """How a product with a few tokens is cut (see qf_selftest_matvec_cut in qf.h)."""
+    token_tiles: int
+    loose: int
+    warps: int
+    kw: int
+    nz: int
+    kz: int
+    kc: int
+    blocks: int
+    grid_x: int
+
+
+def qf_selftest_matvec_cut(fmt: int, M: int, N: int, K: int, experts: int = 0) -> MatvecCut:
+    out = (c_int * 9)()
+    _check(lib().qf_selftest_matvec_cut(fmt, M, N, K, experts, out), "qf_selftest_matvec_cut")
+    return MatvecCut(*out)
 
 
 def qf_selftest_mxfp4_bf16() -> int:

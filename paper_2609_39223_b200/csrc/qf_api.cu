@@ -717,13 +717,17 @@ qf_status_t qf_moe_combine_bwd(const void* dout, qf_dtype_t dout_dtype, const vo
                                    ys, ys_dtype, weights, dys, dweights, st));
 }
 
+// rows of X and of the weight are numbered in 32 bits, up to the end of a listing of 1024 and of a CTA's 512 rows, and so are the
+// bytes from the first to the last row of a tile; other offsets in 64
+static bool matvec_shape_ok(int fmt, int64_t M, int64_t N, int64_t K) {
+  return M >= 0 && N >= 0 && K >= 0 && K % block_of(fmt) == 0 && M <= INT32_MAX - 1024 && N <= INT32_MAX - 1024 && K <= QF_MATVEC_MAX_K;
+}
+
 static qf_status_t matvec_impl(int fmt, const void* X, int64_t M, int64_t x_rows, const void* ids, int ids_dtype, int G, const void* codes,
                                const void* scales, const float* tscale, int64_t N, int64_t K, void* Y, int y_dtype, void* stream) {
   if (!valid_fmt(fmt, false)) return QF_ERR_FORMAT;
   if (!valid_dtype(y_dtype)) return QF_ERR_DTYPE;
-  // rows of X and of the weight are numbered in 32 bits, up to the end of a listing of 1024 and of a CTA's 512 rows, and so are the
-  // bytes from the first to the last row of a tile; other offsets in 64
-  if (M < 0 || N < 0 || K < 0 || K % block_of(fmt) || M > INT32_MAX - 1024 || N > INT32_MAX - 1024 || K > QF_MATVEC_MAX_K) return QF_ERR_SHAPE;
+  if (!matvec_shape_ok(fmt, M, N, K)) return QF_ERR_SHAPE;
   if (x_rows < 0 || (M > 0 && (x_rows < 1 || M % x_rows))) return QF_ERR_SHAPE;
   const bool any = M > 0 && N > 0;
   if (any && (!Y || (K > 0 && (!X || !codes || !scales || (fmt == QF_FMT_NVFP4 && !tscale))))) return QF_ERR_NULL;
@@ -746,6 +750,20 @@ static qf_status_t matvec_impl(int fmt, const void* X, int64_t M, int64_t x_rows
   a.Y = Y;
   a.y_dtype = y_dtype;
   return cu(launch_matvec(a, st));
+}
+
+qf_status_t qf_selftest_matvec_cut(qf_format_t fmt, int64_t M, int64_t N, int64_t K, int G, int cut[9]) {
+  if (!valid_fmt(fmt, false)) return QF_ERR_FORMAT;
+  if (!cut) return QF_ERR_NULL;
+  if (!matvec_shape_ok(fmt, M, N, K) || M == 0 || N == 0 || K == 0 || G < 0 || G > QF_MOE_MAX_EXPERTS) return QF_ERR_SHAPE;
+  MatvecArgs a{};
+  a.fmt = fmt;
+  a.M = M; a.N = N; a.K = K;
+  a.x_div = 1;
+  a.ids = G ? cut : nullptr;
+  a.G = G ? G : 1;
+  matvec_cut(a, cut);
+  return QF_OK;
 }
 
 qf_status_t qf_fq_matvec(qf_format_t fmt, const void* X, int64_t M, const void* codes, const void* scales, const float* tensor_scale,

@@ -394,6 +394,8 @@ struct MatvecArgs {
   int y_dtype;
 };
 cudaError_t launch_matvec(const MatvecArgs& a, cudaStream_t st);
+// How it would be cut (see qf_selftest_matvec_cut); a.ids is looked at for being null alone.
+void matvec_cut(const MatvecArgs& a, int* cut);
 
 cudaError_t launch_selftest_timeout(uint32_t* status, long long limit_cycles, int* gave_up, cudaStream_t st);
 

@@ -35,6 +35,8 @@
 #include <cooperative_groups.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "qf_common.cuh"
 
 namespace cg = cooperative_groups;
@@ -914,10 +916,15 @@ Cut choose_cut(int64_t N, int64_t K, double slots, double tokens, int mt, int nt
 }
 
 template <int FMT, int NT, bool LOOSE>
-cudaError_t launch(MvParams& p, int slots, int mt, cudaStream_t st) {
+Cut cut_of(MvParams& p, int mt) {
   // experts that even routing is expected to meet; the others' CTAs leave at once
   const double busy = p.ids ? p.G * (1.0 - pow(1.0 - 1.0 / p.G, p.M)) : 1.0;
-  const Cut c = choose_cut(p.N, p.K, busy, p.ids ? fmin(mt, fmax(1.0, p.M / busy)) : mt, mt, NT, kStages<NT> * kStepBytes<FMT, LOOSE>, NT == 1 ? mt * 4 * 144 : 8 * kXPitch<NT>, FMT == QF_FMT_Q4_K, LOOSE, p.ids != nullptr, p);
+  return choose_cut(p.N, p.K, busy, p.ids ? fmin(mt, fmax(1.0, p.M / busy)) : mt, mt, NT, kStages<NT> * kStepBytes<FMT, LOOSE>, NT == 1 ? mt * 4 * 144 : 8 * kXPitch<NT>, FMT == QF_FMT_Q4_K, LOOSE, p.ids != nullptr, p);
+}
+
+template <int FMT, int NT, bool LOOSE>
+cudaError_t launch(MvParams& p, int slots, int mt, cudaStream_t st) {
+  const Cut c = cut_of<FMT, NT, LOOSE>(p, mt);
   auto kernel = matvec_kernel<FMT, NT, LOOSE>;
   static bool ready[64] = {};                          // per device
   int dev = 0;
@@ -943,9 +950,7 @@ cudaError_t launch(MvParams& p, int slots, int mt, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-}  // namespace
-
-cudaError_t launch_matvec(const MatvecArgs& a, cudaStream_t st) {
+MvParams params_of(const MatvecArgs& a) {
   MvParams p{};
   p.X = static_cast<const __nv_bfloat16*>(a.X);
   p.codes = static_cast<const uint8_t*>(a.codes);
@@ -959,19 +964,44 @@ cudaError_t launch_matvec(const MatvecArgs& a, cudaStream_t st) {
   p.M = static_cast<int>(a.M); p.N = static_cast<int>(a.N); p.K = static_cast<int>(a.K); p.G = a.G;
   p.y_f32 = a.y_dtype == QF_DT_F32;
   p.by_pair = a.ids && a.M <= a.G;
-  const int slots = !a.ids ? 1 : p.by_pair ? p.M : a.G;
+  return p;
+}
+
+// Calls go(format, token tiles, loose, p, tokens of a pass), the first three as constants, for the kernel that serves a product.
+template <typename Go>
+auto with_kernel(const MatvecArgs& a, Go go) {
+  MvParams p = params_of(a);
   // tokens of a pass: few pairs per expert are the rule in the grouped product
   const int nt = (a.ids ? a.M <= 4ll * a.G || a.M <= 8 : a.M <= 8) ? 1 : 2;
   const int mt = static_cast<int>(a.M < 8 * nt ? a.M : 8 * nt);
   const bool loose = a.K % 128 != 0;
-  constexpr int NV = QF_FMT_NVFP4, MX = QF_FMT_MXFP4, Q4 = QF_FMT_Q4_K;
-  if (a.fmt == Q4) return nt == 1 ? launch<Q4, 1, false>(p, slots, mt, st) : launch<Q4, 2, false>(p, slots, mt, st);
-  if (a.fmt == NV) {
-    if (nt == 1) return loose ? launch<NV, 1, true>(p, slots, mt, st) : launch<NV, 1, false>(p, slots, mt, st);
-    return loose ? launch<NV, 2, true>(p, slots, mt, st) : launch<NV, 2, false>(p, slots, mt, st);
-  }
-  if (nt == 1) return loose ? launch<MX, 1, true>(p, slots, mt, st) : launch<MX, 1, false>(p, slots, mt, st);
-  return loose ? launch<MX, 2, true>(p, slots, mt, st) : launch<MX, 2, false>(p, slots, mt, st);
+  using One = std::integral_constant<int, 1>;
+  using Two = std::integral_constant<int, 2>;
+  auto tiles = [&](auto fmt) {
+    if constexpr (fmt.value != QF_FMT_Q4_K)            // rows of Q4_K are whole super-blocks
+      if (loose) return nt == 1 ? go(fmt, One{}, std::true_type{}, p, mt) : go(fmt, Two{}, std::true_type{}, p, mt);
+    return nt == 1 ? go(fmt, One{}, std::false_type{}, p, mt) : go(fmt, Two{}, std::false_type{}, p, mt);
+  };
+  if (a.fmt == QF_FMT_Q4_K) return tiles(std::integral_constant<int, QF_FMT_Q4_K>{});
+  if (a.fmt == QF_FMT_NVFP4) return tiles(std::integral_constant<int, QF_FMT_NVFP4>{});
+  return tiles(std::integral_constant<int, QF_FMT_MXFP4>{});
+}
+
+}  // namespace
+
+cudaError_t launch_matvec(const MatvecArgs& a, cudaStream_t st) {
+  return with_kernel(a, [&](auto fmt, auto nt, auto loose, MvParams& p, int mt) {
+    const int slots = !p.ids ? 1 : p.by_pair ? p.M : p.G;
+    return launch<fmt.value, nt.value, loose.value>(p, slots, mt, st);
+  });
+}
+
+void matvec_cut(const MatvecArgs& a, int* cut) {
+  with_kernel(a, [&](auto fmt, auto nt, auto loose, MvParams& p, int mt) {
+    const Cut c = cut_of<fmt.value, nt.value, loose.value>(p, mt);
+    const int all[9] = {nt.value, loose.value, c.warps, c.kw, c.nz, p.kz, p.kc, p.blocks, static_cast<int>(c.grid_x)};
+    for (int i = 0; i < 9; ++i) cut[i] = all[i];
+  });
 }
 
 }  // namespace qf
