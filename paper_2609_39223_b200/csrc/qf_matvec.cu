@@ -134,6 +134,14 @@ __device__ __forceinline__ void q4k_unpack(const uint32_t (&m)[4], uint32_t (&v)
   v[3] = ((m[3] >> 4) & 0x0F0F0F0Fu) | ((m[2] >> 2) & 0x30303030u);
 }
 
+// Eight elements of X, by an ordinary load. This grid may be placed while the product that writes X still runs (launch_after_previous), and
+// the read-only path (__ldg) asks for memory that nobody writes as long as the grid lives.
+__device__ __forceinline__ uint4 load_x(const uint4* x) {
+  uint4 v;
+  asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(x));
+  return v;
+}
+
 constexpr int kStep = 256;                            // weights of a row that a warp takes at a time
 constexpr int kWords = 8;                             // words of codes (FP4) or sub-blocks (Q4_K) that a lane holds of a row
 
@@ -472,7 +480,7 @@ __device__ __noinline__ Sums<NT> step_bf16(const MvParams& p, const uint16_t* li
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const uint4 x = __ldg(reinterpret_cast<const uint4*>(xrow[nt] + k));
+        const uint4 x = load_x(reinterpret_cast<const uint4*>(xrow[nt] + k));
         float c[4] = {};
         mma16816<false>(c, w[0][0], w[1][0], w[0][1], w[1][1], __byte_perm(x.x, x.y, 0x5410), __byte_perm(x.x, x.y, 0x7632));
         mma16816<false>(c, w[0][2], w[1][2], w[0][3], w[1][3], __byte_perm(x.z, x.w, 0x5410), __byte_perm(x.z, x.w, 0x7632));
@@ -497,7 +505,7 @@ __device__ __noinline__ Sums<NT> step_bf16(const MvParams& p, const uint16_t* li
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (k < p.K) x = __ldg(reinterpret_cast<const uint4*>(xrow[nt] + k));
+        if (k < p.K) x = load_x(reinterpret_cast<const uint4*>(xrow[nt] + k));
         mma16816<false>(sum.c[nt], w[0][0], w[1][0], w[0][1], w[1][1], __byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632));
         mma16816<false>(sum.c[nt], w[0][2], w[1][2], w[0][3], w[1][3], __byte_perm(x.y, x.w, 0x5410), __byte_perm(x.y, x.w, 0x7632));
       }
@@ -707,7 +715,7 @@ __global__ void __launch_bounds__(32 * kWarpsMost, 1) matvec_kernel(const __grid
                 const int v = (g0 + i * share) * 32 + lane, s = v / (kStep / 8), w = v / 4 % kWords;       // step, word of codes, and lane v % 4
                 const int unit = Q4K ? v : s * (kStep / 8) + (v & 3) * kWords + w;
                 q[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (v < units && kc0 + 8 * unit < p.K) q[i] = __ldg(x + unit);
+                if (v < units && kc0 + 8 * unit < p.K) q[i] = load_x(x + unit);
               }
 #pragma unroll
               for (int i = 0; i < kBatch; ++i) {

@@ -34,7 +34,7 @@ def weight(fmt, N, K, seed, lead=()):
     return codes, scales, None
 
 
-def compare(build, steps):
+def compare(build, steps, least=1e-3):
     """build(seed) gives the buffers; steps(buffers) yields after every call."""
     def run(seed, wait):
         bufs = build(seed)
@@ -48,7 +48,7 @@ def compare(build, steps):
         return bufs
     for seed in range(6):
         want = run(seed, True)
-        assert all(torch.isfinite(w).all() and w.float().abs().max() > 1e-3 for w in want)
+        assert all(torch.isfinite(w).all() and w.float().abs().max() > least for w in want)
         for _ in range(3):
             assert all(torch.equal(a, b) for a, b in zip(run(seed, False), want)), seed
     # the same in a graph, whose launches keep their overlap
@@ -90,6 +90,21 @@ def test_there_and_back(kind, M):
                 api.qf_fq_matvec(fmt, src, *w, Y=dst)
                 yield
     compare(lambda seed: [rows(M, N, seed), nothing(M, N)], steps)
+
+
+@pytest.mark.parametrize("kind", FMTS)
+def test_there_and_back_of_small_values(kind):
+    """Values around 2^-40, below what FP16 holds: every product reads its X a second time, for the BF16 route."""
+    fmt, M, N = FMTS[kind], 5, 2048
+    w = weight(fmt, N, N, 1)
+
+    def steps(bufs):
+        a, b = bufs
+        for _ in range(10):
+            for src, dst in ((a, b), (b, a)):
+                api.qf_fq_matvec(fmt, src, *w, Y=dst)
+                yield
+    compare(lambda seed: [rows(M, N, seed) * 2.0 ** -40, nothing(M, N)], steps, least=2.0 ** -50)
 
 
 @pytest.mark.parametrize("kind", FMTS)
