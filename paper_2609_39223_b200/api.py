@@ -457,32 +457,37 @@ _IDS_DTYPE = {torch.int32: DT_I32, torch.int64: DT_I64}
 _DATA_DTYPE = {torch.bfloat16: DT_BF16, torch.float32: DT_F32}
 
 
-def _tensor(t: torch.Tensor, name: str, dtypes, shape) -> int:
-    """Address of a contiguous CUDA tensor of one of ``dtypes`` and the given shape."""
-    if t.dtype not in dtypes or not t.is_cuda or not t.is_contiguous():
+def _here(t: torch.Tensor, name: str):
+    """The current device, which has to be the tensor's, and its current stream. (The calls below take a few microseconds on the GPU;
+    torch.cuda.current_stream() builds an object and takes three by itself.)"""
+    device = t.get_device()
+    if device < 0:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on cuda:{device}, the current device is cuda:{torch._C._cuda_getDevice()}")
+    return device, torch._C._cuda_getCurrentRawStream(device)
+
+
+def _tensor(t: torch.Tensor, name: str, dtypes, shape, device: int) -> int:
+    """Address of a contiguous CUDA tensor of one of ``dtypes`` and the given shape on ``device``."""
+    at = t.get_device()
+    if t.dtype not in dtypes or at < 0 or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous CUDA tensor of type {' or '.join(map(str, dtypes))}")
+    if at != device:
+        raise ValueError(f"{name} is on cuda:{at}, the current device is cuda:{device}")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     return t.data_ptr()
 
 
-def _out(like: torch.Tensor, given: torch.Tensor | None, name: str, dtypes, shape, dtype):
+def _out(like: torch.Tensor, given: torch.Tensor | None, name: str, dtypes, shape, dtype, device: int):
     """The caller's output, checked, or a new one on the device of ``like``; with its address."""
     if given is not None:
-        return given, _tensor(given, name, dtypes, shape)
+        return given, _tensor(given, name, dtypes, shape, device)
     if dtype not in dtypes:
         raise TypeError(f"{name} cannot be {dtype}")
     new = like.new_empty(shape, dtype=dtype)
     return new, new.data_ptr()
-
-
-def _stream_of(t: torch.Tensor) -> int:
-    """Current stream of the current device, which has to be the tensor's. (The calls below take a few microseconds on the GPU;
-    torch.cuda.current_stream() builds an object and takes three by itself.)"""
-    device = t.get_device()
-    if device != torch._C._cuda_getDevice():
-        raise ValueError(f"tensors are on cuda:{device}, the current device is cuda:{torch._C._cuda_getDevice()}")
-    return torch._C._cuda_getCurrentRawStream(device)
 
 
 _BF16, _F32, _I32, _U8 = (torch.bfloat16,), (torch.float32,), (torch.int32,), (torch.uint8,)
@@ -502,29 +507,31 @@ def qf_moe_sort(expert_ids: torch.Tensor, experts: int, *, rows_padded: int | No
     tokens, top_k = expert_ids.shape
     if rows_padded is None:
         rows_padded = qf_moe_rows_bound(tokens, top_k, experts)
-    ids = _tensor(expert_ids, "expert_ids", _IDS_DTYPE, expert_ids.shape)
+    device, stream = _here(expert_ids, "expert_ids")
+    ids = _tensor(expert_ids, "expert_ids", _IDS_DTYPE, expert_ids.shape, device)
     row_of = expert_ids.new_empty((tokens, top_k), dtype=torch.int32)
     offs = expert_ids.new_empty(experts + 1, dtype=torch.int32)
     counts = expert_ids.new_empty(experts, dtype=torch.int32)
     _check(lib().qf_moe_sort(ids, _IDS_DTYPE[expert_ids.dtype], tokens, top_k, experts, rows_padded, row_of.data_ptr(),
-                             offs.data_ptr(), counts.data_ptr(), _stream_of(expert_ids)), "qf_moe_sort")
+                             offs.data_ptr(), counts.data_ptr(), stream), "qf_moe_sort")
     return MoePlan(row_of, offs, counts, rows_padded)
 
 
-def _plan_ptrs(plan: MoePlan):
+def _plan_ptrs(plan: MoePlan, device: int):
     experts = plan.counts.shape[0]
-    return (_tensor(plan.row_of, "plan.row_of", _I32, plan.row_of.shape), _tensor(plan.group_offsets, "plan.group_offsets", _I32, (experts + 1,)),
-            _tensor(plan.counts, "plan.counts", _I32, (experts,)), experts)
+    return (_tensor(plan.row_of, "plan.row_of", _I32, plan.row_of.shape, device), _tensor(plan.group_offsets, "plan.group_offsets", _I32, (experts + 1,), device),
+            _tensor(plan.counts, "plan.counts", _I32, (experts,), device), experts)
 
 
 def qf_moe_dispatch(x: torch.Tensor, plan: MoePlan, *, xs: torch.Tensor | None = None) -> torch.Tensor:
     """xs [rows_padded, hidden]: row plan.row_of[t, j] holds x[t], every other row is zero."""
     (tokens, top_k), rows = plan.row_of.shape, plan.rows_padded
     hidden = x.shape[-1]
-    px = _tensor(x, "x", _BF16, (tokens, hidden))
-    row_of, offs, counts, experts = _plan_ptrs(plan)
-    xs, po = _out(x, xs, "xs", _BF16, (rows, hidden), torch.bfloat16)
-    _check(lib().qf_moe_dispatch(px, tokens, top_k, hidden, row_of, offs, counts, experts, rows, po, _stream_of(x)), "qf_moe_dispatch")
+    device, stream = _here(x, "x")
+    px = _tensor(x, "x", _BF16, (tokens, hidden), device)
+    row_of, offs, counts, experts = _plan_ptrs(plan, device)
+    xs, po = _out(x, xs, "xs", _BF16, (rows, hidden), torch.bfloat16, device)
+    _check(lib().qf_moe_dispatch(px, tokens, top_k, hidden, row_of, offs, counts, experts, rows, po, stream), "qf_moe_dispatch")
     return xs
 
 
@@ -532,10 +539,11 @@ def qf_moe_dispatch_bwd(dxs: torch.Tensor, plan: MoePlan, *, dx_dtype=torch.bflo
     """dx[t] = sum over j of dxs[plan.row_of[t, j]]."""
     (tokens, top_k), rows = plan.row_of.shape, plan.rows_padded
     hidden = dxs.shape[-1]
-    pd = _tensor(dxs, "dxs", _DATA_DTYPE, (rows, hidden))
-    dx, po = _out(dxs, dx, "dx", _DATA_DTYPE, (tokens, hidden), dx_dtype)
-    _check(lib().qf_moe_dispatch_bwd(pd, _DATA_DTYPE[dxs.dtype], tokens, top_k, hidden, _tensor(plan.row_of, "plan.row_of", _I32, (tokens, top_k)),
-                                     rows, po, _DATA_DTYPE[dx.dtype], _stream_of(dxs)), "qf_moe_dispatch_bwd")
+    device, stream = _here(dxs, "dxs")
+    pd = _tensor(dxs, "dxs", _DATA_DTYPE, (rows, hidden), device)
+    dx, po = _out(dxs, dx, "dx", _DATA_DTYPE, (tokens, hidden), dx_dtype, device)
+    _check(lib().qf_moe_dispatch_bwd(pd, _DATA_DTYPE[dxs.dtype], tokens, top_k, hidden, _tensor(plan.row_of, "plan.row_of", _I32, (tokens, top_k), device),
+                                     rows, po, _DATA_DTYPE[dx.dtype], stream), "qf_moe_dispatch_bwd")
     return dx
 
 
@@ -545,11 +553,12 @@ def qf_moe_combine(ys: torch.Tensor, weights: torch.Tensor, plan: MoePlan | None
     tokens, top_k = weights.shape
     hidden = ys.shape[-1]
     rows = tokens * top_k if plan is None else plan.rows_padded
-    py = _tensor(ys, "ys", _DATA_DTYPE, (rows, hidden))
-    out, po = _out(ys, out, "out", _DATA_DTYPE, (tokens, hidden), out_dtype)
-    row_of = None if plan is None else _tensor(plan.row_of, "plan.row_of", _I32, (tokens, top_k))
-    _check(lib().qf_moe_combine(py, _DATA_DTYPE[ys.dtype], _tensor(weights, "weights", _F32, (tokens, top_k)), tokens, top_k, hidden, row_of, rows,
-                                po, _DATA_DTYPE[out.dtype], _stream_of(ys)), "qf_moe_combine")
+    device, stream = _here(ys, "ys")
+    py = _tensor(ys, "ys", _DATA_DTYPE, (rows, hidden), device)
+    out, po = _out(ys, out, "out", _DATA_DTYPE, (tokens, hidden), out_dtype, device)
+    row_of = None if plan is None else _tensor(plan.row_of, "plan.row_of", _I32, (tokens, top_k), device)
+    _check(lib().qf_moe_combine(py, _DATA_DTYPE[ys.dtype], _tensor(weights, "weights", _F32, (tokens, top_k), device), tokens, top_k, hidden, row_of, rows,
+                                po, _DATA_DTYPE[out.dtype], stream), "qf_moe_combine")
     return out
 
 
@@ -559,14 +568,15 @@ def qf_moe_combine_bwd(dout: torch.Tensor, ys: torch.Tensor | None, weights: tor
     <dout[t], ys[plan.row_of[t, j]]>, zero for dropped pairs (None if not wanted; ys is then not needed)."""
     (tokens, top_k), rows = plan.row_of.shape, plan.rows_padded
     hidden = dout.shape[-1]
-    pd = _tensor(dout, "dout", _DATA_DTYPE, (tokens, hidden))
-    py = _tensor(ys, "ys", _DATA_DTYPE, (rows, hidden)) if want_dweights or ys is not None else None
-    row_of, offs, counts, experts = _plan_ptrs(plan)
-    dys, po = _out(dout, dys, "dys", _BF16, (rows, hidden), torch.bfloat16)
-    dweights, pw = _out(dout, dweights, "dweights", _F32, (tokens, top_k), torch.float32) if want_dweights else (None, None)
+    device, stream = _here(dout, "dout")
+    pd = _tensor(dout, "dout", _DATA_DTYPE, (tokens, hidden), device)
+    py = _tensor(ys, "ys", _DATA_DTYPE, (rows, hidden), device) if want_dweights or ys is not None else None
+    row_of, offs, counts, experts = _plan_ptrs(plan, device)
+    dys, po = _out(dout, dys, "dys", _BF16, (rows, hidden), torch.bfloat16, device)
+    dweights, pw = _out(dout, dweights, "dweights", _F32, (tokens, top_k), torch.float32, device) if want_dweights else (None, None)
     _check(lib().qf_moe_combine_bwd(pd, _DATA_DTYPE[dout.dtype], py, _DATA_DTYPE[ys.dtype] if ys is not None else DT_BF16,
-                                    _tensor(weights, "weights", _F32, (tokens, top_k)), tokens, top_k, hidden, row_of, offs, counts, experts,
-                                    rows, po, pw, _stream_of(dout)), "qf_moe_combine_bwd")
+                                    _tensor(weights, "weights", _F32, (tokens, top_k), device), tokens, top_k, hidden, row_of, offs, counts, experts,
+                                    rows, po, pw, stream), "qf_moe_combine_bwd")
     return dys, dweights
 
 
@@ -577,12 +587,13 @@ def qf_fq_matvec(fmt: int, X: torch.Tensor, codes: torch.Tensor, scales: torch.T
     N = codes.shape[0]
     if fmt not in BLOCK or K % BLOCK[fmt]:
         raise QfError(2 if fmt in BLOCK else 4, "qf_fq_matvec")
-    px = _tensor(X, "X", _BF16, (M, K))
-    Y, po = _out(X, Y, "Y", _DATA_DTYPE, (M, N), y_dtype)
-    ts = _tensor(tensor_scale, "tensor_scale", _F32, (1,)) if fmt == FMT_NVFP4 else None
-    _check(lib().qf_fq_matvec(fmt, px, M, _tensor(codes, "codes", _U8, (N, K // 2)),
-                              _tensor(scales, "scales", _U8, scales_shape(fmt, N, K)), ts, N, K, po, _DATA_DTYPE[Y.dtype],
-                              _stream_of(X)), "qf_fq_matvec")
+    device, stream = _here(X, "X")
+    px = _tensor(X, "X", _BF16, (M, K), device)
+    Y, po = _out(X, Y, "Y", _DATA_DTYPE, (M, N), y_dtype, device)
+    ts = _tensor(tensor_scale, "tensor_scale", _F32, (1,), device) if fmt == FMT_NVFP4 else None
+    _check(lib().qf_fq_matvec(fmt, px, M, _tensor(codes, "codes", _U8, (N, K // 2), device),
+                              _tensor(scales, "scales", _U8, scales_shape(fmt, N, K), device), ts, N, K, po, _DATA_DTYPE[Y.dtype],
+                              stream), "qf_fq_matvec")
     return Y
 
 
@@ -595,13 +606,14 @@ def qf_fq_grouped_matvec(fmt: int, X: torch.Tensor, expert_ids: torch.Tensor, co
     pairs = expert_ids.numel()
     if fmt not in BLOCK or K % BLOCK[fmt]:
         raise QfError(2 if fmt in BLOCK else 4, "qf_fq_grouped_matvec")
-    px = _tensor(X, "X", _BF16, (x_rows, K))
-    Y, po = _out(X, Y, "Y", _DATA_DTYPE, (pairs, N), y_dtype)
-    ts = _tensor(tensor_scales, "tensor_scales", _F32, (G,)) if fmt == FMT_NVFP4 else None
-    _check(lib().qf_fq_grouped_matvec(fmt, px, x_rows, _tensor(expert_ids, "expert_ids", _IDS_DTYPE, expert_ids.shape),
-                                      _IDS_DTYPE[expert_ids.dtype], pairs, G, _tensor(codes, "codes", _U8, (G, N, K // 2)),
-                                      _tensor(scales, "scales", _U8, (G, *scales_shape(fmt, N, K))), ts, N, K, po,
-                                      _DATA_DTYPE[Y.dtype], _stream_of(X)), "qf_fq_grouped_matvec")
+    device, stream = _here(X, "X")
+    px = _tensor(X, "X", _BF16, (x_rows, K), device)
+    Y, po = _out(X, Y, "Y", _DATA_DTYPE, (pairs, N), y_dtype, device)
+    ts = _tensor(tensor_scales, "tensor_scales", _F32, (G,), device) if fmt == FMT_NVFP4 else None
+    _check(lib().qf_fq_grouped_matvec(fmt, px, x_rows, _tensor(expert_ids, "expert_ids", _IDS_DTYPE, expert_ids.shape, device),
+                                      _IDS_DTYPE[expert_ids.dtype], pairs, G, _tensor(codes, "codes", _U8, (G, N, K // 2), device),
+                                      _tensor(scales, "scales", _U8, (G, *scales_shape(fmt, N, K)), device), ts, N, K, po,
+                                      _DATA_DTYPE[Y.dtype], stream), "qf_fq_grouped_matvec")
     return Y
 
 
