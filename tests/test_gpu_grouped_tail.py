@@ -30,7 +30,7 @@ def grouped(X, W, dY, offs, wq, aq, flags, given):
 
 @pytest.mark.parametrize("wq,aq", [(NV, NV), (MX, MX), (NONE, NV), (NV, NONE), (Q4, NONE)])
 @pytest.mark.parametrize("flags,given", [(0, None), (api.FUSED_QDQ, None), (0, 2e-3)])
-@pytest.mark.parametrize("blocks,tail", [((2, 0, 1), 3), ((1, 3, 2, 1), 1), ((2,), 6)])
+@pytest.mark.parametrize("blocks,tail", [((2, 0, 1), 3), ((1, 3, 2, 1), 1), ((2,), 6), ((2,) + (0,) * 299, 1)])
 def test_rows_past_the_last_segment_have_no_part(wq, aq, flags, given, blocks, tail):
     N, K, G = 256, 512, len(blocks)
     rows = 128 * sum(blocks)
