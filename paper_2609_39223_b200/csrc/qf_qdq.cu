@@ -53,25 +53,28 @@ struct LoraLoader {
 // tensor amax
 // ---------------------------------------------------------------------------------------------
 
-// TO_ROWS_END: the activations of a grouped layer, whose maximum ends with the last segment (a kernel of its own: the bound read from memory cost the
-// others 3.5% of an NVFP4 quantization, 4050 -> 3905 GB/s)
+// TO_ROWS_END: the activations of a grouped layer, whose maximum ends with the last segment. The bound comes from memory and is not waited for: chunks
+// are read to the end of the buffer and left out afterwards. It takes registers: at 34 instead of 32 an SM holds seven CTAs of the grid's eight
+// (16384 x 2048: 5 us longer), so that this form is a kernel of its own and held to 32.
 template <typename Loader, bool TO_ROWS_END = false>
-__global__ void __launch_bounds__(kThreads) amax_kernel(Loader src, int64_t nchunks, const int32_t* __restrict__ rows_end, int64_t row_chunks,
+__global__ void __launch_bounds__(kThreads, TO_ROWS_END ? 2048 / kThreads : 0) amax_kernel(Loader src, int64_t nchunks, const int32_t* __restrict__ rows_end, int64_t row_chunks,
                                                         const __nv_bfloat16* __restrict__ tail, int ntail,
                                                         uint32_t* __restrict__ amax_bits) {
   // gridDim.y > 1: one tensor per y-slice (the experts of a grouped layer), nchunks chunks each
   const Loader in = src.slice(static_cast<int64_t>(blockIdx.y) * nchunks);
   amax_bits += blockIdx.y;
   // rows past the last segment of a grouped layer's buffer hold nothing; the entry is read as the products read it
-  if constexpr (TO_ROWS_END) nchunks = min(nchunks, static_cast<int64_t>(max(__ldg(rows_end), 0) & ~127) * row_chunks);
+  int64_t end = nchunks;
+  if constexpr (TO_ROWS_END) end = static_cast<int64_t>(max(__ldg(rows_end), 0) & ~127) * row_chunks;
+  auto amax = [&](const uint4& v, int64_t at) { return !TO_ROWS_END || at < end ? chunk_amax_bits(v) : 0u; };
   uint32_t m = 0;
   const int64_t stride = static_cast<int64_t>(gridDim.x) * kThreads;
   int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
   for (; i + 3 * stride < nchunks; i += 4 * stride) {
     uint4 a = in.chunk(i), b = in.chunk(i + stride), c = in.chunk(i + 2 * stride), d = in.chunk(i + 3 * stride);
-    m = max(m, max(max(chunk_amax_bits(a), chunk_amax_bits(b)), max(chunk_amax_bits(c), chunk_amax_bits(d))));
+    m = max(m, max(max(amax(a, i), amax(b, i + stride)), max(amax(c, i + 2 * stride), amax(d, i + 3 * stride))));
   }
-  for (; i < nchunks; i += stride) m = max(m, chunk_amax_bits(in.chunk(i)));
+  for (; i < nchunks; i += stride) m = max(m, amax(in.chunk(i), i));
   if (blockIdx.x == 0 && threadIdx.x < ntail)
     m = max(m, static_cast<uint32_t>(__bfloat16_as_ushort(tail[threadIdx.x])) & 0x7FFFu);
   m = __reduce_max_sync(0xFFFFFFFFu, m);
