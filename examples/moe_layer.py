@@ -82,7 +82,8 @@ class MoeLayer:
         return packed
 
     def decode(self, packed, x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor) -> torch.Tensor:
-        """The layer for a few tokens, from the codes: every expert's weights are read once, and only those of experts in use."""
+        """The layer for a few tokens, from the codes: an expert's weights are read once per eight of its tokens, and only those of
+        experts in use."""
         gate_up = api.qf_fq_grouped_matvec(self.fmt, x, ids, *packed[0])
         ys = api.qf_fq_grouped_matvec(self.fmt, self.swiglu(gate_up), ids, *packed[1])
         return api.qf_moe_combine(ys, weights)

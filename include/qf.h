@@ -347,7 +347,8 @@ qf_status_t qf_moe_combine_bwd(const void* dout, qf_dtype_t dout_dtype, const vo
  * (like qf_fp4_matmul_native), for Q4_K the sums are sum over sub-blocks of (d*s6) * sum(C*x) - (dmin*m6) * sum(x).
  * The result therefore differs from qf_fq_linear_fwd(X, W, fmt, QF_FMT_NONE) by FP32 summation order and, for NVFP4 and
  * Q4_K, by that rounding. For quantized activations pass X_hat (qf_qdq). Results do not depend on what else runs, and the
- * rows of X do not influence one another.
+ * rows of X do not influence one another; but how the contraction is cut depends on the sizes, M (or pairs) among them, so that the same
+ * row can have other last bits in a call with another number of rows.
  *   X       BF16 [M, K], K a multiple of the format's block and at most QF_MATVEC_MAX_K; Y BF16 or FP32 [M, N], any N
  *   scales       as qf_qdq writes them: E4M3 codes 0x00..0x7E, E8M0 codes 0x00..0xFE (the results of others are not defined)
  *   tensor_scale  NVFP4: device float*; otherwise ignored
@@ -363,7 +364,8 @@ qf_status_t qf_fq_matvec(qf_format_t fmt, const void* X, int64_t M, const void* 
  *   x_rows       rows of X: a divisor of pairs. pairs / top_k (every token's row serves its top_k pairs: gate and up
  *                projections) or pairs (a row per pair: down projection)
  *   expert_ids   device [pairs], ids_dtype QF_DT_I32 or QF_DT_I64; an id outside [0, G) gives a row of zeros
- * The codes of an expert are read once per QF_MATVEC_TOKENS of its pairs; experts that no pair names are not read. G at most
+ * The codes of an expert are read once per 8 of its pairs (per QF_MATVEC_TOKENS of them where there are more than 4 G pairs in
+ * all and more than 8); experts that no pair names are not read. G at most
  * QF_MOE_MAX_EXPERTS. */
 qf_status_t qf_fq_grouped_matvec(qf_format_t fmt, const void* X, int64_t x_rows, const void* expert_ids, qf_dtype_t ids_dtype,
                                  int64_t pairs, int G, const void* codes, const void* scales, const float* tensor_scales, int64_t N,

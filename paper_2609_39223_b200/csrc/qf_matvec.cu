@@ -14,7 +14,10 @@
 //  * B fragments: the CTA stages its slice of X in shared memory once, in the order the lanes read it, as FP16 of 2^6 x. That is
 //    exact for zeros and 2^-23 <= |x| < 1023. A token that has another x in a step of the contraction (or a tile with another p)
 //    takes that step with BF16 fragments, weights and X read again: a sum of exact products either way, so the choice
-//    costs time only (of N(0, 1) values one in ten million falls below). It goes by token: rows of X do not influence one another.
+//    costs time only. It goes by token: rows of X do not influence one another. One of ten million N(0, 1) values falls below,
+//    but 2.5e-6 of silu(g) u with g, u ~ N(0, 1), 5e-5 with N(0, 0.2), 6e-4 with N(0, 0.05); and an all-zero MXFP4 block has scale code
+//    0. A warp that meets one reads all its steps of every tile again: NVFP4 4096 x 14336 with one token takes 13.1 us for N(0, 1) and
+//    for silu(g) u of N(0, 1), 17.5 and 29.0 for N(0, 0.2) and N(0, 0.05); MXFP4 31.4 instead of 12.6 with one row of 64 zero.
 //  * BF16 fragments from FP4 codes: a nibble times 0x1040 puts its sign at bit 15 and its three other bits at bits 8..6, which is
 //    the value as a BF16 number scaled by 2^-126 (subnormals included); a packed product with the scale gives value * scale.
 //    This takes 15 instructions for eight weights where the FP16 route takes 8, which is why it is not the only route.
@@ -434,7 +437,7 @@ __device__ __forceinline__ bool step_f16(const RowPart<FMT> (&r)[2], uint32_t x,
 
 // ---- the same step with BF16 fragments for the tokens in `bad` (all of them if a scale of the tile is out of the FP16 range),
 // weights and X read again from global memory: their sums in the final units (NVFP4: without the tensor scale), zero for the
-// other tokens. Rare, and out of line so that it costs the fast path no registers.
+// other tokens. Out of line, so that it costs the fast path no registers.
 
 template <int NT>
 struct Sums { float c[NT][4]; };
@@ -864,7 +867,8 @@ struct Cut {
 // step_each per warp that the SM holds, 0.5 at least; meeting costs 0.5 in a CTA and 2 in a cluster (3.5 if there are tiles to
 // come, since it empties the rings); a slice of X takes 0.7 and 1 per 30 KB that the SM stages. Over 58 products from
 // 1024 x 4096 to 128256 x 4096 with 1 to 24 tokens the choice took 1.02 times as long as the best cut in the mean, 1.22 at most (128
-// experts of 2048 x 768, one token: 8.3 us, 6.8 with twice the CTAs of two warps a tile).
+// experts of 2048 x 768, one token: 8.3 us, 6.8 with twice the CTAs of two warps a tile). Outside them it can be far off: 128 experts of
+// 1536 x 2048 with one token take 15.3 us (NVFP4) and 16.5 (Q4_K) with 16 warps, 8 a tile, where MXFP4 takes 8.3 with 4 and 2.
 Cut choose_cut(int64_t N, int64_t K, double slots, double tokens, int mt, int nt, int ring_bytes, int x_bytes, bool q4k, bool loose, bool grouped, MvParams& p) {
   Cut best{};
   double best_time = 1e30;

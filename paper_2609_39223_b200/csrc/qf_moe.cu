@@ -26,8 +26,8 @@ __device__ __forceinline__ int expert_of(const Id* __restrict__ ids, int64_t p, 
 // run; the counts, summed over the warps and CTAs before it, give each warp its first row in every segment; then every warp walks
 // its run again, 32 pairs at a time, and numbers equal ids inside a group of 32 by lane: the order of p is kept. One launch,
 // no global scratch: the CTAs of a cluster read one another's counts in shared memory.
-// Bound by instructions and latency, not by the 8 bytes a pair: 131072 pairs to 128 experts 11.1 us, of which a ballot for every bit of the
-// id takes most (142 us with one CTA and a walk by single pairs); 56 pairs 4.0 us, the launch and six barriers.
+// Bound by instructions and latency, not by the 8 bytes a pair: 131072 pairs to 128 experts 11.1 us, with 56% of the issue slots of its 16
+// SMs busy (142 us with one CTA and a walk by single pairs); 56 pairs 4.0 us, the launch and six barriers.
 template <typename Id>
 __global__ void __launch_bounds__(kSortThreads) moe_sort_kernel(const Id* __restrict__ ids, int64_t pairs, int G, int64_t rows,
                                                                 int32_t* __restrict__ row_of, int32_t* __restrict__ offs,
@@ -261,7 +261,9 @@ __global__ void __launch_bounds__(kThreads) moe_combine_kernel(const MoeTable t,
 // dout is read once for kPairs pairs, whose rows of ys are loaded together; the pairs' inner products stay in registers and are
 // reduced at the end: over the lanes by halving (lane bits 4..2 choose the pair, so that a step moves half of what the last one
 // did), then over the warps in their order. Bound by the traffic of ys and dys: 16384 tokens of 2048, 8 pairs each, in BF16: 207 us,
-// 5.84 TB/s. (Three CTAs an SM are asked for: 80 registers; 247 us with the 117 it would take, 226 us with 64.)
+// 5.84 TB/s. (Three CTAs an SM are asked for: 80 registers; 247 us with the 117 it would take, 226 us with 64.) That was found for BF16 ys; with
+// FP32 ys, whose eight rows alone are 64 registers, 256 bytes a thread are spilled in the loop: 373 us (dout BF16) and 443 us (FP32) for
+// 1746 and 1813 MB, 4.7 and 4.1 TB/s. Without dweights, BF16 dout: 153 us for 671 MB, 4.4 TB/s.
 
 constexpr int kPairs = 8;
 
