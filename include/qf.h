@@ -50,7 +50,7 @@ typedef enum {
   QF_ERR_TOO_LARGE = 10 /* the problem needs more scratch than the built-in buffer of qf_fq_linear_fwd_noalloc */
 } qf_status_t;
 
-/* The integer types are for expert ids only (qf_moe_sort, qf_fq_grouped_matvec). */
+/* The integer types are for expert ids (qf_moe_sort, qf_fq_grouped_matvec) and cache slots (qf_kv_append, qf_kv_read) only. */
 typedef enum { QF_DT_BF16 = 0, QF_DT_F32 = 1, QF_DT_I32 = 2, QF_DT_I64 = 3 } qf_dtype_t;
 
 typedef enum {
@@ -59,7 +59,8 @@ typedef enum {
   QF_OP_LINEAR_BWD = 2,
   QF_OP_GROUPED_FWD = 3,
   QF_OP_GROUPED_BWD = 4,
-  QF_OP_QDQ_BATCHED = 5
+  QF_OP_QDQ_BATCHED = 5,
+  QF_OP_KV_ATTENTION = 6
 } qf_op_t;
 
 /* flags */
@@ -103,7 +104,8 @@ int qf_version(void);
 
 /* Bytes of caller-provided scratch a call needs (always a multiple of 256, never 0).
  * op = QF_OP_QDQ: M = rows, K = cols, N ignored. Linear ops: M, N, K as in the call; for grouped ops
- * M = rows_padded and `groups` = number of experts. QF_OP_QDQ_BATCHED: `groups` = number of tensors, M, N, K ignored. */
+ * M = rows_padded and `groups` = number of experts. QF_OP_QDQ_BATCHED: `groups` = number of tensors, M, N, K ignored.
+ * QF_OP_KV_ATTENTION: M = batch * q_len, N = q_heads, K = head_dim, groups = kv_heads. */
 size_t qf_workspace_bytes(qf_op_t op, int64_t M, int64_t N, int64_t K, int groups);
 
 /* Reads the 4-byte status word at the start of a workspace (synchronises `stream` first).
@@ -370,6 +372,73 @@ qf_status_t qf_fq_matvec(qf_format_t fmt, const void* X, int64_t M, const void* 
 qf_status_t qf_fq_grouped_matvec(qf_format_t fmt, const void* X, int64_t x_rows, const void* expert_ids, qf_dtype_t ids_dtype,
                                  int64_t pairs, int G, const void* codes, const void* scales, const float* tensor_scales, int64_t N,
                                  int64_t K, void* Y, qf_dtype_t y_dtype, void* stream);
+
+/* ---- a key/value cache in 4 bits ------------------------------------------------------------------------------------
+ *
+ * What a rollout keeps between the products of its layers (Section 3.4): the keys and values of all earlier tokens, in the formats
+ * that the weights are deployed in. The cache of one layer is paged; a page holds page_size tokens of every key/value head:
+ *     k_codes, v_codes     [pages, kv_heads, page_size, head_dim / 2] bytes, element 2j in the low nibble of byte j
+ *     k_scales, v_scales   [pages, kv_heads, page_size, head_dim / 16] E4M3 bytes (NVFP4) or [..., head_dim / 32] E8M0 bytes (MXFP4)
+ *     k_tscale, v_tscale   NVFP4: device float*, the tensor scales of the layer's keys and values, settled before the first write (from
+ *                          a calibration: they cannot follow data that arrives token by token); otherwise ignored
+ * A row of head_dim elements is quantized as qf_qdq does it with a given tensor scale. Slot s is place s % page_size of page
+ * s / page_size. A page table row lists a sequence's pages in order: key j of the sequence is place j % page_size of page
+ * page_table[b][j / page_size].
+ *   fmt        QF_FMT_NVFP4 or QF_FMT_MXFP4
+ *   head_dim   64, 128 or 256;  page_size a multiple of 16, at most 2^20;  kv_heads at most 65535
+ * All four buffers are 16-byte aligned. The struct is host memory and read during the call only. The tables are device memory, so
+ * the host cannot check them: slots outside [0, pages * page_size) are skipped, page numbers are forced into [0, pages) and lengths
+ * into [0, max_pages * page_size], so that a table that breaks the contract gives meaningless results, never an access out of
+ * range. What stands in places that no key of a sequence owns never matters, whatever it holds. */
+typedef struct {
+  qf_format_t fmt;
+  int kv_heads;
+  int head_dim;
+  int page_size;
+  int64_t pages;
+  void* k_codes;
+  void* k_scales;
+  void* v_codes;
+  void* v_scales;
+  const float* k_tscale;
+  const float* v_tscale;
+} qf_kv_cache_t;
+
+/* Quantizes keys and values as they are written: token t of k and v [tokens, kv_heads, head_dim] BF16 goes to slots[t].
+ *   k_stride, v_stride   elements from one token to the next: at least kv_heads * head_dim, a multiple of 8 (slices of a fused
+ *                        projection's output are taken as they are)
+ *   slots        device [tokens], slots_dtype QF_DT_I32 or QF_DT_I64; a slot outside the cache (-1, say) skips the token. Slots of one
+ *                call have to differ: what a slot that is named twice holds afterwards is not defined
+ *   flags        QF_MXFP4_NO_CLIP */
+qf_status_t qf_kv_append(const qf_kv_cache_t* cache, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t tokens,
+                         const void* slots, qf_dtype_t slots_dtype, uint32_t flags, void* stream);
+
+/* Reads rows back: k, v [rows, kv_heads, head_dim] BF16 (either nullable, not both); row i is slot slots[i], zeros if that is outside
+ * the cache. The values are those of qf_dequant: for NVFP4 rounded to BF16. A slot may be named any number of times. For attention of
+ * many tokens (a prefill that goes on behind a cached prompt), with whatever dense attention the caller has. */
+qf_status_t qf_kv_read(const qf_kv_cache_t* cache, const void* slots, qf_dtype_t slots_dtype, int64_t rows, void* k, void* v, void* stream);
+
+/* Attention of the last q_len tokens of every sequence over its cached keys, their own among them (write them first):
+ *     s_j = softmax_scale * <q, k_j>,   p = softmax over the keys j < seq_lens[b] - q_len + i + 1,   out = sum over j of p_j * v_j
+ * for token i in [0, q_len) of sequence b and every query head; query head h reads key/value head h / (q_heads / kv_heads).
+ * FP32 scores, softmax and sums; the weights p_j enter the value product as FP16 numbers (relative error 2^-11 at most, below the
+ * BF16 result's 2^-8) and the dequantized keys and values are not rounded to BF16, as in qf_fq_matvec. A row without keys (an
+ * empty place of a padded batch, a token of a sequence shorter than q_len) gives zeros. Results do not change from run to run; how
+ * the keys are cut depends on the batch's lengths, so that the same row can have other last bits in another batch.
+ *   q            BF16 [batch, q_len, q_heads, head_dim], q_stride elements from one token to the next (at least q_heads * head_dim, a
+ *                multiple of 8): token i of sequence b is row b * q_len + i
+ *   page_table   device int32 [batch, max_pages]; entries behind a sequence's last page are not read
+ *   seq_lens     device int32 [batch]
+ *   out          BF16 [batch, q_len, q_heads, head_dim]
+ *   lse          FP32 [batch, q_len, q_heads], nullable: receives the logarithm of the sum over j of exp(s_j), -infinity for a row
+ *                without keys: what joining with other keys' attention takes
+ *   workspace    qf_workspace_bytes(QF_OP_KV_ATTENTION, batch * q_len, q_heads, head_dim, kv_heads) bytes, whatever they hold; calls
+ *                that can overlap on the GPU (other streams, graphs) need one each
+ * Meant for a few tokens a sequence (a decode step, drafted tokens checked together): the cache is read once per 16 rows of
+ * q_len * q_heads / kv_heads. For long prompts read the cache back (qf_kv_read). */
+qf_status_t qf_kv_attention(const qf_kv_cache_t* cache, const void* q, int64_t q_stride, int64_t batch, int q_len, int q_heads,
+                            const int32_t* page_table, int64_t max_pages, const int32_t* seq_lens, float softmax_scale, void* out,
+                            float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Allocation-free forward of the quantization-aware linear layer. (The paper has no counterpart:
  * this is a packaging variant of qf_fq_linear_fwd for hosts that cannot hand the library a workspace.)

@@ -15,7 +15,7 @@ import torch
 
 FMT_NONE, FMT_NVFP4, FMT_MXFP4, FMT_Q4_K = 0, 1, 2, 3
 DT_BF16, DT_F32, DT_I32, DT_I64 = 0, 1, 2, 3
-OP_QDQ, OP_LINEAR_FWD, OP_LINEAR_BWD, OP_GROUPED_FWD, OP_GROUPED_BWD, OP_QDQ_BATCHED = 0, 1, 2, 3, 4, 5
+OP_QDQ, OP_LINEAR_FWD, OP_LINEAR_BWD, OP_GROUPED_FWD, OP_GROUPED_BWD, OP_QDQ_BATCHED, OP_KV_ATTENTION = 0, 1, 2, 3, 4, 5, 6
 TENSOR_SCALE_GIVEN = 0x1
 W_TSCALE_GIVEN, A_TSCALE_GIVEN, ACCUMULATE_DW, FUSED_QDQ, AMAX_RUNNING = 0x1, 0x2, 0x4, 0x8, 0x10
 REUSE_W_HAT, REUSE_X_HAT = 0x20, 0x40
@@ -33,6 +33,7 @@ EXPORTS = [
     "qf_selftest_div", "qf_fq_linear_fwd_noalloc", "qf_selftest_mxfp4_bf16", "qf_selftest_timeout", "qf_pack_bytes", "qf_pack", "qf_unpack", "qf_nvfp4_tensor_scale", "qf_qdq_lora",
     "qf_fp4_matmul_native", "qf_qdq_batched", "qf_moe_rows_bound", "qf_moe_sort", "qf_moe_dispatch", "qf_moe_dispatch_bwd",
     "qf_moe_combine", "qf_moe_combine_bwd", "qf_fq_matvec", "qf_fq_grouped_matvec", "qf_selftest_matvec_cut",
+    "qf_kv_append", "qf_kv_read", "qf_kv_attention",
 ]
 NOALLOC_SCRATCH_BYTES = 32 << 20
 LAYOUT_GGUF_Q4_K, LAYOUT_FP4_SWIZZLED_SCALES = 1, 2
@@ -131,6 +132,13 @@ def lib() -> ctypes.CDLL:
                                            c_int64, c_int64, c_void_p, c_int, c_void_p]
         L.qf_selftest_matvec_cut.restype = c_int
         L.qf_selftest_matvec_cut.argtypes = [c_int, c_int64, c_int64, c_int64, c_int, c_void_p]
+        L.qf_kv_append.restype = c_int
+        L.qf_kv_append.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_int64, c_void_p, c_int, c_uint32, c_void_p]
+        L.qf_kv_read.restype = c_int
+        L.qf_kv_read.argtypes = [c_void_p, c_void_p, c_int, c_int64, c_void_p, c_void_p, c_void_p]
+        L.qf_kv_attention.restype = c_int
+        L.qf_kv_attention.argtypes = [c_void_p, c_void_p, c_int64, c_int64, c_int, c_int, c_void_p, c_int64, c_void_p, c_float, c_void_p,
+                                      c_void_p, c_void_p, c_size_t, c_void_p]
         _lib = L
     return _lib
 
@@ -615,6 +623,141 @@ def qf_fq_grouped_matvec(fmt: int, X: torch.Tensor, expert_ids: torch.Tensor, co
                                       _tensor(scales, "scales", _U8, (G, *scales_shape(fmt, N, K)), device), ts, N, K, po,
                                       _DATA_DTYPE[Y.dtype], stream), "qf_fq_grouped_matvec")
     return Y
+
+
+class _KvCacheStruct(ctypes.Structure):
+    _fields_ = [("fmt", c_int), ("kv_heads", c_int), ("head_dim", c_int), ("page_size", c_int), ("pages", c_int64), ("k_codes", c_void_p),
+                ("k_scales", c_void_p), ("v_codes", c_void_p), ("v_scales", c_void_p), ("k_tscale", c_void_p), ("v_tscale", c_void_p)]
+
+
+class KvCache:
+    """The paged key/value cache of one layer in NVFP4 or MXFP4 (see qf_kv_cache_t in qf.h), over the caller's tensors: codes uint8
+    [pages, kv_heads, page_size, head_dim / 2], scales uint8 [pages, kv_heads, page_size, head_dim / block] and, for NVFP4, the
+    FP32 tensor scales [1] of the keys and of the values. The tensors are checked here, once; they stay alive with the cache and must not
+    be resized."""
+
+    def __init__(self, fmt: int, k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Tensor, v_scales: torch.Tensor,
+                 k_tscale: torch.Tensor | None = None, v_tscale: torch.Tensor | None = None):
+        if fmt not in (FMT_NVFP4, FMT_MXFP4):
+            raise QfError(4, "KvCache")
+        if k_codes.dim() != 4:
+            raise ValueError(f"k_codes has shape {tuple(k_codes.shape)}, expected [pages, kv_heads, page_size, head_dim / 2]")
+        device = k_codes.get_device()
+        if device < 0:
+            raise TypeError("k_codes must be a CUDA tensor")
+        shape = k_codes.shape
+        pages, heads, page_size, half = shape
+        sshape = (pages, heads, page_size, 2 * half // BLOCK[fmt])
+        ptrs = [_tensor(k_codes, "k_codes", _U8, shape, device), _tensor(k_scales, "k_scales", _U8, sshape, device),
+                _tensor(v_codes, "v_codes", _U8, shape, device), _tensor(v_scales, "v_scales", _U8, sshape, device)]
+        if fmt == FMT_NVFP4:
+            if k_tscale is None or v_tscale is None:
+                raise TypeError("an NVFP4 cache needs the tensor scales k_tscale and v_tscale")
+            ptrs += [_tensor(k_tscale, "k_tscale", _F32, (1,), device), _tensor(v_tscale, "v_tscale", _F32, (1,), device)]
+        else:
+            k_tscale = v_tscale = None
+            ptrs += [None, None]
+        self.fmt, self.pages, self.kv_heads, self.page_size, self.head_dim = fmt, pages, heads, page_size, 2 * half
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales, self.k_tscale, self.v_tscale = k_codes, k_scales, v_codes, v_scales, k_tscale, v_tscale
+        self.device_index = device
+        self._struct = _KvCacheStruct(fmt, heads, 2 * half, page_size, pages, *ptrs)
+        self._address = ctypes.addressof(self._struct)
+
+    @classmethod
+    def empty(cls, fmt: int, pages: int, page_size: int, kv_heads: int, head_dim: int, k_tscale: torch.Tensor | None = None,
+              v_tscale: torch.Tensor | None = None, *, device="cuda") -> "KvCache":
+        """A cache with nothing written to it."""
+        if fmt not in (FMT_NVFP4, FMT_MXFP4):
+            raise QfError(4, "KvCache.empty")
+        make = lambda last: torch.empty((pages, kv_heads, page_size, last), dtype=torch.uint8, device=device)
+        codes, blocks = head_dim // 2, head_dim // BLOCK[fmt]
+        return cls(fmt, make(codes), make(blocks), make(codes), make(blocks), k_tscale, v_tscale)
+
+
+def _kv_here(cache: KvCache):
+    """The current device, which has to be the cache's, and its current stream."""
+    device = cache.device_index
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"the cache is on cuda:{device}, the current device is cuda:{torch._C._cuda_getDevice()}")
+    return device, torch._C._cuda_getCurrentRawStream(device)
+
+
+def _tokens(t: torch.Tensor, name: str, lead, heads: int, dim: int, device: int):
+    """Address of BF16 [*lead, heads, dim] with whole tokens (heads * dim elements without gaps) at one distance, and that distance."""
+    if t.dtype != torch.bfloat16 or t.get_device() < 0:
+        raise TypeError(f"{name} must be a CUDA tensor of type torch.bfloat16")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is cuda:{device}")
+    if t.shape != (*lead, heads, dim):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(*lead, heads, dim)}")
+    distance = heads * dim
+    if not t.is_contiguous():
+        s = t.stride()
+        whole = s[-1] == 1 and (heads == 1 or s[-2] == dim)
+        span = 0                                                   # from one group of the tokens so far to the next
+        for n, step in zip(reversed(lead), reversed(s[:-2])):
+            if n != 1:
+                whole &= span == 0 or step == span
+                if span == 0:
+                    distance = step
+                span = step * n
+        if not whole:
+            raise TypeError(f"{name} must have whole tokens at one distance, its strides are {s}")
+    return t.data_ptr(), distance
+
+
+def _slots(slots: torch.Tensor, device: int):
+    if slots.dim() != 1:
+        raise ValueError(f"slots has shape {tuple(slots.shape)}, expected one dimension")
+    return _tensor(slots, "slots", _IDS_DTYPE, slots.shape, device), _IDS_DTYPE[slots.dtype], slots.shape[0]
+
+
+def qf_kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, *, flags: int = 0) -> None:
+    """Quantizes k and v [tokens, kv_heads, head_dim] into the cache: token t at slots[t] (int32 or int64; page * page_size + place; one
+    outside the cache skips the token). k and v may be slices of wider rows, such as a fused projection's output."""
+    device, stream = _kv_here(cache)
+    ps, dt, tokens = _slots(slots, device)
+    pk, k_stride = _tokens(k, "k", (tokens,), cache.kv_heads, cache.head_dim, device)
+    pv, v_stride = _tokens(v, "v", (tokens,), cache.kv_heads, cache.head_dim, device)
+    _check(lib().qf_kv_append(cache._address, pk, k_stride, pv, v_stride, tokens, ps, dt, flags & MXFP4_NO_CLIP, stream), "qf_kv_append")
+
+
+def qf_kv_read(cache: KvCache, slots: torch.Tensor, *, want_k: bool = True, want_v: bool = True, k: torch.Tensor | None = None,
+               v: torch.Tensor | None = None):
+    """(k, v), BF16 [rows, kv_heads, head_dim]: the dequantized rows of ``slots`` (zeros where a slot is outside the cache); None for the one
+    that is not wanted."""
+    device, stream = _kv_here(cache)
+    ps, dt, rows = _slots(slots, device)
+    shape = (rows, cache.kv_heads, cache.head_dim)
+    k, pk = _out(slots, k, "k", _BF16, shape, torch.bfloat16, device) if want_k else (None, None)
+    v, pv = _out(slots, v, "v", _BF16, shape, torch.bfloat16, device) if want_v else (None, None)
+    _check(lib().qf_kv_read(cache._address, ps, dt, rows, pk, pv, stream), "qf_kv_read")
+    return k, v
+
+
+def qf_kv_attention(cache: KvCache, q: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor, *, softmax_scale: float | None = None,
+                    want_lse: bool = False, out: torch.Tensor | None = None, lse: torch.Tensor | None = None, ws: torch.Tensor | None = None):
+    """Attention of the last q_len tokens of every sequence, q [batch, q_len, q_heads, head_dim], over its seq_lens[b] cached keys, their
+    own among them: out BF16 of q's shape, and with ``want_lse`` also the FP32 logarithms of the softmax sums [batch, q_len, q_heads].
+    ``page_table`` int32 [batch, max_pages], ``seq_lens`` int32 [batch]. The scale defaults to head_dim ** -0.5. ``ws``: a workspace of
+    workspace(OP_KV_ATTENTION, batch * q_len, q_heads, head_dim, kv_heads) that no overlapping call uses."""
+    device, stream = _kv_here(cache)
+    batch, q_len, q_heads, dim = q.shape
+    if dim != cache.head_dim:
+        raise ValueError(f"q has shape {tuple(q.shape)}, the cache's head_dim is {cache.head_dim}")
+    pq, q_stride = _tokens(q, "q", (batch, q_len), q_heads, dim, device)
+    max_pages = page_table.shape[-1]
+    pt = _tensor(page_table, "page_table", _I32, (batch, max_pages), device)
+    pl = _tensor(seq_lens, "seq_lens", _I32, (batch,), device)
+    out, po = _out(q, out, "out", _BF16, (batch, q_len, q_heads, dim), torch.bfloat16, device)
+    want_lse = want_lse or lse is not None
+    lse, pe = _out(q, lse, "lse", _F32, (batch, q_len, q_heads), torch.float32, device) if want_lse else (None, None)
+    if ws is None:
+        ws = workspace(OP_KV_ATTENTION, batch * q_len, q_heads, dim, cache.kv_heads, device=q.device)
+    pw = _tensor(ws, "ws", _U8, (ws.numel(),), device)
+    _check(lib().qf_kv_attention(cache._address, pq, q_stride, batch, q_len, q_heads, pt, max_pages, pl,
+                                 dim ** -0.5 if softmax_scale is None else softmax_scale, po, pe, pw, ws.numel(), stream), "qf_kv_attention")
+    return (out, lse) if want_lse else out
 
 
 def qf_fp4_matmul_native(fmt: int, a: dict, b: dict, K: int, *, flags: int = 0, ws=None) -> torch.Tensor:

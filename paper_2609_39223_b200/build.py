@@ -14,7 +14,7 @@ ROOT = PKG.parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libqf.so"
 SOURCES = ["qf_api.cu", "qf_qdq.cu", "qf_gemm.cu", "qf_pack.cu", "qf_fp4_gemm.cu",
-           "qf_moe.cu", "qf_matvec.cu"]
+           "qf_moe.cu", "qf_matvec.cu", "qf_kv.cu"]
 NVCC_FLAGS = [*os.environ.get("QF_EXTRA_NVCC", "").split(), "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 

@@ -342,6 +342,7 @@ size_t qf_workspace_bytes(qf_op_t op, int64_t M, int64_t N, int64_t K, int group
   if (K < 0) K = 0;
   if (op == QF_OP_QDQ) return kWsHeader;
   if (op == QF_OP_QDQ_BATCHED) return kWsHeader + round256(8 * static_cast<size_t>(groups > 0 ? groups : 0));
+  if (op == QF_OP_KV_ATTENTION) return kWsHeader + round256(kv_attention_ws_bytes(M, N, K, groups));
   const int64_t g = (op == QF_OP_GROUPED_FWD || op == QF_OP_GROUPED_BWD) ? (groups > 0 ? groups : 1) : 1;
   return linear_ws_bytes(M, N, K, g);
 }
@@ -778,6 +779,89 @@ qf_status_t qf_fq_grouped_matvec(qf_format_t fmt, const void* X, int64_t x_rows,
   if (ids_dtype != QF_DT_I32 && ids_dtype != QF_DT_I64) return QF_ERR_DTYPE;
   if (pairs > 0 && !expert_ids) return QF_ERR_NULL;
   return matvec_impl(fmt, X, pairs, x_rows, expert_ids, ids_dtype, G, codes, scales, tensor_scales, N, K, Y, y_dtype, stream);
+}
+
+// What every call on a cache looks at. Bytes of a buffer stay below 2^60.
+static qf_status_t check_kv(const qf_kv_cache_t* c) {
+  if (!c) return QF_ERR_NULL;
+  if (c->fmt != QF_FMT_NVFP4 && c->fmt != QF_FMT_MXFP4) return QF_ERR_FORMAT;
+  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return QF_ERR_SHAPE;
+  if (c->kv_heads < 1 || c->kv_heads > 65535) return QF_ERR_SHAPE;
+  if (c->page_size < 16 || c->page_size % 16 || c->page_size > (1 << 20)) return QF_ERR_SHAPE;
+  if (c->pages < 0 || c->pages > INT32_MAX || c->pages * c->page_size > (1ll << 36)) return QF_ERR_SHAPE;
+  if (!aligned16(c->k_codes) || !aligned16(c->k_scales) || !aligned16(c->v_codes) || !aligned16(c->v_scales)) return QF_ERR_ALIGN;
+  if ((reinterpret_cast<uintptr_t>(c->k_tscale) | reinterpret_cast<uintptr_t>(c->v_tscale)) & 3u) return QF_ERR_ALIGN;
+  return QF_OK;
+}
+static bool kv_has_buffers(const qf_kv_cache_t* c) {
+  return c->k_codes && c->k_scales && c->v_codes && c->v_scales && (c->fmt != QF_FMT_NVFP4 || (c->k_tscale && c->v_tscale));
+}
+static qf_status_t check_slots(const void* slots, int dtype) {
+  if (dtype != QF_DT_I32 && dtype != QF_DT_I64) return QF_ERR_DTYPE;
+  return reinterpret_cast<uintptr_t>(slots) & (dtype == QF_DT_I64 ? 7u : 3u) ? QF_ERR_ALIGN : QF_OK;
+}
+// CTAs of the row kernels are numbered in 31 bits
+static bool kv_tokens_ok(int64_t tokens, int64_t row) { return tokens >= 0 && tokens <= INT32_MAX && tokens * row <= (1ll << 40); }
+// elements from one token to the next
+static bool kv_stride_ok(int64_t stride, int64_t row) { return stride >= row && stride % 8 == 0 && stride <= INT32_MAX; }
+
+qf_status_t qf_kv_append(const qf_kv_cache_t* cache, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t tokens,
+                         const void* slots, qf_dtype_t slots_dtype, uint32_t flags, void* stream) {
+  if (qf_status_t s = check_kv(cache)) return s;
+  const int64_t row = static_cast<int64_t>(cache->kv_heads) * cache->head_dim;
+  if (!kv_tokens_ok(tokens, row) || !kv_stride_ok(k_stride, row) || !kv_stride_ok(v_stride, row)) return QF_ERR_SHAPE;
+  if (qf_status_t s = check_slots(slots, slots_dtype)) return s;
+  const bool any = tokens > 0 && cache->pages > 0;
+  if (any && (!k || !v || !slots || !kv_has_buffers(cache))) return QF_ERR_NULL;
+  if (!aligned16(k) || !aligned16(v)) return QF_ERR_ALIGN;
+  if (qf_status_t s = check_arch()) return s;
+  if (!any) return QF_OK;
+  return cu(launch_kv_append(*cache, k, k_stride, v, v_stride, tokens, slots, slots_dtype == QF_DT_I64, (flags & QF_MXFP4_NO_CLIP) != 0,
+                             static_cast<cudaStream_t>(stream)));
+}
+
+qf_status_t qf_kv_read(const qf_kv_cache_t* cache, const void* slots, qf_dtype_t slots_dtype, int64_t rows, void* k, void* v, void* stream) {
+  if (qf_status_t s = check_kv(cache)) return s;
+  if (!kv_tokens_ok(rows, static_cast<int64_t>(cache->kv_heads) * cache->head_dim)) return QF_ERR_SHAPE;
+  if (qf_status_t s = check_slots(slots, slots_dtype)) return s;
+  if (rows > 0 && (!slots || (!k && !v) || (cache->pages > 0 && !kv_has_buffers(cache)))) return QF_ERR_NULL;
+  if (!aligned16(k) || !aligned16(v)) return QF_ERR_ALIGN;
+  if (qf_status_t s = check_arch()) return s;
+  if (rows == 0) return QF_OK;
+  return cu(launch_kv_read(*cache, slots, slots_dtype == QF_DT_I64, rows, k, v, static_cast<cudaStream_t>(stream)));
+}
+
+qf_status_t qf_kv_attention(const qf_kv_cache_t* cache, const void* q, int64_t q_stride, int64_t batch, int q_len, int q_heads,
+                            const int32_t* page_table, int64_t max_pages, const int32_t* seq_lens, float softmax_scale, void* out,
+                            float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (qf_status_t s = check_kv(cache)) return s;
+  if (batch < 0 || q_len < 0 || q_heads < 1 || q_heads % cache->kv_heads) return QF_ERR_SHAPE;
+  if (batch > (1 << 20) || q_heads > (1 << 20) || batch * q_len > INT32_MAX || batch * q_len * q_heads > INT32_MAX) return QF_ERR_SHAPE;
+  if (max_pages < 0 || max_pages > INT32_MAX || max_pages * cache->page_size > INT32_MAX - 1024) return QF_ERR_SHAPE;   // keys are numbered in 32 bits
+  if (!kv_stride_ok(q_stride, static_cast<int64_t>(q_heads) * cache->head_dim)) return QF_ERR_SHAPE;
+  const int64_t rows = batch * q_len;
+  if (!workspace || workspace_bytes < qf_workspace_bytes(QF_OP_KV_ATTENTION, rows, q_heads, cache->head_dim, cache->kv_heads)) return QF_ERR_WORKSPACE;
+  const bool keys = max_pages > 0 && cache->pages > 0;
+  if (rows > 0 && (!q || !out || !seq_lens || (keys && (!page_table || !kv_has_buffers(cache))))) return QF_ERR_NULL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return QF_ERR_ALIGN;
+  if ((reinterpret_cast<uintptr_t>(page_table) | reinterpret_cast<uintptr_t>(seq_lens) | reinterpret_cast<uintptr_t>(lse)) & 3u) return QF_ERR_ALIGN;
+  if (qf_status_t s = check_arch()) return s;
+  if (rows == 0) return QF_OK;
+  KvAttentionArgs a{};
+  a.cache = *cache;
+  a.q = q;
+  a.q_stride = q_stride;
+  a.batch = batch;
+  a.q_len = q_len;
+  a.q_heads = q_heads;
+  a.table = page_table;
+  a.max_pages = keys ? max_pages : 0;
+  a.lens = seq_lens;
+  a.scale = softmax_scale;
+  a.out = out;
+  a.lse = lse;
+  a.workspace = static_cast<uint8_t*>(workspace) + kWsHeader;
+  return cu(launch_kv_attention(a, static_cast<cudaStream_t>(stream)));
 }
 
 static qf_status_t check_pack(int layout, int fmt, int64_t rows, int64_t cols) {

@@ -397,6 +397,27 @@ cudaError_t launch_matvec(const MatvecArgs& a, cudaStream_t st);
 // How it would be cut (see qf_selftest_matvec_cut); a.ids is looked at for being null alone.
 void matvec_cut(const MatvecArgs& a, int* cut);
 
+// The 4-bit key/value cache (qf_kv.cu).
+cudaError_t launch_kv_append(const qf_kv_cache_t& c, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t tokens,
+                             const void* slots, bool slots64, bool noclip, cudaStream_t st);
+cudaError_t launch_kv_read(const qf_kv_cache_t& c, const void* slots, bool slots64, int64_t rows, void* k, void* v, cudaStream_t st);
+struct KvAttentionArgs {
+  qf_kv_cache_t cache;
+  const void* q;
+  int64_t q_stride;
+  int64_t batch;
+  int q_len, q_heads;
+  const int32_t* table;
+  int64_t max_pages;
+  const int32_t* lens;
+  float scale;
+  void* out;
+  float* lse;
+  void* workspace;
+};
+size_t kv_attention_ws_bytes(int64_t rows, int q_heads, int head_dim, int kv_heads);       // without the header
+cudaError_t launch_kv_attention(const KvAttentionArgs& a, cudaStream_t st);
+
 cudaError_t launch_selftest_timeout(uint32_t* status, long long limit_cycles, int* gave_up, cudaStream_t st);
 
 }  // namespace qf
