@@ -840,6 +840,7 @@ qf_status_t qf_kv_attention(const qf_kv_cache_t* cache, const void* q, int64_t q
   if (max_pages < 0 || max_pages > INT32_MAX || max_pages * cache->page_size > INT32_MAX - 1024) return QF_ERR_SHAPE;   // keys are numbered in 32 bits
   if (!kv_stride_ok(q_stride, static_cast<int64_t>(q_heads) * cache->head_dim)) return QF_ERR_SHAPE;
   const int64_t rows = batch * q_len;
+  if ((rows * q_heads / 8 + batch * cache->kv_heads) * (max_pages * cache->page_size / 32 + 1) > (1ll << 37)) return QF_ERR_SHAPE;   // a CTA's share of the work is counted in 31 bits
   if (!workspace || workspace_bytes < qf_workspace_bytes(QF_OP_KV_ATTENTION, rows, q_heads, cache->head_dim, cache->kv_heads)) return QF_ERR_WORKSPACE;
   const bool keys = max_pages > 0 && cache->pages > 0;
   if (rows > 0 && (!q || !out || !seq_lens || (keys && (!page_table || !kv_has_buffers(cache))))) return QF_ERR_NULL;

@@ -125,7 +125,27 @@ KvRows kv_rows(const qf_kv_cache_t& c, const void* slots, bool slots64) {
 }
 
 // ---- attention -----------------------------------------------------------------------------------------------------------
-// One CTA per (sequence, token, query head): its four warps take every fourth key, a lane D / 32 of the dimensions.
+// Both products run on mma.sync m16n8k16 with FP16 operands and FP32 sums, keys (values) as the 16-row operand and up to 8 NT rows
+// of queries as columns. A tcgen05 tile would need the decoded keys and values in shared memory, 4 bytes of traffic for each element
+// that takes 0.56 bytes of HBM; here a decoded element never leaves its lane's registers.
+//
+//  * Exactness. An E2M1 value times its block scale is exact in FP16: six significant bits for E4M3 scales; for E8M0 scales a power of
+//    two relative to the largest scale of the same row, exact over 36 binades (what lies below counts as zero) with the row's own
+//    power of two applied in FP32. A query row is scaled by a power of two to a maximum in [2^14, 2^15): exact in FP16 down to 2^-31 of
+//    its largest element, below which FP32 sums would lose it anyway. So scores are FP32 sums of exact products.
+//  * One pass over the keys with a running maximum and sum per query row. The weights are FP16 numbers 2^10 times their value, so that
+//    those below 2^-24 of the largest are the first to lose bits; the sum takes them unrounded. A unit's value product starts from
+//    zero and is added in FP32: the tensor core truncates as it accumulates, and a chain of thousands would drift.
+//    MXFP4 keeps a second maximum, of score plus the value row's power of two, for the value product's weights: wherever
+//    the softmax puts its weight, that is where the FP16 range lies.
+//  * Work is cut into units of 32 keys of one (sequence, key head, tile of query rows), numbered in that order. CTA c of W takes units
+//    [c U / W, (c + 1) U / W): equal shares whatever the lengths. Its warps share what it has of a sequence, and meet in shared
+//    memory. Only a CTA's first and last pieces can be parts of a longer sequence: those go to the workspace, and a second
+//    kernel joins them in order.
+
+constexpr int kUnitKeys = 32;
+constexpr int kAttnWarps = 4;                 // of a CTA
+constexpr int kStages = 2;                    // units a warp has in shared memory or on the way
 
 struct KvAttn {
   const __nv_bfloat16* q;
@@ -140,78 +160,783 @@ struct KvAttn {
   const int32_t* lens;
   __nv_bfloat16* out;
   float* lse;
-  int64_t pages;
-  int max_pages, page_size, q_len, q_heads, kv_heads;
-  float scale;
+  uint8_t* ws;
+  int batch, pages, max_pages, page_size, max_keys;
+  int q_len, q_heads, kv_heads, group;
+  int rows, tiles, segs;                      // query rows of a key head; tiles of them; (key head, tile) pairs of a sequence
+  float scale;                                // times log2 e
 };
 
+// Sizes of the kernel for a format, a head size and query rows in units of 8.
+template <int FMT, int D, int NT>
+struct Shape {
+  static constexpr int BLOCK = FMT == QF_FMT_NVFP4 ? 16 : 32, NB = D / BLOCK;              // blocks of a row
+  static constexpr int HALVES = D == 256 ? 2 : 1;                                          // 128-element halves of a row
+  static constexpr int CODES = kUnitKeys * D / 2, SCALES = kUnitKeys * NB, STAGE = 2 * (CODES + SCALES);
+  static constexpr int KMUL = kUnitKeys * NB * 4, VMUL = kUnitKeys * NB * 2;               // multipliers as FP16: twice a key's, pairs of values'
+  static constexpr int WARP = kStages * STAGE + KMUL + VMUL;
+  static constexpr int MT = D / 16;                                                        // 16-row tiles of the value product
+  static constexpr int PART = (MT * NT * 4 + 4 * NT) * 32 * 4;                             // a warp's sums and maxima, bytes
+  static constexpr int SMEM = kAttnWarps * WARP + kAttnWarps / 2 * PART;
+  static constexpr int CTAS = 232448 / (SMEM + 1024) < 4 ? 232448 / (SMEM + 1024) : 4;     // of an SM
+};
+
+// Workspace: a descriptor per CTA, then two parts per CTA (the piece it continues, the piece it begins).
+struct JoinTask { int more, b, seg, pad; };   // CTAs that continue the piece that this one begins (0: nothing to join)
+
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+  const __half2 h = __hmul2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Eight E2M1 codes -> four FP16 pairs (2i, 2i + 1)
+__device__ __forceinline__ void e2m1_f16(uint32_t q, uint32_t (&w)[4]) {
+  asm("{\n.reg .b8 a, b, c, d;\nmov.b32 {a, b, c, d}, %4;\n"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\ncvt.rn.f16x2.e2m1x2 %1, b;\ncvt.rn.f16x2.e2m1x2 %2, c;\ncvt.rn.f16x2.e2m1x2 %3, d;\n}"
+      : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+      : "r"(q));
+}
+// Four E4M3 codes -> two FP16 pairs
+__device__ __forceinline__ void e4m3_f16(uint32_t s, uint32_t& lo, uint32_t& hi) {
+  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(s));
+}
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+  uint32_t d;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+template <typename T>
+__device__ __forceinline__ T smem_load(uint32_t at) {
+  T v;
+  if constexpr (sizeof(T) == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  else if constexpr (sizeof(T) == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void smem_store(uint32_t at, uint32_t a) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(a) : "memory"); }
+__device__ __forceinline__ void smem_store(uint32_t at, uint32_t a, uint32_t b) {
+  asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(a), "r"(b) : "memory");
+}
+__device__ __forceinline__ void smem_store(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+__device__ __forceinline__ int keys_of(const KvAttn& p, int b) { return min(max(p.lens[b], 0), p.max_keys); }
+// a sequence without keys has one unit, so that somebody writes its zeros
+__device__ __forceinline__ int units_of(int keys) { return max(1, (keys + kUnitKeys - 1) / kUnitKeys); }
+
+// The pieces of a CTA's share, one (sequence, segment) after the other: units [j, j + n) of segment s of sequence b.
+struct Walk {
+  int b, s, keys, units, j, n, left;          // left: units from this piece on
+  __device__ __forceinline__ void next(const KvAttn& p) {
+    left -= n;
+    n = 0;
+    if (left <= 0) return;
+    j = 0;
+    if (++s == p.segs) {
+      s = 0;
+      keys = keys_of(p, ++b);
+      units = units_of(keys);
+    }
+    n = min(left, units);
+  }
+};
+
+// 16-byte piece c of a row's codes lies in place c ^ turn(row): lanes that read together (four consecutive rows, or four from the
+// end of a group of eight) meet different banks.
+template <int D>
+__device__ __forceinline__ int turn(int row) {
+  return D == 64 ? 0 : ((row >> 1) & 1) * 2 + (D == 256 ? (row & 1) * 4 : 0);
+}
+
+// A warp's copies into its ring: its quarter of every piece, unit by unit, ahead of the products.
 template <int FMT, int D>
-__device__ __forceinline__ void row_values(const uint8_t* codes, const uint8_t* scales, int64_t row, int lane, float (&x)[D / 32]) {
-  constexpr int E = D / 32, BLOCK = FMT == QF_FMT_NVFP4 ? 16 : 32;
-  const uint32_t s = scales[row * (D / BLOCK) + lane * E / BLOCK];
-  const float sb = FMT == QF_FMT_NVFP4 ? e4m3_decode(s & 0x7Fu) : e8m0_scale(s);
+struct Copier {
+  using S = Shape<FMT, D, 1>;
+  Walk w;
+  int cur, end, page, off;                    // unit, end of this warp's part of the piece, page and place of its first key
+  int id0, id1;                               // pages of its two groups of 16 keys
+
+  __device__ __forceinline__ void pages_of(const KvAttn& p) {
+    const int32_t* row = p.table + static_cast<int64_t>(w.b) * p.max_pages;
+    const int next = off + 16 < p.page_size ? page : page + 1;
+    const int most = p.pages - 1;
+    id0 = page < p.max_pages ? min(max(row[page], 0), most) : 0;
+    id1 = next < p.max_pages ? min(max(row[next], 0), most) : 0;
+  }
+  __device__ __forceinline__ void piece(const KvAttn& p, int warp) {
+    while (w.n > 0) {
+      cur = w.j + static_cast<int>(static_cast<int64_t>(w.n) * warp / kAttnWarps);
+      end = w.j + static_cast<int>(static_cast<int64_t>(w.n) * (warp + 1) / kAttnWarps);
+      if (cur < end) break;
+      w.next(p);
+    }
+    if (w.n > 0) {
+      page = cur * kUnitKeys / p.page_size;
+      off = cur * kUnitKeys - page * p.page_size;
+      pages_of(p);
+    }
+  }
+  __device__ __forceinline__ void issue(const KvAttn& p, uint32_t stage, int warp, int lane) {
+    if (w.n > 0) {
+      const int h = w.s / p.tiles;
+      constexpr int ROW = D / 2, PIECES = ROW / 16, SROW = S::NB, CHUNKS = 16 * SROW / 16;     // of a row; of 16 rows' scales
 #pragma unroll
-  for (int i = 0; i < E / 2; ++i) {
-    const float2 v = e2m1x2_decode(codes[row * (D / 2) + lane * (E / 2) + i]);
-    x[2 * i] = v.x * sb;
-    x[2 * i + 1] = v.y * sb;
+      for (int half = 0; half < 2; ++half) {
+        const bool here = cur * kUnitKeys + half * 16 < w.keys;
+        if (here) {
+          const int o = half == 0 ? off : off + 16 < p.page_size ? off + 16 : 0;
+          const int64_t row = (static_cast<int64_t>(half ? id1 : id0) * p.kv_heads + h) * p.page_size + o;
+          const uint8_t* kc = p.k_codes + row * ROW;
+          const uint8_t* vc = p.v_codes + row * ROW;
+#pragma unroll
+          for (int i = 0; i < PIECES / 2; ++i) {
+            const int c = i * 32 + lane, r = c / PIECES, piece = c % PIECES;
+            const uint32_t to = stage + (half * 16 + r) * ROW + ((piece ^ turn<D>(r)) * 16);
+            copy16(to, kc + c * 16);
+            copy16(to + S::CODES, vc + c * 16);
+          }
+          if (lane < 2 * CHUNKS) {
+            const bool value = lane >= CHUNKS;
+            const int c = value ? lane - CHUNKS : lane;
+            copy16(stage + 2 * S::CODES + (value ? S::SCALES : 0) + half * 16 * SROW + c * 16, (value ? p.v_scales : p.k_scales) + row * SROW + c * 16);
+          }
+        }
+      }
+      if (++cur < end) {
+        off += kUnitKeys;
+        while (off >= p.page_size) { off -= p.page_size; ++page; }
+        pages_of(p);
+      } else {
+        w.next(p);
+        piece(p, warp);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+};
+
+// What a lane has of a piece: of the value product row 16 i + g (dimension 2i of the lane's, i counting) and row 16 i + g + 8 (dimension
+// 2i + 1), columns (query rows) 8 n + 2t and 8 n + 2t + 1; and of these columns the maximum and the sum.
+template <int MT, int NT>
+struct Sums {
+  float o[MT][NT][4];
+  float m[NT][2], l[NT][2];
+};
+
+// Element of the head that row r (0 or 1) of value tile i holds for lane row g.
+template <int D>
+__device__ __forceinline__ int dim_of(int i, int g) {
+  return D == 64 ? g * 8 + 2 * i : (i >> 3) * 128 + g * 16 + 2 * (i & 7);
+}
+
+__device__ __forceinline__ void join_weights(float ma, float mb, float& m, float& fa, float& fb) {
+  m = fmaxf(ma, mb);
+  fa = m == -INFINITY ? 0.0f : exp2_approx(ma - m);
+  fb = m == -INFINITY ? 0.0f : exp2_approx(mb - m);
+}
+
+__device__ __forceinline__ float log_sum(float m, float l) { return l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY; }
+
+template <int FMT, int D, int NT>
+__global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv_attention_kernel(const __grid_constant__ KvAttn p) {
+  using S = Shape<FMT, D, NT>;
+  constexpr int MT = S::MT, NB = S::NB, HALVES = S::HALVES;
+  constexpr int WORDS = D == 64 ? 2 : 4;                       // words of codes of a key that a lane holds per half
+  constexpr int VWORDS = D == 64 ? 1 : 2;                      // and of a value
+  extern __shared__ __align__(16) uint8_t smem[];
+  launch_after_previous();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + warp * S::WARP;
+  const uint32_t kmul = ring + kStages * S::STAGE, vmul = kmul + S::KMUL;
+  const uint32_t parts = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + kAttnWarps * S::WARP;
+
+  // This CTA's share. All units are counted by all CTAs, each thread a run of the sequences.
+  __shared__ int64_t warp_units[kAttnWarps];
+  __shared__ int first_b, first_unit_s, first_unit_j;
+  const int per = (p.batch + kAttnWarps * 32 - 1) / (kAttnWarps * 32);
+  const int b0 = min(static_cast<int>(threadIdx.x) * per, p.batch), b1 = min(b0 + per, p.batch);
+  int64_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += units_of(keys_of(p, b));
+  mine *= p.segs;
+  int64_t before = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    const int64_t o = __shfl_up_sync(0xFFFFFFFFu, before, d);
+    if (lane >= d) before += o;
+  }
+  if (lane == 31) warp_units[warp] = before;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int i = 0; i < kAttnWarps; ++i) {
+    if (i < warp) before += warp_units[i];
+    total += warp_units[i];
+  }
+  before -= mine;
+  const int ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), (total + kAttnWarps - 1) / kAttnWarps));
+  const int cta = blockIdx.x;
+  JoinTask* tasks = reinterpret_cast<JoinTask*>(p.ws);
+  float4* part_at = reinterpret_cast<float4*>(p.ws + ((gridDim.x * sizeof(JoinTask) + 255) & ~static_cast<size_t>(255)));
+  constexpr int PART4 = S::PART / 16;                          // float4s of a part
+  if (cta >= ctas) {
+    if (threadIdx.x == 0) tasks[cta].more = 0;
+    return;
+  }
+  const int64_t u0 = cta * total / ctas, u1 = (cta + 1) * total / ctas;
+  if (before <= u0 && u0 < before + mine) {
+    int64_t r = u0 - before;
+    int b = b0;
+    for (;; ++b) {
+      const int64_t all = static_cast<int64_t>(units_of(keys_of(p, b))) * p.segs;
+      if (r < all) break;
+      r -= all;
+    }
+    const int units = units_of(keys_of(p, b));
+    first_b = b;
+    first_unit_s = static_cast<int>(r / units);
+    first_unit_j = static_cast<int>(r % units);
+  }
+  __syncthreads();
+  Walk w;
+  w.b = first_b;
+  w.s = first_unit_s;
+  w.j = first_unit_j;
+  w.keys = keys_of(p, w.b);
+  w.units = units_of(w.keys);
+  w.left = static_cast<int>(u1 - u0);
+  w.n = min(w.left, w.units - w.j);
+  if (threadIdx.x == 0) tasks[cta].more = 0;
+
+  Copier<FMT, D> copy;
+  copy.w = w;
+  copy.piece(p, warp);
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) copy.issue(p, ring + i * S::STAGE, warp, lane);
+  int stage = 0;
+
+  // row g of a 16-key tile is key own0 of its first eight, row g + 8 the same of the second; the keys of a lane's columns of the value product
+  // then are t and 7 - t of both eights
+  const int own0 = (g & 1) ? 7 - (g >> 1) : g >> 1;
+  const float vt = FMT == QF_FMT_NVFP4 ? *p.v_tscale : 0x1p-13f;
+  const float kt = p.scale * (FMT == QF_FMT_NVFP4 ? *p.k_tscale : 0x1p-12f);
+
+  for (; w.n > 0; w.next(p)) {
+    const int h = w.s / p.tiles, row0 = (w.s - h * p.tiles) * (8 * NT);
+    // queries of this tile as FP16 fragments, and what a score has to be multiplied with
+    uint32_t qf[NT][D / 16][2];
+    float by[NT][2];
+    int seen[NT][2], least = w.keys;                           // keys that a column sees
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int row = row0 + 8 * n + g;
+      const bool any = row < p.rows;
+      const int token = any ? row / p.group : 0, head = h * p.group + (any ? row - token * p.group : 0);
+      const __nv_bfloat16* src = p.q + (static_cast<int64_t>(w.b) * p.q_len + token) * p.q_stride + static_cast<int64_t>(head) * D;
+      uint4 raw[D / 32];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const int at = D == 64 ? t * 16 + 8 * i : (i >> 2) * 128 + t * 32 + 8 * (i & 3);
+        raw[i] = any ? *reinterpret_cast<const uint4*>(src + at) : make_uint4(0, 0, 0, 0);
+        top = max(top, chunk_amax_bits(raw[i]));
+      }
+      top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+      top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+      const int e = max(static_cast<int>(top >> 7), 14);       // exponent of the row's largest element
+      const float up = __uint_as_float(static_cast<uint32_t>(268 - e) << 23), down = __uint_as_float(static_cast<uint32_t>(e - 14) << 23);
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const uint32_t v[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) qf[n][2 * i + (k >> 1)][k & 1] = f16x2(bf16_lo(v[k]) * up, bf16_hi(v[k]) * up);
+      }
+      const float f = e == 14 ? 0x1p-127f : down;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        by[n][c] = __shfl_sync(0xFFFFFFFFu, f, (2 * t + c) * 4) * kt;
+        const int col = row0 + 8 * n + 2 * t + c;
+        const int tok = min(col, p.rows - 1) / p.group;
+        seen[n][c] = min(max(w.keys - p.q_len + tok + 1, 0), w.keys);
+      }
+      least = min(least, min(max(w.keys - p.q_len + min(row0 + 8 * n, p.rows - 1) / p.group + 1, 0), w.keys));
+    }
+
+    Sums<MT, NT> a;
+    float mv[NT][2];                                           // MXFP4: maximum of the value product's weights
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) { a.m[n][c] = mv[n][c] = -INFINITY; a.l[n][c] = 0.0f; }
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) a.o[i][n][c] = 0.0f;
+    }
+
+    const int from = w.j + static_cast<int>(static_cast<int64_t>(w.n) * warp / kAttnWarps);
+    const int to = w.j + static_cast<int>(static_cast<int64_t>(w.n) * (warp + 1) / kAttnWarps);
+    for (int u = from; u < to; ++u) {
+      copy.issue(p, ring + (stage == 0 ? kStages - 1 : stage - 1) * S::STAGE, warp, lane);
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+      __syncwarp();
+      const uint32_t here = ring + stage * S::STAGE;
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+      const int key0 = u * kUnitKeys;
+
+      // Multipliers of this unit, a key per lane: FP16 scales of its blocks, for keys twice in a word, for values in pairs of keys (a key
+      // and the last, second last, ... of its group of eight); values behind the last key get zeros. MXFP4: relative to the row's largest.
+      float k_by = 1.0f, v_up = 0.0f;
+      {
+        constexpr int NR = NB / 2;                             // FP16 pairs of a row
+        uint32_t kr[NR], vr[NR];
+        const uint32_t ks = here + 2 * S::CODES + lane * NB, vs = ks + S::SCALES;
+        if constexpr (FMT == QF_FMT_NVFP4) {
+#pragma unroll
+          for (int i = 0; i < NB / 4; ++i) {
+            e4m3_f16(smem_load<uint32_t>(ks + 4 * i) & 0x7F7F7F7Fu, kr[2 * i], kr[2 * i + 1]);
+            e4m3_f16(smem_load<uint32_t>(vs + 4 * i) & 0x7F7F7F7Fu, vr[2 * i], vr[2 * i + 1]);
+          }
+        } else {
+#pragma unroll
+          for (int kind = 0; kind < 2; ++kind) {
+            uint32_t word[(NB + 3) / 4];
+#pragma unroll
+            for (int i = 0; i < (NB + 3) / 4; ++i) {
+              if constexpr (NB == 2) {
+                uint16_t two;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(two) : "r"(kind ? vs : ks) : "memory");
+                word[i] = two;
+              } else {
+                word[i] = smem_load<uint32_t>((kind ? vs : ks) + 4 * i);
+              }
+            }
+            int s[NB], top = 0;
+#pragma unroll
+            for (int i = 0; i < NB; ++i) { s[i] = (word[i / 4] >> (8 * (i & 3))) & 0xFF; top = max(top, s[i]); }
+            const int base = 127 + (kind ? 13 : 12) - top;
+#pragma unroll
+            for (int i = 0; i < NR; ++i)
+              (kind ? vr : kr)[i] = f16x2(__uint_as_float(static_cast<uint32_t>(max(s[2 * i] + base, 0)) << 23),
+                                          __uint_as_float(static_cast<uint32_t>(max(s[2 * i + 1] + base, 0)) << 23));
+            if (kind) v_up = static_cast<float>(top - 127);
+            else k_by = e8m0_scale(top);
+          }
+        }
+        if (key0 + lane >= w.keys) {
+#pragma unroll
+          for (int i = 0; i < NR; ++i) vr[i] = 0u;
+        }
+        const uint32_t kto = kmul + lane * NB * 4;
+        if constexpr (NR >= 2) {
+#pragma unroll
+          for (int i = 0; i < NR; i += 2)
+            smem_store(kto + 8 * i, __byte_perm(kr[i], 0, 0x1010), __byte_perm(kr[i], 0, 0x3232), __byte_perm(kr[i + 1], 0, 0x1010), __byte_perm(kr[i + 1], 0, 0x3232));
+        } else {
+          smem_store(kto, __byte_perm(kr[0], 0, 0x1010), __byte_perm(kr[0], 0, 0x3232));
+        }
+        const bool low = (lane & 4) == 0;
+        const int pair = (lane >> 3) * 4 + (low ? lane & 3 : 3 - (lane & 3));
+        const uint32_t vto = vmul + pair * NB * 4;
+        if constexpr (NR >= 2) {
+#pragma unroll
+          for (int i = 0; i < NR / 2; ++i) {                   // the first of a pair writes the first half of the blocks, the other one the second
+            const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, low ? vr[NR / 2 + i] : vr[i], 7);
+            const uint32_t x = low ? vr[i] : got, y = low ? got : vr[NR / 2 + i];
+            smem_store(vto + (low ? 0 : NB * 2) + 8 * i, __byte_perm(x, y, 0x5410), __byte_perm(x, y, 0x7632));
+          }
+        } else {
+          const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, vr[0], 7);
+          smem_store(vto + (low ? 0 : 4), low ? __byte_perm(vr[0], got, 0x5410) : __byte_perm(got, vr[0], 0x7632));
+        }
+      }
+      __syncwarp();
+
+      // scores
+      float s[2][NT][4];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) s[half][n][c] = 0.0f;
+        const int r0 = half * 16 + own0, r1 = r0 + 8;
+#pragma unroll
+        for (int hh = 0; hh < HALVES; ++hh) {
+          uint32_t c0[WORDS], c1[WORDS], x0[2], x1[2];
+          if constexpr (D == 64) {
+            const uint2 v0 = smem_load<uint2>(here + r0 * 32 + t * 8), v1 = smem_load<uint2>(here + r1 * 32 + t * 8);
+            c0[0] = v0.x; c0[1] = v0.y; c1[0] = v1.x; c1[1] = v1.y;
+          } else {
+            const int piece = ((hh * 4 + t) ^ turn<D>(own0)) * 16;          // row r1 = r0 + 8 has the same turn
+            const uint4 v0 = smem_load<uint4>(here + r0 * (D / 2) + piece), v1 = smem_load<uint4>(here + r1 * (D / 2) + piece);
+            c0[0] = v0.x; c0[1] = v0.y; c0[2] = v0.z; c0[3] = v0.w;
+            c1[0] = v1.x; c1[1] = v1.y; c1[2] = v1.z; c1[3] = v1.w;
+          }
+          if constexpr (FMT == QF_FMT_NVFP4 && D != 64) {
+            const uint32_t at = kmul + (hh * 8 + 2 * t) * 4;
+            const uint2 y0 = smem_load<uint2>(at + r0 * NB * 4), y1 = smem_load<uint2>(at + r1 * NB * 4);
+            x0[0] = y0.x; x0[1] = y0.y; x1[0] = y1.x; x1[1] = y1.y;
+          } else {
+            const uint32_t at = kmul + (D == 64 ? (FMT == QF_FMT_NVFP4 ? t : t >> 1) : hh * 4 + t) * 4;
+            x0[0] = x0[1] = smem_load<uint32_t>(at + r0 * NB * 4);
+            x1[0] = x1[1] = smem_load<uint32_t>(at + r1 * NB * 4);
+          }
+#pragma unroll
+          for (int x = 0; x < WORDS; ++x) {
+            uint32_t d0[4], d1[4];
+            e2m1_f16(c0[x], d0);
+            e2m1_f16(c1[x], d1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { d0[i] = hmul2(d0[i], x0[x >> 1]); d1[i] = hmul2(d1[i], x1[x >> 1]); }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const int step = hh * 8 + 2 * x;
+              mma(s[half][n], d0[0], d1[0], d0[1], d1[1], qf[n][step][0], qf[n][step][1]);
+              mma(s[half][n], d0[2], d1[2], d0[3], d1[3], qf[n][step + 1][0], qf[n][step + 1][1]);
+            }
+          }
+        }
+      }
+      // in units of powers of two; MXFP4: the keys' powers of two, and the values' for the second maximum
+      float up[2][2];
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int key = half * 16 + r * 8 + own0;
+          if constexpr (FMT == QF_FMT_MXFP4) {
+            const float f = __shfl_sync(0xFFFFFFFFu, k_by, key);
+            up[half][r] = __shfl_sync(0xFFFFFFFFu, v_up, key);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) { s[half][n][2 * r] *= f; s[half][n][2 * r + 1] *= f; }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) { s[half][n][2 * r] *= by[n][0]; s[half][n][2 * r + 1] *= by[n][1]; }
+        }
+      if (key0 + kUnitKeys > least) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if (key0 + half * 16 + (c >> 1) * 8 + own0 >= seen[n][c & 1]) s[half][n][c] = -INFINITY;
+      }
+      float keep[NT][2];                                       // what the sums so far have to be multiplied with
+      uint32_t pf[2][NT][2];                                   // weights as fragments of the value product
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float base[2], vbase[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float top = fmaxf(fmaxf(s[0][n][c], s[0][n][c + 2]), fmaxf(s[1][n][c], s[1][n][c + 2]));
+          float vtop = FMT == QF_FMT_MXFP4 ? fmaxf(fmaxf(s[0][n][c] + up[0][0], s[0][n][c + 2] + up[0][1]), fmaxf(s[1][n][c] + up[1][0], s[1][n][c + 2] + up[1][1])) : 0.0f;
+#pragma unroll
+          for (int d = 4; d < 32; d *= 2) {
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+            if (FMT == QF_FMT_MXFP4) vtop = fmaxf(vtop, __shfl_xor_sync(0xFFFFFFFFu, vtop, d));
+          }
+          // maxima are kept 10 lower: weights then reach up to 2^10
+          const float now = fmaxf(a.m[n][c], top - 10.0f);
+          base[c] = now == -INFINITY ? 0.0f : now;
+          const float f = exp2_approx(a.m[n][c] - base[c]);
+          a.l[n][c] *= f;
+          a.m[n][c] = now;
+          keep[n][c] = f;
+          if constexpr (FMT == QF_FMT_MXFP4) {
+            const float vnow = fmaxf(mv[n][c], vtop - 10.0f);
+            vbase[c] = vnow == -INFINITY ? 0.0f : vnow;
+            keep[n][c] = exp2_approx(mv[n][c] - vbase[c]);
+            mv[n][c] = vnow;
+          }
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const float e0 = exp2_approx(s[half][n][2 * r] - base[0]), e1 = exp2_approx(s[half][n][2 * r + 1] - base[1]);
+            a.l[n][0] += e0;
+            a.l[n][1] += e1;
+            if constexpr (FMT == QF_FMT_MXFP4)
+              pf[half][n][r] = transpose8x8(f16x2(exp2_approx(s[half][n][2 * r] + up[half][r] - vbase[0]), exp2_approx(s[half][n][2 * r + 1] + up[half][r] - vbase[1])));
+            else
+              pf[half][n][r] = transpose8x8(f16x2(e0, e1));
+          }
+        }
+      }
+      // values
+#pragma unroll
+      for (int hh = 0; hh < HALVES; ++hh) {
+        uint32_t y[2][2];                                      // multipliers of the lane's block, for the pairs of keys t and 7 - t
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const int block = FMT == QF_FMT_NVFP4 ? (D == 64 ? g >> 1 : hh * 8 + g) : (D == 64 ? g >> 2 : hh * 4 + (g >> 1));
+            y[half][r] = smem_load<uint32_t>(vmul + (((half * 2 + r) * 4 + t) * NB + block) * 4);
+          }
+        uint32_t c[2][4][VWORDS];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int r = half * 16 + (k >> 1) * 8 + ((k & 1) ? 7 - t : t);
+            if constexpr (D == 64) {
+              c[half][k][0] = smem_load<uint32_t>(here + S::CODES + r * 32 + g * 4);
+            } else {
+              const uint2 v = smem_load<uint2>(here + S::CODES + r * (D / 2) + (((hh * 4 + (g >> 1)) ^ turn<D>((k & 1) ? 7 - t : t)) * 16) + (g & 1) * 8);
+              c[half][k][0] = v.x;
+              c[half][k][1] = v.y;
+            }
+          }
+#pragma unroll
+        for (int x = 0; x < VWORDS; ++x) {
+          uint32_t d[2][4][4];                                 // [half][even / odd dimensions of the two pairs][tile]
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const uint32_t p0 = c[half][2 * r][x], p1 = c[half][2 * r + 1][x];
+              e2m1_f16((p0 & 0x0F0F0F0Fu) | ((p1 << 4) & 0xF0F0F0F0u), d[half][2 * r]);
+              e2m1_f16(((p0 >> 4) & 0x0F0F0F0Fu) | (p1 & 0xF0F0F0F0u), d[half][2 * r + 1]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) { d[half][2 * r][i] = hmul2(d[half][2 * r][i], y[half][r]); d[half][2 * r + 1][i] = hmul2(d[half][2 * r + 1][i], y[half][r]); }
+            }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+              mma(z, d[0][0][i], d[0][1][i], d[0][2][i], d[0][3][i], pf[0][n][0], pf[0][n][1]);
+              mma(z, d[1][0][i], d[1][1][i], d[1][2][i], d[1][3][i], pf[1][n][0], pf[1][n][1]);
+              float (&o)[4] = a.o[hh * 8 + x * 4 + i][n];
+              o[0] = fmaf(o[0], keep[n][0], z[0]);
+              o[1] = fmaf(o[1], keep[n][1], z[1]);
+              o[2] = fmaf(o[2], keep[n][0], z[2]);
+              o[3] = fmaf(o[3], keep[n][1], z[3]);
+            }
+        }
+      }
+      __syncwarp();
+    }
+
+    // One result of the piece: sums of a column's keys over the lanes, then warps 2 and 3 to 0 and 1, then 1 to 0.
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) a.l[n][c] += __shfl_xor_sync(0xFFFFFFFFu, a.l[n][c], d);
+        if constexpr (FMT == QF_FMT_MXFP4) {
+          const float f = mv[n][c] == -INFINITY ? 0.0f : exp2_approx(mv[n][c] - a.m[n][c]);
+#pragma unroll
+          for (int i = 0; i < MT; ++i) { a.o[i][n][c] *= f; a.o[i][n][c + 2] *= f; }
+        }
+      }
+#pragma unroll
+    for (int d = kAttnWarps / 2; d > 0; d /= 2) {
+      if (warp >= d && warp < 2 * d) {
+        const uint32_t at = parts + (warp - d) * S::PART + lane * 16;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            smem_store(at + (i * NT + n) * 512, __float_as_uint(a.o[i][n][0]), __float_as_uint(a.o[i][n][1]), __float_as_uint(a.o[i][n][2]), __float_as_uint(a.o[i][n][3]));
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          smem_store(at + (MT * NT + n) * 512, __float_as_uint(a.m[n][0]), __float_as_uint(a.l[n][0]), __float_as_uint(a.m[n][1]), __float_as_uint(a.l[n][1]));
+      }
+      __syncthreads();
+      if (warp < d) {
+        const uint32_t at = parts + warp * S::PART + lane * 16;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const uint4 v = smem_load<uint4>(at + (MT * NT + n) * 512);
+          float fa[2], fb[2];
+          join_weights(a.m[n][0], __uint_as_float(v.x), a.m[n][0], fa[0], fb[0]);
+          join_weights(a.m[n][1], __uint_as_float(v.z), a.m[n][1], fa[1], fb[1]);
+          a.l[n][0] = a.l[n][0] * fa[0] + __uint_as_float(v.y) * fb[0];
+          a.l[n][1] = a.l[n][1] * fa[1] + __uint_as_float(v.w) * fb[1];
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            const uint4 o = smem_load<uint4>(at + (i * NT + n) * 512);
+            a.o[i][n][0] = a.o[i][n][0] * fa[0] + __uint_as_float(o.x) * fb[0];
+            a.o[i][n][1] = a.o[i][n][1] * fa[1] + __uint_as_float(o.y) * fb[1];
+            a.o[i][n][2] = a.o[i][n][2] * fa[0] + __uint_as_float(o.z) * fb[0];
+            a.o[i][n][3] = a.o[i][n][3] * fa[1] + __uint_as_float(o.w) * fb[1];
+          }
+        }
+      }
+      __syncthreads();
+    }
+    if (warp == 0) {
+      if (w.n == w.units) {                                    // the whole sequence: the result itself
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const int row = row0 + 8 * n + 2 * t + c;
+            if (row < p.rows) {
+              const int token = row / p.group, head = h * p.group + (row - token * p.group);
+              const int64_t at = (static_cast<int64_t>(w.b) * p.q_len + token) * p.q_heads + head;
+              const float f = a.l[n][c] > 0.0f ? vt / a.l[n][c] : 0.0f;
+              uint32_t* out = reinterpret_cast<uint32_t*>(p.out + at * D);
+#pragma unroll
+              for (int i = 0; i < MT; i += 4)
+                *reinterpret_cast<uint4*>(out + dim_of<D>(i, g) / 2) =
+                    make_uint4(pack_bf16x2(a.o[i][n][c] * f, a.o[i][n][c + 2] * f), pack_bf16x2(a.o[i + 1][n][c] * f, a.o[i + 1][n][c + 2] * f),
+                               pack_bf16x2(a.o[i + 2][n][c] * f, a.o[i + 2][n][c + 2] * f), pack_bf16x2(a.o[i + 3][n][c] * f, a.o[i + 3][n][c + 2] * f));
+              if (p.lse && g == 0) p.lse[at] = log_sum(a.m[n][c], a.l[n][c]);
+            }
+          }
+      } else {
+        const bool begins = w.j == 0;
+        float4* to_part = part_at + static_cast<int64_t>(cta * 2 + (begins ? 1 : 0)) * PART4 + lane;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) to_part[(i * NT + n) * 32] = make_float4(a.o[i][n][0], a.o[i][n][1], a.o[i][n][2], a.o[i][n][3]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) to_part[(MT * NT + n) * 32] = make_float4(a.m[n][0], a.l[n][0], a.m[n][1], a.l[n][1]);
+        if (begins && lane == 0) {
+          const int64_t last = u1 + (w.units - w.n) - 1;       // the sequence's last unit
+          tasks[cta] = JoinTask{static_cast<int>(((last + 1) * ctas - 1) / total) - cta, w.b, w.s, 0};
+        }
+      }
+    }
   }
 }
 
-template <int FMT, int D>
-__global__ void __launch_bounds__(128) kv_attention_kernel(const KvAttn p) {
-  constexpr int E = D / 32;
-  const int head = blockIdx.x % p.q_heads;
-  const int64_t token = blockIdx.x / p.q_heads;
-  const int64_t b = token / p.q_len;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t len = min(static_cast<int64_t>(max(p.lens[b], 0)), static_cast<int64_t>(p.max_pages) * p.page_size);
-  const int64_t keys = len - p.q_len + (token - b * p.q_len) + 1;
-  const int h = head / (p.q_heads / p.kv_heads);
-  float q[E], o[E] = {}, m = -INFINITY, l = 0.0f;
-#pragma unroll
-  for (int i = 0; i < E; ++i) q[i] = __bfloat162float(p.q[token * p.q_stride + head * D + lane * E + i]);
-  const float sk = p.scale * (FMT == QF_FMT_NVFP4 ? *p.k_tscale : 1.0f);
-  for (int64_t j = warp; j < keys; j += 4) {
-    const int64_t page = min(max(static_cast<int64_t>(p.table[b * p.max_pages + j / p.page_size]), static_cast<int64_t>(0)), p.pages - 1);
-    const int64_t row = (page * p.kv_heads + h) * p.page_size + j % p.page_size;
-    float x[E], s = 0.0f;
-    row_values<FMT, D>(p.k_codes, p.k_scales, row, lane, x);
-#pragma unroll
-    for (int i = 0; i < E; ++i) s = fmaf(q[i], x[i], s);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
-    s *= sk;
-    const float top = fmaxf(m, s), keep = expf(m - top), e = expf(s - top);
-    row_values<FMT, D>(p.v_codes, p.v_scales, row, lane, x);
-#pragma unroll
-    for (int i = 0; i < E; ++i) o[i] = fmaf(o[i], keep, e * x[i]);
-    l = fmaf(l, keep, e);
-    m = top;
+// Joins the parts of sequences that several CTAs shared: a CTA per (CTA that began one, value tile), eight warps that take every eighth
+// part each.
+template <int FMT, int D, int NT>
+__global__ void __launch_bounds__(256) kv_join_kernel(const __grid_constant__ KvAttn p, int ctas) {
+  using S = Shape<FMT, D, NT>;
+  constexpr int PART4 = S::PART / 16;
+  launch_after_previous();
+  const JoinTask task = reinterpret_cast<const JoinTask*>(p.ws)[blockIdx.x];
+  if (task.more == 0) return;
+  const float4* parts = reinterpret_cast<const float4*>(p.ws + ((ctas * sizeof(JoinTask) + 255) & ~static_cast<size_t>(255)));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int i = blockIdx.y / NT, n = blockIdx.y % NT;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int k = warp; k <= task.more; k += 8) {
+    const float4* part = parts + (static_cast<int64_t>(blockIdx.x + k) * 2 + (k == 0 ? 1 : 0)) * PART4 + lane;
+    const float4 v = part[(i * NT + n) * 32], ml = part[(S::MT * NT + n) * 32];
+    float fa[2], fb[2];
+    join_weights(m[0], ml.x, m[0], fa[0], fb[0]);
+    join_weights(m[1], ml.z, m[1], fa[1], fb[1]);
+    l[0] = l[0] * fa[0] + ml.y * fb[0];
+    l[1] = l[1] * fa[1] + ml.w * fb[1];
+    o.x = o.x * fa[0] + v.x * fb[0];
+    o.y = o.y * fa[1] + v.y * fb[1];
+    o.z = o.z * fa[0] + v.z * fb[0];
+    o.w = o.w * fa[1] + v.w * fb[1];
   }
-  __shared__ float so[4][D], sm[4], sl[4];
-#pragma unroll
-  for (int i = 0; i < E; ++i) so[warp][lane * E + i] = o[i];
-  if (lane == 0) { sm[warp] = m; sl[warp] = l; }
+  __shared__ float4 so[8][32], sm[8][32];
+  so[warp][lane] = o;
+  sm[warp][lane] = make_float4(m[0], l[0], m[1], l[1]);
   __syncthreads();
-  float top = -INFINITY, total = 0.0f, w[4];
+  if (warp) return;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) top = fmaxf(top, sm[i]);
+  for (int k = 1; k < 8; ++k) {
+    const float4 v = so[k][lane], ml = sm[k][lane];
+    float fa[2], fb[2];
+    join_weights(m[0], ml.x, m[0], fa[0], fb[0]);
+    join_weights(m[1], ml.z, m[1], fa[1], fb[1]);
+    l[0] = l[0] * fa[0] + ml.y * fb[0];
+    l[1] = l[1] * fa[1] + ml.w * fb[1];
+    o.x = o.x * fa[0] + v.x * fb[0];
+    o.y = o.y * fa[1] + v.y * fb[1];
+    o.z = o.z * fa[0] + v.z * fb[0];
+    o.w = o.w * fa[1] + v.w * fb[1];
+  }
+  const float vt = FMT == QF_FMT_NVFP4 ? *p.v_tscale : 0x1p-13f;
+  const int h = task.seg / p.tiles, row0 = (task.seg - h * p.tiles) * (8 * NT) + 8 * n + 2 * t;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { w[i] = top == -INFINITY ? 0.0f : expf(sm[i] - top); total = fmaf(w[i], sl[i], total); }
-  const float by = total > 0.0f ? (FMT == QF_FMT_NVFP4 ? *p.v_tscale : 1.0f) / total : 0.0f;
-  for (int d = threadIdx.x; d < D; d += 128)
-    p.out[(token * p.q_heads + head) * D + d] = __float2bfloat16_rn((w[0] * so[0][d] + w[1] * so[1][d] + w[2] * so[2][d] + w[3] * so[3][d]) * by);
-  if (p.lse && threadIdx.x == 0) p.lse[token * p.q_heads + head] = total > 0.0f ? top + logf(total) : -INFINITY;
+  for (int c = 0; c < 2; ++c) {
+    const int row = row0 + c;
+    if (row >= p.rows) continue;
+    const int token = row / p.group, head = h * p.group + (row - token * p.group);
+    const int64_t at = (static_cast<int64_t>(task.b) * p.q_len + token) * p.q_heads + head;
+    const float f = l[c] > 0.0f ? vt / l[c] : 0.0f;
+    *reinterpret_cast<uint32_t*>(p.out + at * D + dim_of<D>(i, g)) = pack_bf16x2((c ? o.y : o.x) * f, (c ? o.w : o.z) * f);
+    if (p.lse && i == 0 && g == 0) p.lse[at] = log_sum(m[c], l[c]);
+  }
+}
+
+template <typename... Params, typename... Args>
+cudaError_t launch_overlapping(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int FMT, int D, int NT>
+cudaError_t attend(const KvAttn& p, cudaStream_t st) {
+  using S = Shape<FMT, D, NT>;
+  static bool ready[64] = {};                                  // the attribute stays set for the process
+  int dev = 0;
+  if (cudaError_t e = cudaGetDevice(&dev)) return e;
+  if (dev >= 64 || !ready[dev]) {
+    if (cudaError_t e = cudaFuncSetAttribute(kv_attention_kernel<FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM)) return e;
+    if (dev < 64) ready[dev] = true;
+  }
+  // no more CTAs than there can be work for: four units each
+  const int64_t most = static_cast<int64_t>(p.batch) * p.segs * ((p.max_keys + kUnitKeys - 1) / kUnitKeys + (p.max_keys == 0));
+  const int grid = static_cast<int>(most / kAttnWarps + 1 < kNumSMs * S::CTAS ? most / kAttnWarps + 1 : kNumSMs * S::CTAS);
+  if (cudaError_t e = launch_overlapping(kv_attention_kernel<FMT, D, NT>, dim3(grid), kAttnWarps * 32, S::SMEM, st, p)) return e;
+  if (p.max_keys <= kUnitKeys) return cudaSuccess;             // nothing can have been cut
+  return launch_overlapping(kv_join_kernel<FMT, D, NT>, dim3(grid, S::MT * NT), 256, 0, st, p, grid);
 }
 
 template <int FMT>
-cudaError_t attend(const KvAttn& p, int head_dim, int64_t ctas, cudaStream_t st) {
-  const unsigned grid = static_cast<unsigned>(ctas);
-  if (head_dim == 64) kv_attention_kernel<FMT, 64><<<grid, 128, 0, st>>>(p);
-  else if (head_dim == 128) kv_attention_kernel<FMT, 128><<<grid, 128, 0, st>>>(p);
-  else kv_attention_kernel<FMT, 256><<<grid, 128, 0, st>>>(p);
-  return cudaGetLastError();
+cudaError_t attend_format(KvAttn& p, int head_dim, cudaStream_t st) {
+  const bool two = p.rows > 8;
+  p.tiles = (p.rows + (two ? 15 : 7)) / (two ? 16 : 8);
+  p.segs = p.tiles * p.kv_heads;
+  if (head_dim == 64) return two ? attend<FMT, 64, 2>(p, st) : attend<FMT, 64, 1>(p, st);
+  if (head_dim == 128) return two ? attend<FMT, 128, 2>(p, st) : attend<FMT, 128, 1>(p, st);
+  return two ? attend<FMT, 256, 2>(p, st) : attend<FMT, 256, 1>(p, st);
+}
+
+template <int FMT, int D, int NT>
+size_t part_bytes() {
+  using S = Shape<FMT, D, NT>;
+  return static_cast<size_t>(kNumSMs) * S::CTAS * (sizeof(JoinTask) + 2 * S::PART) + 256;
+}
+template <int D>
+size_t ws_bytes() {          // the largest, whatever the format and the tile: how the rows are split over sequences is not known here
+  const size_t a = part_bytes<QF_FMT_NVFP4, D, 1>(), b = part_bytes<QF_FMT_NVFP4, D, 2>(), c = part_bytes<QF_FMT_MXFP4, D, 1>(), d = part_bytes<QF_FMT_MXFP4, D, 2>();
+  const size_t x = a > b ? a : b, y = c > d ? c : d;
+  return x > y ? x : y;
 }
 
 }  // namespace
@@ -242,7 +967,9 @@ cudaError_t launch_kv_read(const qf_kv_cache_t& c, const void* slots, bool slots
   return cudaGetLastError();
 }
 
-size_t kv_attention_ws_bytes(int64_t, int, int, int) { return 0; }
+size_t kv_attention_ws_bytes(int64_t, int, int head_dim, int) {
+  return head_dim <= 64 ? ws_bytes<64>() : head_dim <= 128 ? ws_bytes<128>() : ws_bytes<256>();
+}
 
 cudaError_t launch_kv_attention(const KvAttentionArgs& a, cudaStream_t st) {
   KvAttn p{};
@@ -258,15 +985,19 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a, cudaStream_t st) {
   p.lens = a.lens;
   p.out = static_cast<__nv_bfloat16*>(a.out);
   p.lse = a.lse;
-  p.pages = a.cache.pages;
+  p.ws = static_cast<uint8_t*>(a.workspace);
+  p.batch = static_cast<int>(a.batch);
+  p.pages = static_cast<int>(a.cache.pages);
   p.max_pages = static_cast<int>(a.max_pages);
   p.page_size = a.cache.page_size;
+  p.max_keys = static_cast<int>(a.max_pages * a.cache.page_size);
   p.q_len = a.q_len;
   p.q_heads = a.q_heads;
   p.kv_heads = a.cache.kv_heads;
-  p.scale = a.scale;
-  const int64_t ctas = a.batch * a.q_len * a.q_heads;
-  return a.cache.fmt == QF_FMT_NVFP4 ? attend<QF_FMT_NVFP4>(p, a.cache.head_dim, ctas, st) : attend<QF_FMT_MXFP4>(p, a.cache.head_dim, ctas, st);
+  p.group = a.q_heads / a.cache.kv_heads;
+  p.rows = a.q_len * p.group;
+  p.scale = a.scale * 1.4426950408889634f;
+  return a.cache.fmt == QF_FMT_NVFP4 ? attend_format<QF_FMT_NVFP4>(p, a.cache.head_dim, st) : attend_format<QF_FMT_MXFP4>(p, a.cache.head_dim, st);
 }
 
 }  // namespace qf
