@@ -146,6 +146,8 @@ KvRows kv_rows(const qf_kv_cache_t& c, const void* slots, bool slots64) {
 constexpr int kUnitKeys = 32;
 constexpr int kAttnWarps = 4;                 // of a CTA
 constexpr int kStages = 2;                    // units a warp has in shared memory or on the way
+constexpr int kPieceCost = 4;                 // what a sequence's queries, meeting and result cost, in units
+constexpr float kWeightTop = 6.0f, kWeightRoom = 8.0f;       // weights start at up to 2^6 and may reach 2^14 before their base is moved
 
 struct KvAttn {
   const __nv_bfloat16* q;
@@ -164,6 +166,8 @@ struct KvAttn {
   int batch, pages, max_pages, page_size, max_keys;
   int q_len, q_heads, kv_heads, group;
   int rows, tiles, segs;                      // query rows of a key head; tiles of them; (key head, tile) pairs of a sequence
+  bool by_segment;                            // JoinTasks are numbered by segment, not by CTA
+  int64_t page_codes;                         // bytes of codes in a page
   float scale;                                // times log2 e
 };
 
@@ -173,16 +177,17 @@ struct Shape {
   static constexpr int BLOCK = FMT == QF_FMT_NVFP4 ? 16 : 32, NB = D / BLOCK;              // blocks of a row
   static constexpr int HALVES = D == 256 ? 2 : 1;                                          // 128-element halves of a row
   static constexpr int CODES = kUnitKeys * D / 2, SCALES = kUnitKeys * NB, STAGE = 2 * (CODES + SCALES);
-  static constexpr int KMUL = kUnitKeys * NB * 4, VMUL = kUnitKeys * NB * 2;               // multipliers as FP16: twice a key's, pairs of values'
-  static constexpr int WARP = kStages * STAGE + KMUL + VMUL;
+  static constexpr int VMUL = FMT == QF_FMT_MXFP4 ? kUnitKeys * NB * 2 : 0;                // values' multipliers, where they need a pass of their own
+  static constexpr int WARP = kStages * STAGE + VMUL;
   static constexpr int MT = D / 16;                                                        // 16-row tiles of the value product
   static constexpr int PART = (MT * NT * 4 + 4 * NT) * 32 * 4;                             // a warp's sums and maxima, bytes
   static constexpr int SMEM = kAttnWarps * WARP + kAttnWarps / 2 * PART;
-  static constexpr int CTAS = 232448 / (SMEM + 1024) < 4 ? 232448 / (SMEM + 1024) : 4;     // of an SM
+  static constexpr int FIT = 232448 / (SMEM + 1024), WANT = D == 256 ? (NT == 2 ? 1 : 2) : D == 128 && NT == 2 ? 3 : 4;
+  static constexpr int CTAS = FIT < WANT ? FIT : WANT;                                     // of an SM
 };
 
-// Workspace: a descriptor per CTA, then two parts per CTA (the piece it continues, the piece it begins).
-struct JoinTask { int more, b, seg, pad; };   // CTAs that continue the piece that this one begins (0: nothing to join)
+// Workspace: a task per CTA (or per segment, where there are fewer), then two parts per CTA (the piece it continues, the piece it begins).
+struct JoinTask { int cta, more, b, seg; };   // parts are those of CTAs cta, cta + 1, ..., cta + more (more = 0: nothing to join)
 
 __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
@@ -204,9 +209,16 @@ __device__ __forceinline__ void e2m1_f16(uint32_t q, uint32_t (&w)[4]) {
       : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
       : "r"(q));
 }
-// Four E4M3 codes -> two FP16 pairs
-__device__ __forceinline__ void e4m3_f16(uint32_t s, uint32_t& lo, uint32_t& hi) {
-  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(s));
+// Two E4M3 codes (the low bytes) -> FP16 pair
+__device__ __forceinline__ uint32_t e4m3_pair(uint32_t two) {
+  uint32_t r;
+  asm("{\n.reg .b16 h;\ncvt.u16.u32 h, %1;\ncvt.rn.f16x2.e4m3x2 %0, h;\n}" : "=r"(r) : "r"(two));
+  return r;
+}
+// E8M0 code `i` of four -> its power of two; code 0 -> 0 (zeros, or elements below 2^-124)
+__device__ __forceinline__ float e8m0_of(uint32_t codes, int i) {
+  const uint32_t at = i == 3 ? codes >> 1 : codes << (23 - 8 * i);
+  return __uint_as_float(at & 0x7F800000u);
 }
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -229,6 +241,16 @@ __device__ __forceinline__ T smem_load(uint32_t at) {
   else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
   return v;
 }
+__device__ __forceinline__ uint32_t smem_load_u8(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t smem_load_u16(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
 __device__ __forceinline__ void smem_store(uint32_t at, uint32_t a) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(a) : "memory"); }
 __device__ __forceinline__ void smem_store(uint32_t at, uint32_t a, uint32_t b) {
   asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(a), "r"(b) : "memory");
@@ -238,94 +260,120 @@ __device__ __forceinline__ void smem_store(uint32_t at, uint32_t a, uint32_t b, 
 }
 
 __device__ __forceinline__ int keys_of(const KvAttn& p, int b) { return min(max(p.lens[b], 0), p.max_keys); }
-// a sequence without keys has one unit, so that somebody writes its zeros
-__device__ __forceinline__ int units_of(int keys) { return max(1, (keys + kUnitKeys - 1) / kUnitKeys); }
+__device__ __forceinline__ int units_of(int keys) { return (keys + kUnitKeys - 1) / kUnitKeys; }
+// what a segment of a sequence counts for in the shares: a sequence without keys nothing (its zeros are written beforehand)
+__device__ __forceinline__ int cost_of(int keys) { return keys == 0 ? 0 : units_of(keys) + kPieceCost; }
 
-// The pieces of a CTA's share, one (sequence, segment) after the other: units [j, j + n) of segment s of sequence b.
+// The pieces of a CTA's share, one (sequence, segment) after the other: units [j, j + n) of segment s of sequence b; n = 0 at the end.
+// In a segment's part of the shares kPieceCost places come first, then a place per unit.
 struct Walk {
-  int b, s, keys, units, j, n, left;          // left: units from this piece on
+  int b, s, keys, units, j, n, left, pos;     // left: places of the share behind this piece; pos: place in the segment where the share starts
+  __device__ __forceinline__ void settle(const KvAttn& p) {
+    for (n = 0; left > 0;) {
+      const int here = min(left, units + kPieceCost - pos);
+      j = max(pos - kPieceCost, 0);
+      n = max(pos + here - kPieceCost, 0) - j;
+      left -= here;
+      if (n > 0 || left <= 0) return;
+      segment(p);
+    }
+  }
+  __device__ __forceinline__ void segment(const KvAttn& p) {
+    pos = 0;
+    if (++s < p.segs) return;
+    s = 0;
+    do keys = keys_of(p, ++b);                // places are left, so there is a sequence with keys
+    while (keys == 0);
+    units = units_of(keys);
+  }
   __device__ __forceinline__ void next(const KvAttn& p) {
-    left -= n;
     n = 0;
     if (left <= 0) return;
-    j = 0;
-    if (++s == p.segs) {
-      s = 0;
-      keys = keys_of(p, ++b);
-      units = units_of(keys);
-    }
-    n = min(left, units);
+    segment(p);
+    settle(p);
   }
 };
 
-// 16-byte piece c of a row's codes lies in place c ^ turn(row): lanes that read together (four consecutive rows, or four from the
-// end of a group of eight) meet different banks.
+// 16-byte piece c of a row's codes lies in place c ^ turn(row), so that lanes that read together meet different banks: of keys a row's
+// pieces for two rows (NVFP4) or a piece of each of eight rows (MXFP4), of values half a row's for four rows from either end of eight.
 template <int D>
 __device__ __forceinline__ int turn(int row) {
-  return D == 64 ? 0 : ((row >> 1) & 1) * 2 + (D == 256 ? (row & 1) * 4 : 0);
+  return ((row >> 2) & 1) + (D >= 128 ? ((row >> 1) & 1) * 2 : 0) + (D == 256 ? (row & 1) * 4 : 0);
 }
 
-// A warp's copies into its ring: its quarter of every piece, unit by unit, ahead of the products.
+// A warp's copies into its ring: its quarter of every piece, unit by unit, ahead of the products. Keys come in groups of 16 that lie in
+// one page; the first group of a unit always holds a key, the second may not.
 template <int FMT, int D>
 struct Copier {
   using S = Shape<FMT, D, 1>;
+  static constexpr int ROW = D / 2, PIECES = ROW / 16, SROW = S::NB, CHUNKS = SROW, SHIFT = FMT == QF_FMT_NVFP4 ? 3 : 4;   // ROW = SROW << SHIFT
+  static constexpr bool ONCE = 4 * CHUNKS <= 32;               // one instruction copies the unit's scales
   Walk w;
   int cur, end, page, off;                    // unit, end of this warp's part of the piece, page and place of its first key
-  int id0, id1;                               // pages of its two groups of 16 keys
+  int id0, id1;                               // pages of its two groups
+  const int32_t* pages;                       // of the sequence
+  const uint8_t* kp;                          // this lane's first piece of a group, in page 0 from the head's first key on
+  const uint8_t* vp;
+  const uint8_t* sp;                          // and its scales, keys' or values'
+  uint32_t to, to_scales;                     // their places in a stage
 
-  __device__ __forceinline__ void pages_of(const KvAttn& p) {
-    const int32_t* row = p.table + static_cast<int64_t>(w.b) * p.max_pages;
-    const int next = off + 16 < p.page_size ? page : page + 1;
-    const int most = p.pages - 1;
-    id0 = page < p.max_pages ? min(max(row[page], 0), most) : 0;
-    id1 = next < p.max_pages ? min(max(row[next], 0), most) : 0;
+  __device__ __forceinline__ void ids(const KvAttn& p) {
+    const uint32_t most = static_cast<uint32_t>(p.pages - 1);
+    id1 = id0 = static_cast<int>(min(static_cast<uint32_t>(pages[page]), most));
+    if (off + 16 >= p.page_size && cur * kUnitKeys + 16 < w.keys) id1 = static_cast<int>(min(static_cast<uint32_t>(pages[page + 1]), most));
   }
-  __device__ __forceinline__ void piece(const KvAttn& p, int warp) {
-    while (w.n > 0) {
+  __device__ __forceinline__ void piece(const KvAttn& p, int warp, int lane) {
+    for (; w.n > 0; w.next(p)) {
       cur = w.j + static_cast<int>(static_cast<int64_t>(w.n) * warp / kAttnWarps);
       end = w.j + static_cast<int>(static_cast<int64_t>(w.n) * (warp + 1) / kAttnWarps);
       if (cur < end) break;
-      w.next(p);
     }
-    if (w.n > 0) {
-      page = cur * kUnitKeys / p.page_size;
-      off = cur * kUnitKeys - page * p.page_size;
-      pages_of(p);
+    if (w.n == 0) return;
+    page = cur * kUnitKeys / p.page_size;
+    off = cur * kUnitKeys - page * p.page_size;
+    pages = p.table + static_cast<int64_t>(w.b) * p.max_pages;
+    const int64_t row = static_cast<int64_t>(w.s / p.tiles) * p.page_size;
+    kp = p.k_codes + row * ROW + lane * 16;
+    vp = p.v_codes + row * ROW + lane * 16;
+    const int c = lane % (2 * CHUNKS);
+    sp = (c >= CHUNKS ? p.v_scales : p.k_scales) + row * SROW + c % CHUNKS * 16;
+    ids(p);
+  }
+  __device__ __forceinline__ void start(const KvAttn& p, int warp, int lane) {
+    const int r = lane / PIECES, c = lane % (2 * CHUNKS);
+    to = r * ROW + ((lane % PIECES) ^ turn<D>(r)) * 16;
+    to_scales = 2 * S::CODES + (c >= CHUNKS ? S::SCALES : 0) + c % CHUNKS * 16 + (ONCE ? lane / (2 * CHUNKS) * 16 * SROW : 0);
+    piece(p, warp, lane);
+  }
+  __device__ __forceinline__ void codes(uint32_t stage, int64_t at) const {
+#pragma unroll
+    for (int i = 0; i < PIECES / 2; ++i) {
+      const uint32_t here = D == 256 && (i & 1) ? to ^ 16 : to;          // rows 4 i and on: the lowest bit of their turn
+      copy16(stage + here + i * 512, kp + at + i * 512);
+      copy16(stage + here + S::CODES + i * 512, vp + at + i * 512);
     }
   }
   __device__ __forceinline__ void issue(const KvAttn& p, uint32_t stage, int warp, int lane) {
     if (w.n > 0) {
-      const int h = w.s / p.tiles;
-      constexpr int ROW = D / 2, PIECES = ROW / 16, SROW = S::NB, CHUNKS = 16 * SROW / 16;     // of a row; of 16 rows' scales
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const bool here = cur * kUnitKeys + half * 16 < w.keys;
-        if (here) {
-          const int o = half == 0 ? off : off + 16 < p.page_size ? off + 16 : 0;
-          const int64_t row = (static_cast<int64_t>(half ? id1 : id0) * p.kv_heads + h) * p.page_size + o;
-          const uint8_t* kc = p.k_codes + row * ROW;
-          const uint8_t* vc = p.v_codes + row * ROW;
-#pragma unroll
-          for (int i = 0; i < PIECES / 2; ++i) {
-            const int c = i * 32 + lane, r = c / PIECES, piece = c % PIECES;
-            const uint32_t to = stage + (half * 16 + r) * ROW + ((piece ^ turn<D>(r)) * 16);
-            copy16(to, kc + c * 16);
-            copy16(to + S::CODES, vc + c * 16);
-          }
-          if (lane < 2 * CHUNKS) {
-            const bool value = lane >= CHUNKS;
-            const int c = value ? lane - CHUNKS : lane;
-            copy16(stage + 2 * S::CODES + (value ? S::SCALES : 0) + half * 16 * SROW + c * 16, (value ? p.v_scales : p.k_scales) + row * SROW + c * 16);
-          }
-        }
+      const bool two = cur * kUnitKeys + 16 < w.keys;
+      const int64_t a0 = id0 * p.page_codes + off * ROW;
+      const int64_t a1 = id1 * p.page_codes + (off + 16 < p.page_size ? off + 16 : 0) * ROW;
+      codes(stage, a0);
+      if (two) codes(stage + 16 * ROW, a1);
+      if constexpr (ONCE) {
+        const bool second = lane >= 2 * CHUNKS;
+        if (lane < (two ? 4 : 2) * CHUNKS) copy16(stage + to_scales, sp + ((second ? a1 : a0) >> SHIFT));
+      } else {
+        copy16(stage + to_scales, sp + (a0 >> SHIFT));
+        if (two) copy16(stage + to_scales + 16 * SROW, sp + (a1 >> SHIFT));
       }
       if (++cur < end) {
         off += kUnitKeys;
         while (off >= p.page_size) { off -= p.page_size; ++page; }
-        pages_of(p);
+        ids(p);
       } else {
         w.next(p);
-        piece(p, warp);
+        piece(p, warp, lane);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -346,10 +394,11 @@ __device__ __forceinline__ int dim_of(int i, int g) {
   return D == 64 ? g * 8 + 2 * i : (i >> 3) * 128 + g * 16 + 2 * (i & 7);
 }
 
+constexpr float kNoWeights = -1e30f;           // base of a column without weights: far below any score, and finite
 __device__ __forceinline__ void join_weights(float ma, float mb, float& m, float& fa, float& fb) {
   m = fmaxf(ma, mb);
-  fa = m == -INFINITY ? 0.0f : exp2_approx(ma - m);
-  fb = m == -INFINITY ? 0.0f : exp2_approx(mb - m);
+  fa = exp2_approx(ma - m);
+  fb = exp2_approx(mb - m);
 }
 
 __device__ __forceinline__ float log_sum(float m, float l) { return l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY; }
@@ -358,22 +407,37 @@ template <int FMT, int D, int NT>
 __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv_attention_kernel(const __grid_constant__ KvAttn p) {
   using S = Shape<FMT, D, NT>;
   constexpr int MT = S::MT, NB = S::NB, HALVES = S::HALVES;
-  constexpr int WORDS = D == 64 ? 2 : 4;                       // words of codes of a key that a lane holds per half
-  constexpr int VWORDS = D == 64 ? 1 : 2;                      // and of a value
+  constexpr bool MX = FMT == QF_FMT_MXFP4;
+  constexpr int NW = D / 32;                                   // words of codes of a key that a lane holds
+  constexpr int VWORDS = D == 64 ? 1 : 2;                      // and of a value, per half
   extern __shared__ __align__(16) uint8_t smem[];
   launch_after_previous();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + warp * S::WARP;
-  const uint32_t kmul = ring + kStages * S::STAGE, vmul = kmul + S::KMUL;
+  const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + warp * S::WARP, vmul = ring + kStages * S::STAGE;
   const uint32_t parts = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + kAttnWarps * S::WARP;
+  JoinTask* tasks = reinterpret_cast<JoinTask*>(p.ws);
+  const int cta = blockIdx.x;
+  if (!p.by_segment && threadIdx.x == 0) tasks[cta].more = 0;
 
-  // This CTA's share. All units are counted by all CTAs, each thread a run of the sequences.
-  __shared__ int64_t warp_units[kAttnWarps];
-  __shared__ int first_b, first_unit_s, first_unit_j;
+  // Sequences without keys: zeros, here and there.
+  for (int b = cta; b < p.batch; b += gridDim.x) {
+    if (keys_of(p, b) > 0) continue;
+    const int64_t first = static_cast<int64_t>(b) * p.q_len * p.q_heads, rows = static_cast<int64_t>(p.q_len) * p.q_heads;
+    uint4* out = reinterpret_cast<uint4*>(p.out + first * D);
+    for (int64_t i = threadIdx.x; i < rows * (D / 8); i += kAttnWarps * 32) out[i] = make_uint4(0, 0, 0, 0);
+    if (p.lse)
+      for (int64_t i = threadIdx.x; i < rows; i += kAttnWarps * 32) p.lse[first + i] = -INFINITY;
+    if (p.by_segment)
+      for (int i = threadIdx.x; i < p.segs; i += kAttnWarps * 32) tasks[b * p.segs + i].more = 0;
+  }
+
+  // This CTA's share. All places are counted by all CTAs, each thread a run of the sequences.
+  __shared__ int64_t warp_places[kAttnWarps];
+  __shared__ int first_b, first_s, first_pos;
   const int per = (p.batch + kAttnWarps * 32 - 1) / (kAttnWarps * 32);
   const int b0 = min(static_cast<int>(threadIdx.x) * per, p.batch), b1 = min(b0 + per, p.batch);
   int64_t mine = 0;
-  for (int b = b0; b < b1; ++b) mine += units_of(keys_of(p, b));
+  for (int b = b0; b < b1; ++b) mine += cost_of(keys_of(p, b));
   mine *= p.segs;
   int64_t before = mine;
 #pragma unroll
@@ -381,61 +445,56 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
     const int64_t o = __shfl_up_sync(0xFFFFFFFFu, before, d);
     if (lane >= d) before += o;
   }
-  if (lane == 31) warp_units[warp] = before;
+  if (lane == 31) warp_places[warp] = before;
   __syncthreads();
   int64_t total = 0;
 #pragma unroll
   for (int i = 0; i < kAttnWarps; ++i) {
-    if (i < warp) before += warp_units[i];
-    total += warp_units[i];
+    if (i < warp) before += warp_places[i];
+    total += warp_places[i];
   }
   before -= mine;
   const int ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), (total + kAttnWarps - 1) / kAttnWarps));
-  const int cta = blockIdx.x;
-  JoinTask* tasks = reinterpret_cast<JoinTask*>(p.ws);
   float4* part_at = reinterpret_cast<float4*>(p.ws + ((gridDim.x * sizeof(JoinTask) + 255) & ~static_cast<size_t>(255)));
   constexpr int PART4 = S::PART / 16;                          // float4s of a part
-  if (cta >= ctas) {
-    if (threadIdx.x == 0) tasks[cta].more = 0;
-    return;
-  }
+  if (cta >= ctas) return;
   const int64_t u0 = cta * total / ctas, u1 = (cta + 1) * total / ctas;
   if (before <= u0 && u0 < before + mine) {
     int64_t r = u0 - before;
     int b = b0;
     for (;; ++b) {
-      const int64_t all = static_cast<int64_t>(units_of(keys_of(p, b))) * p.segs;
+      const int64_t all = static_cast<int64_t>(cost_of(keys_of(p, b))) * p.segs;
       if (r < all) break;
       r -= all;
     }
-    const int units = units_of(keys_of(p, b));
+    const int cost = cost_of(keys_of(p, b));
     first_b = b;
-    first_unit_s = static_cast<int>(r / units);
-    first_unit_j = static_cast<int>(r % units);
+    first_s = static_cast<int>(r / cost);
+    first_pos = static_cast<int>(r % cost);
   }
   __syncthreads();
   Walk w;
   w.b = first_b;
-  w.s = first_unit_s;
-  w.j = first_unit_j;
+  w.s = first_s;
+  w.pos = first_pos;
   w.keys = keys_of(p, w.b);
   w.units = units_of(w.keys);
   w.left = static_cast<int>(u1 - u0);
-  w.n = min(w.left, w.units - w.j);
-  if (threadIdx.x == 0) tasks[cta].more = 0;
+  w.settle(p);
 
   Copier<FMT, D> copy;
   copy.w = w;
-  copy.piece(p, warp);
+  copy.start(p, warp, lane);
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) copy.issue(p, ring + i * S::STAGE, warp, lane);
   int stage = 0;
 
-  // row g of a 16-key tile is key own0 of its first eight, row g + 8 the same of the second; the keys of a lane's columns of the value product
-  // then are t and 7 - t of both eights
+  // Row g of a 16-key tile is key own0 of its first eight, row g + 8 the same of the second; the keys of a lane's columns of the value product
+  // then are t and 7 - t of both eights.
   const int own0 = (g & 1) ? 7 - (g >> 1) : g >> 1;
-  const float vt = FMT == QF_FMT_NVFP4 ? *p.v_tscale : 0x1p-13f;
-  const float kt = p.scale * (FMT == QF_FMT_NVFP4 ? *p.k_tscale : 0x1p-12f);
+  const float vt = MX ? 1.0f : *p.v_tscale;
+  const float kt = p.scale * (MX ? 1.0f : *p.k_tscale);
+  const float sign = kt < 0.0f ? -1.0f : 1.0f;                 // of the scale: goes to the queries, so that a column's factor is positive
 
   for (; w.n > 0; w.next(p)) {
     const int h = w.s / p.tiles, row0 = (w.s - h * p.tiles) * (8 * NT);
@@ -449,41 +508,44 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       const bool any = row < p.rows;
       const int token = any ? row / p.group : 0, head = h * p.group + (any ? row - token * p.group : 0);
       const __nv_bfloat16* src = p.q + (static_cast<int64_t>(w.b) * p.q_len + token) * p.q_stride + static_cast<int64_t>(head) * D;
-      uint4 raw[D / 32];
+      uint4 raw[NW];
       uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        const int at = D == 64 ? t * 16 + 8 * i : (i >> 2) * 128 + t * 32 + 8 * (i & 3);
+      for (int i = 0; i < NW; ++i) {
+        const int at = MX ? i * 32 + t * 8 : D == 64 ? t * 16 + 8 * i : (i >> 2) * 128 + t * 32 + 8 * (i & 3);
         raw[i] = any ? *reinterpret_cast<const uint4*>(src + at) : make_uint4(0, 0, 0, 0);
         top = max(top, chunk_amax_bits(raw[i]));
       }
       top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
       top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
       const int e = max(static_cast<int>(top >> 7), 14);       // exponent of the row's largest element
-      const float up = __uint_as_float(static_cast<uint32_t>(268 - e) << 23), down = __uint_as_float(static_cast<uint32_t>(e - 14) << 23);
+      const float up = sign * __uint_as_float(static_cast<uint32_t>(268 - e) << 23);
+      const float down = e == 14 ? 0x1p-127f : __uint_as_float(static_cast<uint32_t>(e - 14) << 23);
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
+      for (int i = 0; i < NW; ++i) {
         const uint32_t v[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) qf[n][2 * i + (k >> 1)][k & 1] = f16x2(bf16_lo(v[k]) * up, bf16_hi(v[k]) * up);
       }
-      const float f = e == 14 ? 0x1p-127f : down;
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        by[n][c] = __shfl_sync(0xFFFFFFFFu, f, (2 * t + c) * 4) * kt;
-        const int col = row0 + 8 * n + 2 * t + c;
-        const int tok = min(col, p.rows - 1) / p.group;
+        // not zero, so that a score of -infinity stays one
+        by[n][c] = fmaxf(__shfl_sync(0xFFFFFFFFu, down, (2 * t + c) * 4) * fabsf(kt), 0x1p-126f);
+        const int tok = min(row0 + 8 * n + 2 * t + c, p.rows - 1) / p.group;
         seen[n][c] = min(max(w.keys - p.q_len + tok + 1, 0), w.keys);
       }
-      least = min(least, min(max(w.keys - p.q_len + min(row0 + 8 * n, p.rows - 1) / p.group + 1, 0), w.keys));
+      if (n == 0) least = min(max(w.keys - p.q_len + row0 / p.group + 1, 0), w.keys);
     }
 
+    // m: base of a column's weights, which are 2^(score - m); l: the lane's share of their sum; ve (MXFP4): o is in units of 2^ve; vref: the
+    // scale code that the values' multipliers refer to (none yet: far below all)
     Sums<MT, NT> a;
-    float mv[NT][2];                                           // MXFP4: maximum of the value product's weights
+    float ve[NT][2];
+    int vref = -100;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c) { a.m[n][c] = mv[n][c] = -INFINITY; a.l[n][c] = 0.0f; }
+      for (int c = 0; c < 2; ++c) { a.m[n][c] = kNoWeights; a.l[n][c] = 0.0f; ve[n][c] = -1000.0f; }
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -496,79 +558,12 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       copy.issue(p, ring + (stage == 0 ? kStages - 1 : stage - 1) * S::STAGE, warp, lane);
       asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
       __syncwarp();
-      const uint32_t here = ring + stage * S::STAGE;
+      const uint32_t here = ring + stage * S::STAGE, kscales = here + 2 * S::CODES, vscales = kscales + S::SCALES;
       stage = stage + 1 == kStages ? 0 : stage + 1;
       const int key0 = u * kUnitKeys;
 
-      // Multipliers of this unit, a key per lane: FP16 scales of its blocks, for keys twice in a word, for values in pairs of keys (a key
-      // and the last, second last, ... of its group of eight); values behind the last key get zeros. MXFP4: relative to the row's largest.
-      float k_by = 1.0f, v_up = 0.0f;
-      {
-        constexpr int NR = NB / 2;                             // FP16 pairs of a row
-        uint32_t kr[NR], vr[NR];
-        const uint32_t ks = here + 2 * S::CODES + lane * NB, vs = ks + S::SCALES;
-        if constexpr (FMT == QF_FMT_NVFP4) {
-#pragma unroll
-          for (int i = 0; i < NB / 4; ++i) {
-            e4m3_f16(smem_load<uint32_t>(ks + 4 * i) & 0x7F7F7F7Fu, kr[2 * i], kr[2 * i + 1]);
-            e4m3_f16(smem_load<uint32_t>(vs + 4 * i) & 0x7F7F7F7Fu, vr[2 * i], vr[2 * i + 1]);
-          }
-        } else {
-#pragma unroll
-          for (int kind = 0; kind < 2; ++kind) {
-            uint32_t word[(NB + 3) / 4];
-#pragma unroll
-            for (int i = 0; i < (NB + 3) / 4; ++i) {
-              if constexpr (NB == 2) {
-                uint16_t two;
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(two) : "r"(kind ? vs : ks) : "memory");
-                word[i] = two;
-              } else {
-                word[i] = smem_load<uint32_t>((kind ? vs : ks) + 4 * i);
-              }
-            }
-            int s[NB], top = 0;
-#pragma unroll
-            for (int i = 0; i < NB; ++i) { s[i] = (word[i / 4] >> (8 * (i & 3))) & 0xFF; top = max(top, s[i]); }
-            const int base = 127 + (kind ? 13 : 12) - top;
-#pragma unroll
-            for (int i = 0; i < NR; ++i)
-              (kind ? vr : kr)[i] = f16x2(__uint_as_float(static_cast<uint32_t>(max(s[2 * i] + base, 0)) << 23),
-                                          __uint_as_float(static_cast<uint32_t>(max(s[2 * i + 1] + base, 0)) << 23));
-            if (kind) v_up = static_cast<float>(top - 127);
-            else k_by = e8m0_scale(top);
-          }
-        }
-        if (key0 + lane >= w.keys) {
-#pragma unroll
-          for (int i = 0; i < NR; ++i) vr[i] = 0u;
-        }
-        const uint32_t kto = kmul + lane * NB * 4;
-        if constexpr (NR >= 2) {
-#pragma unroll
-          for (int i = 0; i < NR; i += 2)
-            smem_store(kto + 8 * i, __byte_perm(kr[i], 0, 0x1010), __byte_perm(kr[i], 0, 0x3232), __byte_perm(kr[i + 1], 0, 0x1010), __byte_perm(kr[i + 1], 0, 0x3232));
-        } else {
-          smem_store(kto, __byte_perm(kr[0], 0, 0x1010), __byte_perm(kr[0], 0, 0x3232));
-        }
-        const bool low = (lane & 4) == 0;
-        const int pair = (lane >> 3) * 4 + (low ? lane & 3 : 3 - (lane & 3));
-        const uint32_t vto = vmul + pair * NB * 4;
-        if constexpr (NR >= 2) {
-#pragma unroll
-          for (int i = 0; i < NR / 2; ++i) {                   // the first of a pair writes the first half of the blocks, the other one the second
-            const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, low ? vr[NR / 2 + i] : vr[i], 7);
-            const uint32_t x = low ? vr[i] : got, y = low ? got : vr[NR / 2 + i];
-            smem_store(vto + (low ? 0 : NB * 2) + 8 * i, __byte_perm(x, y, 0x5410), __byte_perm(x, y, 0x7632));
-          }
-        } else {
-          const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, vr[0], 7);
-          smem_store(vto + (low ? 0 : 4), low ? __byte_perm(vr[0], got, 0x5410) : __byte_perm(got, vr[0], 0x7632));
-        }
-      }
-      __syncwarp();
-
-      // scores
+      // Scores. NVFP4: a lane's words are one or two whole blocks, whose scale goes to the key's elements. MXFP4: word x of the four lanes of a
+      // row is block x, whose power of two goes to the block's sum.
       float s[2][NT][4];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
@@ -577,59 +572,73 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
 #pragma unroll
           for (int c = 0; c < 4; ++c) s[half][n][c] = 0.0f;
         const int r0 = half * 16 + own0, r1 = r0 + 8;
+        if constexpr (MX) {
+          uint32_t f0[(NB + 3) / 4], f1[(NB + 3) / 4];
 #pragma unroll
-        for (int hh = 0; hh < HALVES; ++hh) {
-          uint32_t c0[WORDS], c1[WORDS], x0[2], x1[2];
-          if constexpr (D == 64) {
-            const uint2 v0 = smem_load<uint2>(here + r0 * 32 + t * 8), v1 = smem_load<uint2>(here + r1 * 32 + t * 8);
-            c0[0] = v0.x; c0[1] = v0.y; c1[0] = v1.x; c1[1] = v1.y;
-          } else {
-            const int piece = ((hh * 4 + t) ^ turn<D>(own0)) * 16;          // row r1 = r0 + 8 has the same turn
-            const uint4 v0 = smem_load<uint4>(here + r0 * (D / 2) + piece), v1 = smem_load<uint4>(here + r1 * (D / 2) + piece);
-            c0[0] = v0.x; c0[1] = v0.y; c0[2] = v0.z; c0[3] = v0.w;
-            c1[0] = v1.x; c1[1] = v1.y; c1[2] = v1.z; c1[3] = v1.w;
-          }
-          if constexpr (FMT == QF_FMT_NVFP4 && D != 64) {
-            const uint32_t at = kmul + (hh * 8 + 2 * t) * 4;
-            const uint2 y0 = smem_load<uint2>(at + r0 * NB * 4), y1 = smem_load<uint2>(at + r1 * NB * 4);
-            x0[0] = y0.x; x0[1] = y0.y; x1[0] = y1.x; x1[1] = y1.y;
-          } else {
-            const uint32_t at = kmul + (D == 64 ? (FMT == QF_FMT_NVFP4 ? t : t >> 1) : hh * 4 + t) * 4;
-            x0[0] = x0[1] = smem_load<uint32_t>(at + r0 * NB * 4);
-            x1[0] = x1[1] = smem_load<uint32_t>(at + r1 * NB * 4);
+          for (int i = 0; i < (NB + 3) / 4; ++i) {
+            if constexpr (NB == 2) {
+              f0[i] = smem_load_u16(kscales + r0 * NB);
+              f1[i] = smem_load_u16(kscales + r1 * NB);
+            } else {
+              f0[i] = smem_load<uint32_t>(kscales + r0 * NB + 4 * i);
+              f1[i] = smem_load<uint32_t>(kscales + r1 * NB + 4 * i);
+            }
           }
 #pragma unroll
-          for (int x = 0; x < WORDS; ++x) {
+          for (int x = 0; x < NW; ++x) {
+            const int piece = (x ^ turn<D>(own0)) * 16 + t * 4;
             uint32_t d0[4], d1[4];
-            e2m1_f16(c0[x], d0);
-            e2m1_f16(c1[x], d1);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { d0[i] = hmul2(d0[i], x0[x >> 1]); d1[i] = hmul2(d1[i], x1[x >> 1]); }
+            e2m1_f16(smem_load<uint32_t>(here + r0 * (D / 2) + piece), d0);
+            e2m1_f16(smem_load<uint32_t>(here + r1 * (D / 2) + piece), d1);
+            const float y0 = e8m0_of(f0[x / 4], x & 3), y1 = e8m0_of(f1[x / 4], x & 3);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              const int step = hh * 8 + 2 * x;
-              mma(s[half][n], d0[0], d1[0], d0[1], d1[1], qf[n][step][0], qf[n][step][1]);
-              mma(s[half][n], d0[2], d1[2], d0[3], d1[3], qf[n][step + 1][0], qf[n][step + 1][1]);
+              float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+              mma(z, d0[0], d1[0], d0[1], d1[1], qf[n][2 * x][0], qf[n][2 * x][1]);
+              mma(z, d0[2], d1[2], d0[3], d1[3], qf[n][2 * x + 1][0], qf[n][2 * x + 1][1]);
+              s[half][n][0] = fmaf(z[0], y0, s[half][n][0]);
+              s[half][n][1] = fmaf(z[1], y0, s[half][n][1]);
+              s[half][n][2] = fmaf(z[2], y1, s[half][n][2]);
+              s[half][n][3] = fmaf(z[3], y1, s[half][n][3]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int hh = 0; hh < HALVES; ++hh) {
+            constexpr int WORDS = D == 64 ? 2 : 4;
+            uint32_t c0[WORDS], c1[WORDS], x0[2], x1[2];
+            if constexpr (D == 64) {
+              const int piece = ((t >> 1) ^ turn<D>(own0)) * 16 + (t & 1) * 8;
+              const uint2 v0 = smem_load<uint2>(here + r0 * 32 + piece), v1 = smem_load<uint2>(here + r1 * 32 + piece);
+              c0[0] = v0.x; c0[1] = v0.y; c1[0] = v1.x; c1[1] = v1.y;
+              x0[0] = e4m3_pair(smem_load_u8(kscales + r0 * NB + t) * 0x0101u);
+              x1[0] = e4m3_pair(smem_load_u8(kscales + r1 * NB + t) * 0x0101u);
+            } else {
+              const int piece = ((hh * 4 + t) ^ turn<D>(own0)) * 16;
+              const uint4 v0 = smem_load<uint4>(here + r0 * (D / 2) + piece), v1 = smem_load<uint4>(here + r1 * (D / 2) + piece);
+              c0[0] = v0.x; c0[1] = v0.y; c0[2] = v0.z; c0[3] = v0.w;
+              c1[0] = v1.x; c1[1] = v1.y; c1[2] = v1.z; c1[3] = v1.w;
+              const uint32_t y0 = e4m3_pair(smem_load_u16(kscales + r0 * NB + hh * 8 + 2 * t)), y1 = e4m3_pair(smem_load_u16(kscales + r1 * NB + hh * 8 + 2 * t));
+              x0[0] = __byte_perm(y0, 0, 0x1010); x0[1] = __byte_perm(y0, 0, 0x3232);
+              x1[0] = __byte_perm(y1, 0, 0x1010); x1[1] = __byte_perm(y1, 0, 0x3232);
+            }
+#pragma unroll
+            for (int x = 0; x < WORDS; ++x) {
+              uint32_t d0[4], d1[4];
+              e2m1_f16(c0[x], d0);
+              e2m1_f16(c1[x], d1);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) { d0[i] = hmul2(d0[i], x0[x >> 1]); d1[i] = hmul2(d1[i], x1[x >> 1]); }
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+                const int step = hh * 8 + 2 * x;
+                mma(s[half][n], d0[0], d1[0], d0[1], d1[1], qf[n][step][0], qf[n][step][1]);
+                mma(s[half][n], d0[2], d1[2], d0[3], d1[3], qf[n][step + 1][0], qf[n][step + 1][1]);
+              }
             }
           }
         }
       }
-      // in units of powers of two; MXFP4: the keys' powers of two, and the values' for the second maximum
-      float up[2][2];
-#pragma unroll
-      for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int key = half * 16 + r * 8 + own0;
-          if constexpr (FMT == QF_FMT_MXFP4) {
-            const float f = __shfl_sync(0xFFFFFFFFu, k_by, key);
-            up[half][r] = __shfl_sync(0xFFFFFFFFu, v_up, key);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) { s[half][n][2 * r] *= f; s[half][n][2 * r + 1] *= f; }
-          }
-#pragma unroll
-          for (int n = 0; n < NT; ++n) { s[half][n][2 * r] *= by[n][0]; s[half][n][2 * r + 1] *= by[n][1]; }
-        }
       if (key0 + kUnitKeys > least) {
 #pragma unroll
         for (int half = 0; half < 2; ++half)
@@ -639,69 +648,186 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
             for (int c = 0; c < 4; ++c)
               if (key0 + half * 16 + (c >> 1) * 8 + own0 >= seen[n][c & 1]) s[half][n][c] = -INFINITY;
       }
-      float keep[NT][2];                                       // what the sums so far have to be multiplied with
-      uint32_t pf[2][NT][2];                                   // weights as fragments of the value product
+
+      // Bases. They move only when a score passes one by more than the room there is.
+      float top[NT][2];
+      bool move = false;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float base[2], vbase[2];
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          float top = fmaxf(fmaxf(s[0][n][c], s[0][n][c + 2]), fmaxf(s[1][n][c], s[1][n][c + 2]));
-          float vtop = FMT == QF_FMT_MXFP4 ? fmaxf(fmaxf(s[0][n][c] + up[0][0], s[0][n][c + 2] + up[0][1]), fmaxf(s[1][n][c] + up[1][0], s[1][n][c + 2] + up[1][1])) : 0.0f;
+          top[n][c] = fmaxf(fmaxf(s[0][n][c], s[0][n][c + 2]), fmaxf(s[1][n][c], s[1][n][c + 2])) * by[n][c];
+          move |= top[n][c] > a.m[n][c] + (kWeightTop + kWeightRoom);
+        }
+      // MXFP4: largest and smallest scale code of the unit's values (a code of 0 comes with zeros). Code c is taken as the FP16 number
+      // 2^(c - vref + 5), which is exact and in range for c in [vref - 19, vref + 8]. Units of a wider range take the other way below.
+      int key_top = 0, vtop = 0;
+      bool wide = false, refer = false;
+      uint32_t vword[(NB + 3) / 4];
+      if constexpr (MX) {
+        int low = 255;
 #pragma unroll
-          for (int d = 4; d < 32; d *= 2) {
-            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-            if (FMT == QF_FMT_MXFP4) vtop = fmaxf(vtop, __shfl_xor_sync(0xFFFFFFFFu, vtop, d));
-          }
-          // maxima are kept 10 lower: weights then reach up to 2^10
-          const float now = fmaxf(a.m[n][c], top - 10.0f);
-          base[c] = now == -INFINITY ? 0.0f : now;
-          const float f = exp2_approx(a.m[n][c] - base[c]);
-          a.l[n][c] *= f;
-          a.m[n][c] = now;
-          keep[n][c] = f;
-          if constexpr (FMT == QF_FMT_MXFP4) {
-            const float vnow = fmaxf(mv[n][c], vtop - 10.0f);
-            vbase[c] = vnow == -INFINITY ? 0.0f : vnow;
-            keep[n][c] = exp2_approx(mv[n][c] - vbase[c]);
-            mv[n][c] = vnow;
+        for (int i = 0; i < (NB + 3) / 4; ++i) {
+          if constexpr (NB == 2) vword[i] = smem_load_u16(vscales + lane * NB);
+          else vword[i] = smem_load<uint32_t>(vscales + lane * NB + 4 * i);
+        }
+        if (key0 + lane < w.keys) {
+#pragma unroll
+          for (int i = 0; i < NB; ++i) {
+            const int code = (vword[i / 4] >> (8 * (i & 3))) & 0xFF;
+            key_top = max(key_top, code);
+            low = min(low, code == 0 ? 255 : code);
           }
         }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const float e0 = exp2_approx(s[half][n][2 * r] - base[0]), e1 = exp2_approx(s[half][n][2 * r + 1] - base[1]);
-            a.l[n][0] += e0;
-            a.l[n][1] += e1;
-            if constexpr (FMT == QF_FMT_MXFP4)
-              pf[half][n][r] = transpose8x8(f16x2(exp2_approx(s[half][n][2 * r] + up[half][r] - vbase[0]), exp2_approx(s[half][n][2 * r + 1] + up[half][r] - vbase[1])));
-            else
-              pf[half][n][r] = transpose8x8(f16x2(e0, e1));
-          }
-        }
+        vtop = __reduce_max_sync(0xFFFFFFFFu, key_top);
+        low = __reduce_min_sync(0xFFFFFFFFu, low);
+        wide = vtop - low > 19;
+        refer = vtop > vref + 8 || low < vref - 19;
+        move |= wide | refer;
       }
-      // values
+      if (__any_sync(0xFFFFFFFFu, move)) {
+        float was[NT][2];                                      // logarithm of what the weights so far have to be multiplied with
+        bool drop = false;
 #pragma unroll
-      for (int hh = 0; hh < HALVES; ++hh) {
-        uint32_t y[2][2];                                      // multipliers of the lane's block, for the pairs of keys t and 7 - t
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float most = top[n][c];
+#pragma unroll
+            for (int d = 4; d < 32; d *= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+            const float now = fmaxf(a.m[n][c], most - kWeightTop);
+            was[n][c] = a.m[n][c] - now;
+            a.m[n][c] = now;
+            a.l[n][c] *= exp2_approx(was[n][c]);
+            drop |= was[n][c] + ve[n][c] - static_cast<float>(vtop - 132) > 60.0f;       // sums in units so small could overflow
+          }
+        if constexpr (MX) {
+          wide |= refer && __any_sync(0xFFFFFFFFu, drop);
+          if (wide) {
+            // A key's value codes relative to its own largest one, exact over 36 binades, with that one's power of two in the weight: the
+            // weights of the value product are kept in FP16's range by a maximum of their own.
+            const float key_up = static_cast<float>(key_top - 140);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                float most = -INFINITY;
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                  for (int r = 0; r < 2; ++r)
+                    most = fmaxf(most, fmaf(s[half][n][2 * r + c], by[n][c], -a.m[n][c]) + __shfl_sync(0xFFFFFFFFu, key_up, half * 16 + r * 8 + own0));
+#pragma unroll
+                for (int d = 4; d < 32; d *= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+                const float so_far = ve[n][c] + was[n][c];
+                ve[n][c] = fmaxf(so_far, most - kWeightTop);
+                was[n][c] = so_far - ve[n][c];
+              }
+            vref = -100;
+          } else if (refer) {
+            vref = vtop;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                was[n][c] += ve[n][c] - static_cast<float>(vtop - 132);
+                ve[n][c] = static_cast<float>(vtop - 132);
+              }
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const float f = exp2_approx(was[n][c]);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) { a.o[i][n][c] *= f; a.o[i][n][c + 2] *= f; }
+          }
+      }
+
+      // weights, as fragments of the value product
+      uint32_t pf[2][NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const float2 by2 = make_float2(by[n][0], by[n][1]), m2 = make_float2(-a.m[n][0], -a.m[n][1]);
+        float2 l2 = make_float2(a.l[n][0], a.l[n][1]);
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            const int block = FMT == QF_FMT_NVFP4 ? (D == 64 ? g >> 1 : hh * 8 + g) : (D == 64 ? g >> 2 : hh * 4 + (g >> 1));
-            y[half][r] = smem_load<uint32_t>(vmul + (((half * 2 + r) * 4 + t) * NB + block) * 4);
+            const float2 x = __ffma2_rn(make_float2(s[half][n][2 * r], s[half][n][2 * r + 1]), by2, m2);
+            const float2 e = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+            l2 = __fadd2_rn(l2, e);
+            if (MX && wide) {
+              const float up = __shfl_sync(0xFFFFFFFFu, static_cast<float>(key_top - 140), half * 16 + r * 8 + own0);
+              pf[half][n][r] = transpose8x8(f16x2(exp2_approx(x.x + up - ve[n][0]), exp2_approx(x.y + up - ve[n][1])));
+            } else {
+              pf[half][n][r] = transpose8x8(f16x2(e.x, e.y));
+            }
           }
+        a.l[n][0] = l2.x;
+        a.l[n][1] = l2.y;
+      }
+      if (MX && wide) {
+        // multipliers, a key per lane, in pairs of a key and the last, second last, ... of its group of eight
+        constexpr int NR = NB / 2 > 0 ? NB / 2 : 1;            // FP16 pairs of a row
+        uint32_t vr[NR];
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+          const int c0 = (vword[i / 2] >> (16 * (i & 1))) & 0xFF, c1 = (vword[i / 2] >> (16 * (i & 1) + 8)) & 0xFF;
+          vr[i] = f16x2(__uint_as_float(static_cast<uint32_t>(max(c0 - key_top + 140, 0)) << 23), __uint_as_float(static_cast<uint32_t>(max(c1 - key_top + 140, 0)) << 23));
+        }
+        const bool low = (lane & 4) == 0;
+        const uint32_t vto = vmul + ((lane >> 3) * 4 + (low ? lane & 3 : 3 - (lane & 3))) * NB * 4;
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+          const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, vr[i], 7);
+          if (low) smem_store(vto + 8 * i, __byte_perm(vr[i], got, 0x5410), __byte_perm(vr[i], got, 0x7632));
+        }
+        __syncwarp();
+      }
+
+      // values
+#pragma unroll
+      for (int hh = 0; hh < HALVES; ++hh) {
+        uint32_t y[2][2];                                      // multipliers of the lane's block, for the pairs of keys t and 7 - t
+        const int block = FMT == QF_FMT_NVFP4 ? (D == 64 ? g >> 1 : hh * 8 + g) : (D == 64 ? g >> 2 : hh * 4 + (g >> 1));
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            if (MX && wide) {
+              y[half][r] = smem_load<uint32_t>(vmul + (((half * 2 + r) * 4 + t) * NB + block) * 4);
+              continue;
+            }
+            const uint32_t first = smem_load_u8(vscales + (half * 16 + r * 8 + t) * NB + block);
+            const uint32_t second = smem_load_u8(vscales + (half * 16 + r * 8 + 7 - t) * NB + block);
+            if constexpr (MX) {
+              const uint32_t d = static_cast<uint32_t>(20 - vref) & 0xFFFFu;
+              y[half][r] = __viaddmax_s16x2_relu(__byte_perm(first, second, 0x5410), d * 0x10001u, 0) << 10;
+            } else {
+              y[half][r] = e4m3_pair(__byte_perm(first, second, 0x0040));
+            }
+          }
+        if (key0 + kUnitKeys > w.keys) {                       // what stands behind the last key
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const int key = key0 + half * 16 + r * 8;
+              y[half][r] &= (key + t < w.keys ? 0xFFFFu : 0u) | (key + 7 - t < w.keys ? 0xFFFF0000u : 0u);
+            }
+        }
         uint32_t c[2][4][VWORDS];
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const int r = half * 16 + (k >> 1) * 8 + ((k & 1) ? 7 - t : t);
+            const int own = (k & 1) ? 7 - t : t, r = half * 16 + (k >> 1) * 8 + own;
             if constexpr (D == 64) {
-              c[half][k][0] = smem_load<uint32_t>(here + S::CODES + r * 32 + g * 4);
+              c[half][k][0] = smem_load<uint32_t>(here + S::CODES + r * 32 + (((g >> 2) ^ turn<D>(own)) * 16) + (g & 3) * 4);
             } else {
-              const uint2 v = smem_load<uint2>(here + S::CODES + r * (D / 2) + (((hh * 4 + (g >> 1)) ^ turn<D>((k & 1) ? 7 - t : t)) * 16) + (g & 1) * 8);
+              const uint2 v = smem_load<uint2>(here + S::CODES + r * (D / 2) + (((hh * 4 + (g >> 1)) ^ turn<D>(own)) * 16) + (g & 1) * 8);
               c[half][k][0] = v.x;
               c[half][k][1] = v.y;
             }
@@ -727,27 +853,25 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
               mma(z, d[0][0][i], d[0][1][i], d[0][2][i], d[0][3][i], pf[0][n][0], pf[0][n][1]);
               mma(z, d[1][0][i], d[1][1][i], d[1][2][i], d[1][3][i], pf[1][n][0], pf[1][n][1]);
               float (&o)[4] = a.o[hh * 8 + x * 4 + i][n];
-              o[0] = fmaf(o[0], keep[n][0], z[0]);
-              o[1] = fmaf(o[1], keep[n][1], z[1]);
-              o[2] = fmaf(o[2], keep[n][0], z[2]);
-              o[3] = fmaf(o[3], keep[n][1], z[3]);
+              const float2 lo = __fadd2_rn(make_float2(o[0], o[1]), make_float2(z[0], z[1])), hi = __fadd2_rn(make_float2(o[2], o[3]), make_float2(z[2], z[3]));
+              o[0] = lo.x; o[1] = lo.y; o[2] = hi.x; o[3] = hi.y;
             }
         }
       }
       __syncwarp();
     }
 
-    // One result of the piece: sums of a column's keys over the lanes, then warps 2 and 3 to 0 and 1, then 1 to 0.
+    // One result of the piece: sums of a column's weights over the lanes, then warps 2 and 3 to 0 and 1, then 1 to 0.
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
 #pragma unroll
         for (int d = 4; d < 32; d *= 2) a.l[n][c] += __shfl_xor_sync(0xFFFFFFFFu, a.l[n][c], d);
-        if constexpr (FMT == QF_FMT_MXFP4) {
-          const float f = mv[n][c] == -INFINITY ? 0.0f : exp2_approx(mv[n][c] - a.m[n][c]);
+        if constexpr (MX) {
+          const float f = exp2_approx(0.5f * ve[n][c]);        // twice: 2^ve itself may be below FP32's range where the product is not
 #pragma unroll
-          for (int i = 0; i < MT; ++i) { a.o[i][n][c] *= f; a.o[i][n][c + 2] *= f; }
+          for (int i = 0; i < MT; ++i) { a.o[i][n][c] = a.o[i][n][c] * f * f; a.o[i][n][c + 2] = a.o[i][n][c + 2] * f * f; }
         }
       }
 #pragma unroll
@@ -787,6 +911,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       __syncthreads();
     }
     if (warp == 0) {
+      const bool begins = w.j == 0;
       if (w.n == w.units) {                                    // the whole sequence: the result itself
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -807,7 +932,6 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
             }
           }
       } else {
-        const bool begins = w.j == 0;
         float4* to_part = part_at + static_cast<int64_t>(cta * 2 + (begins ? 1 : 0)) * PART4 + lane;
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -815,72 +939,80 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
           for (int n = 0; n < NT; ++n) to_part[(i * NT + n) * 32] = make_float4(a.o[i][n][0], a.o[i][n][1], a.o[i][n][2], a.o[i][n][3]);
 #pragma unroll
         for (int n = 0; n < NT; ++n) to_part[(MT * NT + n) * 32] = make_float4(a.m[n][0], a.l[n][0], a.m[n][1], a.l[n][1]);
-        if (begins && lane == 0) {
-          const int64_t last = u1 + (w.units - w.n) - 1;       // the sequence's last unit
-          tasks[cta] = JoinTask{static_cast<int>(((last + 1) * ctas - 1) / total) - cta, w.b, w.s, 0};
-        }
+      }
+      if (begins && lane == 0 && (p.by_segment || w.n < w.units)) {
+        const int64_t last = u1 + (w.units - w.n) - 1;         // place of the sequence's last unit, if others go on with it
+        const int more = w.n < w.units ? static_cast<int>(((last + 1) * ctas - 1) / total) - cta : 0;
+        tasks[p.by_segment ? w.b * p.segs + w.s : cta] = JoinTask{cta, more, w.b, w.s};
       }
     }
   }
 }
 
-// Joins the parts of sequences that several CTAs shared: a CTA per (CTA that began one, value tile), eight warps that take every eighth
-// part each.
+// Joins the parts of sequences that several CTAs shared. A task's value tiles go to the eight warps of gridDim.y CTAs, one after the
+// other; or, where there are many parts, a tile at a time to a CTA whose warps take every eighth part each. In a fixed order either way.
 template <int FMT, int D, int NT>
 __global__ void __launch_bounds__(256) kv_join_kernel(const __grid_constant__ KvAttn p, int ctas) {
   using S = Shape<FMT, D, NT>;
-  constexpr int PART4 = S::PART / 16;
+  constexpr int PART4 = S::PART / 16, TILES = S::MT * NT;
   launch_after_previous();
   const JoinTask task = reinterpret_cast<const JoinTask*>(p.ws)[blockIdx.x];
   if (task.more == 0) return;
-  const float4* parts = reinterpret_cast<const float4*>(p.ws + ((ctas * sizeof(JoinTask) + 255) & ~static_cast<size_t>(255)));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int i = blockIdx.y / NT, n = blockIdx.y % NT;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-  for (int k = warp; k <= task.more; k += 8) {
-    const float4* part = parts + (static_cast<int64_t>(blockIdx.x + k) * 2 + (k == 0 ? 1 : 0)) * PART4 + lane;
-    const float4 v = part[(i * NT + n) * 32], ml = part[(S::MT * NT + n) * 32];
-    float fa[2], fb[2];
-    join_weights(m[0], ml.x, m[0], fa[0], fb[0]);
-    join_weights(m[1], ml.z, m[1], fa[1], fb[1]);
-    l[0] = l[0] * fa[0] + ml.y * fb[0];
-    l[1] = l[1] * fa[1] + ml.w * fb[1];
-    o.x = o.x * fa[0] + v.x * fb[0];
-    o.y = o.y * fa[1] + v.y * fb[1];
-    o.z = o.z * fa[0] + v.z * fb[0];
-    o.w = o.w * fa[1] + v.w * fb[1];
-  }
+  const float4* parts = reinterpret_cast<const float4*>(p.ws + ((ctas * sizeof(JoinTask) + 255) & ~static_cast<size_t>(255))) +
+                        static_cast<int64_t>(task.cta) * 2 * PART4 + lane;
+  const float vt = FMT == QF_FMT_NVFP4 ? *p.v_tscale : 1.0f;
+  const int h = task.seg / p.tiles, row0 = (task.seg - h * p.tiles) * (8 * NT) + 2 * t;
   __shared__ float4 so[8][32], sm[8][32];
-  so[warp][lane] = o;
-  sm[warp][lane] = make_float4(m[0], l[0], m[1], l[1]);
-  __syncthreads();
-  if (warp) return;
-#pragma unroll
-  for (int k = 1; k < 8; ++k) {
-    const float4 v = so[k][lane], ml = sm[k][lane];
+  float4 o, ml;
+  const auto add = [&](const float4& v, const float4& w) {
     float fa[2], fb[2];
-    join_weights(m[0], ml.x, m[0], fa[0], fb[0]);
-    join_weights(m[1], ml.z, m[1], fa[1], fb[1]);
-    l[0] = l[0] * fa[0] + ml.y * fb[0];
-    l[1] = l[1] * fa[1] + ml.w * fb[1];
+    join_weights(ml.x, w.x, ml.x, fa[0], fb[0]);
+    join_weights(ml.z, w.z, ml.z, fa[1], fb[1]);
+    ml.y = ml.y * fa[0] + w.y * fb[0];
+    ml.w = ml.w * fa[1] + w.w * fb[1];
     o.x = o.x * fa[0] + v.x * fb[0];
     o.y = o.y * fa[1] + v.y * fb[1];
     o.z = o.z * fa[0] + v.z * fb[0];
     o.w = o.w * fa[1] + v.w * fb[1];
-  }
-  const float vt = FMT == QF_FMT_NVFP4 ? *p.v_tscale : 0x1p-13f;
-  const int h = task.seg / p.tiles, row0 = (task.seg - h * p.tiles) * (8 * NT) + 8 * n + 2 * t;
+  };
+  const auto write = [&](int tile) {
+    const int i = tile / NT, n = tile % NT;
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const int row = row0 + c;
-    if (row >= p.rows) continue;
-    const int token = row / p.group, head = h * p.group + (row - token * p.group);
-    const int64_t at = (static_cast<int64_t>(task.b) * p.q_len + token) * p.q_heads + head;
-    const float f = l[c] > 0.0f ? vt / l[c] : 0.0f;
-    *reinterpret_cast<uint32_t*>(p.out + at * D + dim_of<D>(i, g)) = pack_bf16x2((c ? o.y : o.x) * f, (c ? o.w : o.z) * f);
-    if (p.lse && i == 0 && g == 0) p.lse[at] = log_sum(m[c], l[c]);
+    for (int c = 0; c < 2; ++c) {
+      const int row = row0 + 8 * n + c;
+      if (row >= p.rows) continue;
+      const int token = row / p.group, head = h * p.group + (row - token * p.group);
+      const int64_t at = (static_cast<int64_t>(task.b) * p.q_len + token) * p.q_heads + head;
+      const float l = c ? ml.w : ml.y, f = l > 0.0f ? vt / l : 0.0f;
+      *reinterpret_cast<uint32_t*>(p.out + at * D + dim_of<D>(i, g)) = pack_bf16x2((c ? o.y : o.x) * f, (c ? o.w : o.z) * f);
+      if (p.lse && i == 0 && g == 0) p.lse[at] = log_sum(c ? ml.z : ml.x, l);
+    }
+  };
+  const bool many = task.more >= 8;
+  for (int tile = many ? blockIdx.y : blockIdx.y * 8 + warp; tile < TILES; tile += gridDim.y * (many ? 1 : 8)) {
+    o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    ml = make_float4(kNoWeights, 0.0f, kNoWeights, 0.0f);
+    const float4* part = parts + tile * 32;
+    const float4* weights = parts + (TILES + tile % NT) * 32;
+#pragma unroll 4
+    for (int k = many ? warp : 0; k <= task.more; k += many ? 8 : 1) {
+      const int64_t at = static_cast<int64_t>(2 * k + (k == 0 ? 1 : 0)) * PART4;
+      add(part[at], weights[at]);
+    }
+    if (many) {
+      so[warp][lane] = o;
+      sm[warp][lane] = ml;
+      __syncthreads();
+      if (warp == 0) {
+#pragma unroll
+        for (int k = 1; k < 8; ++k) add(so[k][lane], sm[k][lane]);
+        write(tile);
+      }
+      __syncthreads();
+    } else {
+      write(tile);
+    }
   }
 }
 
@@ -900,7 +1032,7 @@ cudaError_t launch_overlapping(void (*kernel)(Params...), dim3 grid, int threads
 }
 
 template <int FMT, int D, int NT>
-cudaError_t attend(const KvAttn& p, cudaStream_t st) {
+cudaError_t attend(KvAttn& p, cudaStream_t st) {
   using S = Shape<FMT, D, NT>;
   static bool ready[64] = {};                                  // the attribute stays set for the process
   int dev = 0;
@@ -909,12 +1041,17 @@ cudaError_t attend(const KvAttn& p, cudaStream_t st) {
     if (cudaError_t e = cudaFuncSetAttribute(kv_attention_kernel<FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM)) return e;
     if (dev < 64) ready[dev] = true;
   }
-  // no more CTAs than there can be work for: four units each
-  const int64_t most = static_cast<int64_t>(p.batch) * p.segs * ((p.max_keys + kUnitKeys - 1) / kUnitKeys + (p.max_keys == 0));
-  const int grid = static_cast<int>(most / kAttnWarps + 1 < kNumSMs * S::CTAS ? most / kAttnWarps + 1 : kNumSMs * S::CTAS);
+  // no more CTAs than there can be work for
+  const int64_t segments = static_cast<int64_t>(p.batch) * p.segs;
+  const int64_t most = segments * ((p.max_keys + kUnitKeys - 1) / kUnitKeys + kPieceCost) / kAttnWarps + 1;
+  const int grid = static_cast<int>(most < kNumSMs * S::CTAS ? most : kNumSMs * S::CTAS);
+  p.by_segment = segments <= grid;
   if (cudaError_t e = launch_overlapping(kv_attention_kernel<FMT, D, NT>, dim3(grid), kAttnWarps * 32, S::SMEM, st, p)) return e;
   if (p.max_keys <= kUnitKeys) return cudaSuccess;             // nothing can have been cut
-  return launch_overlapping(kv_join_kernel<FMT, D, NT>, dim3(grid, S::MT * NT), 256, 0, st, p, grid);
+  // the fewer sequences, the more parts each may have: up to a CTA per value tile
+  const int tasks = p.by_segment ? static_cast<int>(segments) : grid;
+  const int share = 4 * kNumSMs / tasks;
+  return launch_overlapping(kv_join_kernel<FMT, D, NT>, dim3(tasks, share < 1 ? 1 : share < S::MT * NT ? share : S::MT * NT), 256, 0, st, p, grid);
 }
 
 template <int FMT>
@@ -997,6 +1134,7 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a, cudaStream_t st) {
   p.group = a.q_heads / a.cache.kv_heads;
   p.rows = a.q_len * p.group;
   p.scale = a.scale * 1.4426950408889634f;
+  p.page_codes = static_cast<int64_t>(p.kv_heads) * p.page_size * (a.cache.head_dim / 2);
   return a.cache.fmt == QF_FMT_NVFP4 ? attend_format<QF_FMT_NVFP4>(p, a.cache.head_dim, st) : attend_format<QF_FMT_MXFP4>(p, a.cache.head_dim, st);
 }
 
