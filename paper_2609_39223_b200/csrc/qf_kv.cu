@@ -7,8 +7,12 @@ namespace qf {
 namespace {
 
 // ---- writing and reading rows --------------------------------------------------------------------------------------------
-// A thread owns 16 consecutive elements of one head's row, of the keys or of the values: an NVFP4 block, or half an MXFP4 block (one
-// shuffle with its neighbour). Neighbouring threads own neighbouring parts, then heads, then values after keys, then tokens.
+// Writing, a thread owns 16 consecutive elements of one head's row, of the keys or of the values: an NVFP4 block, or half an MXFP4 block
+// (one shuffle with its neighbour). Reading, it owns 8, so that a warp's store is 512 bytes on end. A CTA takes a few tokens (slots): where their rows lie is found once per token, and a thread keeps its head
+// and part while it goes through them, so that little is left to do per row but the row itself.
+
+constexpr int kRowsTokens = 64;      // tokens of a CTA at most
+constexpr int kAppendTurns = 4, kReadTurns = 16;              // rows of a thread, where there are enough
 
 struct KvRows {
   const __nv_bfloat16* k;
@@ -24,90 +28,130 @@ struct KvRows {
   const float* k_tscale;
   const float* v_tscale;
   int64_t slots_most;                // of the cache
-  int64_t units;                     // parts of 16 elements in all
-  int page_size, heads, parts;       // parts: of a row
+  int64_t tokens;
+  int each;                          // tokens of a CTA
+  int page_size, heads;
+  int units;                         // parts of a token
+  int span, side;                    // threads for a token, tokens side by side: span * side <= kQdqThreads
+  int shift;                         // parts of a head's row: 1 << shift
   bool slots64, noclip;
 };
 
-__device__ __forceinline__ int64_t slot_of(const KvRows& p, int64_t t) {
-  const int64_t s = p.slots64 ? static_cast<const int64_t*>(p.slots)[t] : static_cast<const int32_t*>(p.slots)[t];
-  return s >= 0 && s < p.slots_most ? s : -1;
-}
-
-// Part `part` of head h at a slot, in units of 16 elements.
-__device__ __forceinline__ int64_t cache_unit(const KvRows& p, int64_t slot, int h, int part) {
-  const int64_t page = slot / p.page_size;
-  return ((page * p.heads + h) * p.page_size + (slot - page * p.page_size)) * p.parts + part;
-}
-
-template <int FMT>
-__global__ void __launch_bounds__(kQdqThreads) kv_append_kernel(const KvRows p) {
-  const int64_t u = static_cast<int64_t>(blockIdx.x) * kQdqThreads + threadIdx.x;
-  const bool any = u < p.units;
-  const int64_t i = any ? u : p.units - 1;
-  const int part = static_cast<int>(i % p.parts);
-  const int64_t row = i / p.parts;
-  const int64_t t = row / (2 * p.heads);
-  const int hv = static_cast<int>(row - t * 2 * p.heads);
-  const bool value = hv >= p.heads;
-  const int h = value ? hv - p.heads : hv;
-  const uint4* in = reinterpret_cast<const uint4*>((value ? p.v + t * p.v_stride : p.k + t * p.k_stride) + (h * p.parts + part) * 16);
-  const uint4 a = in[0], b = in[1];
-  const int64_t slot = slot_of(p, t);
-  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-  uint32_t m = unit_amax_bits(w), scale_code;
-  UnitOut r;
-  if (FMT == QF_FMT_MXFP4) {
-    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-    r = mxfp4_unit(w, m, p.noclip, scale_code);
-  } else {
-    const Nvfp4Tensor nt = nvfp4_tensor(*(value ? p.v_tscale : p.k_tscale));
-    const float amax_b = __uint_as_float(m << 16);
-    if (__all_sync(0xFFFFFFFFu, nt.denom_safe && (amax_b == 0.0f || amax_b >= 0x1p-60f)))
-      r = nvfp4_unit<true>(w, amax_b, nt.s_t, nt.denom, nt.rc_denom, scale_code);
-    else r = nvfp4_unit<false>(w, amax_b, nt.s_t, nt.denom, nt.rc_denom, scale_code);
+// Rows of the CTA's tokens in the cache: head h of token t lies in row at[t] + h * page_size; -1 outside the cache.
+__device__ __forceinline__ int find_rows(const KvRows& p, int64_t (&at)[kRowsTokens]) {
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * p.each;
+  const int here = static_cast<int>(min(static_cast<int64_t>(p.each), p.tokens - first));
+  if (threadIdx.x < here) {
+    const int64_t t = first + threadIdx.x, s = p.slots64 ? static_cast<const int64_t*>(p.slots)[t] : static_cast<const int32_t*>(p.slots)[t];
+    const bool in = s >= 0 && s < p.slots_most;
+    const int64_t page = !in ? 0 : s <= UINT32_MAX ? static_cast<uint32_t>(s) / static_cast<uint32_t>(p.page_size) : s / p.page_size;
+    at[threadIdx.x] = in ? page * p.heads * p.page_size + (s - page * p.page_size) : -1;
   }
-  if (!any || slot < 0) return;
-  const int64_t at = cache_unit(p, slot, h, part);
-  reinterpret_cast<uint2*>(value ? p.v_codes : p.k_codes)[at] = r.codes;
-  uint8_t* scales = value ? p.v_scales : p.k_scales;
-  if (FMT == QF_FMT_NVFP4) scales[at] = static_cast<uint8_t>(scale_code);
-  else if ((part & 1) == 0) scales[at >> 1] = static_cast<uint8_t>(scale_code);
+  __syncthreads();
+  return here;
 }
 
 template <int FMT>
-__global__ void __launch_bounds__(kQdqThreads) kv_read_kernel(const KvRows p) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kQdqThreads + threadIdx.x;
-  if (i >= p.units) return;
-  const bool both = p.k_out && p.v_out;
-  const int part = static_cast<int>(i % p.parts);
-  const int64_t row = i / p.parts;
-  const int rows = both ? 2 * p.heads : p.heads;
-  const int64_t t = row / rows;
-  const int hv = static_cast<int>(row - t * rows);
-  const bool value = both ? hv >= p.heads : !p.k_out;
-  const int h = both && value ? hv - p.heads : hv;
-  const int64_t slot = slot_of(p, t);
-  uint32_t w[8] = {};
-  if (slot >= 0) {
-    const int64_t at = cache_unit(p, slot, h, part);
-    const uint2 c = reinterpret_cast<const uint2*>(value ? p.v_codes : p.k_codes)[at];
-    const uint8_t* scales = value ? p.v_scales : p.k_scales;
-    const float2 st = splat(FMT == QF_FMT_NVFP4 ? *(value ? p.v_tscale : p.k_tscale) : 1.0f);
-    const float2 sb = splat(FMT == QF_FMT_NVFP4 ? e4m3_decode(scales[at] & 0x7Fu) : e8m0_scale(scales[at >> 1]));
+__global__ void __launch_bounds__(kQdqThreads) kv_append_kernel(const __grid_constant__ KvRows p) {
+  constexpr int TURNS = 2;           // rows of a thread on the way together
+  launch_after_previous();
+  __shared__ int64_t at[kRowsTokens];
+  const int here = find_rows(p, at);
+  const int column = static_cast<int>(threadIdx.x) % p.span, beside = static_cast<int>(threadIdx.x) / p.span;
+  for (int r0 = 0; r0 < p.units; r0 += p.span) {
+    const int r = r0 + column;
+    const bool mine = r < p.units && beside < p.side, value = (r >> p.shift) >= p.heads;
+    const int part = r & ((1 << p.shift) - 1), h = mine ? (r >> p.shift) - (value ? p.heads : 0) : 0;
+    const int64_t stride = value ? p.v_stride : p.k_stride;
+    const __nv_bfloat16* in = (value ? p.v : p.k) + static_cast<int64_t>(blockIdx.x) * p.each * stride + ((h << p.shift) + part) * 16;
+    const int64_t row0 = static_cast<int64_t>(h) * p.page_size;
+    uint8_t* codes = (value ? p.v_codes : p.k_codes) + ((row0 << p.shift) + part) * 8;
+    uint8_t* scales = (value ? p.v_scales : p.k_scales) + (FMT == QF_FMT_NVFP4 ? (row0 << p.shift) + part : ((row0 << p.shift) + part) >> 1);
+    const Nvfp4Tensor nt = nvfp4_tensor(FMT == QF_FMT_NVFP4 ? *(value ? p.v_tscale : p.k_tscale) : 1.0f);
+    for (int t0 = 0; t0 < here; t0 += TURNS * p.side) {
+      uint4 x[TURNS][2];
+      int64_t row[TURNS];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float2 o = __fmul2_rn(sb, e2m1x2_decode(((j < 4 ? c.x : c.y) >> (8 * (j & 3))) & 0xFFu));
-      if (FMT == QF_FMT_NVFP4) o = __fmul2_rn(o, st);
-      w[j] = pack_bf16x2(o.x, o.y);
+      for (int i = 0; i < TURNS; ++i) {
+        const int t = t0 + i * p.side + beside;
+        row[i] = mine && t < here ? at[t] : -1;
+        x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
+        if (row[i] >= 0) {
+          const uint4* from = reinterpret_cast<const uint4*>(in + t * stride);
+          x[i][0] = from[0];
+          x[i][1] = from[1];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < TURNS; ++i) {
+        const uint32_t w[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
+        uint32_t m = unit_amax_bits(w), scale_code;
+        UnitOut o;
+        if (FMT == QF_FMT_MXFP4) {
+          m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+          o = mxfp4_unit(w, m, p.noclip, scale_code);
+        } else {
+          const float amax_b = __uint_as_float(m << 16);
+          if (__all_sync(0xFFFFFFFFu, nt.denom_safe && (amax_b == 0.0f || amax_b >= 0x1p-60f)))
+            o = nvfp4_unit<true>(w, amax_b, nt.s_t, nt.denom, nt.rc_denom, scale_code);
+          else o = nvfp4_unit<false>(w, amax_b, nt.s_t, nt.denom, nt.rc_denom, scale_code);
+        }
+        if (row[i] < 0) continue;
+        *reinterpret_cast<uint2*>(codes + (row[i] << (p.shift + 3))) = o.codes;
+        if (FMT == QF_FMT_NVFP4) scales[row[i] << p.shift] = static_cast<uint8_t>(scale_code);
+        else if ((part & 1) == 0) scales[row[i] << (p.shift - 1)] = static_cast<uint8_t>(scale_code);
+      }
     }
   }
-  uint4* out = reinterpret_cast<uint4*>((value ? p.v_out : p.k_out) + ((t * p.heads + h) * p.parts + part) * 16);
-  out[0] = make_uint4(w[0], w[1], w[2], w[3]);
-  out[1] = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
-KvRows kv_rows(const qf_kv_cache_t& c, const void* slots, bool slots64) {
+template <int FMT>
+__global__ void __launch_bounds__(kQdqThreads) kv_read_kernel(const __grid_constant__ KvRows p) {
+  constexpr int TURNS = 4;
+  launch_after_previous();
+  __shared__ int64_t at[kRowsTokens];
+  const int here = find_rows(p, at);
+  const int column = static_cast<int>(threadIdx.x) % p.span, beside = static_cast<int>(threadIdx.x) / p.span;
+  if (beside >= p.side) return;
+  for (int r = column; r < p.units; r += p.span) {
+    const bool value = !p.k_out || (r >> p.shift) >= p.heads;
+    const int part = r & ((1 << p.shift) - 1), h = (r >> p.shift) - ((r >> p.shift) >= p.heads ? p.heads : 0);
+    const int64_t first = ((static_cast<int64_t>(h) * p.page_size) << p.shift) + part, pitch = static_cast<int64_t>(p.heads) << p.shift;
+    const uint32_t* codes = reinterpret_cast<const uint32_t*>(value ? p.v_codes : p.k_codes) + first;
+    const uint8_t* scales = (value ? p.v_scales : p.k_scales) + (first >> (FMT == QF_FMT_NVFP4 ? 1 : 2));
+    uint4* out = reinterpret_cast<uint4*>(value ? p.v_out : p.k_out) + static_cast<int64_t>(blockIdx.x) * p.each * pitch + (h << p.shift) + part;
+    const float2 st = splat(FMT == QF_FMT_NVFP4 ? *(value ? p.v_tscale : p.k_tscale) : 1.0f);
+    for (int t0 = beside; t0 < here; t0 += TURNS * p.side) {
+      uint32_t c[TURNS], sc[TURNS];
+#pragma unroll
+      for (int i = 0; i < TURNS; ++i) {
+        const int t = t0 + i * p.side;
+        const int64_t row = t < here ? at[t] : -1;
+        c[i] = sc[i] = 0u;
+        if (row >= 0) {
+          c[i] = codes[row << p.shift];
+          sc[i] = scales[row << (p.shift - (FMT == QF_FMT_NVFP4 ? 1 : 2))];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < TURNS; ++i) {
+        const int t = t0 + i * p.side;
+        if (t >= here) break;
+        const float2 sb = splat(FMT == QF_FMT_NVFP4 ? e4m3_decode(sc[i] & 0x7Fu) : e8m0_scale(sc[i]));
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float2 o = __fmul2_rn(sb, e2m1x2_decode((c[i] >> (8 * j)) & 0xFFu));
+          if (FMT == QF_FMT_NVFP4) o = __fmul2_rn(o, st);
+          w[j] = pack_bf16x2(o.x, o.y);
+        }
+        out[t * pitch] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+}
+
+KvRows kv_rows(const qf_kv_cache_t& c, const void* slots, bool slots64, int64_t tokens) {
   KvRows p{};
   p.k_codes = static_cast<uint8_t*>(c.k_codes);
   p.k_scales = static_cast<uint8_t*>(c.k_scales);
@@ -118,10 +162,37 @@ KvRows kv_rows(const qf_kv_cache_t& c, const void* slots, bool slots64) {
   p.slots = slots;
   p.slots64 = slots64;
   p.slots_most = c.pages * c.page_size;
+  p.tokens = tokens;
   p.page_size = c.page_size;
   p.heads = c.kv_heads;
-  p.parts = c.head_dim / 16;
   return p;
+}
+
+template <typename... Params, typename... Args>
+cudaError_t launch_overlapping(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// parts: of a head's row (a power of two from 4 on); kinds: keys, values or both. A CTA gets tokens for a few turns of its threads, fewer where that would leave SMs without a CTA.
+cudaError_t launch_rows(void (*kernel)(KvRows), KvRows& p, int parts, int kinds, int turns, cudaStream_t st) {
+  for (p.shift = 2; 1 << p.shift < parts; ++p.shift) {}
+  p.units = kinds * p.heads << p.shift;
+  p.span = p.units < kQdqThreads ? p.units : kQdqThreads;
+  p.side = kQdqThreads / p.span;
+  const int64_t even = p.tokens / (12 * kNumSMs * 4 * p.side) * (4 * p.side);
+  const int64_t each = even == 0 ? p.side : even < turns * p.side ? even : turns * p.side;
+  p.each = static_cast<int>(each < kRowsTokens ? each : kRowsTokens);
+  return launch_overlapping(kernel, dim3(static_cast<unsigned>((p.tokens + p.each - 1) / p.each)), kQdqThreads, 0, st, p);
 }
 
 // ---- attention -----------------------------------------------------------------------------------------------------------
@@ -147,6 +218,7 @@ constexpr int kUnitKeys = 32;
 constexpr int kAttnWarps = 4;                 // of a CTA
 constexpr int kStages = 2;                    // units a warp has in shared memory or on the way
 constexpr int kPieceCost = 4;                 // what a sequence's queries, meeting and result cost, in units
+constexpr int kWhole = 12;                    // sequences of up to so many units are not cut
 constexpr float kWeightTop = 6.0f, kWeightRoom = 8.0f;       // weights start at up to 2^6 and may reach 2^14 before their base is moved
 
 struct KvAttn {
@@ -182,7 +254,7 @@ struct Shape {
   static constexpr int MT = D / 16;                                                        // 16-row tiles of the value product
   static constexpr int PART = (MT * NT * 4 + 4 * NT) * 32 * 4;                             // a warp's sums and maxima, bytes
   static constexpr int SMEM = kAttnWarps * WARP + kAttnWarps / 2 * PART;
-  static constexpr int FIT = 232448 / (SMEM + 1024), WANT = D == 256 ? (NT == 2 ? 1 : 2) : D == 128 && NT == 2 ? 3 : 4;
+  static constexpr int FIT = 232448 / (SMEM + 1024), WANT = D == 256 ? 3 - NT : D == 128 ? 4 - NT : 4;
   static constexpr int CTAS = FIT < WANT ? FIT : WANT;                                     // of an SM
 };
 
@@ -251,7 +323,6 @@ __device__ __forceinline__ uint32_t smem_load_u16(uint32_t at) {
   asm volatile("ld.shared.u16 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
   return v;
 }
-__device__ __forceinline__ void smem_store(uint32_t at, uint32_t a) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(a) : "memory"); }
 __device__ __forceinline__ void smem_store(uint32_t at, uint32_t a, uint32_t b) {
   asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(a), "r"(b) : "memory");
 }
@@ -263,6 +334,10 @@ __device__ __forceinline__ int keys_of(const KvAttn& p, int b) { return min(max(
 __device__ __forceinline__ int units_of(int keys) { return (keys + kUnitKeys - 1) / kUnitKeys; }
 // what a segment of a sequence counts for in the shares: a sequence without keys nothing (its zeros are written beforehand)
 __device__ __forceinline__ int cost_of(int keys) { return keys == 0 ? 0 : units_of(keys) + kPieceCost; }
+
+// token of a query row of a key head, key head of a segment
+__device__ __forceinline__ int token_of(const KvAttn& p, int row) { return p.q_len == 1 ? 0 : row / p.group; }
+__device__ __forceinline__ int head_of(const KvAttn& p, int segment) { return p.tiles == 1 ? segment : segment / p.tiles; }
 
 // The pieces of a CTA's share, one (sequence, segment) after the other: units [j, j + n) of segment s of sequence b; n = 0 at the end.
 // In a segment's part of the shares kPieceCost places come first, then a place per unit.
@@ -332,7 +407,7 @@ struct Copier {
     page = cur * kUnitKeys / p.page_size;
     off = cur * kUnitKeys - page * p.page_size;
     pages = p.table + static_cast<int64_t>(w.b) * p.max_pages;
-    const int64_t row = static_cast<int64_t>(w.s / p.tiles) * p.page_size;
+    const int64_t row = static_cast<int64_t>(head_of(p, w.s)) * p.page_size;
     kp = p.k_codes + row * ROW + lane * 16;
     vp = p.v_codes + row * ROW + lane * 16;
     const int c = lane % (2 * CHUNKS);
@@ -431,9 +506,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       for (int i = threadIdx.x; i < p.segs; i += kAttnWarps * 32) tasks[b * p.segs + i].more = 0;
   }
 
-  // This CTA's share. All places are counted by all CTAs, each thread a run of the sequences.
-  __shared__ int64_t warp_places[kAttnWarps];
-  __shared__ int first_b, first_s, first_pos;
+  // This CTA's share. All places are counted by all CTAs, each thread a run of the sequences. A border between two shares that falls into a
+  // short sequence moves to the nearer end of it, for both of them.
+  __shared__ int64_t warp_places[kAttnWarps], border[2];
+  __shared__ int first_b, first_s, first_pos, first_keys;
   const int per = (p.batch + kAttnWarps * 32 - 1) / (kAttnWarps * 32);
   const int b0 = min(static_cast<int>(threadIdx.x) * per, p.batch), b1 = min(b0 + per, p.batch);
   int64_t mine = 0;
@@ -458,30 +534,59 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   float4* part_at = reinterpret_cast<float4*>(p.ws + ((gridDim.x * sizeof(JoinTask) + 255) & ~static_cast<size_t>(255)));
   constexpr int PART4 = S::PART / 16;                          // float4s of a part
   if (cta >= ctas) return;
-  const int64_t u0 = cta * total / ctas, u1 = (cta + 1) * total / ctas;
-  if (before <= u0 && u0 < before + mine) {
-    int64_t r = u0 - before;
-    int b = b0;
-    for (;; ++b) {
-      const int64_t all = static_cast<int64_t>(cost_of(keys_of(p, b))) * p.segs;
-      if (r < all) break;
-      r -= all;
+  // c * total / ctas without the long product
+  const bool small = total <= UINT32_MAX;
+  const int64_t q0 = small ? static_cast<uint32_t>(total) / static_cast<uint32_t>(ctas) : total / ctas;
+  const uint32_t rest = static_cast<uint32_t>(total - q0 * ctas);
+  const int64_t u0 = cta * q0 + cta * rest / static_cast<uint32_t>(ctas), u1 = (cta + 1) * q0 + (cta + 1) * rest / static_cast<uint32_t>(ctas);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int64_t u = i ? u1 : u0;
+    if (u == total && threadIdx.x == 0) border[i] = total;
+    if (u < before || u >= before + mine) continue;
+    int64_t r = u - before;
+    int b = b0, keys = keys_of(p, b);
+    for (; r >= static_cast<int64_t>(cost_of(keys)) * p.segs; keys = keys_of(p, ++b)) r -= static_cast<int64_t>(cost_of(keys)) * p.segs;
+    const int cost = cost_of(keys), s = static_cast<int>(r <= UINT32_MAX ? static_cast<uint32_t>(r) / static_cast<uint32_t>(cost) : r / cost);
+    int pos = static_cast<int>(r - static_cast<int64_t>(s) * cost);
+    const int moved = cost > kWhole + kPieceCost ? pos : 2 * pos < cost ? 0 : cost;
+    border[i] = u + (moved - pos);
+    if (i == 0) {
+      first_b = b;
+      first_s = s;
+      first_pos = moved;
+      first_keys = keys;
     }
-    const int cost = cost_of(keys_of(p, b));
-    first_b = b;
-    first_s = static_cast<int>(r / cost);
-    first_pos = static_cast<int>(r % cost);
   }
   __syncthreads();
+  if (border[1] <= border[0]) return;
   Walk w;
   w.b = first_b;
   w.s = first_s;
   w.pos = first_pos;
-  w.keys = keys_of(p, w.b);
+  w.keys = first_keys;
   w.units = units_of(w.keys);
-  w.left = static_cast<int>(u1 - u0);
+  w.left = static_cast<int>(border[1] - border[0]);
   w.settle(p);
 
+  // Queries of a piece: 8 rows to a tile, row g of which is this lane's
+  uint4 raw[NT][NW];
+  const auto fetch = [&](const Walk& x) {
+    const int h = head_of(p, x.s), row0 = (x.s - h * p.tiles) * (8 * NT);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int row = row0 + 8 * n + g;
+      const bool any = x.n > 0 && row < p.rows;
+      const int token = any ? token_of(p, row) : 0, head = h * p.group + (any ? row - token * p.group : 0);
+      const __nv_bfloat16* src = p.q + (static_cast<int64_t>(x.b) * p.q_len + token) * p.q_stride + static_cast<int64_t>(head) * D;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) {
+        const int at = MX ? i * 32 + t * 8 : D == 64 ? t * 16 + 8 * i : (i >> 2) * 128 + t * 32 + 8 * (i & 3);
+        raw[n][i] = any ? *reinterpret_cast<const uint4*>(src + at) : make_uint4(0, 0, 0, 0);
+      }
+    }
+  };
+  fetch(w);
   Copier<FMT, D> copy;
   copy.w = w;
   copy.start(p, warp, lane);
@@ -496,26 +601,17 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   const float kt = p.scale * (MX ? 1.0f : *p.k_tscale);
   const float sign = kt < 0.0f ? -1.0f : 1.0f;                 // of the scale: goes to the queries, so that a column's factor is positive
 
-  for (; w.n > 0; w.next(p)) {
-    const int h = w.s / p.tiles, row0 = (w.s - h * p.tiles) * (8 * NT);
+  for (Walk next; w.n > 0; w = next) {
+    const int h = head_of(p, w.s), row0 = (w.s - h * p.tiles) * (8 * NT);
     // queries of this tile as FP16 fragments, and what a score has to be multiplied with
     uint32_t qf[NT][D / 16][2];
     float by[NT][2];
     int seen[NT][2], least = w.keys;                           // keys that a column sees
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int row = row0 + 8 * n + g;
-      const bool any = row < p.rows;
-      const int token = any ? row / p.group : 0, head = h * p.group + (any ? row - token * p.group : 0);
-      const __nv_bfloat16* src = p.q + (static_cast<int64_t>(w.b) * p.q_len + token) * p.q_stride + static_cast<int64_t>(head) * D;
-      uint4 raw[NW];
       uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < NW; ++i) {
-        const int at = MX ? i * 32 + t * 8 : D == 64 ? t * 16 + 8 * i : (i >> 2) * 128 + t * 32 + 8 * (i & 3);
-        raw[i] = any ? *reinterpret_cast<const uint4*>(src + at) : make_uint4(0, 0, 0, 0);
-        top = max(top, chunk_amax_bits(raw[i]));
-      }
+      for (int i = 0; i < NW; ++i) top = max(top, chunk_amax_bits(raw[n][i]));
       top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
       top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
       const int e = max(static_cast<int>(top >> 7), 14);       // exponent of the row's largest element
@@ -523,7 +619,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       const float down = e == 14 ? 0x1p-127f : __uint_as_float(static_cast<uint32_t>(e - 14) << 23);
 #pragma unroll
       for (int i = 0; i < NW; ++i) {
-        const uint32_t v[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+        const uint32_t v[4] = {raw[n][i].x, raw[n][i].y, raw[n][i].z, raw[n][i].w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) qf[n][2 * i + (k >> 1)][k & 1] = f16x2(bf16_lo(v[k]) * up, bf16_hi(v[k]) * up);
       }
@@ -531,10 +627,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       for (int c = 0; c < 2; ++c) {
         // not zero, so that a score of -infinity stays one
         by[n][c] = fmaxf(__shfl_sync(0xFFFFFFFFu, down, (2 * t + c) * 4) * fabsf(kt), 0x1p-126f);
-        const int tok = min(row0 + 8 * n + 2 * t + c, p.rows - 1) / p.group;
+        const int tok = token_of(p, min(row0 + 8 * n + 2 * t + c, p.rows - 1));
         seen[n][c] = min(max(w.keys - p.q_len + tok + 1, 0), w.keys);
       }
-      if (n == 0) least = min(max(w.keys - p.q_len + row0 / p.group + 1, 0), w.keys);
+      if (n == 0) least = min(max(w.keys - p.q_len + token_of(p, row0) + 1, 0), w.keys);
     }
 
     // m: base of a column's weights, which are 2^(score - m); l: the lane's share of their sum; ve (MXFP4): o is in units of 2^ve; vref: the
@@ -861,6 +957,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       __syncwarp();
     }
 
+    next = w;
+    next.next(p);
+    fetch(next);                                               // on the way while this piece's parts meet
     // One result of the piece: sums of a column's weights over the lanes, then warps 2 and 3 to 0 and 1, then 1 to 0.
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -919,7 +1018,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
           for (int c = 0; c < 2; ++c) {
             const int row = row0 + 8 * n + 2 * t + c;
             if (row < p.rows) {
-              const int token = row / p.group, head = h * p.group + (row - token * p.group);
+              const int token = token_of(p, row), head = h * p.group + (row - token * p.group);
               const int64_t at = (static_cast<int64_t>(w.b) * p.q_len + token) * p.q_heads + head;
               const float f = a.l[n][c] > 0.0f ? vt / a.l[n][c] : 0.0f;
               uint32_t* out = reinterpret_cast<uint32_t*>(p.out + at * D);
@@ -949,86 +1048,71 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   }
 }
 
-// Joins the parts of sequences that several CTAs shared. A task's value tiles go to the eight warps of gridDim.y CTAs, one after the
-// other; or, where there are many parts, a tile at a time to a CTA whose warps take every eighth part each. In a fixed order either way.
+// Joins the parts of sequences that several CTAs shared. A task's value tiles go to the warps of gridDim.y CTAs, one after the
+// other; or, where there are many parts, a tile at a time to a CTA whose warps share them. In a fixed order either way.
 template <int FMT, int D, int NT>
-__global__ void __launch_bounds__(256) kv_join_kernel(const __grid_constant__ KvAttn p, int ctas) {
+__global__ void __launch_bounds__(1024) kv_join_kernel(const __grid_constant__ KvAttn p, int ctas) {
   using S = Shape<FMT, D, NT>;
   constexpr int PART4 = S::PART / 16, TILES = S::MT * NT;
   launch_after_previous();
+  const float vt = FMT == QF_FMT_NVFP4 ? *p.v_tscale : 1.0f;
   const JoinTask task = reinterpret_cast<const JoinTask*>(p.ws)[blockIdx.x];
   if (task.more == 0) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const float4* parts = reinterpret_cast<const float4*>(p.ws + ((ctas * sizeof(JoinTask) + 255) & ~static_cast<size_t>(255))) +
                         static_cast<int64_t>(task.cta) * 2 * PART4 + lane;
-  const float vt = FMT == QF_FMT_NVFP4 ? *p.v_tscale : 1.0f;
-  const int h = task.seg / p.tiles, row0 = (task.seg - h * p.tiles) * (8 * NT) + 2 * t;
-  __shared__ float4 so[8][32], sm[8][32];
-  float4 o, ml;
-  const auto add = [&](const float4& v, const float4& w) {
-    float fa[2], fb[2];
-    join_weights(ml.x, w.x, ml.x, fa[0], fb[0]);
-    join_weights(ml.z, w.z, ml.z, fa[1], fb[1]);
-    ml.y = ml.y * fa[0] + w.y * fb[0];
-    ml.w = ml.w * fa[1] + w.w * fb[1];
-    o.x = o.x * fa[0] + v.x * fb[0];
-    o.y = o.y * fa[1] + v.y * fb[1];
-    o.z = o.z * fa[0] + v.z * fb[0];
-    o.w = o.w * fa[1] + v.w * fb[1];
-  };
-  const auto write = [&](int tile) {
+  const int h = head_of(p, task.seg), row0 = (task.seg - h * p.tiles) * (8 * NT) + 2 * t;
+  extern __shared__ __align__(16) uint8_t smem[];
+  float4* met = reinterpret_cast<float4*>(smem);               // sums and weights of every warp
+  const bool many = task.more >= 8;
+  const int first = many ? warp : 0, step = many ? warps : 1;
+  for (int tile = many ? blockIdx.y : blockIdx.y * warps + warp; tile < TILES; tile += gridDim.y * (many ? 1 : warps)) {
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f), ml = make_float4(kNoWeights, 0.0f, kNoWeights, 0.0f);
+    const auto add = [&](const float4& v, const float4& w) {
+      float fa[2], fb[2];
+      join_weights(ml.x, w.x, ml.x, fa[0], fb[0]);
+      join_weights(ml.z, w.z, ml.z, fa[1], fb[1]);
+      ml.y = ml.y * fa[0] + w.y * fb[0];
+      ml.w = ml.w * fa[1] + w.w * fb[1];
+      o.x = o.x * fa[0] + v.x * fb[0];
+      o.y = o.y * fa[1] + v.y * fb[1];
+      o.z = o.z * fa[0] + v.z * fb[0];
+      o.w = o.w * fa[1] + v.w * fb[1];
+    };
+    for (int k0 = first; k0 <= task.more; k0 += 4 * step) {    // four parts on the way together
+      float4 v[4], w[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = min(k0 + j * step, task.more);
+        const float4* part = parts + static_cast<int64_t>(2 * k + (k == 0 ? 1 : 0)) * PART4;
+        v[j] = part[tile * 32];
+        w[j] = part[(TILES + tile % NT) * 32];
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (k0 + j * step <= task.more) add(v[j], w[j]);
+    }
+    if (many) {
+      met[warp * 64 + lane] = o;
+      met[warp * 64 + 32 + lane] = ml;
+      __syncthreads();
+      if (warp == 0)
+        for (int k = 1; k < warps; ++k) add(met[k * 64 + lane], met[k * 64 + 32 + lane]);
+      __syncthreads();
+      if (warp != 0) continue;
+    }
     const int i = tile / NT, n = tile % NT;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int row = row0 + 8 * n + c;
       if (row >= p.rows) continue;
-      const int token = row / p.group, head = h * p.group + (row - token * p.group);
+      const int token = token_of(p, row), head = h * p.group + (row - token * p.group);
       const int64_t at = (static_cast<int64_t>(task.b) * p.q_len + token) * p.q_heads + head;
       const float l = c ? ml.w : ml.y, f = l > 0.0f ? vt / l : 0.0f;
       *reinterpret_cast<uint32_t*>(p.out + at * D + dim_of<D>(i, g)) = pack_bf16x2((c ? o.y : o.x) * f, (c ? o.w : o.z) * f);
       if (p.lse && i == 0 && g == 0) p.lse[at] = log_sum(c ? ml.z : ml.x, l);
     }
-  };
-  const bool many = task.more >= 8;
-  for (int tile = many ? blockIdx.y : blockIdx.y * 8 + warp; tile < TILES; tile += gridDim.y * (many ? 1 : 8)) {
-    o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    ml = make_float4(kNoWeights, 0.0f, kNoWeights, 0.0f);
-    const float4* part = parts + tile * 32;
-    const float4* weights = parts + (TILES + tile % NT) * 32;
-#pragma unroll 4
-    for (int k = many ? warp : 0; k <= task.more; k += many ? 8 : 1) {
-      const int64_t at = static_cast<int64_t>(2 * k + (k == 0 ? 1 : 0)) * PART4;
-      add(part[at], weights[at]);
-    }
-    if (many) {
-      so[warp][lane] = o;
-      sm[warp][lane] = ml;
-      __syncthreads();
-      if (warp == 0) {
-#pragma unroll
-        for (int k = 1; k < 8; ++k) add(so[k][lane], sm[k][lane]);
-        write(tile);
-      }
-      __syncthreads();
-    } else {
-      write(tile);
-    }
   }
-}
-
-template <typename... Params, typename... Args>
-cudaError_t launch_overlapping(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 template <int FMT, int D, int NT>
@@ -1047,11 +1131,11 @@ cudaError_t attend(KvAttn& p, cudaStream_t st) {
   const int grid = static_cast<int>(most < kNumSMs * S::CTAS ? most : kNumSMs * S::CTAS);
   p.by_segment = segments <= grid;
   if (cudaError_t e = launch_overlapping(kv_attention_kernel<FMT, D, NT>, dim3(grid), kAttnWarps * 32, S::SMEM, st, p)) return e;
-  if (p.max_keys <= kUnitKeys) return cudaSuccess;             // nothing can have been cut
+  if (p.max_keys <= kWhole * kUnitKeys) return cudaSuccess;    // nothing can have been cut
   // the fewer sequences, the more parts each may have: up to a CTA per value tile
   const int tasks = p.by_segment ? static_cast<int>(segments) : grid;
-  const int share = 4 * kNumSMs / tasks;
-  return launch_overlapping(kv_join_kernel<FMT, D, NT>, dim3(tasks, share < 1 ? 1 : share < S::MT * NT ? share : S::MT * NT), 256, 0, st, p, grid);
+  const int share = 4 * kNumSMs / tasks, threads = grid / tasks < 32 ? 256 : 1024;
+  return launch_overlapping(kv_join_kernel<FMT, D, NT>, dim3(tasks, share < 1 ? 1 : share < S::MT * NT ? share : S::MT * NT), threads, threads * 32, st, p, grid);
 }
 
 template <int FMT>
@@ -1080,28 +1164,20 @@ size_t ws_bytes() {          // the largest, whatever the format and the tile: h
 
 cudaError_t launch_kv_append(const qf_kv_cache_t& c, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t tokens,
                              const void* slots, bool slots64, bool noclip, cudaStream_t st) {
-  KvRows p = kv_rows(c, slots, slots64);
+  KvRows p = kv_rows(c, slots, slots64, tokens);
   p.k = static_cast<const __nv_bfloat16*>(k);
   p.v = static_cast<const __nv_bfloat16*>(v);
   p.k_stride = k_stride;
   p.v_stride = v_stride;
   p.noclip = noclip;
-  p.units = tokens * 2 * p.heads * p.parts;
-  const unsigned grid = static_cast<unsigned>((p.units + kQdqThreads - 1) / kQdqThreads);
-  if (c.fmt == QF_FMT_NVFP4) kv_append_kernel<QF_FMT_NVFP4><<<grid, kQdqThreads, 0, st>>>(p);
-  else kv_append_kernel<QF_FMT_MXFP4><<<grid, kQdqThreads, 0, st>>>(p);
-  return cudaGetLastError();
+  return launch_rows(c.fmt == QF_FMT_NVFP4 ? kv_append_kernel<QF_FMT_NVFP4> : kv_append_kernel<QF_FMT_MXFP4>, p, c.head_dim / 16, 2, kAppendTurns, st);
 }
 
 cudaError_t launch_kv_read(const qf_kv_cache_t& c, const void* slots, bool slots64, int64_t rows, void* k, void* v, cudaStream_t st) {
-  KvRows p = kv_rows(c, slots, slots64);
+  KvRows p = kv_rows(c, slots, slots64, rows);
   p.k_out = static_cast<__nv_bfloat16*>(k);
   p.v_out = static_cast<__nv_bfloat16*>(v);
-  p.units = rows * (k && v ? 2 : 1) * p.heads * p.parts;
-  const unsigned grid = static_cast<unsigned>((p.units + kQdqThreads - 1) / kQdqThreads);
-  if (c.fmt == QF_FMT_NVFP4) kv_read_kernel<QF_FMT_NVFP4><<<grid, kQdqThreads, 0, st>>>(p);
-  else kv_read_kernel<QF_FMT_MXFP4><<<grid, kQdqThreads, 0, st>>>(p);
-  return cudaGetLastError();
+  return launch_rows(c.fmt == QF_FMT_NVFP4 ? kv_read_kernel<QF_FMT_NVFP4> : kv_read_kernel<QF_FMT_MXFP4>, p, c.head_dim / 8, k && v ? 2 : 1, kReadTurns, st);
 }
 
 size_t kv_attention_ws_bytes(int64_t, int, int head_dim, int) {
