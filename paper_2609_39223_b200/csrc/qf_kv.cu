@@ -305,29 +305,19 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+// Places in dynamic shared memory are bytes from its start: plain accesses, which the compiler may order between the barriers.
 template <typename T>
 __device__ __forceinline__ T smem_load(uint32_t at) {
-  T v;
-  if constexpr (sizeof(T) == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-  else if constexpr (sizeof(T) == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
-  else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-  return v;
+  extern __shared__ __align__(128) uint8_t smem[];
+  return *reinterpret_cast<const T*>(smem + at);
 }
-__device__ __forceinline__ uint32_t smem_load_u8(uint32_t at) {
-  uint32_t v;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-  return v;
+__device__ __forceinline__ void smem_store(uint32_t at, const uint2& v) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  *reinterpret_cast<uint2*>(smem + at) = v;
 }
-__device__ __forceinline__ uint32_t smem_load_u16(uint32_t at) {
-  uint32_t v;
-  asm volatile("ld.shared.u16 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-  return v;
-}
-__device__ __forceinline__ void smem_store(uint32_t at, uint32_t a, uint32_t b) {
-  asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(a), "r"(b) : "memory");
-}
-__device__ __forceinline__ void smem_store(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+__device__ __forceinline__ void smem_store(uint32_t at, const float4& v) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  *reinterpret_cast<float4*>(smem + at) = v;
 }
 
 __device__ __forceinline__ int keys_of(const KvAttn& p, int b) { return min(max(p.lens[b], 0), p.max_keys); }
@@ -485,26 +475,32 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   constexpr bool MX = FMT == QF_FMT_MXFP4;
   constexpr int NW = D / 32;                                   // words of codes of a key that a lane holds
   constexpr int VWORDS = D == 64 ? 1 : 2;                      // and of a value, per half
-  extern __shared__ __align__(16) uint8_t smem[];
+  extern __shared__ __align__(128) uint8_t smem[];
   launch_after_previous();
   const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + warp * S::WARP, vmul = ring + kStages * S::STAGE;
-  const uint32_t parts = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + kAttnWarps * S::WARP;
+  const uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(smem));
+  const uint32_t ring = warp * S::WARP, vmul = ring + kStages * S::STAGE, parts = kAttnWarps * S::WARP;
   JoinTask* tasks = reinterpret_cast<JoinTask*>(p.ws);
   const int cta = blockIdx.x;
   if (!p.by_segment && threadIdx.x == 0) tasks[cta].more = 0;
 
-  // Sequences without keys: zeros, here and there.
-  for (int b = cta; b < p.batch; b += gridDim.x) {
-    if (keys_of(p, b) > 0) continue;
-    const int64_t first = static_cast<int64_t>(b) * p.q_len * p.q_heads, rows = static_cast<int64_t>(p.q_len) * p.q_heads;
-    uint4* out = reinterpret_cast<uint4*>(p.out + first * D);
-    for (int64_t i = threadIdx.x; i < rows * (D / 8); i += kAttnWarps * 32) out[i] = make_uint4(0, 0, 0, 0);
-    if (p.lse)
-      for (int64_t i = threadIdx.x; i < rows; i += kAttnWarps * 32) p.lse[first + i] = -INFINITY;
-    if (p.by_segment)
-      for (int i = threadIdx.x; i < p.segs; i += kAttnWarps * 32) tasks[b * p.segs + i].more = 0;
-  }
+  const float vt = MX ? 1.0f : *p.v_tscale;
+  const float kt = p.scale * (MX ? 1.0f : *p.k_tscale);
+  const float sign = kt < 0.0f ? -1.0f : 1.0f;                 // of the scale: goes to the queries, so that a column's factor is positive
+
+  // Sequences without keys: zeros, a sequence to a CTA.
+  const auto write_zeros = [&]() {
+    for (int b = cta; b < p.batch; b += gridDim.x) {
+      if (keys_of(p, b) > 0) continue;
+      const int64_t first = static_cast<int64_t>(b) * p.q_len * p.q_heads, rows = static_cast<int64_t>(p.q_len) * p.q_heads;
+      uint4* out = reinterpret_cast<uint4*>(p.out + first * D);
+      for (int64_t i = threadIdx.x; i < rows * (D / 8); i += kAttnWarps * 32) out[i] = make_uint4(0, 0, 0, 0);
+      if (p.lse)
+        for (int64_t i = threadIdx.x; i < rows; i += kAttnWarps * 32) p.lse[first + i] = -INFINITY;
+      if (p.by_segment)
+        for (int i = threadIdx.x; i < p.segs; i += kAttnWarps * 32) tasks[b * p.segs + i].more = 0;
+    }
+  };
 
   // This CTA's share. All places are counted by all CTAs, each thread a run of the sequences. A border between two shares that falls into a
   // short sequence moves to the nearer end of it, for both of them.
@@ -512,8 +508,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   __shared__ int first_b, first_s, first_pos, first_keys;
   const int per = (p.batch + kAttnWarps * 32 - 1) / (kAttnWarps * 32);
   const int b0 = min(static_cast<int>(threadIdx.x) * per, p.batch), b1 = min(b0 + per, p.batch);
-  int64_t mine = 0;
-  for (int b = b0; b < b1; ++b) mine += cost_of(keys_of(p, b));
+  const int keys0 = b0 < b1 ? keys_of(p, b0) : 0;              // of the run's first
+  int64_t mine = cost_of(keys0);
+  for (int b = b0 + 1; b < b1; ++b) mine += cost_of(keys_of(p, b));
   mine *= p.segs;
   int64_t before = mine;
 #pragma unroll
@@ -533,7 +530,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   const int ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), (total + kAttnWarps - 1) / kAttnWarps));
   float4* part_at = reinterpret_cast<float4*>(p.ws + ((gridDim.x * sizeof(JoinTask) + 255) & ~static_cast<size_t>(255)));
   constexpr int PART4 = S::PART / 16;                          // float4s of a part
-  if (cta >= ctas) return;
+  if (cta >= ctas) {
+    write_zeros();
+    return;
+  }
   // c * total / ctas without the long product
   const bool small = total <= UINT32_MAX;
   const int64_t q0 = small ? static_cast<uint32_t>(total) / static_cast<uint32_t>(ctas) : total / ctas;
@@ -545,7 +545,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
     if (u == total && threadIdx.x == 0) border[i] = total;
     if (u < before || u >= before + mine) continue;
     int64_t r = u - before;
-    int b = b0, keys = keys_of(p, b);
+    int b = b0, keys = keys0;
     for (; r >= static_cast<int64_t>(cost_of(keys)) * p.segs; keys = keys_of(p, ++b)) r -= static_cast<int64_t>(cost_of(keys)) * p.segs;
     const int cost = cost_of(keys), s = static_cast<int>(r <= UINT32_MAX ? static_cast<uint32_t>(r) / static_cast<uint32_t>(cost) : r / cost);
     int pos = static_cast<int>(r - static_cast<int64_t>(s) * cost);
@@ -559,7 +559,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
     }
   }
   __syncthreads();
-  if (border[1] <= border[0]) return;
+  if (border[1] <= border[0]) {
+    write_zeros();
+    return;
+  }
   Walk w;
   w.b = first_b;
   w.s = first_s;
@@ -591,16 +594,13 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   copy.w = w;
   copy.start(p, warp, lane);
 #pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) copy.issue(p, ring + i * S::STAGE, warp, lane);
+  for (int i = 0; i < kStages - 1; ++i) copy.issue(p, base + ring + i * S::STAGE, warp, lane);
   int stage = 0;
+  write_zeros();                                               // while the first keys are on their way
 
   // Row g of a 16-key tile is key own0 of its first eight, row g + 8 the same of the second; the keys of a lane's columns of the value product
   // then are t and 7 - t of both eights.
   const int own0 = (g & 1) ? 7 - (g >> 1) : g >> 1;
-  const float vt = MX ? 1.0f : *p.v_tscale;
-  const float kt = p.scale * (MX ? 1.0f : *p.k_tscale);
-  const float sign = kt < 0.0f ? -1.0f : 1.0f;                 // of the scale: goes to the queries, so that a column's factor is positive
-
   for (Walk next; w.n > 0; w = next) {
     const int h = head_of(p, w.s), row0 = (w.s - h * p.tiles) * (8 * NT);
     // queries of this tile as FP16 fragments, and what a score has to be multiplied with
@@ -651,7 +651,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
     const int from = w.j + static_cast<int>(static_cast<int64_t>(w.n) * warp / kAttnWarps);
     const int to = w.j + static_cast<int>(static_cast<int64_t>(w.n) * (warp + 1) / kAttnWarps);
     for (int u = from; u < to; ++u) {
-      copy.issue(p, ring + (stage == 0 ? kStages - 1 : stage - 1) * S::STAGE, warp, lane);
+      copy.issue(p, base + ring + (stage == 0 ? kStages - 1 : stage - 1) * S::STAGE, warp, lane);
       asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
       __syncwarp();
       const uint32_t here = ring + stage * S::STAGE, kscales = here + 2 * S::CODES, vscales = kscales + S::SCALES;
@@ -673,8 +673,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
 #pragma unroll
           for (int i = 0; i < (NB + 3) / 4; ++i) {
             if constexpr (NB == 2) {
-              f0[i] = smem_load_u16(kscales + r0 * NB);
-              f1[i] = smem_load_u16(kscales + r1 * NB);
+              f0[i] = smem_load<uint16_t>(kscales + r0 * NB);
+              f1[i] = smem_load<uint16_t>(kscales + r1 * NB);
             } else {
               f0[i] = smem_load<uint32_t>(kscales + r0 * NB + 4 * i);
               f1[i] = smem_load<uint32_t>(kscales + r1 * NB + 4 * i);
@@ -707,14 +707,14 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
               const int piece = ((t >> 1) ^ turn<D>(own0)) * 16 + (t & 1) * 8;
               const uint2 v0 = smem_load<uint2>(here + r0 * 32 + piece), v1 = smem_load<uint2>(here + r1 * 32 + piece);
               c0[0] = v0.x; c0[1] = v0.y; c1[0] = v1.x; c1[1] = v1.y;
-              x0[0] = e4m3_pair(smem_load_u8(kscales + r0 * NB + t) * 0x0101u);
-              x1[0] = e4m3_pair(smem_load_u8(kscales + r1 * NB + t) * 0x0101u);
+              x0[0] = e4m3_pair(smem_load<uint8_t>(kscales + r0 * NB + t) * 0x0101u);
+              x1[0] = e4m3_pair(smem_load<uint8_t>(kscales + r1 * NB + t) * 0x0101u);
             } else {
               const int piece = ((hh * 4 + t) ^ turn<D>(own0)) * 16;
               const uint4 v0 = smem_load<uint4>(here + r0 * (D / 2) + piece), v1 = smem_load<uint4>(here + r1 * (D / 2) + piece);
               c0[0] = v0.x; c0[1] = v0.y; c0[2] = v0.z; c0[3] = v0.w;
               c1[0] = v1.x; c1[1] = v1.y; c1[2] = v1.z; c1[3] = v1.w;
-              const uint32_t y0 = e4m3_pair(smem_load_u16(kscales + r0 * NB + hh * 8 + 2 * t)), y1 = e4m3_pair(smem_load_u16(kscales + r1 * NB + hh * 8 + 2 * t));
+              const uint32_t y0 = e4m3_pair(smem_load<uint16_t>(kscales + r0 * NB + hh * 8 + 2 * t)), y1 = e4m3_pair(smem_load<uint16_t>(kscales + r1 * NB + hh * 8 + 2 * t));
               x0[0] = __byte_perm(y0, 0, 0x1010); x0[1] = __byte_perm(y0, 0, 0x3232);
               x1[0] = __byte_perm(y1, 0, 0x1010); x1[1] = __byte_perm(y1, 0, 0x3232);
             }
@@ -755,35 +755,32 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
           top[n][c] = fmaxf(fmaxf(s[0][n][c], s[0][n][c + 2]), fmaxf(s[1][n][c], s[1][n][c + 2])) * by[n][c];
           move |= top[n][c] > a.m[n][c] + (kWeightTop + kWeightRoom);
         }
-      // MXFP4: largest and smallest scale code of the unit's values (a code of 0 comes with zeros). Code c is taken as the FP16 number
-      // 2^(c - vref + 5), which is exact and in range for c in [vref - 19, vref + 8]. Units of a wider range take the other way below.
-      int key_top = 0, vtop = 0;
-      bool wide = false, refer = false;
+      // MXFP4: a scale code c of the values is taken as the FP16 number 2^(c - vref + 5), which is exact and in range for c in
+      // [vref - 19, vref + 8]; a code of 0 comes with zeros, whatever it is taken for. A lane looks at its key's codes: largest, and
+      // smallest but 0, less 1.
+      int key_top = 0, key_low = 0xFFFF;
+      bool wide = false;
       uint32_t vword[(NB + 3) / 4];
       if constexpr (MX) {
-        int low = 255;
+        uint32_t top2 = 0, low2 = 0xFFFFFFFFu;
 #pragma unroll
         for (int i = 0; i < (NB + 3) / 4; ++i) {
-          if constexpr (NB == 2) vword[i] = smem_load_u16(vscales + lane * NB);
+          if constexpr (NB == 2) vword[i] = __byte_perm(smem_load<uint16_t>(vscales + lane * NB), 0, 0x4140);
           else vword[i] = smem_load<uint32_t>(vscales + lane * NB + 4 * i);
+          const uint32_t even = NB == 2 ? vword[i] : vword[i] & 0x00FF00FFu, odd = NB == 2 ? even : __byte_perm(vword[i], 0, 0x4341);
+          top2 = __vmaxu2(top2, __vmaxu2(even, odd));
+          low2 = __viaddmin_u16x2(even, 0xFFFFFFFFu, __viaddmin_u16x2(odd, 0xFFFFFFFFu, low2));
         }
         if (key0 + lane < w.keys) {
-#pragma unroll
-          for (int i = 0; i < NB; ++i) {
-            const int code = (vword[i / 4] >> (8 * (i & 3))) & 0xFF;
-            key_top = max(key_top, code);
-            low = min(low, code == 0 ? 255 : code);
-          }
+          key_top = max(top2 & 0xFFFFu, top2 >> 16);
+          key_low = min(low2 & 0xFFFFu, low2 >> 16);
         }
-        vtop = __reduce_max_sync(0xFFFFFFFFu, key_top);
-        low = __reduce_min_sync(0xFFFFFFFFu, low);
-        wide = vtop - low > 19;
-        refer = vtop > vref + 8 || low < vref - 19;
-        move |= wide | refer;
+        move |= key_top > vref + 8 || key_low < vref - 20;
       }
       if (__any_sync(0xFFFFFFFFu, move)) {
         float was[NT][2];                                      // logarithm of what the weights so far have to be multiplied with
         bool drop = false;
+        const int vtop = MX ? __reduce_max_sync(0xFFFFFFFFu, key_top) : 0, vlow = MX ? __reduce_min_sync(0xFFFFFFFFu, key_low) + 1 : 0;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -798,7 +795,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
             drop |= was[n][c] + ve[n][c] - static_cast<float>(vtop - 132) > 60.0f;       // sums in units so small could overflow
           }
         if constexpr (MX) {
-          wide |= refer && __any_sync(0xFFFFFFFFu, drop);
+          const bool refer = vtop > vref + 8 || vlow < vref - 19;
+          wide = vtop - vlow > 19 || (refer && __any_sync(0xFFFFFFFFu, drop));
           if (wide) {
             // A key's value codes relative to its own largest one, exact over 36 binades, with that one's power of two in the weight: the
             // weights of the value product are kept in FP16's range by a maximum of their own.
@@ -843,44 +841,49 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
 
       // weights, as fragments of the value product
       uint32_t pf[2][NT][2];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const float2 by2 = make_float2(by[n][0], by[n][1]), m2 = make_float2(-a.m[n][0], -a.m[n][1]);
-        float2 l2 = make_float2(a.l[n][0], a.l[n][1]);
+      if (MX && wide) {
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            const float2 x = __ffma2_rn(make_float2(s[half][n][2 * r], s[half][n][2 * r + 1]), by2, m2);
-            const float2 e = make_float2(exp2_approx(x.x), exp2_approx(x.y));
-            l2 = __fadd2_rn(l2, e);
-            if (MX && wide) {
-              const float up = __shfl_sync(0xFFFFFFFFu, static_cast<float>(key_top - 140), half * 16 + r * 8 + own0);
-              pf[half][n][r] = transpose8x8(f16x2(exp2_approx(x.x + up - ve[n][0]), exp2_approx(x.y + up - ve[n][1])));
-            } else {
-              pf[half][n][r] = transpose8x8(f16x2(e.x, e.y));
+            const float up = __shfl_sync(0xFFFFFFFFu, static_cast<float>(key_top - 140), half * 16 + r * 8 + own0);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const float x0 = fmaf(s[half][n][2 * r], by[n][0], -a.m[n][0]), x1 = fmaf(s[half][n][2 * r + 1], by[n][1], -a.m[n][1]);
+              a.l[n][0] += exp2_approx(x0);
+              a.l[n][1] += exp2_approx(x1);
+              pf[half][n][r] = transpose8x8(f16x2(exp2_approx(x0 + up - ve[n][0]), exp2_approx(x1 + up - ve[n][1])));
             }
           }
-        a.l[n][0] = l2.x;
-        a.l[n][1] = l2.y;
-      }
-      if (MX && wide) {
         // multipliers, a key per lane, in pairs of a key and the last, second last, ... of its group of eight
-        constexpr int NR = NB / 2 > 0 ? NB / 2 : 1;            // FP16 pairs of a row
-        uint32_t vr[NR];
-#pragma unroll
-        for (int i = 0; i < NR; ++i) {
-          const int c0 = (vword[i / 2] >> (16 * (i & 1))) & 0xFF, c1 = (vword[i / 2] >> (16 * (i & 1) + 8)) & 0xFF;
-          vr[i] = f16x2(__uint_as_float(static_cast<uint32_t>(max(c0 - key_top + 140, 0)) << 23), __uint_as_float(static_cast<uint32_t>(max(c1 - key_top + 140, 0)) << 23));
-        }
         const bool low = (lane & 4) == 0;
         const uint32_t vto = vmul + ((lane >> 3) * 4 + (low ? lane & 3 : 3 - (lane & 3))) * NB * 4;
 #pragma unroll
-        for (int i = 0; i < NR; ++i) {
-          const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, vr[i], 7);
-          if (low) smem_store(vto + 8 * i, __byte_perm(vr[i], got, 0x5410), __byte_perm(vr[i], got, 0x7632));
+        for (int i = 0; i < NB / 2; ++i) {
+          const uint32_t two = NB == 2 ? __byte_perm(vword[0], 0, 0x4420) : vword[i / 2] >> (16 * (i & 1));
+          const int c0 = two & 0xFF, c1 = (two >> 8) & 0xFF;
+          const uint32_t own = f16x2(__uint_as_float(static_cast<uint32_t>(max(c0 - key_top + 140, 0)) << 23), __uint_as_float(static_cast<uint32_t>(max(c1 - key_top + 140, 0)) << 23));
+          const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, own, 7);
+          if (low) smem_store(vto + 8 * i, make_uint2(__byte_perm(own, got, 0x5410), __byte_perm(own, got, 0x7632)));
         }
         __syncwarp();
+      } else {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const float2 by2 = make_float2(by[n][0], by[n][1]), m2 = make_float2(-a.m[n][0], -a.m[n][1]);
+          float2 l2 = make_float2(a.l[n][0], a.l[n][1]);
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const float2 x = __ffma2_rn(make_float2(s[half][n][2 * r], s[half][n][2 * r + 1]), by2, m2);
+              const float2 e = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+              l2 = __fadd2_rn(l2, e);
+              pf[half][n][r] = transpose8x8(f16x2(e.x, e.y));
+            }
+          a.l[n][0] = l2.x;
+          a.l[n][1] = l2.y;
+        }
       }
 
       // values
@@ -888,23 +891,23 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       for (int hh = 0; hh < HALVES; ++hh) {
         uint32_t y[2][2];                                      // multipliers of the lane's block, for the pairs of keys t and 7 - t
         const int block = FMT == QF_FMT_NVFP4 ? (D == 64 ? g >> 1 : hh * 8 + g) : (D == 64 ? g >> 2 : hh * 4 + (g >> 1));
+        if (MX && wide) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+          for (int half = 0; half < 2; ++half)
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            if (MX && wide) {
-              y[half][r] = smem_load<uint32_t>(vmul + (((half * 2 + r) * 4 + t) * NB + block) * 4);
-              continue;
+            for (int r = 0; r < 2; ++r) y[half][r] = smem_load<uint32_t>(vmul + (((half * 2 + r) * 4 + t) * NB + block) * 4);
+        } else {
+          const uint32_t up = (static_cast<uint32_t>(20 - vref) & 0xFFFFu) * 0x10001u;
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const uint32_t first = smem_load<uint8_t>(vscales + (half * 16 + r * 8 + t) * NB + block);
+              const uint32_t second = smem_load<uint8_t>(vscales + (half * 16 + r * 8 + 7 - t) * NB + block);
+              if constexpr (MX) y[half][r] = __viaddmax_s16x2_relu(__byte_perm(first, second, 0x5410), up, 0) << 10;
+              else y[half][r] = e4m3_pair(__byte_perm(first, second, 0x0040));
             }
-            const uint32_t first = smem_load_u8(vscales + (half * 16 + r * 8 + t) * NB + block);
-            const uint32_t second = smem_load_u8(vscales + (half * 16 + r * 8 + 7 - t) * NB + block);
-            if constexpr (MX) {
-              const uint32_t d = static_cast<uint32_t>(20 - vref) & 0xFFFFu;
-              y[half][r] = __viaddmax_s16x2_relu(__byte_perm(first, second, 0x5410), d * 0x10001u, 0) << 10;
-            } else {
-              y[half][r] = e4m3_pair(__byte_perm(first, second, 0x0040));
-            }
-          }
+        }
         if (key0 + kUnitKeys > w.keys) {                       // what stands behind the last key
 #pragma unroll
           for (int half = 0; half < 2; ++half)
@@ -981,29 +984,29 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int n = 0; n < NT; ++n)
-            smem_store(at + (i * NT + n) * 512, __float_as_uint(a.o[i][n][0]), __float_as_uint(a.o[i][n][1]), __float_as_uint(a.o[i][n][2]), __float_as_uint(a.o[i][n][3]));
+            smem_store(at + (i * NT + n) * 512, make_float4(a.o[i][n][0], a.o[i][n][1], a.o[i][n][2], a.o[i][n][3]));
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          smem_store(at + (MT * NT + n) * 512, __float_as_uint(a.m[n][0]), __float_as_uint(a.l[n][0]), __float_as_uint(a.m[n][1]), __float_as_uint(a.l[n][1]));
+          smem_store(at + (MT * NT + n) * 512, make_float4(a.m[n][0], a.l[n][0], a.m[n][1], a.l[n][1]));
       }
       __syncthreads();
       if (warp < d) {
         const uint32_t at = parts + warp * S::PART + lane * 16;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const uint4 v = smem_load<uint4>(at + (MT * NT + n) * 512);
+          const float4 v = smem_load<float4>(at + (MT * NT + n) * 512);
           float fa[2], fb[2];
-          join_weights(a.m[n][0], __uint_as_float(v.x), a.m[n][0], fa[0], fb[0]);
-          join_weights(a.m[n][1], __uint_as_float(v.z), a.m[n][1], fa[1], fb[1]);
-          a.l[n][0] = a.l[n][0] * fa[0] + __uint_as_float(v.y) * fb[0];
-          a.l[n][1] = a.l[n][1] * fa[1] + __uint_as_float(v.w) * fb[1];
+          join_weights(a.m[n][0], v.x, a.m[n][0], fa[0], fb[0]);
+          join_weights(a.m[n][1], v.z, a.m[n][1], fa[1], fb[1]);
+          a.l[n][0] = a.l[n][0] * fa[0] + v.y * fb[0];
+          a.l[n][1] = a.l[n][1] * fa[1] + v.w * fb[1];
 #pragma unroll
           for (int i = 0; i < MT; ++i) {
-            const uint4 o = smem_load<uint4>(at + (i * NT + n) * 512);
-            a.o[i][n][0] = a.o[i][n][0] * fa[0] + __uint_as_float(o.x) * fb[0];
-            a.o[i][n][1] = a.o[i][n][1] * fa[1] + __uint_as_float(o.y) * fb[1];
-            a.o[i][n][2] = a.o[i][n][2] * fa[0] + __uint_as_float(o.z) * fb[0];
-            a.o[i][n][3] = a.o[i][n][3] * fa[1] + __uint_as_float(o.w) * fb[1];
+            const float4 o = smem_load<float4>(at + (i * NT + n) * 512);
+            a.o[i][n][0] = a.o[i][n][0] * fa[0] + o.x * fb[0];
+            a.o[i][n][1] = a.o[i][n][1] * fa[1] + o.y * fb[1];
+            a.o[i][n][2] = a.o[i][n][2] * fa[0] + o.z * fb[0];
+            a.o[i][n][3] = a.o[i][n][3] * fa[1] + o.w * fb[1];
           }
         }
       }
@@ -1062,8 +1065,8 @@ __global__ void __launch_bounds__(1024) kv_join_kernel(const __grid_constant__ K
   const float4* parts = reinterpret_cast<const float4*>(p.ws + ((ctas * sizeof(JoinTask) + 255) & ~static_cast<size_t>(255))) +
                         static_cast<int64_t>(task.cta) * 2 * PART4 + lane;
   const int h = head_of(p, task.seg), row0 = (task.seg - h * p.tiles) * (8 * NT) + 2 * t;
-  extern __shared__ __align__(16) uint8_t smem[];
-  float4* met = reinterpret_cast<float4*>(smem);               // sums and weights of every warp
+  extern __shared__ __align__(128) uint8_t smem[];
+  float4* met = reinterpret_cast<float4*>(smem);               // sums and weights of a warp, from the second half of the warps
   const bool many = task.more >= 8;
   const int first = many ? warp : 0, step = many ? warps : 1;
   for (int tile = many ? blockIdx.y : blockIdx.y * warps + warp; tile < TILES; tile += gridDim.y * (many ? 1 : warps)) {
@@ -1093,12 +1096,15 @@ __global__ void __launch_bounds__(1024) kv_join_kernel(const __grid_constant__ K
         if (k0 + j * step <= task.more) add(v[j], w[j]);
     }
     if (many) {
-      met[warp * 64 + lane] = o;
-      met[warp * 64 + 32 + lane] = ml;
-      __syncthreads();
-      if (warp == 0)
-        for (int k = 1; k < warps; ++k) add(met[k * 64 + lane], met[k * 64 + 32 + lane]);
-      __syncthreads();
+      for (int d = warps / 2; d > 0; d /= 2) {
+        if (warp >= d && warp < 2 * d) {
+          met[(warp - d) * 64 + lane] = o;
+          met[(warp - d) * 64 + 32 + lane] = ml;
+        }
+        __syncthreads();
+        if (warp < d) add(met[warp * 64 + lane], met[warp * 64 + 32 + lane]);
+        __syncthreads();
+      }
       if (warp != 0) continue;
     }
     const int i = tile / NT, n = tile % NT;
@@ -1134,8 +1140,8 @@ cudaError_t attend(KvAttn& p, cudaStream_t st) {
   if (p.max_keys <= kWhole * kUnitKeys) return cudaSuccess;    // nothing can have been cut
   // the fewer sequences, the more parts each may have: up to a CTA per value tile
   const int tasks = p.by_segment ? static_cast<int>(segments) : grid;
-  const int share = 4 * kNumSMs / tasks, threads = grid / tasks < 32 ? 256 : 1024;
-  return launch_overlapping(kv_join_kernel<FMT, D, NT>, dim3(tasks, share < 1 ? 1 : share < S::MT * NT ? share : S::MT * NT), threads, threads * 32, st, p, grid);
+  const int share = 4 * kNumSMs / tasks, parts = grid / tasks, threads = parts < 32 ? 256 : parts < 128 ? 512 : 1024;
+  return launch_overlapping(kv_join_kernel<FMT, D, NT>, dim3(tasks, share < 1 ? 1 : share < S::MT * NT ? share : S::MT * NT), threads, threads * 16, st, p, grid);
 }
 
 template <int FMT>
