@@ -217,7 +217,7 @@ cudaError_t launch_rows(void (*kernel)(KvRows), KvRows& p, int parts, int kinds,
 constexpr int kUnitKeys = 32;
 constexpr int kAttnWarps = 4;                 // of a CTA
 constexpr int kStages = 2;                    // units a warp has in shared memory or on the way
-constexpr int kPieceCost = 4;                 // what a sequence's queries, meeting and result cost, in units
+constexpr int kPieceCost = 8;                 // what a sequence's queries, meeting and result cost, in units
 constexpr int kWhole = 12;                    // sequences of up to so many units are not cut
 constexpr float kWeightTop = 6.0f, kWeightRoom = 8.0f;       // weights start at up to 2^6 and may reach 2^14 before their base is moved
 
@@ -254,7 +254,7 @@ struct Shape {
   static constexpr int MT = D / 16;                                                        // 16-row tiles of the value product
   static constexpr int PART = (MT * NT * 4 + 4 * NT) * 32 * 4;                             // a warp's sums and maxima, bytes
   static constexpr int SMEM = kAttnWarps * WARP + kAttnWarps / 2 * PART;
-  static constexpr int FIT = 232448 / (SMEM + 1024), WANT = D == 256 ? 3 - NT : D == 128 ? 4 - NT : 4;
+  static constexpr int FIT = 232448 / (SMEM + 1024), WANT = D == 256 ? 2 : D == 128 ? (NT == 1 ? 3 : 2) : NT < 3 ? 4 : 6 - NT;
   static constexpr int CTAS = FIT < WANT ? FIT : WANT;                                     // of an SM
 };
 
@@ -1144,26 +1144,36 @@ cudaError_t attend(KvAttn& p, cudaStream_t st) {
   return launch_overlapping(kv_join_kernel<FMT, D, NT>, dim3(tasks, share < 1 ? 1 : share < S::MT * NT ? share : S::MT * NT), threads, threads * 16, st, p, grid);
 }
 
+// Query rows of a tile, in units of 8, at most: what registers hold next to the decoded words. (Heads of 256 with 16 rows: one CTA an SM and
+// spills, 100 us for 32 sequences of 4096 keys where two tiles of 8 rows take 73.)
+constexpr int tile_most(int head_dim) { return head_dim == 64 ? 4 : head_dim == 128 ? 3 : 1; }
+
+// The cache is decoded once per tile, which costs as much as the products of 14 rows (32 sequences of 4096 keys, heads of 128: 38, 52 and
+// 66 us for 8, 16 and 24 rows): as few tiles as can be, evenly filled.
 template <int FMT>
 cudaError_t attend_format(KvAttn& p, int head_dim, cudaStream_t st) {
-  const bool two = p.rows > 8;
-  p.tiles = (p.rows + (two ? 15 : 7)) / (two ? 16 : 8);
+  const int eights = (p.rows + 7) / 8, most = tile_most(head_dim);
+  p.tiles = (eights + most - 1) / most;
+  const int nt = (eights + p.tiles - 1) / p.tiles;
   p.segs = p.tiles * p.kv_heads;
-  if (head_dim == 64) return two ? attend<FMT, 64, 2>(p, st) : attend<FMT, 64, 1>(p, st);
-  if (head_dim == 128) return two ? attend<FMT, 128, 2>(p, st) : attend<FMT, 128, 1>(p, st);
-  return two ? attend<FMT, 256, 2>(p, st) : attend<FMT, 256, 1>(p, st);
+  if (head_dim == 64) return nt == 1 ? attend<FMT, 64, 1>(p, st) : nt == 2 ? attend<FMT, 64, 2>(p, st) : nt == 3 ? attend<FMT, 64, 3>(p, st) : attend<FMT, 64, 4>(p, st);
+  if (head_dim == 128) return nt == 1 ? attend<FMT, 128, 1>(p, st) : nt == 2 ? attend<FMT, 128, 2>(p, st) : attend<FMT, 128, 3>(p, st);
+  return attend<FMT, 256, 1>(p, st);
 }
 
+// Workspace: for the largest kernel of a head size, whatever the format and the tile, since how the rows are split over sequences is
+// not known when it is asked for.
 template <int FMT, int D, int NT>
-size_t part_bytes() {
+constexpr size_t part_bytes() {
   using S = Shape<FMT, D, NT>;
   return static_cast<size_t>(kNumSMs) * S::CTAS * (sizeof(JoinTask) + 2 * S::PART) + 256;
 }
-template <int D>
-size_t ws_bytes() {          // the largest, whatever the format and the tile: how the rows are split over sequences is not known here
-  const size_t a = part_bytes<QF_FMT_NVFP4, D, 1>(), b = part_bytes<QF_FMT_NVFP4, D, 2>(), c = part_bytes<QF_FMT_MXFP4, D, 1>(), d = part_bytes<QF_FMT_MXFP4, D, 2>();
-  const size_t x = a > b ? a : b, y = c > d ? c : d;
-  return x > y ? x : y;
+constexpr size_t larger(size_t a, size_t b) { return a > b ? a : b; }
+template <int D, int NT>
+constexpr size_t ws_bytes() {
+  const size_t here = larger(part_bytes<QF_FMT_NVFP4, D, NT>(), part_bytes<QF_FMT_MXFP4, D, NT>());
+  if constexpr (NT > 1) return larger(here, ws_bytes<D, NT - 1>());
+  else return here;
 }
 
 }  // namespace
@@ -1187,7 +1197,7 @@ cudaError_t launch_kv_read(const qf_kv_cache_t& c, const void* slots, bool slots
 }
 
 size_t kv_attention_ws_bytes(int64_t, int, int head_dim, int) {
-  return head_dim <= 64 ? ws_bytes<64>() : head_dim <= 128 ? ws_bytes<128>() : ws_bytes<256>();
+  return head_dim <= 64 ? ws_bytes<64, tile_most(64)>() : head_dim <= 128 ? ws_bytes<128, tile_most(128)>() : ws_bytes<256, tile_most(256)>();
 }
 
 cudaError_t launch_kv_attention(const KvAttentionArgs& a, cudaStream_t st) {

@@ -208,6 +208,70 @@ def test_a_large_ragged_batch(fmt):
 
 
 @fmts
+@pytest.mark.parametrize("batch,most,page", [(130, 400, 16), (700, 70, 32), (3000, 20, 16), (40, 385, 64)])
+def test_many_short_sequences(fmt, batch, most, page):
+    """More sequences than threads look at, than CTAs, and of the length from which on sequences are cut."""
+    r = np.random.default_rng(batch)
+    lens = [int(x) for x in r.integers(0, most + 1, batch)]
+    lens[0] = most
+    attend(fmt, lens, page, 1, 3, 64)
+
+
+@fmts
+def test_a_batch_without_keys(fmt):
+    c = random_cache(fmt, 2, 16, 2, 128)
+    q = torch.randn((300, 3, 8, 128), generator=gen(0), device="cuda").to(BF)
+    out, lse = torch.full_like(q, 7.0), torch.zeros((300, 3, 8), device="cuda")
+    api.qf_kv_attention(c, q, torch.full((300, 4), -1, dtype=torch.int32, device="cuda"), torch.zeros(300, dtype=torch.int32, device="cuda"), out=out, lse=lse)
+    assert (out == 0).all() and torch.isinf(lse).all() and (lse < 0).all()
+
+
+@fmts
+@pytest.mark.parametrize("order", ["rising", "falling", "steps"])
+def test_scores_that_move_the_maximum(fmt, order):
+    """Scores that rise by dozens from page to page, fall, or jump both ways."""
+    page, heads, dim, n = 16, 2, 128, 2000
+    c = random_cache(fmt, n // page, page, heads, dim, 9)
+    c.k_codes.fill_(0x22)
+    at = torch.arange(n // page, device="cuda")
+    level = {"rising": at % 40, "falling": 40 - at % 40, "steps": (at * 7) % 40}[order]
+    if fmt == api.FMT_NVFP4:
+        c.k_scales.copy_((0x20 + level).to(torch.uint8)[:, None, None, None].expand_as(c.k_scales))
+        c.k_tscale.fill_(1.0)
+    else:
+        c.k_scales.copy_((110 + level // 2).to(torch.uint8)[:, None, None, None].expand_as(c.k_scales))
+    q = (1.0 + torch.rand((1, 2, 8, dim), generator=gen(2), device="cuda")).to(BF)
+    table = at.to(torch.int32)[None]
+    for scale in (dim ** -0.5, 0.01, -0.02):
+        out, lse = api.qf_kv_attention(c, q, table, torch.tensor([n], dtype=torch.int32, device="cuda"), softmax_scale=scale, want_lse=True)
+        check_attention(c, q, table, [n], scale, out, lse)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("scale", [0.001, 0.05])
+def test_value_ranges_that_change_along_a_sequence(dim, scale):
+    """MXFP4 pages whose value scales lie close together, far apart, far below or above the page before, or are those of zeros."""
+    page, heads, n = 16, 2, 3000
+    g = gen(dim)
+    c = random_cache(api.FMT_MXFP4, n // page + 1, page, heads, dim, 9)
+    kinds = ((120, 128), (100, 140), (60, 70), (180, 190), (127, 128), (108, 136))
+    for i in range(c.pages):
+        low, high = kinds[(i * i + i // 7) % len(kinds)]
+        c.v_scales[i].copy_(torch.randint(low, high, c.v_scales[i].shape, generator=g, device="cuda", dtype=torch.uint8))
+        if i % 9 == 4:
+            c.v_scales[i, :, ::3] = 0
+            c.v_codes[i, :, ::3] = 0
+    table = torch.randperm(c.pages, generator=g, device="cuda").to(torch.int32)[None]
+    for group, q_len, m in ((4, 1, n), (5, 4, n - 7), (1, 1, 100)):
+        q = torch.randn((1, q_len, heads * group, dim), generator=g, device="cuda").to(BF)
+        out, lse = api.qf_kv_attention(c, q, table, torch.tensor([m], dtype=torch.int32, device="cuda"), softmax_scale=scale, want_lse=True)
+        check_attention(c, q, table, [m], scale, out, lse)
+    flat = api.KvCache(api.FMT_MXFP4, c.k_codes, c.k_scales, c.v_codes, torch.full_like(c.v_scales, 20), None, None)      # all far below 1
+    out, lse = api.qf_kv_attention(flat, q, table, torch.tensor([m], dtype=torch.int32, device="cuda"), softmax_scale=scale, want_lse=True)
+    check_attention(flat, q, table, [m], scale, out, lse)
+
+
+@fmts
 @pytest.mark.parametrize("dim", [64, 128, 256])
 def test_whatever_stands_behind_the_last_key(fmt, dim):
     """Places that no key owns hold NaN scales and extreme codes; unused table entries hold nonsense."""
