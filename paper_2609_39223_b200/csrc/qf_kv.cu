@@ -1,7 +1,10 @@
 // The 4-bit key/value cache: keys and values quantized as they are written, rows read back, and attention of a few tokens over it.
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include "qf_qdq_body.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace qf {
 namespace {
@@ -169,17 +172,20 @@ KvRows kv_rows(const qf_kv_cache_t& c, const void* slots, bool slots64, int64_t 
 }
 
 template <typename... Params, typename... Args>
-cudaError_t launch_overlapping(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, Args... args) {
+cudaError_t launch_overlapping(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, Args... args) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
@@ -192,7 +198,7 @@ cudaError_t launch_rows(void (*kernel)(KvRows), KvRows& p, int parts, int kinds,
   const int64_t even = p.tokens / (12 * kNumSMs * 4 * p.side) * (4 * p.side);
   const int64_t each = even == 0 ? p.side : even < turns * p.side ? even : turns * p.side;
   p.each = static_cast<int>(each < kRowsTokens ? each : kRowsTokens);
-  return launch_overlapping(kernel, dim3(static_cast<unsigned>((p.tokens + p.each - 1) / p.each)), kQdqThreads, 0, st, p);
+  return launch_overlapping(kernel, dim3(static_cast<unsigned>((p.tokens + p.each - 1) / p.each)), kQdqThreads, 0, st, 1, p);
 }
 
 // ---- attention -----------------------------------------------------------------------------------------------------------
@@ -219,6 +225,7 @@ constexpr int kAttnWarps = 4;                 // of a CTA
 constexpr int kStages = 2;                    // units a warp has in shared memory or on the way
 constexpr int kPieceCost = 8;                 // what a sequence's queries, meeting and result cost, in units
 constexpr int kWhole = 12;                    // sequences of up to so many units are not cut
+constexpr int kDirectUnits = 24;              // of a CTA, where every sequence gets CTAs of its own
 constexpr float kWeightTop = 6.0f, kWeightRoom = 8.0f;       // weights start at up to 2^6 and may reach 2^14 before their base is moved
 
 struct KvAttn {
@@ -238,6 +245,7 @@ struct KvAttn {
   int batch, pages, max_pages, page_size, max_keys;
   int q_len, q_heads, kv_heads, group;
   int rows, tiles, segs;                      // query rows of a key head; tiles of them; (key head, tile) pairs of a sequence
+  int split;                                  // CTAs of a segment, a cluster, where each has its own
   bool by_segment;                            // JoinTasks are numbered by segment, not by CTA
   int64_t page_codes;                         // bytes of codes in a page
   float scale;                                // times log2 e
@@ -460,15 +468,70 @@ __device__ __forceinline__ int dim_of(int i, int g) {
 }
 
 constexpr float kNoWeights = -1e30f;           // base of a column without weights: far below any score, and finite
-__device__ __forceinline__ void join_weights(float ma, float mb, float& m, float& fa, float& fb) {
-  m = fmaxf(ma, mb);
-  fa = exp2_approx(ma - m);
-  fb = exp2_approx(mb - m);
+// Power of two that brings a sum of weights into [1/4, 1/2) (zero stays zero); its base moves by what is returned in `by`. MXFP4's values
+// may fill FP32's range: sums of them stay in it as long as their weights add up to less than one.
+__device__ __forceinline__ float even_out(float l, float& by) {
+  const int e = static_cast<int>(__float_as_uint(l) >> 23);
+  by = static_cast<float>(e - 125);
+  return __uint_as_float(static_cast<uint32_t>(252 - e) << 23);
 }
+// Two columns of weights into one: factors of the sums that belong to them, base and sum.
+template <bool EVEN>
+__device__ __forceinline__ void join_weights(float& m, float& l, float mb, float lb, float& fa, float& fb) {
+  const float most = fmaxf(m, mb);
+  fa = exp2_approx(m - most);
+  fb = exp2_approx(mb - most);
+  l = l * fa + lb * fb;
+  m = most;
+  if constexpr (EVEN) {
+    float by;
+    const float f = even_out(l, by);
+    fa *= f;
+    fb *= f;
+    l *= f;
+    m += by;
+  }
+}
+
+// A value tile's sums over several parts, with the bases and sums of the lane's two columns.
+template <bool EVEN>
+struct Joint {
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f), ml = make_float4(kNoWeights, 0.0f, kNoWeights, 0.0f);
+  __device__ __forceinline__ void add(const float4& v, const float4& w) {
+    float fa[2], fb[2];
+    join_weights<EVEN>(ml.x, ml.y, w.x, w.y, fa[0], fb[0]);
+    join_weights<EVEN>(ml.z, ml.w, w.z, w.w, fa[1], fb[1]);
+    o.x = o.x * fa[0] + v.x * fb[0];
+    o.y = o.y * fa[1] + v.y * fb[1];
+    o.z = o.z * fa[0] + v.z * fb[0];
+    o.w = o.w * fa[1] + v.w * fb[1];
+  }
+};
 
 __device__ __forceinline__ float log_sum(float m, float l) { return l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY; }
 
-template <int FMT, int D, int NT>
+__device__ __forceinline__ float4* parts_of(const KvAttn& p, int grid) {
+  return reinterpret_cast<float4*>(p.ws + ((grid * sizeof(JoinTask) + 255) & ~static_cast<size_t>(255)));
+}
+
+template <int D, int NT, bool EVEN>
+__device__ __forceinline__ void write_tile(const KvAttn& p, const Joint<EVEN>& sum, int b, int segment, int tile, int lane, float vt) {
+  const int h = head_of(p, segment), i = tile / NT, n = tile % NT, g = lane >> 2, t = lane & 3;
+  const int row0 = (segment - h * p.tiles) * (8 * NT) + 8 * n + 2 * t;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int row = row0 + c;
+    if (row >= p.rows) continue;
+    const int token = token_of(p, row), head = h * p.group + (row - token * p.group);
+    const int64_t at = (static_cast<int64_t>(b) * p.q_len + token) * p.q_heads + head;
+    const float l = c ? sum.ml.w : sum.ml.y, f = l > 0.0f ? vt / l : 0.0f;
+    *reinterpret_cast<uint32_t*>(p.out + at * D + dim_of<D>(i, g)) = pack_bf16x2((c ? sum.o.y : sum.o.x) * f, (c ? sum.o.w : sum.o.z) * f);
+    if (p.lse && i == 0 && g == 0) p.lse[at] = log_sum(c ? sum.ml.z : sum.ml.x, l);
+  }
+}
+
+// DIRECT: a cluster of p.split CTAs (or one CTA) to every segment, in place of equal shares of all of them.
+template <int FMT, int D, int NT, bool DIRECT>
 __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv_attention_kernel(const __grid_constant__ KvAttn p) {
   using S = Shape<FMT, D, NT>;
   constexpr int MT = S::MT, NB = S::NB, HALVES = S::HALVES;
@@ -482,95 +545,106 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   const uint32_t ring = warp * S::WARP, vmul = ring + kStages * S::STAGE, parts = kAttnWarps * S::WARP;
   JoinTask* tasks = reinterpret_cast<JoinTask*>(p.ws);
   const int cta = blockIdx.x;
-  if (!p.by_segment && threadIdx.x == 0) tasks[cta].more = 0;
+  if (!DIRECT && !p.by_segment && threadIdx.x == 0) tasks[cta].more = 0;
 
   const float vt = MX ? 1.0f : *p.v_tscale;
   const float kt = p.scale * (MX ? 1.0f : *p.k_tscale);
   const float sign = kt < 0.0f ? -1.0f : 1.0f;                 // of the scale: goes to the queries, so that a column's factor is positive
 
-  // Sequences without keys: zeros, a sequence to a CTA.
-  const auto write_zeros = [&]() {
-    for (int b = cta; b < p.batch; b += gridDim.x) {
-      if (keys_of(p, b) > 0) continue;
-      const int64_t first = static_cast<int64_t>(b) * p.q_len * p.q_heads, rows = static_cast<int64_t>(p.q_len) * p.q_heads;
-      uint4* out = reinterpret_cast<uint4*>(p.out + first * D);
-      for (int64_t i = threadIdx.x; i < rows * (D / 8); i += kAttnWarps * 32) out[i] = make_uint4(0, 0, 0, 0);
-      if (p.lse)
-        for (int64_t i = threadIdx.x; i < rows; i += kAttnWarps * 32) p.lse[first + i] = -INFINITY;
-      if (p.by_segment)
-        for (int i = threadIdx.x; i < p.segs; i += kAttnWarps * 32) tasks[b * p.segs + i].more = 0;
-    }
+  // A sequence without keys: zeros. (With keys: nothing.)
+  const auto write_zeros = [&](int b) {
+    if (keys_of(p, b) > 0) return;
+    const int64_t first = static_cast<int64_t>(b) * p.q_len * p.q_heads, rows = static_cast<int64_t>(p.q_len) * p.q_heads;
+    uint4* out = reinterpret_cast<uint4*>(p.out + first * D);
+    for (int64_t i = threadIdx.x; i < rows * (D / 8); i += kAttnWarps * 32) out[i] = make_uint4(0, 0, 0, 0);
+    if (p.lse)
+      for (int64_t i = threadIdx.x; i < rows; i += kAttnWarps * 32) p.lse[first + i] = -INFINITY;
+    if (p.by_segment)
+      for (int i = threadIdx.x; i < p.segs; i += kAttnWarps * 32) tasks[b * p.segs + i].more = 0;
   };
 
-  // This CTA's share. All places are counted by all CTAs, each thread a run of the sequences. A border between two shares that falls into a
-  // short sequence moves to the nearer end of it, for both of them.
-  __shared__ int64_t warp_places[kAttnWarps], border[2];
-  __shared__ int first_b, first_s, first_pos, first_keys;
-  const int per = (p.batch + kAttnWarps * 32 - 1) / (kAttnWarps * 32);
-  const int b0 = min(static_cast<int>(threadIdx.x) * per, p.batch), b1 = min(b0 + per, p.batch);
-  const int keys0 = b0 < b1 ? keys_of(p, b0) : 0;              // of the run's first
-  int64_t mine = cost_of(keys0);
-  for (int b = b0 + 1; b < b1; ++b) mine += cost_of(keys_of(p, b));
-  mine *= p.segs;
-  int64_t before = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d *= 2) {
-    const int64_t o = __shfl_up_sync(0xFFFFFFFFu, before, d);
-    if (lane >= d) before += o;
-  }
-  if (lane == 31) warp_places[warp] = before;
-  __syncthreads();
-  int64_t total = 0;
-#pragma unroll
-  for (int i = 0; i < kAttnWarps; ++i) {
-    if (i < warp) before += warp_places[i];
-    total += warp_places[i];
-  }
-  before -= mine;
-  const int ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), (total + kAttnWarps - 1) / kAttnWarps));
-  float4* part_at = reinterpret_cast<float4*>(p.ws + ((gridDim.x * sizeof(JoinTask) + 255) & ~static_cast<size_t>(255)));
-  constexpr int PART4 = S::PART / 16;                          // float4s of a part
-  if (cta >= ctas) {
-    write_zeros();
-    return;
-  }
-  // c * total / ctas without the long product
-  const bool small = total <= UINT32_MAX;
-  const int64_t q0 = small ? static_cast<uint32_t>(total) / static_cast<uint32_t>(ctas) : total / ctas;
-  const uint32_t rest = static_cast<uint32_t>(total - q0 * ctas);
-  const int64_t u0 = cta * q0 + cta * rest / static_cast<uint32_t>(ctas), u1 = (cta + 1) * q0 + (cta + 1) * rest / static_cast<uint32_t>(ctas);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int64_t u = i ? u1 : u0;
-    if (u == total && threadIdx.x == 0) border[i] = total;
-    if (u < before || u >= before + mine) continue;
-    int64_t r = u - before;
-    int b = b0, keys = keys0;
-    for (; r >= static_cast<int64_t>(cost_of(keys)) * p.segs; keys = keys_of(p, ++b)) r -= static_cast<int64_t>(cost_of(keys)) * p.segs;
-    const int cost = cost_of(keys), s = static_cast<int>(r <= UINT32_MAX ? static_cast<uint32_t>(r) / static_cast<uint32_t>(cost) : r / cost);
-    int pos = static_cast<int>(r - static_cast<int64_t>(s) * cost);
-    const int moved = cost > kWhole + kPieceCost ? pos : 2 * pos < cost ? 0 : cost;
-    border[i] = u + (moved - pos);
-    if (i == 0) {
-      first_b = b;
-      first_s = s;
-      first_pos = moved;
-      first_keys = keys;
-    }
-  }
-  __syncthreads();
-  if (border[1] <= border[0]) {
-    write_zeros();
-    return;
-  }
   Walk w;
-  w.b = first_b;
-  w.s = first_s;
-  w.pos = first_pos;
-  w.keys = first_keys;
-  w.units = units_of(w.keys);
-  w.left = static_cast<int>(border[1] - border[0]);
-  w.settle(p);
+  int ctas = 0;                                                // shares
+  int64_t total = 0, u1 = 0;                                   // places of all, end of this share
+  if constexpr (DIRECT) {
+    const int segment = cta / p.split, rank = cta - segment * p.split;
+    w.b = segment / p.segs;
+    w.s = segment - w.b * p.segs;
+    w.keys = keys_of(p, w.b);
+    if (w.keys == 0) {
+      if (w.s == 0 && rank == 0) write_zeros(w.b);
+      return;
+    }
+    w.units = units_of(w.keys);
+    w.j = static_cast<int>(static_cast<int64_t>(w.units) * rank / p.split);
+    w.n = static_cast<int>(static_cast<int64_t>(w.units) * (rank + 1) / p.split) - w.j;
+    w.left = w.pos = 0;
+  } else {
+    // This CTA's share. All places are counted by all CTAs, each thread a run of the sequences. A border between two shares that falls into
+    // a short sequence moves to the nearer end of it, for both of them.
+    __shared__ int64_t warp_places[kAttnWarps], border[2];
+    __shared__ int first_b, first_s, first_pos, first_keys;
+    const int per = (p.batch + kAttnWarps * 32 - 1) / (kAttnWarps * 32);
+    const int b0 = min(static_cast<int>(threadIdx.x) * per, p.batch), b1 = min(b0 + per, p.batch);
+    const int keys0 = b0 < b1 ? keys_of(p, b0) : 0;            // of the run's first
+    int64_t mine = cost_of(keys0);
+    for (int b = b0 + 1; b < b1; ++b) mine += cost_of(keys_of(p, b));
+    mine *= p.segs;
+    int64_t before = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const int64_t o = __shfl_up_sync(0xFFFFFFFFu, before, d);
+      if (lane >= d) before += o;
+    }
+    if (lane == 31) warp_places[warp] = before;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kAttnWarps; ++i) {
+      if (i < warp) before += warp_places[i];
+      total += warp_places[i];
+    }
+    before -= mine;
+    ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), (total + kAttnWarps - 1) / kAttnWarps));
+    bool idle = cta >= ctas;
+    if (!idle) {
+      // c * total / ctas without the long product
+      const int64_t q0 = total <= UINT32_MAX ? static_cast<uint32_t>(total) / static_cast<uint32_t>(ctas) : total / ctas;
+      const uint32_t rest = static_cast<uint32_t>(total - q0 * ctas);
+      u1 = (cta + 1) * q0 + (cta + 1) * rest / static_cast<uint32_t>(ctas);
+#pragma unroll 1
+      for (int i = 0; i < 2; ++i) {
+        const int64_t u = i ? u1 : cta * q0 + cta * rest / static_cast<uint32_t>(ctas);
+        if (u == total && threadIdx.x == 0) border[i] = total;
+        if (u < before || u >= before + mine) continue;
+        int64_t r = u - before;
+        int b = b0, keys = keys0;
+        for (; r >= static_cast<int64_t>(cost_of(keys)) * p.segs; keys = keys_of(p, ++b)) r -= static_cast<int64_t>(cost_of(keys)) * p.segs;
+        const int cost = cost_of(keys), s = static_cast<int>(r <= UINT32_MAX ? static_cast<uint32_t>(r) / static_cast<uint32_t>(cost) : r / cost);
+        const int pos = static_cast<int>(r - static_cast<int64_t>(s) * cost);
+        const int moved = cost > kWhole + kPieceCost ? pos : 2 * pos < cost ? 0 : cost;
+        border[i] = u + (moved - pos);
+        if (i == 0) {
+          first_b = b;
+          first_s = s;
+          first_pos = moved;
+          first_keys = keys;
+        }
+      }
+      __syncthreads();
+      idle = border[1] <= border[0];
+    }
+    if (idle) {
+      for (int b = cta; b < p.batch; b += gridDim.x) write_zeros(b);
+      return;
+    }
+    w.b = first_b;
+    w.s = first_s;
+    w.pos = first_pos;
+    w.keys = first_keys;
+    w.units = units_of(w.keys);
+    w.left = static_cast<int>(border[1] - border[0]);
+    w.settle(p);
+  }
 
   // Queries of a piece: 8 rows to a tile, row g of which is this lane's
   uint4 raw[NT][NW];
@@ -596,12 +670,14 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) copy.issue(p, base + ring + i * S::STAGE, warp, lane);
   int stage = 0;
-  write_zeros();                                               // while the first keys are on their way
+  if constexpr (!DIRECT)
+    for (int b = cta; b < p.batch; b += gridDim.x) write_zeros(b);       // while the first keys are on their way
 
   // Row g of a 16-key tile is key own0 of its first eight, row g + 8 the same of the second; the keys of a lane's columns of the value product
   // then are t and 7 - t of both eights.
   const int own0 = (g & 1) ? 7 - (g >> 1) : g >> 1;
-  for (Walk next; w.n > 0; w = next) {
+  // (a CTA of a cluster may have no unit of its segment, and meets the others all the same)
+  for (Walk next; DIRECT || w.n > 0; w = next) {
     const int h = head_of(p, w.s), row0 = (w.s - h * p.tiles) * (8 * NT);
     // queries of this tile as FP16 fragments, and what a score has to be multiplied with
     uint32_t qf[NT][D / 16][2];
@@ -637,7 +713,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
     // scale code that the values' multipliers refer to (none yet: far below all)
     Sums<MT, NT> a;
     float ve[NT][2];
-    int vref = -100;
+    int vref = -100, vhigh = 0;                                // vhigh: largest scale code so far
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -779,7 +855,6 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       }
       if (__any_sync(0xFFFFFFFFu, move)) {
         float was[NT][2];                                      // logarithm of what the weights so far have to be multiplied with
-        bool drop = false;
         const int vtop = MX ? __reduce_max_sync(0xFFFFFFFFu, key_top) : 0, vlow = MX ? __reduce_min_sync(0xFFFFFFFFu, key_low) + 1 : 0;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -792,11 +867,11 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
             was[n][c] = a.m[n][c] - now;
             a.m[n][c] = now;
             a.l[n][c] *= exp2_approx(was[n][c]);
-            drop |= was[n][c] + ve[n][c] - static_cast<float>(vtop - 132) > 60.0f;       // sums in units so small could overflow
           }
         if constexpr (MX) {
           const bool refer = vtop > vref + 8 || vlow < vref - 19;
-          wide = vtop - vlow > 19 || (refer && __any_sync(0xFFFFFFFFu, drop));
+          vhigh = max(vhigh, vtop);
+          wide = vtop - vlow > 19 || (refer && vhigh - vtop > 60);       // sums in units of so much less than their values could overflow
           if (wide) {
             // A key's value codes relative to its own largest one, exact over 36 binades, with that one's power of two in the weight: the
             // weights of the value product are kept in FP16's range by a maximum of their own.
@@ -961,8 +1036,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
     }
 
     next = w;
-    next.next(p);
-    fetch(next);                                               // on the way while this piece's parts meet
+    if constexpr (!DIRECT) next.next(p);
+    if constexpr (!DIRECT) fetch(next);                                               // on the way while this piece's parts meet
     // One result of the piece: sums of a column's weights over the lanes, then warps 2 and 3 to 0 and 1, then 1 to 0.
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -971,7 +1046,11 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
 #pragma unroll
         for (int d = 4; d < 32; d *= 2) a.l[n][c] += __shfl_xor_sync(0xFFFFFFFFu, a.l[n][c], d);
         if constexpr (MX) {
-          const float f = exp2_approx(0.5f * ve[n][c]);        // twice: 2^ve itself may be below FP32's range where the product is not
+          float moved;
+          const float even = even_out(a.l[n][c], moved);
+          a.l[n][c] *= even;
+          a.m[n][c] += moved;
+          const float f = exp2_approx(0.5f * (ve[n][c] - moved));        // twice: the power itself may be out of FP32's range where the product is not
 #pragma unroll
           for (int i = 0; i < MT; ++i) { a.o[i][n][c] = a.o[i][n][c] * f * f; a.o[i][n][c + 2] = a.o[i][n][c + 2] * f * f; }
         }
@@ -996,10 +1075,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
         for (int n = 0; n < NT; ++n) {
           const float4 v = smem_load<float4>(at + (MT * NT + n) * 512);
           float fa[2], fb[2];
-          join_weights(a.m[n][0], v.x, a.m[n][0], fa[0], fb[0]);
-          join_weights(a.m[n][1], v.z, a.m[n][1], fa[1], fb[1]);
-          a.l[n][0] = a.l[n][0] * fa[0] + v.y * fb[0];
-          a.l[n][1] = a.l[n][1] * fa[1] + v.w * fb[1];
+          join_weights<MX>(a.m[n][0], a.l[n][0], v.x, v.y, fa[0], fb[0]);
+          join_weights<MX>(a.m[n][1], a.l[n][1], v.z, v.w, fa[1], fb[1]);
 #pragma unroll
           for (int i = 0; i < MT; ++i) {
             const float4 o = smem_load<float4>(at + (i * NT + n) * 512);
@@ -1012,9 +1089,31 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       }
       __syncthreads();
     }
-    if (warp == 0) {
+    if (DIRECT && p.split > 1) {
+      // the cluster's CTAs put their sums into shared memory, and take turns at the value tiles
+      constexpr int TILES = MT * NT;
+      if (warp == 0) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) smem_store(parts + lane * 16 + (i * NT + n) * 512, make_float4(a.o[i][n][0], a.o[i][n][1], a.o[i][n][2], a.o[i][n][3]));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) smem_store(parts + lane * 16 + (TILES + n) * 512, make_float4(a.m[n][0], a.l[n][0], a.m[n][1], a.l[n][1]));
+      }
+      const cg::cluster_group cluster = cg::this_cluster();
+      cluster.sync();
+      for (int tile = static_cast<int>(cluster.block_rank()) * kAttnWarps + warp; tile < TILES; tile += p.split * kAttnWarps) {
+        Joint<MX> sum;
+        for (int k = 0; k < p.split; ++k) {
+          const float4* part = cluster.map_shared_rank(reinterpret_cast<const float4*>(smem + parts), k) + lane;
+          sum.add(part[tile * 32], part[(TILES + tile % NT) * 32]);
+        }
+        write_tile<D, NT>(p, sum, w.b, w.s, tile, lane, vt);
+      }
+      cluster.sync();
+    } else if (warp == 0) {
       const bool begins = w.j == 0;
-      if (w.n == w.units) {                                    // the whole sequence: the result itself
+      if (DIRECT || w.n == w.units) {                          // the whole sequence: the result itself
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -1034,7 +1133,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
             }
           }
       } else {
-        float4* to_part = part_at + static_cast<int64_t>(cta * 2 + (begins ? 1 : 0)) * PART4 + lane;
+        float4* to_part = parts_of(p, gridDim.x) + static_cast<int64_t>(cta * 2 + (begins ? 1 : 0)) * (S::PART / 16) + lane;
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -1042,12 +1141,13 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
 #pragma unroll
         for (int n = 0; n < NT; ++n) to_part[(MT * NT + n) * 32] = make_float4(a.m[n][0], a.l[n][0], a.m[n][1], a.l[n][1]);
       }
-      if (begins && lane == 0 && (p.by_segment || w.n < w.units)) {
+      if (!DIRECT && begins && lane == 0 && (p.by_segment || w.n < w.units)) {
         const int64_t last = u1 + (w.units - w.n) - 1;         // place of the sequence's last unit, if others go on with it
         const int more = w.n < w.units ? static_cast<int>(((last + 1) * ctas - 1) / total) - cta : 0;
         tasks[p.by_segment ? w.b * p.segs + w.s : cta] = JoinTask{cta, more, w.b, w.s};
       }
     }
+    if constexpr (DIRECT) return;
   }
 }
 
@@ -1061,27 +1161,14 @@ __global__ void __launch_bounds__(1024) kv_join_kernel(const __grid_constant__ K
   const float vt = FMT == QF_FMT_NVFP4 ? *p.v_tscale : 1.0f;
   const JoinTask task = reinterpret_cast<const JoinTask*>(p.ws)[blockIdx.x];
   if (task.more == 0) return;
-  const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const float4* parts = reinterpret_cast<const float4*>(p.ws + ((ctas * sizeof(JoinTask) + 255) & ~static_cast<size_t>(255))) +
-                        static_cast<int64_t>(task.cta) * 2 * PART4 + lane;
-  const int h = head_of(p, task.seg), row0 = (task.seg - h * p.tiles) * (8 * NT) + 2 * t;
+  const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+  const float4* parts = parts_of(p, ctas) + static_cast<int64_t>(task.cta) * 2 * PART4 + lane;
   extern __shared__ __align__(128) uint8_t smem[];
   float4* met = reinterpret_cast<float4*>(smem);               // sums and weights of a warp, from the second half of the warps
   const bool many = task.more >= 8;
   const int first = many ? warp : 0, step = many ? warps : 1;
   for (int tile = many ? blockIdx.y : blockIdx.y * warps + warp; tile < TILES; tile += gridDim.y * (many ? 1 : warps)) {
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f), ml = make_float4(kNoWeights, 0.0f, kNoWeights, 0.0f);
-    const auto add = [&](const float4& v, const float4& w) {
-      float fa[2], fb[2];
-      join_weights(ml.x, w.x, ml.x, fa[0], fb[0]);
-      join_weights(ml.z, w.z, ml.z, fa[1], fb[1]);
-      ml.y = ml.y * fa[0] + w.y * fb[0];
-      ml.w = ml.w * fa[1] + w.w * fb[1];
-      o.x = o.x * fa[0] + v.x * fb[0];
-      o.y = o.y * fa[1] + v.y * fb[1];
-      o.z = o.z * fa[0] + v.z * fb[0];
-      o.w = o.w * fa[1] + v.w * fb[1];
-    };
+    Joint<FMT == QF_FMT_MXFP4> sum;
     for (int k0 = first; k0 <= task.more; k0 += 4 * step) {    // four parts on the way together
       float4 v[4], w[4];
 #pragma unroll
@@ -1093,55 +1180,57 @@ __global__ void __launch_bounds__(1024) kv_join_kernel(const __grid_constant__ K
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (k0 + j * step <= task.more) add(v[j], w[j]);
+        if (k0 + j * step <= task.more) sum.add(v[j], w[j]);
     }
     if (many) {
       for (int d = warps / 2; d > 0; d /= 2) {
         if (warp >= d && warp < 2 * d) {
-          met[(warp - d) * 64 + lane] = o;
-          met[(warp - d) * 64 + 32 + lane] = ml;
+          met[(warp - d) * 64 + lane] = sum.o;
+          met[(warp - d) * 64 + 32 + lane] = sum.ml;
         }
         __syncthreads();
-        if (warp < d) add(met[warp * 64 + lane], met[warp * 64 + 32 + lane]);
+        if (warp < d) sum.add(met[warp * 64 + lane], met[warp * 64 + 32 + lane]);
         __syncthreads();
       }
       if (warp != 0) continue;
     }
-    const int i = tile / NT, n = tile % NT;
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int row = row0 + 8 * n + c;
-      if (row >= p.rows) continue;
-      const int token = token_of(p, row), head = h * p.group + (row - token * p.group);
-      const int64_t at = (static_cast<int64_t>(task.b) * p.q_len + token) * p.q_heads + head;
-      const float l = c ? ml.w : ml.y, f = l > 0.0f ? vt / l : 0.0f;
-      *reinterpret_cast<uint32_t*>(p.out + at * D + dim_of<D>(i, g)) = pack_bf16x2((c ? o.y : o.x) * f, (c ? o.w : o.z) * f);
-      if (p.lse && i == 0 && g == 0) p.lse[at] = log_sum(c ? ml.z : ml.x, l);
-    }
+    write_tile<D, NT>(p, sum, task.b, task.seg, tile, lane, vt);
   }
 }
 
-template <int FMT, int D, int NT>
-cudaError_t attend(KvAttn& p, cudaStream_t st) {
+template <int FMT, int D, int NT, bool DIRECT>
+cudaError_t launch_attention(const KvAttn& p, int64_t ctas, int cluster, cudaStream_t st) {
   using S = Shape<FMT, D, NT>;
   static bool ready[64] = {};                                  // the attribute stays set for the process
   int dev = 0;
   if (cudaError_t e = cudaGetDevice(&dev)) return e;
   if (dev >= 64 || !ready[dev]) {
-    if (cudaError_t e = cudaFuncSetAttribute(kv_attention_kernel<FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM)) return e;
+    if (cudaError_t e = cudaFuncSetAttribute(kv_attention_kernel<FMT, D, NT, DIRECT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM)) return e;
     if (dev < 64) ready[dev] = true;
   }
-  // no more CTAs than there can be work for
+  return launch_overlapping(kv_attention_kernel<FMT, D, NT, DIRECT>, dim3(static_cast<unsigned>(ctas)), kAttnWarps * 32, S::SMEM, st, cluster, p);
+}
+
+template <int FMT, int D, int NT>
+cudaError_t attend(KvAttn& p, cudaStream_t st) {
+  using S = Shape<FMT, D, NT>;
+  constexpr int64_t ROOM = kNumSMs * S::CTAS;
   const int64_t segments = static_cast<int64_t>(p.batch) * p.segs;
-  const int64_t most = segments * ((p.max_keys + kUnitKeys - 1) / kUnitKeys + kPieceCost) / kAttnWarps + 1;
-  const int grid = static_cast<int>(most < kNumSMs * S::CTAS ? most : kNumSMs * S::CTAS);
+  const int units = (p.max_keys + kUnitKeys - 1) / kUnitKeys;
+  // Short sequences, by what the page table holds: CTAs of their own for each, so that nothing has to be counted, nor joined by a second
+  // kernel. As many as there is room for and as have a unit for every warp.
+  p.split = 1;
+  while (p.split < 8 && p.split * kAttnWarps < units && 2 * p.split * segments <= ROOM) p.split *= 2;
+  if (p.split * kDirectUnits >= units && segments <= INT32_MAX) return launch_attention<FMT, D, NT, true>(p, segments * p.split, p.split, st);
+  // no more CTAs than there can be work for
+  const int64_t most = segments * (units + kPieceCost) / kAttnWarps + 1;
+  const int grid = static_cast<int>(most < ROOM ? most : ROOM);
   p.by_segment = segments <= grid;
-  if (cudaError_t e = launch_overlapping(kv_attention_kernel<FMT, D, NT>, dim3(grid), kAttnWarps * 32, S::SMEM, st, p)) return e;
-  if (p.max_keys <= kWhole * kUnitKeys) return cudaSuccess;    // nothing can have been cut
+  if (cudaError_t e = launch_attention<FMT, D, NT, false>(p, grid, 1, st)) return e;
   // the fewer sequences, the more parts each may have: up to a CTA per value tile
   const int tasks = p.by_segment ? static_cast<int>(segments) : grid;
   const int share = 4 * kNumSMs / tasks, parts = grid / tasks, threads = parts < 32 ? 256 : parts < 128 ? 512 : 1024;
-  return launch_overlapping(kv_join_kernel<FMT, D, NT>, dim3(tasks, share < 1 ? 1 : share < S::MT * NT ? share : S::MT * NT), threads, threads * 16, st, p, grid);
+  return launch_overlapping(kv_join_kernel<FMT, D, NT>, dim3(tasks, share < 1 ? 1 : share < S::MT * NT ? share : S::MT * NT), threads, threads * 16, st, 1, p, grid);
 }
 
 // Query rows of a tile, in units of 8, at most: what registers hold next to the decoded words. (Heads of 256 with 16 rows: one CTA an SM and

@@ -208,6 +208,29 @@ def test_a_large_ragged_batch(fmt):
 
 
 @fmts
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("q_len,group", [(1, 4), (5, 4), (3, 8)])
+def test_short_sequences_in_a_wide_page_table(fmt, dim, q_len, group):
+    """A table for 20000 keys: how the work is cut goes by what the table can hold, the lengths are short, empty and in between."""
+    attend(fmt, [1, 0, 31, 32, 33, 100, 383, 384, 385, 416, 0, 700, 1500, 7], 16, 3, group, dim, q_len=q_len, max_pages=1250)
+    attend(fmt, [300], 32, 1, group, dim, q_len=q_len, max_pages=625)
+    attend(fmt, [20, 0, 0], 32, 1, group, dim, q_len=q_len, max_pages=625)
+
+
+@fmts
+def test_the_same_rows_whatever_the_table_can_hold(fmt):
+    """Two ways to cut the work give the same rows up to FP32 sums and weights."""
+    lens, page = [700, 3, 0, 260, 129], 16
+    table, n, pages = paged(lens, page)
+    wide, _, _ = paged(lens, page, max_pages=2000)
+    c = random_cache(fmt, pages, page, 2, 128, 3)
+    q = torch.randn((5, 1, 8, 128), generator=gen(4), device="cuda").to(BF)
+    (a, la), (b, lb) = (api.qf_kv_attention(c, q, x, n, want_lse=True) for x in (table, wide))
+    check_attention(c, q, table, lens, 128 ** -0.5, a, la)
+    check_attention(c, q, wide, lens, 128 ** -0.5, b, lb)
+
+
+@fmts
 @pytest.mark.parametrize("batch,most,page", [(130, 400, 16), (700, 70, 32), (3000, 20, 16), (40, 385, 64)])
 def test_many_short_sequences(fmt, batch, most, page):
     """More sequences than threads look at, than CTAs, and of the length from which on sequences are cut."""
@@ -266,6 +289,14 @@ def test_value_ranges_that_change_along_a_sequence(dim, scale):
         q = torch.randn((1, q_len, heads * group, dim), generator=g, device="cuda").to(BF)
         out, lse = api.qf_kv_attention(c, q, table, torch.tensor([m], dtype=torch.int32, device="cuda"), softmax_scale=scale, want_lse=True)
         check_attention(c, q, table, [m], scale, out, lse)
+    # falling and rising by up to 2^60 a step, over and over
+    for codes in ((190, 132, 74, 16), (16, 74, 132, 190), (250, 190, 130, 70, 10)):
+        for i in range(c.pages):
+            c.v_scales[i].fill_(codes[(i // 2) % len(codes)])
+        q = torch.randn((1, 1, heads * 4, dim), generator=g, device="cuda").to(BF)
+        for m in (40, 190, n):
+            out, lse = api.qf_kv_attention(c, q, table, torch.tensor([m], dtype=torch.int32, device="cuda"), softmax_scale=scale, want_lse=True)
+            check_attention(c, q, table, [m], scale, out, lse)
     flat = api.KvCache(api.FMT_MXFP4, c.k_codes, c.k_scales, c.v_codes, torch.full_like(c.v_scales, 20), None, None)      # all far below 1
     out, lse = api.qf_kv_attention(flat, q, table, torch.tensor([m], dtype=torch.int32, device="cuda"), softmax_scale=scale, want_lse=True)
     check_attention(flat, q, table, [m], scale, out, lse)
