@@ -422,9 +422,10 @@ qf_status_t qf_kv_read(const qf_kv_cache_t* cache, const void* slots, qf_dtype_t
  *     s_j = softmax_scale * <q, k_j>,   p = softmax over the keys j < seq_lens[b] - q_len + i + 1,   out = sum over j of p_j * v_j
  * for token i in [0, q_len) of sequence b and every query head; query head h reads key/value head h / (q_heads / kv_heads).
  * FP32 scores, softmax and sums; the weights p_j enter the value product as FP16 numbers (relative error 2^-11 at most, below the
- * BF16 result's 2^-8) and the dequantized keys and values are not rounded to BF16, as in qf_fq_matvec. A row without keys (an
- * empty place of a padded batch, a token of a sequence shorter than q_len) gives zeros. Results do not change from run to run; how
- * the keys are cut depends on the batch's lengths, so that the same row can have other last bits in another batch.
+ * BF16 result's 2^-8) and the dequantized keys and values are not rounded to BF16, as in qf_fq_matvec. MXFP4: key blocks of scale
+ * 2^-127 count as zeros, and so may value blocks whose scale is less than 2^-36 of the largest of the same key and head. A row without
+ * keys (an empty place of a padded batch, a token of a sequence shorter than q_len) gives zeros. Results do not change from run to run;
+ * how the keys are cut depends on the batch's lengths and on max_pages, so that the same row can have other last bits in another batch.
  *   q            BF16 [batch, q_len, q_heads, head_dim], q_stride elements from one token to the next (at least q_heads * head_dim, a
  *                multiple of 8): token i of sequence b is row b * q_len + i
  *   page_table   device int32 [batch, max_pages]; entries behind a sequence's last page are not read
@@ -434,8 +435,9 @@ qf_status_t qf_kv_read(const qf_kv_cache_t* cache, const void* slots, qf_dtype_t
  *                without keys: what joining with other keys' attention takes
  *   workspace    qf_workspace_bytes(QF_OP_KV_ATTENTION, batch * q_len, q_heads, head_dim, kv_heads) bytes, whatever they hold; calls
  *                that can overlap on the GPU (other streams, graphs) need one each
- * Meant for a few tokens a sequence (a decode step, drafted tokens checked together): the cache is read once per 16 rows of
- * q_len * q_heads / kv_heads. For long prompts read the cache back (qf_kv_read). */
+ * Meant for a few tokens a sequence (a decode step, drafted tokens checked together): the cache is read and decoded once per 24 rows of
+ * q_len * q_heads / kv_heads (32 for head_dim 64, 8 for 256). For long prompts read the cache back (qf_kv_read). A page table no wider than
+ * the sequences need gives short sequences the shorter way (no second kernel for up to 6144 keys, where there are few). */
 qf_status_t qf_kv_attention(const qf_kv_cache_t* cache, const void* q, int64_t q_stride, int64_t batch, int q_len, int q_heads,
                             const int32_t* page_table, int64_t max_pages, const int32_t* seq_lens, float softmax_scale, void* out,
                             float* lse, void* workspace, size_t workspace_bytes, void* stream);

@@ -730,7 +730,11 @@ def qf_kv_read(cache: KvCache, slots: torch.Tensor, *, want_k: bool = True, want
     ps, dt, rows = _slots(slots, device)
     shape = (rows, cache.kv_heads, cache.head_dim)
     k, pk = _out(slots, k, "k", _BF16, shape, torch.bfloat16, device) if want_k else (None, None)
-    v, pv = _out(slots, v, "v", _BF16, shape, torch.bfloat16, device) if want_v else (None, None)
+    if v is None and want_v and k is not None:                     # (like the other, which takes less time than by shape and type)
+        v = torch.empty_like(k)
+        pv = v.data_ptr()
+    else:
+        v, pv = _out(slots, v, "v", _BF16, shape, torch.bfloat16, device) if want_v else (None, None)
     _check(lib().qf_kv_read(cache._address, ps, dt, rows, pk, pv, stream), "qf_kv_read")
     return k, v
 
@@ -749,7 +753,11 @@ def qf_kv_attention(cache: KvCache, q: torch.Tensor, page_table: torch.Tensor, s
     max_pages = page_table.shape[-1]
     pt = _tensor(page_table, "page_table", _I32, (batch, max_pages), device)
     pl = _tensor(seq_lens, "seq_lens", _I32, (batch,), device)
-    out, po = _out(q, out, "out", _BF16, (batch, q_len, q_heads, dim), torch.bfloat16, device)
+    if out is None and q.is_contiguous():
+        out = torch.empty_like(q)
+        po = out.data_ptr()
+    else:
+        out, po = _out(q, out, "out", _BF16, (batch, q_len, q_heads, dim), torch.bfloat16, device)
     want_lse = want_lse or lse is not None
     lse, pe = _out(q, lse, "lse", _F32, (batch, q_len, q_heads), torch.float32, device) if want_lse else (None, None)
     if ws is None:

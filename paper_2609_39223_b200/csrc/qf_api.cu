@@ -793,9 +793,9 @@ static qf_status_t check_kv(const qf_kv_cache_t* c) {
   if ((reinterpret_cast<uintptr_t>(c->k_tscale) | reinterpret_cast<uintptr_t>(c->v_tscale)) & 3u) return QF_ERR_ALIGN;
   return QF_OK;
 }
-static bool kv_has_buffers(const qf_kv_cache_t* c) {
-  return c->k_codes && c->k_scales && c->v_codes && c->v_scales && (c->fmt != QF_FMT_NVFP4 || (c->k_tscale && c->v_tscale));
-}
+// the kernels read the tensor scales whether or not there is a page
+static bool kv_has_scales(const qf_kv_cache_t* c) { return c->fmt != QF_FMT_NVFP4 || (c->k_tscale && c->v_tscale); }
+static bool kv_has_buffers(const qf_kv_cache_t* c) { return c->k_codes && c->k_scales && c->v_codes && c->v_scales && kv_has_scales(c); }
 static qf_status_t check_slots(const void* slots, int dtype) {
   if (dtype != QF_DT_I32 && dtype != QF_DT_I64) return QF_ERR_DTYPE;
   return reinterpret_cast<uintptr_t>(slots) & (dtype == QF_DT_I64 ? 7u : 3u) ? QF_ERR_ALIGN : QF_OK;
@@ -824,7 +824,7 @@ qf_status_t qf_kv_read(const qf_kv_cache_t* cache, const void* slots, qf_dtype_t
   if (qf_status_t s = check_kv(cache)) return s;
   if (!kv_tokens_ok(rows, static_cast<int64_t>(cache->kv_heads) * cache->head_dim)) return QF_ERR_SHAPE;
   if (qf_status_t s = check_slots(slots, slots_dtype)) return s;
-  if (rows > 0 && (!slots || (!k && !v) || (cache->pages > 0 && !kv_has_buffers(cache)))) return QF_ERR_NULL;
+  if (rows > 0 && (!slots || (!k && !v) || !kv_has_scales(cache) || (cache->pages > 0 && !kv_has_buffers(cache)))) return QF_ERR_NULL;
   if (!aligned16(k) || !aligned16(v)) return QF_ERR_ALIGN;
   if (qf_status_t s = check_arch()) return s;
   if (rows == 0) return QF_OK;
@@ -843,7 +843,7 @@ qf_status_t qf_kv_attention(const qf_kv_cache_t* cache, const void* q, int64_t q
   if ((rows * q_heads / 8 + batch * cache->kv_heads) * (max_pages * cache->page_size / 32 + 1) > (1ll << 37)) return QF_ERR_SHAPE;   // a CTA's share of the work is counted in 31 bits
   if (!workspace || workspace_bytes < qf_workspace_bytes(QF_OP_KV_ATTENTION, rows, q_heads, cache->head_dim, cache->kv_heads)) return QF_ERR_WORKSPACE;
   const bool keys = max_pages > 0 && cache->pages > 0;
-  if (rows > 0 && (!q || !out || !seq_lens || (keys && (!page_table || !kv_has_buffers(cache))))) return QF_ERR_NULL;
+  if (rows > 0 && (!q || !out || !seq_lens || !kv_has_scales(cache) || (keys && (!page_table || !kv_has_buffers(cache))))) return QF_ERR_NULL;
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return QF_ERR_ALIGN;
   if ((reinterpret_cast<uintptr_t>(page_table) | reinterpret_cast<uintptr_t>(seq_lens) | reinterpret_cast<uintptr_t>(lse)) & 3u) return QF_ERR_ALIGN;
   if (qf_status_t s = check_arch()) return s;

@@ -47,8 +47,10 @@ def test_caches_that_are_refused(which):
         assert f({n: P + 2}) == ALIGN and f({n: None}) == NULL, n
         if HERE:
             assert f({"fmt": api.FMT_MXFP4, n: None}) == HERE
+        if which > 0:                                              # a cache without pages is read as nothing, but its scales are looked at
+            assert f({"pages": 0, n: None}) == NULL
     if HERE:
-        assert f() == HERE
+        assert f() == HERE and f(dict(pages=0, k_codes=None, v_scales=None)) == HERE
 
 
 def test_append_refusals():
