@@ -676,6 +676,19 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   // Row g of a 16-key tile is key own0 of its first eight, row g + 8 the same of the second; the keys of a lane's columns of the value product
   // then are t and 7 - t of both eights.
   const int own0 = (g & 1) ? 7 - (g >> 1) : g >> 1;
+  // This lane's places in a stage: its words of keys, their scales; its words of values for keys t and 7 - t, and their scales. (Kept as they
+  // are: the compiler would work them out for every unit.)
+  uint32_t k_at = own0 * (D / 2) + (MX ? turn<D>(own0) * 16 + t * 4 : D == 64 ? ((t >> 1) ^ turn<D>(own0)) * 16 + (t & 1) * 8 : (t ^ turn<D>(own0)) * 16);
+  uint32_t ks_at = 2 * S::CODES + own0 * NB + (MX ? 0 : D == 64 ? t : 2 * t);
+  uint32_t v_at[2], vs_at[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int own = i ? 7 - t : t, block = MX ? (D == 64 ? g >> 2 : g >> 1) : D == 64 ? g >> 1 : g;
+    v_at[i] = S::CODES + own * (D / 2) + (D == 64 ? ((g >> 2) ^ turn<D>(own)) * 16 + (g & 3) * 4 : ((g >> 1) ^ turn<D>(own)) * 16 + (g & 1) * 8);
+    vs_at[i] = 2 * S::CODES + S::SCALES + own * NB + block;
+    asm volatile("" : "+r"(v_at[i]), "+r"(vs_at[i]));
+  }
+  asm volatile("" : "+r"(k_at), "+r"(ks_at));
   // (a CTA of a cluster may have no unit of its segment, and meets the others all the same)
   for (Walk next; DIRECT || w.n > 0; w = next) {
     const int h = head_of(p, w.s), row0 = (w.s - h * p.tiles) * (8 * NT);
@@ -730,7 +743,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       copy.issue(p, base + ring + (stage == 0 ? kStages - 1 : stage - 1) * S::STAGE, warp, lane);
       asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
       __syncwarp();
-      const uint32_t here = ring + stage * S::STAGE, kscales = here + 2 * S::CODES, vscales = kscales + S::SCALES;
+      const uint32_t here = ring + stage * S::STAGE;
       stage = stage + 1 == kStages ? 0 : stage + 1;
       const int key0 = u * kUnitKeys;
 
@@ -743,25 +756,25 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int c = 0; c < 4; ++c) s[half][n][c] = 0.0f;
-        const int r0 = half * 16 + own0, r1 = r0 + 8;
+        const uint32_t keys = here + k_at + half * 16 * (D / 2), kscales = here + ks_at + half * 16 * NB;      // row g; row g + 8 is 8 rows on
         if constexpr (MX) {
           uint32_t f0[(NB + 3) / 4], f1[(NB + 3) / 4];
 #pragma unroll
           for (int i = 0; i < (NB + 3) / 4; ++i) {
             if constexpr (NB == 2) {
-              f0[i] = smem_load<uint16_t>(kscales + r0 * NB);
-              f1[i] = smem_load<uint16_t>(kscales + r1 * NB);
+              f0[i] = smem_load<uint16_t>(kscales);
+              f1[i] = smem_load<uint16_t>(kscales + 8 * NB);
             } else {
-              f0[i] = smem_load<uint32_t>(kscales + r0 * NB + 4 * i);
-              f1[i] = smem_load<uint32_t>(kscales + r1 * NB + 4 * i);
+              f0[i] = smem_load<uint32_t>(kscales + 4 * i);
+              f1[i] = smem_load<uint32_t>(kscales + 8 * NB + 4 * i);
             }
           }
 #pragma unroll
           for (int x = 0; x < NW; ++x) {
-            const int piece = (x ^ turn<D>(own0)) * 16 + t * 4;
+            const uint32_t word = here + (k_at ^ (x * 16)) + half * 16 * (D / 2);
             uint32_t d0[4], d1[4];
-            e2m1_f16(smem_load<uint32_t>(here + r0 * (D / 2) + piece), d0);
-            e2m1_f16(smem_load<uint32_t>(here + r1 * (D / 2) + piece), d1);
+            e2m1_f16(smem_load<uint32_t>(word), d0);
+            e2m1_f16(smem_load<uint32_t>(word + 8 * (D / 2)), d1);
             const float y0 = e8m0_of(f0[x / 4], x & 3), y1 = e8m0_of(f1[x / 4], x & 3);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -780,17 +793,16 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
             constexpr int WORDS = D == 64 ? 2 : 4;
             uint32_t c0[WORDS], c1[WORDS], x0[2], x1[2];
             if constexpr (D == 64) {
-              const int piece = ((t >> 1) ^ turn<D>(own0)) * 16 + (t & 1) * 8;
-              const uint2 v0 = smem_load<uint2>(here + r0 * 32 + piece), v1 = smem_load<uint2>(here + r1 * 32 + piece);
+              const uint2 v0 = smem_load<uint2>(keys), v1 = smem_load<uint2>(keys + 8 * 32);
               c0[0] = v0.x; c0[1] = v0.y; c1[0] = v1.x; c1[1] = v1.y;
-              x0[0] = e4m3_pair(smem_load<uint8_t>(kscales + r0 * NB + t) * 0x0101u);
-              x1[0] = e4m3_pair(smem_load<uint8_t>(kscales + r1 * NB + t) * 0x0101u);
+              x0[0] = e4m3_pair(smem_load<uint8_t>(kscales) * 0x0101u);
+              x1[0] = e4m3_pair(smem_load<uint8_t>(kscales + 8 * NB) * 0x0101u);
             } else {
-              const int piece = ((hh * 4 + t) ^ turn<D>(own0)) * 16;
-              const uint4 v0 = smem_load<uint4>(here + r0 * (D / 2) + piece), v1 = smem_load<uint4>(here + r1 * (D / 2) + piece);
+              const uint32_t words = hh == 0 ? keys : here + (k_at ^ 64) + half * 16 * (D / 2);
+              const uint4 v0 = smem_load<uint4>(words), v1 = smem_load<uint4>(words + 8 * (D / 2));
               c0[0] = v0.x; c0[1] = v0.y; c0[2] = v0.z; c0[3] = v0.w;
               c1[0] = v1.x; c1[1] = v1.y; c1[2] = v1.z; c1[3] = v1.w;
-              const uint32_t y0 = e4m3_pair(smem_load<uint16_t>(kscales + r0 * NB + hh * 8 + 2 * t)), y1 = e4m3_pair(smem_load<uint16_t>(kscales + r1 * NB + hh * 8 + 2 * t));
+              const uint32_t y0 = e4m3_pair(smem_load<uint16_t>(kscales + hh * 8)), y1 = e4m3_pair(smem_load<uint16_t>(kscales + 8 * NB + hh * 8));
               x0[0] = __byte_perm(y0, 0, 0x1010); x0[1] = __byte_perm(y0, 0, 0x3232);
               x1[0] = __byte_perm(y1, 0, 0x1010); x1[1] = __byte_perm(y1, 0, 0x3232);
             }
@@ -841,8 +853,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
         uint32_t top2 = 0, low2 = 0xFFFFFFFFu;
 #pragma unroll
         for (int i = 0; i < (NB + 3) / 4; ++i) {
-          if constexpr (NB == 2) vword[i] = __byte_perm(smem_load<uint16_t>(vscales + lane * NB), 0, 0x4140);
-          else vword[i] = smem_load<uint32_t>(vscales + lane * NB + 4 * i);
+          if constexpr (NB == 2) vword[i] = __byte_perm(smem_load<uint16_t>(here + 2 * S::CODES + S::SCALES + lane * NB), 0, 0x4140);
+          else vword[i] = smem_load<uint32_t>(here + 2 * S::CODES + S::SCALES + lane * NB + 4 * i);
           const uint32_t even = NB == 2 ? vword[i] : vword[i] & 0x00FF00FFu, odd = NB == 2 ? even : __byte_perm(vword[i], 0, 0x4341);
           top2 = __vmaxu2(top2, __vmaxu2(even, odd));
           low2 = __viaddmin_u16x2(even, 0xFFFFFFFFu, __viaddmin_u16x2(odd, 0xFFFFFFFFu, low2));
@@ -977,8 +989,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
           for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-              const uint32_t first = smem_load<uint8_t>(vscales + (half * 16 + r * 8 + t) * NB + block);
-              const uint32_t second = smem_load<uint8_t>(vscales + (half * 16 + r * 8 + 7 - t) * NB + block);
+              const uint32_t first = smem_load<uint8_t>(here + vs_at[0] + (half * 16 + r * 8) * NB + hh * (128 / S::BLOCK));
+              const uint32_t second = smem_load<uint8_t>(here + vs_at[1] + (half * 16 + r * 8) * NB + hh * (128 / S::BLOCK));
               if constexpr (MX) y[half][r] = __viaddmax_s16x2_relu(__byte_perm(first, second, 0x5410), up, 0) << 10;
               else y[half][r] = e4m3_pair(__byte_perm(first, second, 0x0040));
             }
@@ -997,11 +1009,11 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const int own = (k & 1) ? 7 - t : t, r = half * 16 + (k >> 1) * 8 + own;
+            const uint32_t words = here + (hh == 0 ? v_at[k & 1] : v_at[k & 1] ^ 64) + (half * 16 + (k >> 1) * 8) * (D / 2);
             if constexpr (D == 64) {
-              c[half][k][0] = smem_load<uint32_t>(here + S::CODES + r * 32 + (((g >> 2) ^ turn<D>(own)) * 16) + (g & 3) * 4);
+              c[half][k][0] = smem_load<uint32_t>(words);
             } else {
-              const uint2 v = smem_load<uint2>(here + S::CODES + r * (D / 2) + (((hh * 4 + (g >> 1)) ^ turn<D>(own)) * 16) + (g & 1) * 8);
+              const uint2 v = smem_load<uint2>(words);
               c[half][k][0] = v.x;
               c[half][k][1] = v.y;
             }
