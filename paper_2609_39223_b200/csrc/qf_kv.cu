@@ -41,25 +41,26 @@ struct KvRows {
 };
 
 // Rows of the CTA's tokens in the cache: head h of token t lies in row at[t] + h * page_size; -1 outside the cache.
-__device__ __forceinline__ int find_rows(const KvRows& p, int64_t (&at)[kRowsTokens]) {
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * p.each;
-  const int here = static_cast<int>(min(static_cast<int64_t>(p.each), p.tokens - first));
-  if (threadIdx.x < here) {
-    const int64_t t = first + threadIdx.x, s = p.slots64 ? static_cast<const int64_t*>(p.slots)[t] : static_cast<const int32_t*>(p.slots)[t];
+__device__ __forceinline__ int tokens_here(const KvRows& p) {
+  return static_cast<int>(min(static_cast<int64_t>(p.each), p.tokens - static_cast<int64_t>(blockIdx.x) * p.each));
+}
+__device__ __forceinline__ void find_rows(const KvRows& p, int64_t (&at)[kRowsTokens]) {
+  if (threadIdx.x < tokens_here(p)) {
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * p.each + threadIdx.x;
+    const int64_t s = p.slots64 ? static_cast<const int64_t*>(p.slots)[t] : static_cast<const int32_t*>(p.slots)[t];
     const bool in = s >= 0 && s < p.slots_most;
     const int64_t page = !in ? 0 : s <= UINT32_MAX ? static_cast<uint32_t>(s) / static_cast<uint32_t>(p.page_size) : s / p.page_size;
     at[threadIdx.x] = in ? page * p.heads * p.page_size + (s - page * p.page_size) : -1;
   }
   __syncthreads();
-  return here;
 }
 
 template <int FMT>
 __global__ void __launch_bounds__(kQdqThreads) kv_append_kernel(const __grid_constant__ KvRows p) {
-  constexpr int TURNS = 2;           // rows of a thread on the way together
+  constexpr int TURNS = 2;           // rows of a thread that are loaded together, the next ones before these are quantized
   launch_after_previous();
   __shared__ int64_t at[kRowsTokens];
-  const int here = find_rows(p, at);
+  const int here = tokens_here(p);
   const int column = static_cast<int>(threadIdx.x) % p.span, beside = static_cast<int>(threadIdx.x) / p.span;
   for (int r0 = 0; r0 < p.units; r0 += p.span) {
     const int r = r0 + column;
@@ -70,39 +71,50 @@ __global__ void __launch_bounds__(kQdqThreads) kv_append_kernel(const __grid_con
     const int64_t row0 = static_cast<int64_t>(h) * p.page_size;
     uint8_t* codes = (value ? p.v_codes : p.k_codes) + ((row0 << p.shift) + part) * 8;
     uint8_t* scales = (value ? p.v_scales : p.k_scales) + (FMT == QF_FMT_NVFP4 ? (row0 << p.shift) + part : ((row0 << p.shift) + part) >> 1);
-    const Nvfp4Tensor nt = nvfp4_tensor(FMT == QF_FMT_NVFP4 ? *(value ? p.v_tscale : p.k_tscale) : 1.0f);
-    for (int t0 = 0; t0 < here; t0 += TURNS * p.side) {
-      uint4 x[TURNS][2];
-      int64_t row[TURNS];
+    // tokens that go nowhere are loaded as well: their slots need not be known yet
+    uint4 x[TURNS][2];
+    const auto load = [&](int t0) {
 #pragma unroll
       for (int i = 0; i < TURNS; ++i) {
         const int t = t0 + i * p.side + beside;
-        row[i] = mine && t < here ? at[t] : -1;
         x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
-        if (row[i] >= 0) {
+        if (mine && t < here) {
           const uint4* from = reinterpret_cast<const uint4*>(in + t * stride);
           x[i][0] = from[0];
           x[i][1] = from[1];
         }
       }
+    };
+    load(0);
+    const Nvfp4Tensor nt = nvfp4_tensor(FMT == QF_FMT_NVFP4 ? *(value ? p.v_tscale : p.k_tscale) : 1.0f);
+    if (r0 == 0) find_rows(p, at);
+    for (int t0 = 0; t0 < here; t0 += TURNS * p.side) {
+      uint32_t w[TURNS][8];
 #pragma unroll
       for (int i = 0; i < TURNS; ++i) {
-        const uint32_t w[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
-        uint32_t m = unit_amax_bits(w), scale_code;
+        w[i][0] = x[i][0].x; w[i][1] = x[i][0].y; w[i][2] = x[i][0].z; w[i][3] = x[i][0].w;
+        w[i][4] = x[i][1].x; w[i][5] = x[i][1].y; w[i][6] = x[i][1].z; w[i][7] = x[i][1].w;
+      }
+      load(t0 + TURNS * p.side);
+#pragma unroll
+      for (int i = 0; i < TURNS; ++i) {
+        const int t = t0 + i * p.side + beside;
+        const int64_t row = mine && t < here ? at[t] : -1;
+        uint32_t m = unit_amax_bits(w[i]), scale_code;
         UnitOut o;
         if (FMT == QF_FMT_MXFP4) {
           m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-          o = mxfp4_unit(w, m, p.noclip, scale_code);
+          o = mxfp4_unit(w[i], m, p.noclip, scale_code);
         } else {
           const float amax_b = __uint_as_float(m << 16);
           if (__all_sync(0xFFFFFFFFu, nt.denom_safe && (amax_b == 0.0f || amax_b >= 0x1p-60f)))
-            o = nvfp4_unit<true>(w, amax_b, nt.s_t, nt.denom, nt.rc_denom, scale_code);
-          else o = nvfp4_unit<false>(w, amax_b, nt.s_t, nt.denom, nt.rc_denom, scale_code);
+            o = nvfp4_unit<true>(w[i], amax_b, nt.s_t, nt.denom, nt.rc_denom, scale_code);
+          else o = nvfp4_unit<false>(w[i], amax_b, nt.s_t, nt.denom, nt.rc_denom, scale_code);
         }
-        if (row[i] < 0) continue;
-        *reinterpret_cast<uint2*>(codes + (row[i] << (p.shift + 3))) = o.codes;
-        if (FMT == QF_FMT_NVFP4) scales[row[i] << p.shift] = static_cast<uint8_t>(scale_code);
-        else if ((part & 1) == 0) scales[row[i] << (p.shift - 1)] = static_cast<uint8_t>(scale_code);
+        if (row < 0) continue;
+        *reinterpret_cast<uint2*>(codes + (row << (p.shift + 3))) = o.codes;
+        if (FMT == QF_FMT_NVFP4) scales[row << p.shift] = static_cast<uint8_t>(scale_code);
+        else if ((part & 1) == 0) scales[row << (p.shift - 1)] = static_cast<uint8_t>(scale_code);
       }
     }
   }
@@ -113,7 +125,8 @@ __global__ void __launch_bounds__(kQdqThreads) kv_read_kernel(const __grid_const
   constexpr int TURNS = 4;
   launch_after_previous();
   __shared__ int64_t at[kRowsTokens];
-  const int here = find_rows(p, at);
+  find_rows(p, at);
+  const int here = tokens_here(p);
   const int column = static_cast<int>(threadIdx.x) % p.span, beside = static_cast<int>(threadIdx.x) / p.span;
   if (beside >= p.side) return;
   for (int r = column; r < p.units; r += p.span) {
