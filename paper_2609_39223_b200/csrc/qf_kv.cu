@@ -10,9 +10,14 @@ namespace qf {
 namespace {
 
 // ---- writing and reading rows --------------------------------------------------------------------------------------------
+// Bound by memory: 2 bytes an element on one side, 0.53 or 0.56 on the other.
 // Writing, a thread owns 16 consecutive elements of one head's row, of the keys or of the values: an NVFP4 block, or half an MXFP4 block
-// (one shuffle with its neighbour). Reading, it owns 8, so that a warp's store is 512 bytes on end. A CTA takes a few tokens (slots): where their rows lie is found once per token, and a thread keeps its head
-// and part while it goes through them, so that little is left to do per row but the row itself.
+// (one shuffle with its neighbour). Reading, it owns 8, so that a warp's store is 512 bytes on end (with 16 elements and two stores of
+// 32-byte steps the L1's write path was 75% busy: 78 us for 16 contexts of up to 8192 tokens, 62 now, 0.91 of the copy rate). A CTA takes
+// a few tokens (slots): where their rows lie is found once per token, and a thread keeps its head and part while it goes through them, so
+// that little is left to do per row but the row itself (divisions for every part: 94 us). Writing 16384 tokens of 8 heads of 128 takes
+// 18.1 us in MXFP4 and 21.2 in NVFP4 (0.73 and 0.63 of the copy rate): half of the issue slots are the quantizer's arithmetic, the rest waits for
+// rows. One row of a thread on the way instead of two: 19.5 and 20.3; four: 21.1 and 26.1 (registers).
 
 constexpr int kRowsTokens = 64;      // tokens of a CTA at most
 constexpr int kAppendTurns = 4, kReadTurns = 16;              // rows of a thread, where there are enough
@@ -202,7 +207,8 @@ cudaError_t launch_overlapping(void (*kernel)(Params...), dim3 grid, int threads
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// parts: of a head's row (a power of two from 4 on); kinds: keys, values or both. A CTA gets tokens for a few turns of its threads, fewer where that would leave SMs without a CTA.
+// parts: of a head's row (a power of two from 4 on); kinds: keys, values or both. A CTA gets tokens for a few turns of its threads, fewer
+// where that would leave SMs without a CTA.
 cudaError_t launch_rows(void (*kernel)(KvRows), KvRows& p, int parts, int kinds, int turns, cudaStream_t st) {
   for (p.shift = 2; 1 << p.shift < parts; ++p.shift) {}
   p.units = kinds * p.heads << p.shift;
@@ -215,23 +221,38 @@ cudaError_t launch_rows(void (*kernel)(KvRows), KvRows& p, int parts, int kinds,
 }
 
 // ---- attention -----------------------------------------------------------------------------------------------------------
-// Both products run on mma.sync m16n8k16 with FP16 operands and FP32 sums, keys (values) as the 16-row operand and up to 8 NT rows
-// of queries as columns. A tcgen05 tile would need the decoded keys and values in shared memory, 4 bytes of traffic for each element
-// that takes 0.56 bytes of HBM; here a decoded element never leaves its lane's registers.
+// The floor is one read of the sequences' codes and scales. Both products run on mma.sync m16n8k16 with FP16 operands and FP32 sums, keys
+// (values) as the 16-row operand and up to 8 NT rows of queries as columns. A tcgen05 tile would need the decoded keys and values in shared
+// memory, 4 bytes of traffic for each element that takes 0.56 bytes of HBM; here a decoded element never leaves its lane's registers.
 //
-//  * Exactness. An E2M1 value times its block scale is exact in FP16: six significant bits for E4M3 scales; for E8M0 scales a power of
-//    two relative to the largest scale of the same row, exact over 36 binades (what lies below counts as zero) with the row's own
-//    power of two applied in FP32. A query row is scaled by a power of two to a maximum in [2^14, 2^15): exact in FP16 down to 2^-31 of
-//    its largest element, below which FP32 sums would lose it anyway. So scores are FP32 sums of exact products.
-//  * One pass over the keys with a running maximum and sum per query row. The weights are FP16 numbers 2^10 times their value, so that
-//    those below 2^-24 of the largest are the first to lose bits; the sum takes them unrounded. A unit's value product starts from
-//    zero and is added in FP32: the tensor core truncates as it accumulates, and a chain of thousands would drift.
-//    MXFP4 keeps a second maximum, of score plus the value row's power of two, for the value product's weights: wherever
-//    the softmax puts its weight, that is where the FP16 range lies.
-//  * Work is cut into units of 32 keys of one (sequence, key head, tile of query rows), numbered in that order. CTA c of W takes units
-//    [c U / W, (c + 1) U / W): equal shares whatever the lengths. Its warps share what it has of a sequence, and meet in shared
-//    memory. Only a CTA's first and last pieces can be parts of a longer sequence: those go to the workspace, and a second
-//    kernel joins them in order.
+//  * Decoding. One conversion for two codes, one packed product for two scales. Keys: a lane's codes of a row are pairs of dimensions, and
+//    which dimensions is free as long as the queries agree. Values: the contraction runs over keys, so the pairs are of two keys: the
+//    nibbles of two rows' words are interleaved first (two logic operations for eight values).
+//  * Exactness. An E2M1 value times its E4M3 scale has six significant bits and is exact in FP16. MXFP4 keys: the E2M1 values alone are
+//    multiplied, and a block's sum gets its power of two in FP32. MXFP4 values: FP16 powers of two relative to a scale code that moves
+//    with the data (28 binades without a move). A unit whose values' scales lie further apart takes them relative to each key's largest
+//    (exact over 36 binades, below counts as zero) and that one's power into the key's weight, with a maximum of score plus power for the
+//    FP16 range: wherever the softmax puts its weight. A query row is scaled by a power of two to a maximum in [2^14, 2^15): exact in
+//    FP16 down to 2^-31 of its largest element. So scores are FP32 sums of exact products.
+//  * One pass over the keys. A row's weights are 2^(score - base); they enter the value product as FP16 numbers (relative error 2^-11 at
+//    most), the sum of weights takes them unrounded. The base is 2^6 below the largest score of the unit that set it and moves when a score
+//    passes it by 2^14: rarely, so that most units need no exchange between lanes but one vote (as against a maximum over the lanes
+//    and a product with all sums for every unit: 32 instructions of 600). A unit's value product starts from zero and is added in FP32:
+//    the tensor core truncates as it accumulates, and a chain of thousands would drift.
+//  * Copies: cp.async, two units a warp, with the pieces of a row in an order that keeps all reads free of bank conflicts.
+//  * Work. Units of 32 keys of one (sequence, key head, tile of query rows) are numbered in that order, with 8 places for the start of each:
+//    CTA c of W takes places [c U / W, (c + 1) U / W), equal shares whatever the lengths (sequences of up to 384 keys are not cut). Its warps
+//    share what it has of a sequence and meet in shared memory. Only a CTA's first and last pieces can be parts of longer sequences:
+//    those go to the workspace, and a second kernel joins them in order. Where the page table holds short sequences only, each gets a
+//    cluster of up to 8 CTAs instead, which meets in distributed shared memory: nothing to count, no second kernel (1 x 1000 keys: 8.6 us
+//    without, 5.5 with; 64 x 100: 9.4 and 7.6).
+//
+// What bounds it: instructions. 8 heads of 128, up to 8 rows: 594 a unit in NVFP4 (164 for keys, 250 for values, 72 for copies; 637 in MXFP4),
+// of which the ALU's 260 run at half rate; a copy at the full rate leaves an SM's scheduler 806 cycles for a unit. 128 x 8192: 231 us NVFP4,
+// 241 MXFP4 (0.81 and 0.74 of the copy rate), heads of 256 215 and 227, of 64 (16 of them) 292 and 310. Three CTAs an SM with 168 registers: four with
+// 128 take 1.01 times as long, two with 64 keys a unit 0.98 (and 1.03 to 1.2 times at ragged and short ones). Around the keys a call
+// spends 3.7 us until the first data, up to 4 us on shares that the memory serves unevenly, 2 us where warps meet and 3.5 us in the
+// second kernel: 1 x 131072 keys take 38 us where 23.4 is the floor.
 
 constexpr int kUnitKeys = 32;
 constexpr int kAttnWarps = 4;                 // of a CTA
