@@ -684,32 +684,35 @@ def _kv_here(cache: KvCache):
 
 def _tokens(t: torch.Tensor, name: str, lead, heads: int, dim: int, device: int):
     """Address of BF16 [*lead, heads, dim] with whole tokens (heads * dim elements without gaps) at one distance, and that distance."""
-    if t.dtype != torch.bfloat16 or t.get_device() < 0:
+    at = t.get_device()
+    if t.dtype is not torch.bfloat16 or at < 0:
         raise TypeError(f"{name} must be a CUDA tensor of type torch.bfloat16")
-    if t.get_device() != device:
-        raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is cuda:{device}")
+    if at != device:
+        raise ValueError(f"{name} is on cuda:{at}, the current device is cuda:{device}")
     if t.shape != (*lead, heads, dim):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(*lead, heads, dim)}")
     distance = heads * dim
     if not t.is_contiguous():
         s = t.stride()
         whole = s[-1] == 1 and (heads == 1 or s[-2] == dim)
-        span = 0                                                   # from one group of the tokens so far to the next
-        for n, step in zip(reversed(lead), reversed(s[:-2])):
-            if n != 1:
-                whole &= span == 0 or step == span
-                if span == 0:
-                    distance = step
-                span = step * n
+        if len(lead) == 1:
+            distance = s[0] if lead[0] > 1 else distance
+        elif lead[1] == 1:
+            distance = s[0] if lead[0] > 1 else distance
+        else:
+            distance = s[1]
+            whole &= lead[0] == 1 or s[0] == s[1] * lead[1]
         if not whole:
             raise TypeError(f"{name} must have whole tokens at one distance, its strides are {s}")
     return t.data_ptr(), distance
 
 
 def _slots(slots: torch.Tensor, device: int):
-    if slots.dim() != 1:
-        raise ValueError(f"slots has shape {tuple(slots.shape)}, expected one dimension")
-    return _tensor(slots, "slots", _IDS_DTYPE, slots.shape, device), _IDS_DTYPE[slots.dtype], slots.shape[0]
+    """Address, type and number of the slots."""
+    shape, dtype = slots.shape, _IDS_DTYPE.get(slots.dtype)
+    if len(shape) != 1:
+        raise ValueError(f"slots has shape {tuple(shape)}, expected one dimension")
+    return _tensor(slots, "slots", _IDS_DTYPE, shape, device), dtype, shape[0]
 
 
 def qf_kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, *, flags: int = 0) -> None:

@@ -241,7 +241,7 @@ cudaError_t launch_rows(void (*kernel)(KvRows), KvRows& p, int parts, int kinds,
 //    the tensor core truncates as it accumulates, and a chain of thousands would drift.
 //  * Copies: cp.async, two units a warp, with the pieces of a row in an order that keeps all reads free of bank conflicts.
 //  * Work. Units of 32 keys of one (sequence, key head, tile of query rows) are numbered in that order, with 8 places for the start of each:
-//    CTA c of W takes places [c U / W, (c + 1) U / W), equal shares whatever the lengths (sequences of up to 384 keys are not cut). Its warps
+//    the CTAs take equal runs of them, whatever the lengths (sequences of up to 384 keys are not cut). A CTA's warps
 //    share what it has of a sequence and meet in shared memory. Only a CTA's first and last pieces can be parts of longer sequences:
 //    those go to the workspace, and a second kernel joins them in order. Where the page table holds short sequences only, each gets a
 //    cluster of up to 8 CTAs instead, which meets in distributed shared memory: nothing to count, no second kernel (1 x 1000 keys: 8.6 us
@@ -599,7 +599,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
 
   Walk w;
   int ctas = 0;                                                // shares
-  int64_t total = 0, u1 = 0;                                   // places of all, end of this share
+  int64_t total = 0, share = 0, u1 = 0;                        // places of all, places of a share, end of this one
   if constexpr (DIRECT) {
     const int segment = cta / p.split, rank = cta - segment * p.split;
     w.b = segment / p.segs;
@@ -641,13 +641,13 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
     ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), (total + kAttnWarps - 1) / kAttnWarps));
     bool idle = cta >= ctas;
     if (!idle) {
-      // c * total / ctas without the long product
-      const int64_t q0 = total <= UINT32_MAX ? static_cast<uint32_t>(total) / static_cast<uint32_t>(ctas) : total / ctas;
-      const uint32_t rest = static_cast<uint32_t>(total - q0 * ctas);
-      u1 = (cta + 1) * q0 + (cta + 1) * rest / static_cast<uint32_t>(ctas);
+      // the first CTAs take a place more each, as many as are left over
+      share = total <= UINT32_MAX ? static_cast<uint32_t>(total) / static_cast<uint32_t>(ctas) : total / ctas;
+      const int rest = static_cast<int>(total - share * ctas);
+      u1 = (cta + 1) * share + min(cta + 1, rest);
 #pragma unroll 1
       for (int i = 0; i < 2; ++i) {
-        const int64_t u = i ? u1 : cta * q0 + cta * rest / static_cast<uint32_t>(ctas);
+        const int64_t u = i ? u1 : cta * share + min(cta, rest);
         if (u == total && threadIdx.x == 0) border[i] = total;
         if (u < before || u >= before + mine) continue;
         int64_t r = u - before;
@@ -1189,7 +1189,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       }
       if (!DIRECT && begins && lane == 0 && (p.by_segment || w.n < w.units)) {
         const int64_t last = u1 + (w.units - w.n) - 1;         // place of the sequence's last unit, if others go on with it
-        const int more = w.n < w.units ? static_cast<int>(((last + 1) * ctas - 1) / total) - cta : 0;
+        const int64_t wider = (total - share * ctas) * (share + 1);            // end of the shares with a place more
+        const int more = w.n < w.units ? static_cast<int>(last < wider ? last / (share + 1) : (last - wider) / share + (total - share * ctas)) - cta : 0;
         tasks[p.by_segment ? w.b * p.segs + w.s : cta] = JoinTask{cta, more, w.b, w.s};
       }
     }

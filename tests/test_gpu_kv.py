@@ -490,6 +490,41 @@ def test_decode_steps_in_a_graph(fmt):
 
 
 @fmts
+@pytest.mark.parametrize("max_pages", [4, 64, 2000])
+def test_captured_calls_of_every_cut(fmt, max_pages):
+    """One CTA a sequence, a cluster, shares with a second kernel: captured twice in a row with one workspace, replayed with other lengths
+    and queries, on two graphs that share the workspace one after the other."""
+    batch, heads, group, dim, page = 3, 2, 4, 128, 16
+    g = gen(max_pages)
+    c = random_cache(fmt, 200, page, heads, dim, 7)
+    table = torch.randint(0, 200, (batch, max_pages), generator=g, device="cuda", dtype=torch.int32)
+    lens = torch.tensor([1, max_pages * page, 0], dtype=torch.int32, device="cuda")
+    q = torch.randn((batch, 1, heads * group, dim), generator=g, device="cuda").to(BF)
+    ws = api.workspace(api.OP_KV_ATTENTION, batch, heads * group, dim, heads)
+    outs = [torch.empty_like(q) for _ in range(4)]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        api.qf_kv_attention(c, q, table, lens, out=outs[0], ws=ws)
+        graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+        for i, graph in enumerate(graphs):
+            with torch.cuda.graph(graph, stream=s):
+                api.qf_kv_attention(c, q, table, lens, out=outs[2 * i], ws=ws)
+                api.qf_kv_attention(c, outs[2 * i], table, lens, out=outs[2 * i + 1], ws=ws)
+        for n in ([5, 30, 64], [0, 0, 0], [max_pages * page, 1, 17]):
+            lens.copy_(torch.tensor(n, dtype=torch.int32))
+            q.copy_(torch.randn(q.shape, generator=g, device="cuda"))
+            for graph in graphs:
+                graph.replay()
+            first = api.qf_kv_attention(c, q, table, lens)
+            second = api.qf_kv_attention(c, first, table, lens)
+            for i in (0, 1):
+                assert torch.equal(outs[2 * i], first) and torch.equal(outs[2 * i + 1], second)
+            check_attention(c, q, table, [min(x, max_pages * page) for x in n], dim ** -0.5, first)
+    s.synchronize()
+
+
+@fmts
 def test_two_streams_with_a_workspace_each(fmt):
     cases = []
     for seed in (1, 2):
