@@ -40,7 +40,7 @@ struct KvRows {
   int each;                          // tokens of a CTA
   int page_size, heads;
   int units;                         // parts of a token
-  int span, side;                    // threads for a token, tokens side by side: span * side <= kQdqThreads
+  int span, side;                    // threads for a token (CTAs beside one another have the next), tokens side by side: span * side <= kQdqThreads
   int shift;                         // parts of a head's row: 1 << shift
   bool slots64, noclip;
 };
@@ -67,60 +67,58 @@ __global__ void __launch_bounds__(kQdqThreads) kv_append_kernel(const __grid_con
   __shared__ int64_t at[kRowsTokens];
   const int here = tokens_here(p);
   const int column = static_cast<int>(threadIdx.x) % p.span, beside = static_cast<int>(threadIdx.x) / p.span;
-  for (int r0 = 0; r0 < p.units; r0 += p.span) {
-    const int r = r0 + column;
-    const bool mine = r < p.units && beside < p.side, value = (r >> p.shift) >= p.heads;
-    const int part = r & ((1 << p.shift) - 1), h = mine ? (r >> p.shift) - (value ? p.heads : 0) : 0;
-    const int64_t stride = value ? p.v_stride : p.k_stride;
-    const __nv_bfloat16* in = (value ? p.v : p.k) + static_cast<int64_t>(blockIdx.x) * p.each * stride + ((h << p.shift) + part) * 16;
-    const int64_t row0 = static_cast<int64_t>(h) * p.page_size;
-    uint8_t* codes = (value ? p.v_codes : p.k_codes) + ((row0 << p.shift) + part) * 8;
-    uint8_t* scales = (value ? p.v_scales : p.k_scales) + (FMT == QF_FMT_NVFP4 ? (row0 << p.shift) + part : ((row0 << p.shift) + part) >> 1);
-    // tokens that go nowhere are loaded as well: their slots need not be known yet
-    uint4 x[TURNS][2];
-    const auto load = [&](int t0) {
+  const int r = static_cast<int>(blockIdx.y) * p.span + column;
+  const bool mine = r < p.units && beside < p.side, value = (r >> p.shift) >= p.heads;
+  const int part = r & ((1 << p.shift) - 1), h = mine ? (r >> p.shift) - (value ? p.heads : 0) : 0;
+  const int64_t stride = value ? p.v_stride : p.k_stride;
+  const __nv_bfloat16* in = (value ? p.v : p.k) + static_cast<int64_t>(blockIdx.x) * p.each * stride + ((h << p.shift) + part) * 16;
+  const int64_t row0 = static_cast<int64_t>(h) * p.page_size;
+  uint8_t* codes = (value ? p.v_codes : p.k_codes) + ((row0 << p.shift) + part) * 8;
+  uint8_t* scales = (value ? p.v_scales : p.k_scales) + (FMT == QF_FMT_NVFP4 ? (row0 << p.shift) + part : ((row0 << p.shift) + part) >> 1);
+  // tokens that go nowhere are loaded as well: their slots need not be known yet
+  uint4 x[TURNS][2];
+  const auto load = [&](int t0) {
 #pragma unroll
-      for (int i = 0; i < TURNS; ++i) {
-        const int t = t0 + i * p.side + beside;
-        x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
-        if (mine && t < here) {
-          const uint4* from = reinterpret_cast<const uint4*>(in + t * stride);
-          x[i][0] = from[0];
-          x[i][1] = from[1];
-        }
+    for (int i = 0; i < TURNS; ++i) {
+      const int t = t0 + i * p.side + beside;
+      x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
+      if (mine && t < here) {
+        const uint4* from = reinterpret_cast<const uint4*>(in + t * stride);
+        x[i][0] = from[0];
+        x[i][1] = from[1];
       }
-    };
-    load(0);
-    const Nvfp4Tensor nt = nvfp4_tensor(FMT == QF_FMT_NVFP4 ? *(value ? p.v_tscale : p.k_tscale) : 1.0f);
-    if (r0 == 0) find_rows(p, at);
-    for (int t0 = 0; t0 < here; t0 += TURNS * p.side) {
-      uint32_t w[TURNS][8];
+    }
+  };
+  load(0);
+  const Nvfp4Tensor nt = nvfp4_tensor(FMT == QF_FMT_NVFP4 ? *(value ? p.v_tscale : p.k_tscale) : 1.0f);
+  find_rows(p, at);
+  for (int t0 = 0; t0 < here; t0 += TURNS * p.side) {
+    uint32_t w[TURNS][8];
 #pragma unroll
-      for (int i = 0; i < TURNS; ++i) {
-        w[i][0] = x[i][0].x; w[i][1] = x[i][0].y; w[i][2] = x[i][0].z; w[i][3] = x[i][0].w;
-        w[i][4] = x[i][1].x; w[i][5] = x[i][1].y; w[i][6] = x[i][1].z; w[i][7] = x[i][1].w;
-      }
-      load(t0 + TURNS * p.side);
+    for (int i = 0; i < TURNS; ++i) {
+      w[i][0] = x[i][0].x; w[i][1] = x[i][0].y; w[i][2] = x[i][0].z; w[i][3] = x[i][0].w;
+      w[i][4] = x[i][1].x; w[i][5] = x[i][1].y; w[i][6] = x[i][1].z; w[i][7] = x[i][1].w;
+    }
+    load(t0 + TURNS * p.side);
 #pragma unroll
-      for (int i = 0; i < TURNS; ++i) {
-        const int t = t0 + i * p.side + beside;
-        const int64_t row = mine && t < here ? at[t] : -1;
-        uint32_t m = unit_amax_bits(w[i]), scale_code;
-        UnitOut o;
-        if (FMT == QF_FMT_MXFP4) {
-          m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-          o = mxfp4_unit(w[i], m, p.noclip, scale_code);
-        } else {
-          const float amax_b = __uint_as_float(m << 16);
-          if (__all_sync(0xFFFFFFFFu, nt.denom_safe && (amax_b == 0.0f || amax_b >= 0x1p-60f)))
-            o = nvfp4_unit<true>(w[i], amax_b, nt.s_t, nt.denom, nt.rc_denom, scale_code);
-          else o = nvfp4_unit<false>(w[i], amax_b, nt.s_t, nt.denom, nt.rc_denom, scale_code);
-        }
-        if (row < 0) continue;
-        *reinterpret_cast<uint2*>(codes + (row << (p.shift + 3))) = o.codes;
-        if (FMT == QF_FMT_NVFP4) scales[row << p.shift] = static_cast<uint8_t>(scale_code);
-        else if ((part & 1) == 0) scales[row << (p.shift - 1)] = static_cast<uint8_t>(scale_code);
+    for (int i = 0; i < TURNS; ++i) {
+      const int t = t0 + i * p.side + beside;
+      const int64_t row = mine && t < here ? at[t] : -1;
+      uint32_t m = unit_amax_bits(w[i]), scale_code;
+      UnitOut o;
+      if (FMT == QF_FMT_MXFP4) {
+        m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+        o = mxfp4_unit(w[i], m, p.noclip, scale_code);
+      } else {
+        const float amax_b = __uint_as_float(m << 16);
+        if (__all_sync(0xFFFFFFFFu, nt.denom_safe && (amax_b == 0.0f || amax_b >= 0x1p-60f)))
+          o = nvfp4_unit<true>(w[i], amax_b, nt.s_t, nt.denom, nt.rc_denom, scale_code);
+        else o = nvfp4_unit<false>(w[i], amax_b, nt.s_t, nt.denom, nt.rc_denom, scale_code);
       }
+      if (row < 0) continue;
+      *reinterpret_cast<uint2*>(codes + (row << (p.shift + 3))) = o.codes;
+      if (FMT == QF_FMT_NVFP4) scales[row << p.shift] = static_cast<uint8_t>(scale_code);
+      else if ((part & 1) == 0) scales[row << (p.shift - 1)] = static_cast<uint8_t>(scale_code);
     }
   }
 }
@@ -133,41 +131,40 @@ __global__ void __launch_bounds__(kQdqThreads) kv_read_kernel(const __grid_const
   find_rows(p, at);
   const int here = tokens_here(p);
   const int column = static_cast<int>(threadIdx.x) % p.span, beside = static_cast<int>(threadIdx.x) / p.span;
-  if (beside >= p.side) return;
-  for (int r = column; r < p.units; r += p.span) {
-    const bool value = !p.k_out || (r >> p.shift) >= p.heads;
-    const int part = r & ((1 << p.shift) - 1), h = (r >> p.shift) - ((r >> p.shift) >= p.heads ? p.heads : 0);
-    const int64_t first = ((static_cast<int64_t>(h) * p.page_size) << p.shift) + part, pitch = static_cast<int64_t>(p.heads) << p.shift;
-    const uint32_t* codes = reinterpret_cast<const uint32_t*>(value ? p.v_codes : p.k_codes) + first;
-    const uint8_t* scales = (value ? p.v_scales : p.k_scales) + (first >> (FMT == QF_FMT_NVFP4 ? 1 : 2));
-    uint4* out = reinterpret_cast<uint4*>(value ? p.v_out : p.k_out) + static_cast<int64_t>(blockIdx.x) * p.each * pitch + (h << p.shift) + part;
-    const float2 st = splat(FMT == QF_FMT_NVFP4 ? *(value ? p.v_tscale : p.k_tscale) : 1.0f);
-    for (int t0 = beside; t0 < here; t0 += TURNS * p.side) {
-      uint32_t c[TURNS], sc[TURNS];
+  const int r = static_cast<int>(blockIdx.y) * p.span + column;
+  if (beside >= p.side || r >= p.units) return;
+  const bool value = !p.k_out || (r >> p.shift) >= p.heads;
+  const int part = r & ((1 << p.shift) - 1), h = (r >> p.shift) - ((r >> p.shift) >= p.heads ? p.heads : 0);
+  const int64_t first = ((static_cast<int64_t>(h) * p.page_size) << p.shift) + part, pitch = static_cast<int64_t>(p.heads) << p.shift;
+  const uint32_t* codes = reinterpret_cast<const uint32_t*>(value ? p.v_codes : p.k_codes) + first;
+  const uint8_t* scales = (value ? p.v_scales : p.k_scales) + (first >> (FMT == QF_FMT_NVFP4 ? 1 : 2));
+  uint4* out = reinterpret_cast<uint4*>(value ? p.v_out : p.k_out) + static_cast<int64_t>(blockIdx.x) * p.each * pitch + (h << p.shift) + part;
+  const float2 st = splat(FMT == QF_FMT_NVFP4 ? *(value ? p.v_tscale : p.k_tscale) : 1.0f);
+  for (int t0 = beside; t0 < here; t0 += TURNS * p.side) {
+    uint32_t c[TURNS], sc[TURNS];
 #pragma unroll
-      for (int i = 0; i < TURNS; ++i) {
-        const int t = t0 + i * p.side;
-        const int64_t row = t < here ? at[t] : -1;
-        c[i] = sc[i] = 0u;
-        if (row >= 0) {
-          c[i] = codes[row << p.shift];
-          sc[i] = scales[row << (p.shift - (FMT == QF_FMT_NVFP4 ? 1 : 2))];
-        }
+    for (int i = 0; i < TURNS; ++i) {
+      const int t = t0 + i * p.side;
+      const int64_t row = t < here ? at[t] : -1;
+      c[i] = sc[i] = 0u;
+      if (row >= 0) {
+        c[i] = codes[row << p.shift];
+        sc[i] = scales[row << (p.shift - (FMT == QF_FMT_NVFP4 ? 1 : 2))];
       }
+    }
 #pragma unroll
-      for (int i = 0; i < TURNS; ++i) {
-        const int t = t0 + i * p.side;
-        if (t >= here) break;
-        const float2 sb = splat(FMT == QF_FMT_NVFP4 ? e4m3_decode(sc[i] & 0x7Fu) : e8m0_scale(sc[i]));
-        uint32_t w[4];
+    for (int i = 0; i < TURNS; ++i) {
+      const int t = t0 + i * p.side;
+      if (t >= here) break;
+      const float2 sb = splat(FMT == QF_FMT_NVFP4 ? e4m3_decode(sc[i] & 0x7Fu) : e8m0_scale(sc[i]));
+      uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float2 o = __fmul2_rn(sb, e2m1x2_decode((c[i] >> (8 * j)) & 0xFFu));
-          if (FMT == QF_FMT_NVFP4) o = __fmul2_rn(o, st);
-          w[j] = pack_bf16x2(o.x, o.y);
-        }
-        out[t * pitch] = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int j = 0; j < 4; ++j) {
+        float2 o = __fmul2_rn(sb, e2m1x2_decode((c[i] >> (8 * j)) & 0xFFu));
+        if (FMT == QF_FMT_NVFP4) o = __fmul2_rn(o, st);
+        w[j] = pack_bf16x2(o.x, o.y);
       }
+      out[t * pitch] = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
 }
@@ -214,10 +211,11 @@ cudaError_t launch_rows(void (*kernel)(KvRows), KvRows& p, int parts, int kinds,
   p.units = kinds * p.heads << p.shift;
   p.span = p.units < kQdqThreads ? p.units : kQdqThreads;
   p.side = kQdqThreads / p.span;
-  const int64_t even = p.tokens / (12 * kNumSMs * 4 * p.side) * (4 * p.side);
-  const int64_t each = even == 0 ? p.side : even < turns * p.side ? even : turns * p.side;
+  const int columns = (p.units + p.span - 1) / p.span;         // CTAs side by side for a token's row
+  const int64_t step = 4 * p.side, work = p.tokens * columns, even = work / (12 * kNumSMs * step) * step;
+  const int64_t each = even >= turns * p.side ? turns * p.side : even > 0 ? even : work >= 2 * kNumSMs * step ? step : p.side;
   p.each = static_cast<int>(each < kRowsTokens ? each : kRowsTokens);
-  return launch_overlapping(kernel, dim3(static_cast<unsigned>((p.tokens + p.each - 1) / p.each)), kQdqThreads, 0, st, 1, p);
+  return launch_overlapping(kernel, dim3(static_cast<unsigned>((p.tokens + p.each - 1) / p.each), columns), kQdqThreads, 0, st, 1, p);
 }
 
 // ---- attention -----------------------------------------------------------------------------------------------------------
