@@ -436,8 +436,9 @@ qf_status_t qf_kv_read(const qf_kv_cache_t* cache, const void* slots, qf_dtype_t
  *   workspace    qf_workspace_bytes(QF_OP_KV_ATTENTION, batch * q_len, q_heads, head_dim, kv_heads) bytes, whatever they hold; calls
  *                that can overlap on the GPU (other streams, graphs) need one each
  * Meant for a few tokens a sequence (a decode step, drafted tokens checked together): the cache is read and decoded once per 24 rows of
- * q_len * q_heads / kv_heads (32 for head_dim 64, 8 for 256). For long prompts read the cache back (qf_kv_read). A page table no wider than
- * the sequences need gives short sequences the shorter way (no second kernel for up to 6144 keys, where there are few). */
+ * q_len * q_heads / kv_heads (32 for head_dim 64, 16 for 256; per 8 where there is little to read). For long prompts read the cache
+ * back (qf_kv_read). A page table no wider than the sequences need gives short sequences the shorter way (no second kernel for up to
+ * 6144 keys, where there are few). */
 qf_status_t qf_kv_attention(const qf_kv_cache_t* cache, const void* q, int64_t q_stride, int64_t batch, int q_len, int q_heads,
                             const int32_t* page_table, int64_t max_pages, const int32_t* seq_lens, float softmax_scale, void* out,
                             float* lse, void* workspace, size_t workspace_bytes, void* stream);

@@ -351,13 +351,10 @@ __device__ __forceinline__ T smem_load(uint32_t at) {
   extern __shared__ __align__(128) uint8_t smem[];
   return *reinterpret_cast<const T*>(smem + at);
 }
-__device__ __forceinline__ void smem_store(uint32_t at, const uint2& v) {
+template <typename T>
+__device__ __forceinline__ void smem_store(uint32_t at, const T& v) {
   extern __shared__ __align__(128) uint8_t smem[];
-  *reinterpret_cast<uint2*>(smem + at) = v;
-}
-__device__ __forceinline__ void smem_store(uint32_t at, const float4& v) {
-  extern __shared__ __align__(128) uint8_t smem[];
-  *reinterpret_cast<float4*>(smem + at) = v;
+  *reinterpret_cast<T*>(smem + at) = v;
 }
 
 __device__ __forceinline__ int keys_of(const KvAttn& p, int b) { return min(max(p.lens[b], 0), p.max_keys); }
@@ -570,6 +567,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   constexpr bool MX = FMT == QF_FMT_MXFP4;
   constexpr int NW = D / 32;                                   // words of codes of a key that a lane holds
   constexpr int VWORDS = D == 64 ? 1 : 2;                      // and of a value, per half
+  constexpr bool QS = D == 256 && NT == 2;                     // queries in shared memory (where the parts meet later) instead of 64 registers
   extern __shared__ __align__(128) uint8_t smem[];
   launch_after_previous();
   const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -754,6 +752,22 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       if (n == 0) least = min(max(w.keys - p.q_len + token_of(p, row0) + 1, 0), w.keys);
     }
 
+    if constexpr (QS) {
+      if (warp == 0) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < NW; ++i)
+            smem_store(parts + ((n * NW + i) * 32 + lane) * 16, make_uint4(qf[n][2 * i][0], qf[n][2 * i][1], qf[n][2 * i + 1][0], qf[n][2 * i + 1][1]));
+      }
+      __syncthreads();
+    }
+    // fragments of word i of the rows of tile n
+    const auto query = [&](int n, int i) {
+      if constexpr (QS) return smem_load<uint4>(parts + ((n * NW + i) * 32 + lane) * 16);
+      else return make_uint4(qf[n][2 * i][0], qf[n][2 * i][1], qf[n][2 * i + 1][0], qf[n][2 * i + 1][1]);
+    };
+
     // m: base of a column's weights, which are 2^(score - m); l: the lane's share of their sum; ve (MXFP4): o is in units of 2^ve; vref: the
     // scale code that the values' multipliers refer to (none yet: far below all)
     Sums<MT, NT> a;
@@ -811,8 +825,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
               float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-              mma(z, d0[0], d1[0], d0[1], d1[1], qf[n][2 * x][0], qf[n][2 * x][1]);
-              mma(z, d0[2], d1[2], d0[3], d1[3], qf[n][2 * x + 1][0], qf[n][2 * x + 1][1]);
+              const uint4 q = query(n, x);
+              mma(z, d0[0], d1[0], d0[1], d1[1], q.x, q.y);
+              mma(z, d0[2], d1[2], d0[3], d1[3], q.z, q.w);
               s[half][n][0] = fmaf(z[0], y0, s[half][n][0]);
               s[half][n][1] = fmaf(z[1], y0, s[half][n][1]);
               s[half][n][2] = fmaf(z[2], y1, s[half][n][2]);
@@ -847,9 +862,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
               for (int i = 0; i < 4; ++i) { d0[i] = hmul2(d0[i], x0[x >> 1]); d1[i] = hmul2(d1[i], x1[x >> 1]); }
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
-                const int step = hh * 8 + 2 * x;
-                mma(s[half][n], d0[0], d1[0], d0[1], d1[1], qf[n][step][0], qf[n][step][1]);
-                mma(s[half][n], d0[2], d1[2], d0[3], d1[3], qf[n][step + 1][0], qf[n][step + 1][1]);
+                const uint4 q = query(n, hh * 4 + x);
+                mma(s[half][n], d0[0], d1[0], d0[1], d1[1], q.x, q.y);
+                mma(s[half][n], d0[2], d1[2], d0[3], d1[3], q.z, q.w);
               }
             }
           }
@@ -1082,6 +1097,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
     next = w;
     if constexpr (!DIRECT) next.next(p);
     if constexpr (!DIRECT) fetch(next);                                               // on the way while this piece's parts meet
+    if constexpr (QS) __syncthreads();                         // the queries have been read
     // One result of the piece: sums of a column's weights over the lanes, then warps 2 and 3 to 0 and 1, then 1 to 0.
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -1278,21 +1294,27 @@ cudaError_t attend(KvAttn& p, cudaStream_t st) {
   return launch_overlapping(kv_join_kernel<FMT, D, NT>, dim3(tasks, share < 1 ? 1 : share < S::MT * NT ? share : S::MT * NT), threads, threads * 16, st, 1, p, grid);
 }
 
-// Query rows of a tile, in units of 8, at most: what registers hold next to the decoded words. (Heads of 256 with 16 rows: one CTA an SM and
-// spills, 100 us for 32 sequences of 4096 keys where two tiles of 8 rows take 73.)
-constexpr int tile_most(int head_dim) { return head_dim == 64 ? 4 : head_dim == 128 ? 3 : 1; }
+// Query rows of a tile, in units of 8, at most: what registers hold next to the decoded words. (Heads of 256 with 16 rows: only with the
+// queries in shared memory, 50 us for 12 rows of 4 heads over 32 sequences of 4096 keys where two tiles of 8 rows take 62.)
+constexpr int tile_most(int head_dim) { return head_dim == 64 ? 4 : head_dim == 128 ? 3 : 2; }
 
 // The cache is decoded once per tile, which costs as much as the products of 14 rows (32 sequences of 4096 keys, heads of 128: 38, 52 and
-// 66 us for 8, 16 and 24 rows): as few tiles as can be, evenly filled.
+// 66 us for 8, 16 and 24 rows): as few tiles as can be, evenly filled. But where a table holds few keys, smaller tiles give more CTAs a
+// part and each less to do after its last key: as long as all tiles' units are no more than about three a warp (4 heads of 128, 40 rows
+// each: one sequence of 300 keys 6.1 us instead of 9.1, 7 of them 8.0 instead of 10.4; 7 of 2500 keys 17.4, with tiles of 8 rows 20.0).
+constexpr int64_t kTileUnits = 3 * 2 * kNumSMs * kAttnWarps;
 template <int FMT>
 cudaError_t attend_format(KvAttn& p, int head_dim, cudaStream_t st) {
   const int eights = (p.rows + 7) / 8, most = tile_most(head_dim);
-  p.tiles = (eights + most - 1) / most;
-  const int nt = (eights + p.tiles - 1) / p.tiles;
+  const int64_t units = static_cast<int64_t>(p.batch) * p.kv_heads * ((p.max_keys + kUnitKeys - 1) / kUnitKeys);
+  int nt = 1;
+  while (nt < most && (eights + nt - 1) / nt * units > kTileUnits) ++nt;
+  p.tiles = (eights + nt - 1) / nt;
+  nt = (eights + p.tiles - 1) / p.tiles;
   p.segs = p.tiles * p.kv_heads;
   if (head_dim == 64) return nt == 1 ? attend<FMT, 64, 1>(p, st) : nt == 2 ? attend<FMT, 64, 2>(p, st) : nt == 3 ? attend<FMT, 64, 3>(p, st) : attend<FMT, 64, 4>(p, st);
   if (head_dim == 128) return nt == 1 ? attend<FMT, 128, 1>(p, st) : nt == 2 ? attend<FMT, 128, 2>(p, st) : attend<FMT, 128, 3>(p, st);
-  return attend<FMT, 256, 1>(p, st);
+  return nt == 1 ? attend<FMT, 256, 1>(p, st) : attend<FMT, 256, 2>(p, st);
 }
 
 // Workspace: for the largest kernel of a head size, whatever the format and the tile, since how the rows are split over sequences is

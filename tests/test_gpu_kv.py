@@ -218,6 +218,17 @@ def test_short_sequences_in_a_wide_page_table(fmt, dim, q_len, group):
 
 
 @fmts
+@pytest.mark.parametrize("dim,q_len,group", [(64, 1, 12), (64, 5, 4), (64, 4, 8), (64, 3, 11), (128, 3, 4), (128, 3, 8), (128, 5, 8), (256, 1, 12), (256, 2, 8), (256, 3, 8)])
+@pytest.mark.parametrize("batch,heads,most", [(20, 3, 1536), (50, 4, 700), (8, 3, 10000)])
+def test_every_tile_of_query_rows_with_every_cut(fmt, dim, q_len, group, batch, heads, most):
+    """Tables large enough for the larger tiles, in clusters, with a CTA a sequence, and in shares; few of the sequences fill them."""
+    r = np.random.default_rng(dim + group)
+    lens = [int(x) for x in r.integers(0, 150, batch)]
+    lens[1], lens[2], lens[-1] = min(most, 1100), 0, min(most, 700)
+    attend(fmt, lens, 16, heads, group, dim, q_len=q_len, max_pages=-(-most // 16))
+
+
+@fmts
 def test_the_same_rows_whatever_the_table_can_hold(fmt):
     """Two ways to cut the work give the same rows up to FP32 sums and weights."""
     lens, page = [700, 3, 0, 260, 129], 16
