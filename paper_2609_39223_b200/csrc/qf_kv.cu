@@ -16,7 +16,7 @@ namespace {
 // 32-byte steps the L1's write path was 75% busy: 78 us for 16 contexts of up to 8192 tokens, 62 now, 0.91 of the copy rate). A CTA takes
 // a few tokens (slots): where their rows lie is found once per token, and a thread keeps its head and part while it goes through them, so
 // that little is left to do per row but the row itself (divisions for every part: 94 us). Writing 16384 tokens of 8 heads of 128 takes
-// 18.1 us in MXFP4 and 21.2 in NVFP4 (0.73 and 0.63 of the copy rate): half of the issue slots are the quantizer's arithmetic, the rest waits for
+// 16.5 us in MXFP4 and 20.9 in NVFP4 (0.80 and 0.64 of the copy rate): half of the issue slots are the quantizer's arithmetic, the rest waits for
 // rows. One row of a thread on the way instead of two: 19.5 and 20.3; four: 21.1 and 26.1 (registers).
 
 constexpr int kRowsTokens = 64;      // tokens of a CTA at most
@@ -243,7 +243,7 @@ cudaError_t launch_rows(void (*kernel)(KvRows), KvRows& p, int parts, int kinds,
 //    share what it has of a sequence and meet in shared memory. Only a CTA's first and last pieces can be parts of longer sequences:
 //    those go to the workspace, and a second kernel joins them in order. Where the page table holds short sequences only, each gets a
 //    cluster of up to 8 CTAs instead, which meets in distributed shared memory: nothing to count, no second kernel (1 x 1000 keys: 8.6 us
-//    without, 5.5 with; 64 x 100: 9.4 and 7.6).
+//    without, 5.5 with); or, where there are many, a warp: no meeting either.
 //
 // What bounds it: instructions. 8 heads of 128, up to 8 rows: 594 a unit in NVFP4 (164 for keys, 250 for values, 72 for copies; 637 in MXFP4),
 // of which the ALU's 260 run at half rate; a copy at the full rate leaves an SM's scheduler 806 cycles for a unit. 128 x 8192: 231 us NVFP4,
@@ -253,11 +253,12 @@ cudaError_t launch_rows(void (*kernel)(KvRows), KvRows& p, int parts, int kinds,
 // second kernel: 1 x 131072 keys take 38 us where 23.4 is the floor.
 
 constexpr int kUnitKeys = 32;
-constexpr int kAttnWarps = 4;                 // of a CTA
+constexpr int kAttnWarpBits = 2, kAttnWarps = 1 << kAttnWarpBits;       // of a CTA
 constexpr int kStages = 2;                    // units a warp has in shared memory or on the way
 constexpr int kPieceCost = 8;                 // what a sequence's queries, meeting and result cost, in units
 constexpr int kWhole = 12;                    // sequences of up to so many units are not cut
 constexpr int kDirectUnits = 24;              // of a CTA, where every sequence gets CTAs of its own
+constexpr int kAloneUnits = 4, kAloneMost = 64;              // of a warp, where every sequence gets a warp: per round of CTAs otherwise, at most
 constexpr float kWeightTop = 6.0f, kWeightRoom = 8.0f;       // weights start at up to 2^6 and may reach 2^14 before their base is moved
 
 struct KvAttn {
@@ -277,7 +278,7 @@ struct KvAttn {
   int batch, pages, max_pages, page_size, max_keys;
   int q_len, q_heads, kv_heads, group;
   int rows, tiles, segs;                      // query rows of a key head; tiles of them; (key head, tile) pairs of a sequence
-  int split;                                  // CTAs of a segment, a cluster, where each has its own
+  int split;                                  // CTAs of a segment, a cluster, where each has its own; 0: a warp each
   bool by_segment;                            // JoinTasks are numbered by segment, not by CTA
   int64_t page_codes;                         // bytes of codes in a page
   float scale;                                // times log2 e
@@ -362,6 +363,8 @@ __device__ __forceinline__ int units_of(int keys) { return (keys + kUnitKeys - 1
 // what a segment of a sequence counts for in the shares: a sequence without keys nothing (its zeros are written beforehand)
 __device__ __forceinline__ int cost_of(int keys) { return keys == 0 ? 0 : units_of(keys) + kPieceCost; }
 
+// end of part i - 1 of 1 << bits parts of n units, start of part i
+__device__ __forceinline__ int part_of(int n, int i, int bits) { return static_cast<int>(static_cast<int64_t>(n) * i >> bits); }
 // token of a query row of a key head, key head of a segment
 __device__ __forceinline__ int token_of(const KvAttn& p, int row) { return p.q_len == 1 ? 0 : row / p.group; }
 __device__ __forceinline__ int head_of(const KvAttn& p, int segment) { return p.tiles == 1 ? segment : segment / p.tiles; }
@@ -424,10 +427,10 @@ struct Copier {
     id1 = id0 = static_cast<int>(min(static_cast<uint32_t>(pages[page]), most));
     if (off + 16 >= p.page_size && cur * kUnitKeys + 16 < w.keys) id1 = static_cast<int>(min(static_cast<uint32_t>(pages[page + 1]), most));
   }
-  __device__ __forceinline__ void piece(const KvAttn& p, int warp, int lane) {
+  __device__ __forceinline__ void piece(const KvAttn& p, int warp, int bits, int lane) {
     for (; w.n > 0; w.next(p)) {
-      cur = w.j + static_cast<int>(static_cast<int64_t>(w.n) * warp / kAttnWarps);
-      end = w.j + static_cast<int>(static_cast<int64_t>(w.n) * (warp + 1) / kAttnWarps);
+      cur = w.j + part_of(w.n, warp, bits);
+      end = w.j + part_of(w.n, warp + 1, bits);
       if (cur < end) break;
     }
     if (w.n == 0) return;
@@ -441,11 +444,11 @@ struct Copier {
     sp = (c >= CHUNKS ? p.v_scales : p.k_scales) + row * SROW + c % CHUNKS * 16;
     ids(p);
   }
-  __device__ __forceinline__ void start(const KvAttn& p, int warp, int lane) {
+  __device__ __forceinline__ void start(const KvAttn& p, int warp, int bits, int lane) {
     const int r = lane / PIECES, c = lane % (2 * CHUNKS);
     to = r * ROW + ((lane % PIECES) ^ turn<D>(r)) * 16;
     to_scales = 2 * S::CODES + (c >= CHUNKS ? S::SCALES : 0) + c % CHUNKS * 16 + (ONCE ? lane / (2 * CHUNKS) * 16 * SROW : 0);
-    piece(p, warp, lane);
+    piece(p, warp, bits, lane);
   }
   __device__ __forceinline__ void codes(uint32_t stage, int64_t at) const {
 #pragma unroll
@@ -455,7 +458,7 @@ struct Copier {
       copy16(stage + here + S::CODES + i * 512, vp + at + i * 512);
     }
   }
-  __device__ __forceinline__ void issue(const KvAttn& p, uint32_t stage, int warp, int lane) {
+  __device__ __forceinline__ void issue(const KvAttn& p, uint32_t stage, int warp, int bits, int lane) {
     if (w.n > 0) {
       const bool two = cur * kUnitKeys + 16 < w.keys;
       const int64_t a0 = id0 * p.page_codes + off * ROW;
@@ -475,7 +478,7 @@ struct Copier {
         ids(p);
       } else {
         w.next(p);
-        piece(p, warp, lane);
+        piece(p, warp, bits, lane);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -568,6 +571,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   constexpr int NW = D / 32;                                   // words of codes of a key that a lane holds
   constexpr int VWORDS = D == 64 ? 1 : 2;                      // and of a value, per half
   constexpr bool QS = D == 256 && NT == 2;                     // queries in shared memory (where the parts meet later) instead of 64 registers
+  constexpr uint32_t QUERIES = NT * NW * 512;                  // of a warp
+  static_assert(!QS || kAttnWarps * QUERIES <= kAttnWarps / 2 * S::PART, "a warp's queries for each");
   extern __shared__ __align__(128) uint8_t smem[];
   launch_after_previous();
   const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -575,6 +580,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   const uint32_t ring = warp * S::WARP, vmul = ring + kStages * S::STAGE, parts = kAttnWarps * S::WARP;
   JoinTask* tasks = reinterpret_cast<JoinTask*>(p.ws);
   const int cta = blockIdx.x;
+  const bool alone = DIRECT && p.split == 0;                   // this warp has a segment for itself: no meeting anywhere below
+  const int part = alone ? 0 : warp, bits = alone ? 0 : kAttnWarpBits;
   if (!DIRECT && !p.by_segment && threadIdx.x == 0) tasks[cta].more = 0;
 
   const float vt = MX ? 1.0f : *p.v_tscale;
@@ -585,10 +592,11 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   const auto write_zeros = [&](int b) {
     if (keys_of(p, b) > 0) return;
     const int64_t first = static_cast<int64_t>(b) * p.q_len * p.q_heads, rows = static_cast<int64_t>(p.q_len) * p.q_heads;
+    const int thread = alone ? lane : threadIdx.x, threads = alone ? 32 : kAttnWarps * 32;
     uint4* out = reinterpret_cast<uint4*>(p.out + first * D);
-    for (int64_t i = threadIdx.x; i < rows * (D / 8); i += kAttnWarps * 32) out[i] = make_uint4(0, 0, 0, 0);
+    for (int64_t i = thread; i < rows * (D / 8); i += threads) out[i] = make_uint4(0, 0, 0, 0);
     if (p.lse)
-      for (int64_t i = threadIdx.x; i < rows; i += kAttnWarps * 32) p.lse[first + i] = -INFINITY;
+      for (int64_t i = thread; i < rows; i += threads) p.lse[first + i] = -INFINITY;
     if (p.by_segment)
       for (int i = threadIdx.x; i < p.segs; i += kAttnWarps * 32) tasks[b * p.segs + i].more = 0;
   };
@@ -597,8 +605,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   int ctas = 0;                                                // shares
   int64_t total = 0, share = 0, u1 = 0;                        // places of all, places of a share, end of this one
   if constexpr (DIRECT) {
-    const int segment = cta / p.split, rank = cta - segment * p.split;
+    const int split = alone ? 1 : p.split;
+    const int segment = alone ? cta * kAttnWarps + warp : cta / split, rank = alone ? 0 : cta - segment * split;
     w.b = segment / p.segs;
+    if (w.b >= p.batch) return;                                // (warps of their own only)
     w.s = segment - w.b * p.segs;
     w.keys = keys_of(p, w.b);
     if (w.keys == 0) {
@@ -606,8 +616,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       return;
     }
     w.units = units_of(w.keys);
-    w.j = static_cast<int>(static_cast<int64_t>(w.units) * rank / p.split);
-    w.n = static_cast<int>(static_cast<int64_t>(w.units) * (rank + 1) / p.split) - w.j;
+    w.j = static_cast<int>(static_cast<int64_t>(w.units) * rank / split);
+    w.n = static_cast<int>(static_cast<int64_t>(w.units) * (rank + 1) / split) - w.j;
     w.left = w.pos = 0;
   } else {
     // This CTA's share. All places are counted by all CTAs, each thread a run of the sequences. A border between two shares that falls into
@@ -696,9 +706,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   fetch(w);
   Copier<FMT, D> copy;
   copy.w = w;
-  copy.start(p, warp, lane);
+  copy.start(p, part, bits, lane);
 #pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) copy.issue(p, base + ring + i * S::STAGE, warp, lane);
+  for (int i = 0; i < kStages - 1; ++i) copy.issue(p, base + ring + i * S::STAGE, part, bits, lane);
   int stage = 0;
   if constexpr (!DIRECT)
     for (int b = cta; b < p.batch; b += gridDim.x) write_zeros(b);       // while the first keys are on their way
@@ -752,19 +762,21 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       if (n == 0) least = min(max(w.keys - p.q_len + token_of(p, row0) + 1, 0), w.keys);
     }
 
+    const uint32_t queries = parts + (alone ? warp * QUERIES : 0);
     if constexpr (QS) {
-      if (warp == 0) {
+      if (warp == 0 || alone) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int i = 0; i < NW; ++i)
-            smem_store(parts + ((n * NW + i) * 32 + lane) * 16, make_uint4(qf[n][2 * i][0], qf[n][2 * i][1], qf[n][2 * i + 1][0], qf[n][2 * i + 1][1]));
+            smem_store(queries + ((n * NW + i) * 32 + lane) * 16, make_uint4(qf[n][2 * i][0], qf[n][2 * i][1], qf[n][2 * i + 1][0], qf[n][2 * i + 1][1]));
       }
-      __syncthreads();
+      if (alone) __syncwarp();
+      else __syncthreads();
     }
     // fragments of word i of the rows of tile n
     const auto query = [&](int n, int i) {
-      if constexpr (QS) return smem_load<uint4>(parts + ((n * NW + i) * 32 + lane) * 16);
+      if constexpr (QS) return smem_load<uint4>(queries + ((n * NW + i) * 32 + lane) * 16);
       else return make_uint4(qf[n][2 * i][0], qf[n][2 * i][1], qf[n][2 * i + 1][0], qf[n][2 * i + 1][1]);
     };
 
@@ -783,10 +795,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
         for (int c = 0; c < 4; ++c) a.o[i][n][c] = 0.0f;
     }
 
-    const int from = w.j + static_cast<int>(static_cast<int64_t>(w.n) * warp / kAttnWarps);
-    const int to = w.j + static_cast<int>(static_cast<int64_t>(w.n) * (warp + 1) / kAttnWarps);
+    const int from = w.j + part_of(w.n, part, bits), to = w.j + part_of(w.n, part + 1, bits);
     for (int u = from; u < to; ++u) {
-      copy.issue(p, base + ring + (stage == 0 ? kStages - 1 : stage - 1) * S::STAGE, warp, lane);
+      copy.issue(p, base + ring + (stage == 0 ? kStages - 1 : stage - 1) * S::STAGE, part, bits, lane);
       asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
       __syncwarp();
       const uint32_t here = ring + stage * S::STAGE;
@@ -1097,7 +1108,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
     next = w;
     if constexpr (!DIRECT) next.next(p);
     if constexpr (!DIRECT) fetch(next);                                               // on the way while this piece's parts meet
-    if constexpr (QS) __syncthreads();                         // the queries have been read
+    if (QS && !alone) __syncthreads();                         // the queries have been read
     // One result of the piece: sums of a column's weights over the lanes, then warps 2 and 3 to 0 and 1, then 1 to 0.
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -1117,6 +1128,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       }
 #pragma unroll
     for (int d = kAttnWarps / 2; d > 0; d /= 2) {
+      if (alone) break;
       if (warp >= d && warp < 2 * d) {
         const uint32_t at = parts + (warp - d) * S::PART + lane * 16;
 #pragma unroll
@@ -1171,7 +1183,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
         write_tile<D, NT>(p, sum, w.b, w.s, tile, lane, vt);
       }
       cluster.sync();
-    } else if (warp == 0) {
+    } else if (warp == 0 || alone) {
       const bool begins = w.j == 0;
       if (DIRECT || w.n == w.units) {                          // the whole sequence: the result itself
 #pragma unroll
@@ -1278,7 +1290,15 @@ cudaError_t attend(KvAttn& p, cudaStream_t st) {
   constexpr int64_t ROOM = kNumSMs * S::CTAS;
   const int64_t segments = static_cast<int64_t>(p.batch) * p.segs;
   const int units = (p.max_keys + kUnitKeys - 1) / kUnitKeys;
-  // Short sequences, by what the page table holds: CTAs of their own for each, so that nothing has to be counted, nor joined by a second
+  // Many short sequences, by what the page table holds: a warp each. A CTA each would be several rounds of CTAs, each with a start and
+  // a meeting for a few units a warp, and equal shares have those to count and to pay for too (heads of 128, ragged: 3200 segments of up to 8
+  // keys 27.3 us with CTAs, 8.4 with warps; of up to 380 43.2 and 32.1; 8000 of up to 1500 218 with shares, 198 with warps; but 720 of up to 240
+  // 11.3 with CTAs, 12.9 with warps, whose units then take longer than a second round). At most 64, for the one long sequence among short ones.
+  if (segments > ROOM && units <= kAloneMost && units * ROOM <= kAloneUnits * segments && segments <= INT32_MAX) {
+    p.split = 0;
+    return launch_attention<FMT, D, NT, true>(p, (segments + kAttnWarps - 1) / kAttnWarps, 1, st);
+  }
+  // Short sequences: CTAs of their own for each, so that nothing has to be counted, nor joined by a second
   // kernel. As many as there is room for and as have a unit for every warp.
   p.split = 1;
   while (p.split < 8 && p.split * kAttnWarps < units && 2 * p.split * segments <= ROOM) p.split *= 2;

@@ -229,6 +229,17 @@ def test_every_tile_of_query_rows_with_every_cut(fmt, dim, q_len, group, batch, 
 
 
 @fmts
+@pytest.mark.parametrize("dim,q_len,group", [(64, 1, 1), (64, 3, 4), (64, 3, 8), (64, 4, 8), (64, 9, 4), (128, 1, 8), (128, 3, 4), (128, 3, 8), (128, 5, 8), (256, 1, 4), (256, 3, 4), (256, 3, 8)])
+@pytest.mark.parametrize("most", [1, 130])
+def test_a_warp_a_sequence(fmt, dim, q_len, group, most):
+    """More (sequence, head) pairs than CTAs, not a multiple of a CTA's warps, of empty to short sequences."""
+    r = np.random.default_rng(dim + group)
+    lens = [int(x) for x in r.integers(0, most + 1, 701)]
+    lens[0], lens[-1] = most, 0
+    attend(fmt, lens, 16, 3, group, dim, q_len=q_len)
+
+
+@fmts
 def test_the_same_rows_whatever_the_table_can_hold(fmt):
     """Two ways to cut the work give the same rows up to FP32 sums and weights."""
     lens, page = [700, 3, 0, 260, 129], 16
