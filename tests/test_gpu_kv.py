@@ -103,6 +103,13 @@ def test_rows_are_the_oracles_and_nothing_else_changes(fmt, tokens, heads, dim, 
 
 
 @fmts
+@pytest.mark.parametrize("tokens,heads,dim,page,dtype", [(61, 14, 256, 16, torch.int64), (700, 33, 128, 32, torch.int32), (6001, 7, 128, 64, torch.int64),
+                                                         (20011, 1, 64, 16, torch.int32), (5, 70, 256, 16, torch.int64)])
+def test_rows_that_need_several_CTAs_and_CTAs_of_several_rows(fmt, tokens, heads, dim, page, dtype):
+    test_rows_are_the_oracles_and_nothing_else_changes(fmt, tokens, heads, dim, page, dtype)
+
+
+@fmts
 @pytest.mark.parametrize("noclip", [False, True])
 def test_every_magnitude(fmt, noclip):
     """Raw BF16 patterns over the whole finite range, with the tensor scale far from them as well."""
