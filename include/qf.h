@@ -421,9 +421,11 @@ qf_status_t qf_kv_read(const qf_kv_cache_t* cache, const void* slots, qf_dtype_t
 /* Attention of the last q_len tokens of every sequence over its cached keys, their own among them (write them first):
  *     s_j = softmax_scale * <q, k_j>,   p = softmax over the keys j < seq_lens[b] - q_len + i + 1,   out = sum over j of p_j * v_j
  * for token i in [0, q_len) of sequence b and every query head; query head h reads key/value head h / (q_heads / kv_heads).
- * FP32 scores, softmax and sums; the weights p_j enter the value product as FP16 numbers (relative error 2^-11 at most, below the
- * BF16 result's 2^-8) and the dequantized keys and values are not rounded to BF16, as in qf_fq_matvec. MXFP4: key blocks of scale
- * 2^-127 count as zeros, and so may value blocks whose scale is less than 2^-36 of the largest of the same key and head. A row without
+ * FP32 scores, softmax and sums; the weights p_j enter the value product as FP16 numbers (off by 2^-11 of themselves at most, below the
+ * BF16 result's 2^-8, or, for weights below 2^-20 of the row's largest, by up to 2^-31 of that one) and the dequantized keys and values are
+ * not rounded to BF16, as in qf_fq_matvec. MXFP4: key blocks of scale 2^-127 count as zeros, and so may value blocks whose scale is less
+ * than 2^-36 of the largest of the same key and head; where the sizes of the values differ by more than 2^8, small weights of large values
+ * are kept as well, and products p_j * v_j below 2^-31 of the largest may count as zeros. A row without
  * keys (an empty place of a padded batch, a token of a sequence shorter than q_len) gives zeros. Results do not change from run to run;
  * how the keys are cut depends on the batch's lengths and on max_pages, so that the same row can have other last bits in another batch.
  *   q            BF16 [batch, q_len, q_heads, head_dim], q_stride elements from one token to the next (at least q_heads * head_dim, a

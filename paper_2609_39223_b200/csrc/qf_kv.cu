@@ -230,13 +230,15 @@ cudaError_t launch_rows(void (*kernel)(KvRows), KvRows& p, int parts, int kinds,
 //    multiplied, and a block's sum gets its power of two in FP32. MXFP4 values: FP16 powers of two relative to a scale code that moves
 //    with the data (28 binades without a move). A unit whose values' scales lie further apart takes them relative to each key's largest
 //    (exact over 36 binades, below counts as zero) and that one's power into the key's weight, with a maximum of score plus power for the
-//    FP16 range: wherever the softmax puts its weight. A query row is scaled by a power of two to a maximum in [2^14, 2^15): exact in
-//    FP16 down to 2^-31 of its largest element. So scores are FP32 sums of exact products.
-//  * One pass over the keys. A row's weights are 2^(score - base); they enter the value product as FP16 numbers (relative error 2^-11 at
-//    most), the sum of weights takes them unrounded. The base is 2^6 below the largest score of the unit that set it and moves when a score
-//    passes it by 2^14: rarely, so that most units need no exchange between lanes but one vote (as against a maximum over the lanes
-//    and a product with all sums for every unit: 32 instructions of 600). A unit's value product starts from zero and is added in FP32:
-//    the tensor core truncates as it accumulates, and a chain of thousands would drift.
+//    FP16 range. Where the reference moves up, a row's base (below) moves down with it as far as its products so far allow. A query row is
+//    scaled by a power of two to a maximum in [2^14, 2^15): exact in FP16 down to 2^-31 of its largest element. So scores are FP32 sums of
+//    exact products.
+//  * One pass over the keys. A row's weights are 2^(score - base); they enter the value product as FP16 numbers (off by 2^-11 of
+//    themselves at most, or, below 2^-20 of the largest, by 2^-31 of that), the sum of weights takes them unrounded. The base is 2^6 below
+//    the largest score of the unit that set it and moves when a score passes it by 2^14: rarely, so that most units need no exchange
+//    between lanes but one vote (as against a maximum over the lanes and a product with all sums for every unit: 32 instructions of
+//    600). A unit's value product starts from zero and is added in FP32: the tensor core truncates as it accumulates, and a chain of
+//    thousands would drift.
 //  * Copies: cp.async, two units a warp, with the pieces of a row in an order that keeps all reads free of bank conflicts.
 //  * Work. Units of 32 keys of one (sequence, key head, tile of query rows) are numbered in that order, with 8 places for the start of each:
 //    the CTAs take equal runs of them, whatever the lengths (sequences of up to 384 keys are not cut). A CTA's warps
@@ -926,6 +928,34 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       if (__any_sync(0xFFFFFFFFu, move)) {
         float was[NT][2];                                      // logarithm of what the weights so far have to be multiplied with
         const int vtop = MX ? __reduce_max_sync(0xFFFFFFFFu, key_top) : 0, vlow = MX ? __reduce_min_sync(0xFFFFFFFFu, key_low) + 1 : 0;
+        // (scores of keys without values, vtop 0, do not bind the values' weights either)
+        const bool refer = MX && (vtop > vref + 8 || vlow < vref - 19 || vtop == 0), first = vref < 0 && vhigh == 0;
+        vhigh = max(vhigh, vtop);
+        wide = MX && (vtop - vlow > 19 || (refer && vhigh - vtop > 60));         // sums in units of so much less than their values could overflow
+        if (__builtin_expect(MX && refer && !wide && !first, false)) {
+          // Far larger values may matter with weights that are lost as FP16 numbers under a base that follows the scores alone. It goes down,
+          // to where theirs start at 2^6, as long as the sums of products so far stay below 2^21 in the new unit (what they hold is
+          // not outweighed then) and the sum of weights below 2^101.
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              float sums = 0.0f, weights = a.l[n][c];
+#pragma unroll
+              for (int i = 0; i < MT; ++i) sums = fmaxf(sums, fmaxf(fabsf(a.o[i][n][c]), fabsf(a.o[i][n][c + 2])));
+#pragma unroll
+              for (int d = 4; d < 32; d *= 2) {
+                sums = fmaxf(sums, __shfl_xor_sync(0xFFFFFFFFu, sums, d));
+                weights += __shfl_xor_sync(0xFFFFFFFFu, weights, d);
+              }
+              const int sums_log = max(static_cast<int>(__float_as_uint(sums) >> 23) - 127, -80), weights_log = max(static_cast<int>(__float_as_uint(weights) >> 23) - 127, 0);
+              float down = fminf(fmaxf(ve[n][c] - static_cast<float>(vtop - 132 + 20 - sums_log), static_cast<float>(weights_log - 100)), 0.0f);
+              down = a.m[n][c] + down - a.m[n][c];             // as far as the base can follow
+              a.m[n][c] += down;
+              a.l[n][c] *= exp2_approx(-down);
+              ve[n][c] -= down;                                // (the sums follow with their new unit)
+            }
+        }
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -939,9 +969,6 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
             a.l[n][c] *= exp2_approx(was[n][c]);
           }
         if constexpr (MX) {
-          const bool refer = vtop > vref + 8 || vlow < vref - 19;
-          vhigh = max(vhigh, vtop);
-          wide = vtop - vlow > 19 || (refer && vhigh - vtop > 60);       // sums in units of so much less than their values could overflow
           if (wide) {
             // A key's value codes relative to its own largest one, exact over 36 binades, with that one's power of two in the weight: the
             // weights of the value product are kept in FP16's range by a maximum of their own.

@@ -1,0 +1,53 @@
+"""Attention over the 4-bit cache at the ends of its ranges: values whose size changes along a sequence the other way round than their
+scores, NaN and infinities, scores of any size. The 64-bit form and the derived bounds are those of the other attention tests."""
+import math
+
+import pytest
+import torch
+
+from kv_reference import check_attention
+from paper_2609_39223_b200 import api
+from test_gpu_kv import BF, fmts, gen, random_cache
+
+pytestmark = pytest.mark.gpu
+
+
+def paged_in_order(batch, n, page):
+    """A page table of `batch` sequences of n keys each, one behind the other, and the number of pages."""
+    each = -(-n // page)
+    return torch.arange(batch * each, dtype=torch.int32, device="cuda").view(batch, each), torch.full((batch,), n, dtype=torch.int32, device="cuda"), batch * each
+
+
+@pytest.mark.parametrize("apart", [20, 27, 33, 45])
+@pytest.mark.parametrize("rise", [9, 30, 60, 75])
+@pytest.mark.parametrize("dim,q_len,group,batch,heads,n", [(128, 1, 4, 3, 2, 320), (128, 1, 4, 3, 2, 3000), (64, 1, 1, 300, 2, 320), (128, 3, 8, 2, 2, 1500),
+                                                           (256, 2, 8, 2, 1, 1500), (64, 4, 8, 40, 4, 1600)])
+def test_values_that_grow_where_scores_fall(dim, q_len, group, batch, heads, n, rise, apart):
+    """MXFP4: units of 32 keys in turn, one with high scores and small values, one with scores 2^-apart below and values 2^rise above, in either
+    order; then the first kind behind the second for good, and the other way round; and values of zero under the high scores."""
+    page = 32
+    table, lens, pages = paged_in_order(batch, n, page)
+    c = random_cache(api.FMT_MXFP4, pages, page, heads, dim, 3)
+    c.k_scales.fill_(127)
+    place = torch.arange(pages, device="cuda") % table.shape[1]
+    q = torch.ones((batch, q_len, heads * group, dim), dtype=BF, device="cuda")
+    scale = apart * math.log(2.0) / (2 * dim)                       # keys of 1 and -1
+    half = table.shape[1] // 2
+    for large in (place % 2 == 1, place % 2 == 0, place >= half, place < half, place % 5 == 3):
+        c.k_codes.copy_(torch.where(large, 0xAA, 0x22).to(torch.uint8)[:, None, None, None].expand_as(c.k_codes))
+        c.v_scales.copy_(torch.where(large, 100 + rise, 100).to(torch.uint8)[:, None, None, None].expand_as(c.v_scales))
+        out, lse = api.qf_kv_attention(c, q, table, lens, softmax_scale=scale, want_lse=True)
+        check_attention(c, q[:2], table[:2], [n] * min(batch, 2), scale, out[:2], lse[:2])
+    c.v_scales.copy_(torch.where(large, 127, 0).to(torch.uint8)[:, None, None, None].expand_as(c.v_scales))
+    codes = c.v_codes.clone()
+    c.v_codes.mul_(large[:, None, None, None].to(torch.uint8))
+    out, lse = api.qf_kv_attention(c, q, table, lens, softmax_scale=scale, want_lse=True)
+    check_attention(c, q[:2], table[:2], [n] * min(batch, 2), scale, out[:2], lse[:2])
+    c.v_codes.copy_(codes)
+    # several levels, each further down in scores and further up in values than the one before, over and over and back
+    level = (place % 6 - 3).abs()                                   # 3 2 1 0 1 2
+    c.k_codes.fill_(0x22)
+    c.k_scales.copy_((127 - level).to(torch.uint8)[:, None, None, None].expand_as(c.k_scales))
+    c.v_scales.copy_((60 + level * rise * 2 // 3).to(torch.uint8)[:, None, None, None].expand_as(c.v_scales))
+    out, lse = api.qf_kv_attention(c, q, table, lens, softmax_scale=2 * scale, want_lse=True)
+    check_attention(c, q[:2], table[:2], [n] * min(batch, 2), 2 * scale, out[:2], lse[:2])
