@@ -434,7 +434,8 @@ qf_status_t qf_kv_read(const qf_kv_cache_t* cache, const void* slots, qf_dtype_t
  *   seq_lens     device int32 [batch]
  *   out          BF16 [batch, q_len, q_heads, head_dim]
  *   lse          FP32 [batch, q_len, q_heads], nullable: receives the logarithm of the sum over j of exp(s_j), -infinity for a row
- *                without keys: what joining with other keys' attention takes
+ *                without keys: what joining with other keys' attention takes. A score that is NaN or +infinity makes the row's out and
+ *                lse NaN
  *   workspace    qf_workspace_bytes(QF_OP_KV_ATTENTION, batch * q_len, q_heads, head_dim, kv_heads) bytes, whatever they hold; calls
  *                that can overlap on the GPU (other streams, graphs) need one each
  * Meant for a few tokens a sequence (a decode step, drafted tokens checked together): the cache is read and decoded once per 24 rows of

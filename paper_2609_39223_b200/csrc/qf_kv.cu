@@ -542,7 +542,8 @@ struct Joint {
   }
 };
 
-__device__ __forceinline__ float log_sum(float m, float l) { return l > 0.0f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY; }
+// Of no weight at all: -infinity; of a sum that is NaN: NaN, like the row's outputs.
+__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f; }
 
 __device__ __forceinline__ float4* parts_of(const KvAttn& p, int grid) {
   return reinterpret_cast<float4*>(p.ws + ((grid * sizeof(JoinTask) + 255) & ~static_cast<size_t>(255)));
@@ -558,7 +559,7 @@ __device__ __forceinline__ void write_tile(const KvAttn& p, const Joint<EVEN>& s
     if (row >= p.rows) continue;
     const int token = token_of(p, row), head = h * p.group + (row - token * p.group);
     const int64_t at = (static_cast<int64_t>(b) * p.q_len + token) * p.q_heads + head;
-    const float l = c ? sum.ml.w : sum.ml.y, f = l > 0.0f ? vt / l : 0.0f;
+    const float l = c ? sum.ml.w : sum.ml.y, f = l == 0.0f ? 0.0f : vt / l;
     *reinterpret_cast<uint32_t*>(p.out + at * D + dim_of<D>(i, g)) = pack_bf16x2((c ? sum.o.y : sum.o.x) * f, (c ? sum.o.w : sum.o.z) * f);
     if (p.lse && i == 0 && g == 0) p.lse[at] = log_sum(c ? sum.ml.z : sum.ml.x, l);
   }
@@ -1221,7 +1222,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
             if (row < p.rows) {
               const int token = token_of(p, row), head = h * p.group + (row - token * p.group);
               const int64_t at = (static_cast<int64_t>(w.b) * p.q_len + token) * p.q_heads + head;
-              const float f = a.l[n][c] > 0.0f ? vt / a.l[n][c] : 0.0f;
+              const float f = a.l[n][c] == 0.0f ? 0.0f : vt / a.l[n][c];
               uint32_t* out = reinterpret_cast<uint32_t*>(p.out + at * D);
 #pragma unroll
               for (int i = 0; i < MT; i += 4)

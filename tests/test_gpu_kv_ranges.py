@@ -51,3 +51,32 @@ def test_values_that_grow_where_scores_fall(dim, q_len, group, batch, heads, n, 
     c.v_scales.copy_((60 + level * rise * 2 // 3).to(torch.uint8)[:, None, None, None].expand_as(c.v_scales))
     out, lse = api.qf_kv_attention(c, q, table, lens, softmax_scale=2 * scale, want_lse=True)
     check_attention(c, q[:2], table[:2], [n] * min(batch, 2), 2 * scale, out[:2], lse[:2])
+
+
+# one sequence to a warp, a CTA, a cluster, and in shares that a second kernel joins
+CUTS = pytest.mark.parametrize("batch,heads,n", [(300, 2, 100), (20, 3, 600), (2, 2, 1000), (2, 2, 30000)], ids=["warps", "CTAs", "clusters", "shares"])
+
+
+@fmts
+@CUTS
+@pytest.mark.parametrize("dim,q_len,group", [(64, 1, 3), (128, 2, 8), (256, 2, 8)])
+def test_queries_with_nan_and_infinity(fmt, dim, q_len, group, batch, heads, n):
+    """NaN in the outputs and the logarithm of such a row, as the formula has it, and in no other. (The others' last bits may
+    differ: the bases of a tile's rows move together, where any of them has to, and a weight 2^(score - base) is rounded to FP16. So they are held
+    to the bounds, which no base enters.)"""
+    table, lens, pages = paged_in_order(batch, n, 16)
+    c = random_cache(fmt, pages, 16, heads, dim, 3)
+    q = torch.randn((batch, q_len, heads * group, dim), generator=gen(1), device="cuda").to(BF)
+    clean, (clean_out, clean_lse) = q.clone(), api.qf_kv_attention(c, q, table, lens, want_lse=True)
+    rows = torch.zeros(q.shape[:3], dtype=torch.bool, device="cuda")
+    for i, what in enumerate((math.nan, math.inf, -math.inf)):
+        at = (i % batch, (i + 1) % q_len, (2 * i) % (heads * group))
+        q[at][(7 * i) % dim] = what
+        rows[at] = True
+    rows[0, 0, 1] = True
+    q[0, 0, 1] = math.nan
+    out, lse = api.qf_kv_attention(c, q, table, lens, want_lse=True)
+    assert torch.isnan(out[rows]).all() and torch.isnan(lse[rows]).all()
+    out, lse = torch.where(rows[..., None], clean_out, out), torch.where(rows, clean_lse, lse)
+    check_attention(c, clean[:3], table[:3], lens[:3], dim ** -0.5, out[:3], lse[:3])
+    assert torch.equal(out[3:], clean_out[3:]) and torch.equal(lse[3:], clean_lse[3:])
