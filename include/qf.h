@@ -378,7 +378,8 @@ qf_status_t qf_fq_grouped_matvec(qf_format_t fmt, const void* X, int64_t x_rows,
  * What a rollout keeps between the products of its layers (Section 3.4): the keys and values of all earlier tokens, in the formats
  * that the weights are deployed in. The cache of one layer is paged; a page holds page_size tokens of every key/value head:
  *     k_codes, v_codes     [pages, kv_heads, page_size, head_dim / 2] bytes, element 2j in the low nibble of byte j
- *     k_scales, v_scales   [pages, kv_heads, page_size, head_dim / 16] E4M3 bytes (NVFP4) or [..., head_dim / 32] E8M0 bytes (MXFP4)
+ *     k_scales, v_scales   [pages, kv_heads, page_size, head_dim / 16] E4M3 bytes (NVFP4; sign bit clear, 0x7F is 480 as in qf_dequant) or
+ *                          [..., head_dim / 32] E8M0 bytes (MXFP4)
  *     k_tscale, v_tscale   NVFP4: device float*, the tensor scales of the layer's keys and values, settled before the first write (from
  *                          a calibration: they cannot follow data that arrives token by token); otherwise ignored
  * A row of head_dim elements is quantized as qf_qdq does it with a given tensor scale. Slot s is place s % page_size of page

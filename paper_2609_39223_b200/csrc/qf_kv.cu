@@ -324,12 +324,12 @@ __device__ __forceinline__ void e2m1_f16(uint32_t q, uint32_t (&w)[4]) {
       : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
       : "r"(q));
 }
-// Two E4M3 codes (the low bytes) -> FP16 pair
-__device__ __forceinline__ uint32_t e4m3_pair(uint32_t two) {
-  uint32_t r;
-  asm("{\n.reg .b16 h;\ncvt.u16.u32 h, %1;\ncvt.rn.f16x2.e4m3x2 %0, h;\n}" : "=r"(r) : "r"(two));
-  return r;
-}
+// An E4M3 code's seven bits under FP16's exponent are its value times 2^-8, exactly, subnormals included, and code 0x7F, the scale of a
+// block of NaNs, is the number 480 that reading it back takes it for. (As the NaN of the conversion instruction it would reach the sums of
+// tokens that do not see its key.)
+constexpr float kE4m3Up = 256.0f;
+__device__ __forceinline__ uint32_t e4m3_twice(uint32_t code) { return code * 0x00800080u; }
+__device__ __forceinline__ uint32_t e4m3_pair(uint32_t low, uint32_t high) { return low * 0x80u + high * 0x00800000u; }
 // E8M0 code `i` of four -> its power of two; code 0 -> 0 (zeros, or elements below 2^-124)
 __device__ __forceinline__ float e8m0_of(uint32_t codes, int i) {
   const uint32_t at = i == 3 ? codes >> 1 : codes << (23 - 8 * i);
@@ -587,8 +587,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   const int part = alone ? 0 : warp, bits = alone ? 0 : kAttnWarpBits;
   if (!DIRECT && !p.by_segment && threadIdx.x == 0) tasks[cta].more = 0;
 
-  const float vt = MX ? 1.0f : *p.v_tscale;
-  const float kt = p.scale * (MX ? 1.0f : *p.k_tscale);
+  const float vt = MX ? 1.0f : *p.v_tscale * kE4m3Up;
+  const float kt = p.scale * (MX ? 1.0f : *p.k_tscale * kE4m3Up);
   const float sign = kt < 0.0f ? -1.0f : 1.0f;                 // of the scale: goes to the queries, so that a column's factor is positive
 
   // A sequence without keys: zeros. (With keys: nothing.)
@@ -856,16 +856,16 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
             if constexpr (D == 64) {
               const uint2 v0 = smem_load<uint2>(keys), v1 = smem_load<uint2>(keys + 8 * 32);
               c0[0] = v0.x; c0[1] = v0.y; c1[0] = v1.x; c1[1] = v1.y;
-              x0[0] = e4m3_pair(smem_load<uint8_t>(kscales) * 0x0101u);
-              x1[0] = e4m3_pair(smem_load<uint8_t>(kscales + 8 * NB) * 0x0101u);
+              x0[0] = e4m3_twice(smem_load<uint8_t>(kscales));
+              x1[0] = e4m3_twice(smem_load<uint8_t>(kscales + 8 * NB));
             } else {
               const uint32_t words = hh == 0 ? keys : here + (k_at ^ 64) + half * 16 * (D / 2);
               const uint4 v0 = smem_load<uint4>(words), v1 = smem_load<uint4>(words + 8 * (D / 2));
               c0[0] = v0.x; c0[1] = v0.y; c0[2] = v0.z; c0[3] = v0.w;
               c1[0] = v1.x; c1[1] = v1.y; c1[2] = v1.z; c1[3] = v1.w;
-              const uint32_t y0 = e4m3_pair(smem_load<uint16_t>(kscales + hh * 8)), y1 = e4m3_pair(smem_load<uint16_t>(kscales + 8 * NB + hh * 8));
-              x0[0] = __byte_perm(y0, 0, 0x1010); x0[1] = __byte_perm(y0, 0, 0x3232);
-              x1[0] = __byte_perm(y1, 0, 0x1010); x1[1] = __byte_perm(y1, 0, 0x3232);
+              const uint32_t y0 = smem_load<uint16_t>(kscales + hh * 8), y1 = smem_load<uint16_t>(kscales + 8 * NB + hh * 8);
+              x0[0] = e4m3_twice(y0 & 0xFFu); x0[1] = e4m3_twice(y0 >> 8);
+              x1[0] = e4m3_twice(y1 & 0xFFu); x1[1] = e4m3_twice(y1 >> 8);
             }
 #pragma unroll
             for (int x = 0; x < WORDS; ++x) {
@@ -1078,7 +1078,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
               const uint32_t first = smem_load<uint8_t>(here + vs_at[0] + (half * 16 + r * 8) * NB + hh * (128 / S::BLOCK));
               const uint32_t second = smem_load<uint8_t>(here + vs_at[1] + (half * 16 + r * 8) * NB + hh * (128 / S::BLOCK));
               if constexpr (MX) y[half][r] = __viaddmax_s16x2_relu(__byte_perm(first, second, 0x5410), up, 0) << 10;
-              else y[half][r] = e4m3_pair(__byte_perm(first, second, 0x0040));
+              else y[half][r] = e4m3_pair(first, second);
             }
         }
         if (key0 + kUnitKeys > w.keys) {                       // what stands behind the last key
@@ -1259,7 +1259,7 @@ __global__ void __launch_bounds__(1024) kv_join_kernel(const __grid_constant__ K
   using S = Shape<FMT, D, NT>;
   constexpr int PART4 = S::PART / 16, TILES = S::MT * NT;
   launch_after_previous();
-  const float vt = FMT == QF_FMT_NVFP4 ? *p.v_tscale : 1.0f;
+  const float vt = FMT == QF_FMT_NVFP4 ? *p.v_tscale * kE4m3Up : 1.0f;
   const JoinTask task = reinterpret_cast<const JoinTask*>(p.ws)[blockIdx.x];
   if (task.more == 0) return;
   const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31;

@@ -80,3 +80,30 @@ def test_queries_with_nan_and_infinity(fmt, dim, q_len, group, batch, heads, n):
     out, lse = torch.where(rows[..., None], clean_out, out), torch.where(rows, clean_lse, lse)
     check_attention(c, clean[:3], table[:3], lens[:3], dim ** -0.5, out[:3], lse[:3])
     assert torch.equal(out[3:], clean_out[3:]) and torch.equal(lse[3:], clean_lse[3:])
+
+
+@fmts
+@CUTS
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_tokens_before_one_of_nans(fmt, dim, batch, heads, n):
+    """Four tokens of every sequence, the last of which was written with keys and values of NaN: the three that do not see it stay as they
+    are. NVFP4: the one that sees it takes it for what qf_kv_read says."""
+    table, lens, pages = paged_in_order(batch, n, 16)
+    c = random_cache(fmt, pages, 16, heads, dim, 3)
+    at = (lens - 1).long()
+    slots = table.gather(1, (at // 16)[:, None])[:, 0].long() * 16 + at % 16
+    x = torch.full((batch, heads, dim), math.nan, dtype=BF, device="cuda")
+    api.qf_kv_append(c, x, x, slots)
+    q = torch.randn((batch, 4, heads * 2, dim), generator=gen(1), device="cuda").to(BF)
+    q[:, 3] = 0                                                     # scores of 0: the mean of all values
+    out, lse = api.qf_kv_attention(c, q, table, lens, want_lse=True)
+    check_attention(c, q[:3, :3], table[:3], lens[:3] - 1, dim ** -0.5, out[:3, :3], lse[:3, :3])
+    assert torch.isfinite(out[:, :3].float()).all()
+    if fmt == api.FMT_NVFP4:
+        for b in range(min(batch, 3)):
+            every = table[b].long().repeat_interleave(16) * 16 + torch.arange(16, device="cuda").repeat(table.shape[1])
+            _, v = api.qf_kv_read(c, every[:n], want_k=False)
+            mean, mass = v.double().mean(0).repeat_interleave(2, 0), v.double().abs().mean(0).repeat_interleave(2, 0)
+            # BF16 values read back and the BF16 result are off by 2^-9 each, weights by 2^-11, sums by less than 2^-19
+            assert ((out[b, 3].double() - mean).abs() <= mean.abs() * 2.0 ** -9 + mass * (2.0 ** -9 + 2.0 ** -11 + 2.0 ** -19)).all()
+            assert (lse[b, 3].double() - math.log(n)).abs().max() <= 2.0 ** -20 * (1.0 + math.log(n))
