@@ -327,7 +327,7 @@ __device__ __forceinline__ void e2m1_f16(uint32_t q, uint32_t (&w)[4]) {
 // An E4M3 code's seven bits under FP16's exponent are its value times 2^-8, exactly, subnormals included, and code 0x7F, the scale of a
 // block of NaNs, is the number 480 that reading it back takes it for. (As the NaN of the conversion instruction it would reach the sums of
 // tokens that do not see its key.)
-constexpr float kE4m3Up = 256.0f;
+constexpr int kE4m3Down = 8;
 __device__ __forceinline__ uint32_t e4m3_twice(uint32_t code) { return code * 0x00800080u; }
 __device__ __forceinline__ uint32_t e4m3_pair(uint32_t low, uint32_t high) { return low * 0x80u + high * 0x00800000u; }
 // E8M0 code `i` of four -> its power of two; code 0 -> 0 (zeros, or elements below 2^-124)
@@ -542,6 +542,9 @@ struct Joint {
   }
 };
 
+// What sums of products have to be multiplied with, for a sum of weights
+template <bool MX>
+__device__ __forceinline__ float part_factor(float vt, float l) { return l == 0.0f ? 0.0f : vt / (MX ? l : l * (1.0f / (1 << kE4m3Down))); }
 // Of no weight at all: -infinity; of a sum that is NaN: NaN, like the row's outputs.
 __device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f; }
 
@@ -559,7 +562,7 @@ __device__ __forceinline__ void write_tile(const KvAttn& p, const Joint<EVEN>& s
     if (row >= p.rows) continue;
     const int token = token_of(p, row), head = h * p.group + (row - token * p.group);
     const int64_t at = (static_cast<int64_t>(b) * p.q_len + token) * p.q_heads + head;
-    const float l = c ? sum.ml.w : sum.ml.y, f = l == 0.0f ? 0.0f : vt / l;
+    const float l = c ? sum.ml.w : sum.ml.y, f = part_factor<EVEN>(vt, l);
     *reinterpret_cast<uint32_t*>(p.out + at * D + dim_of<D>(i, g)) = pack_bf16x2((c ? sum.o.y : sum.o.x) * f, (c ? sum.o.w : sum.o.z) * f);
     if (p.lse && i == 0 && g == 0) p.lse[at] = log_sum(c ? sum.ml.z : sum.ml.x, l);
   }
@@ -587,8 +590,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
   const int part = alone ? 0 : warp, bits = alone ? 0 : kAttnWarpBits;
   if (!DIRECT && !p.by_segment && threadIdx.x == 0) tasks[cta].more = 0;
 
-  const float vt = MX ? 1.0f : *p.v_tscale * kE4m3Up;
-  const float kt = p.scale * (MX ? 1.0f : *p.k_tscale * kE4m3Up);
+  const float vt = MX ? 1.0f : *p.v_tscale;
+  const float kt = p.scale * (MX ? 1.0f : *p.k_tscale);
   const float sign = kt < 0.0f ? -1.0f : 1.0f;                 // of the scale: goes to the queries, so that a column's factor is positive
 
   // A sequence without keys: zeros. (With keys: nothing.)
@@ -748,7 +751,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
       const int e = max(static_cast<int>(top >> 7), 14);       // exponent of the row's largest element
       const float up = sign * __uint_as_float(static_cast<uint32_t>(268 - e) << 23);
-      const float down = e == 14 ? 0x1p-127f : __uint_as_float(static_cast<uint32_t>(e - 14) << 23);
+      const int undo = e - 14 + (MX ? 0 : kE4m3Down);
+      const float down = undo == 0 ? 0x1p-127f : __uint_as_float(static_cast<uint32_t>(undo) << 23);
 #pragma unroll
       for (int i = 0; i < NW; ++i) {
         const uint32_t v[4] = {raw[n][i].x, raw[n][i].y, raw[n][i].z, raw[n][i].w};
@@ -1222,7 +1226,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
             if (row < p.rows) {
               const int token = token_of(p, row), head = h * p.group + (row - token * p.group);
               const int64_t at = (static_cast<int64_t>(w.b) * p.q_len + token) * p.q_heads + head;
-              const float f = a.l[n][c] == 0.0f ? 0.0f : vt / a.l[n][c];
+              const float f = part_factor<MX>(vt, a.l[n][c]);
               uint32_t* out = reinterpret_cast<uint32_t*>(p.out + at * D);
 #pragma unroll
               for (int i = 0; i < MT; i += 4)
@@ -1259,7 +1263,7 @@ __global__ void __launch_bounds__(1024) kv_join_kernel(const __grid_constant__ K
   using S = Shape<FMT, D, NT>;
   constexpr int PART4 = S::PART / 16, TILES = S::MT * NT;
   launch_after_previous();
-  const float vt = FMT == QF_FMT_NVFP4 ? *p.v_tscale * kE4m3Up : 1.0f;
+  const float vt = FMT == QF_FMT_NVFP4 ? *p.v_tscale : 1.0f;
   const JoinTask task = reinterpret_cast<const JoinTask*>(p.ws)[blockIdx.x];
   if (task.more == 0) return;
   const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5, lane = threadIdx.x & 31;
