@@ -501,13 +501,15 @@ __device__ __forceinline__ int dim_of(int i, int g) {
   return D == 64 ? g * 8 + 2 * i : (i >> 3) * 128 + g * 16 + 2 * (i & 7);
 }
 
-constexpr float kNoWeights = -1e30f;           // base of a column without weights: far below any score, and finite
-// Power of two that brings a sum of weights into [1/4, 1/2) (zero stays zero); its base moves by what is returned in `by`. MXFP4's values
-// may fill FP32's range: sums of them stay in it as long as their weights add up to less than one.
-__device__ __forceinline__ float even_out(float l, float& by) {
-  const int e = static_cast<int>(__float_as_uint(l) >> 23);
-  by = static_cast<float>(e - 125);
-  return __uint_as_float(static_cast<uint32_t>(252 - e) << 23);
+constexpr float kNoWeights = -3.4028234663852886e38f;        // base of a column without weights: no finite score is below it
+// Power of two that brings a sum of weights into [1/4, 1/2) (zero stays zero) and its base along with it; what the base moved by is
+// returned in `by`. MXFP4's values may fill FP32's range: sums of them stay in it as long as their weights add up to less than one. (A
+// base so large that its steps are whole powers moves as far as it can, and the sum with it.)
+__device__ __forceinline__ float even_out(float& m, float l, float& by) {
+  const float to = m + static_cast<float>(static_cast<int>(__float_as_uint(l) >> 23) - 125);
+  by = to - m;
+  m = to;
+  return exp2_approx(-by);
 }
 // Two columns of weights into one: factors of the sums that belong to them, base and sum.
 template <bool EVEN>
@@ -519,11 +521,10 @@ __device__ __forceinline__ void join_weights(float& m, float& l, float mb, float
   m = most;
   if constexpr (EVEN) {
     float by;
-    const float f = even_out(l, by);
+    const float f = even_out(m, l, by);
     fa *= f;
     fb *= f;
     l *= f;
-    m += by;
   }
 }
 
@@ -898,16 +899,27 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
               if (key0 + half * 16 + (c >> 1) * 8 + own0 >= seen[n][c & 1]) s[half][n][c] = -INFINITY;
       }
 
-      // Bases. They move only when a score passes one by more than the room there is.
+      // Scores, rounded for themselves: of the unrounded product less its base something would be left over, and be more than the room
+      // there is where scores are large. Bases move only when a score passes one by more than that.
       float top[NT][2];
       bool move = false;
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n) {
+        const float2 by2 = make_float2(by[n][0], by[n][1]);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const float2 x = __fmul2_rn(make_float2(s[half][n][2 * r], s[half][n][2 * r + 1]), by2);
+            s[half][n][2 * r] = x.x;
+            s[half][n][2 * r + 1] = x.y;
+          }
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          top[n][c] = fmaxf(fmaxf(s[0][n][c], s[0][n][c + 2]), fmaxf(s[1][n][c], s[1][n][c + 2])) * by[n][c];
-          move |= top[n][c] > a.m[n][c] + (kWeightTop + kWeightRoom);
+          top[n][c] = fmaxf(fmaxf(s[0][n][c], s[0][n][c + 2]), fmaxf(s[1][n][c], s[1][n][c + 2]));
+          move |= top[n][c] - a.m[n][c] > kWeightTop + kWeightRoom;
         }
+      }
       // MXFP4: a scale code c of the values is taken as the FP16 number 2^(c - vref + 5), which is exact and in range for c in
       // [vref - 19, vref + 8]; a code of 0 comes with zeros, whatever it is taken for. A lane looks at its key's codes: largest, and
       // smallest but 0, less 1.
@@ -987,7 +999,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
                 for (int half = 0; half < 2; ++half)
 #pragma unroll
                   for (int r = 0; r < 2; ++r)
-                    most = fmaxf(most, fmaf(s[half][n][2 * r + c], by[n][c], -a.m[n][c]) + __shfl_sync(0xFFFFFFFFu, key_up, half * 16 + r * 8 + own0));
+                    most = fmaxf(most, s[half][n][2 * r + c] - a.m[n][c] + __shfl_sync(0xFFFFFFFFu, key_up, half * 16 + r * 8 + own0));
 #pragma unroll
                 for (int d = 4; d < 32; d *= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
                 const float so_far = ve[n][c] + was[n][c];
@@ -1026,7 +1038,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
             const float up = __shfl_sync(0xFFFFFFFFu, static_cast<float>(key_top - 140), half * 16 + r * 8 + own0);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              const float x0 = fmaf(s[half][n][2 * r], by[n][0], -a.m[n][0]), x1 = fmaf(s[half][n][2 * r + 1], by[n][1], -a.m[n][1]);
+              const float x0 = s[half][n][2 * r] - a.m[n][0], x1 = s[half][n][2 * r + 1] - a.m[n][1];
               a.l[n][0] += exp2_approx(x0);
               a.l[n][1] += exp2_approx(x1);
               pf[half][n][r] = transpose8x8(f16x2(exp2_approx(x0 + up - ve[n][0]), exp2_approx(x1 + up - ve[n][1])));
@@ -1047,13 +1059,13 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
       } else {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const float2 by2 = make_float2(by[n][0], by[n][1]), m2 = make_float2(-a.m[n][0], -a.m[n][1]);
+          const float2 m2 = make_float2(-a.m[n][0], -a.m[n][1]);
           float2 l2 = make_float2(a.l[n][0], a.l[n][1]);
 #pragma unroll
           for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-              const float2 x = __ffma2_rn(make_float2(s[half][n][2 * r], s[half][n][2 * r + 1]), by2, m2);
+              const float2 x = __fadd2_rn(make_float2(s[half][n][2 * r], s[half][n][2 * r + 1]), m2);
               const float2 e = make_float2(exp2_approx(x.x), exp2_approx(x.y));
               l2 = __fadd2_rn(l2, e);
               pf[half][n][r] = transpose8x8(f16x2(e.x, e.y));
@@ -1150,9 +1162,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
         for (int d = 4; d < 32; d *= 2) a.l[n][c] += __shfl_xor_sync(0xFFFFFFFFu, a.l[n][c], d);
         if constexpr (MX) {
           float moved;
-          const float even = even_out(a.l[n][c], moved);
+          const float even = even_out(a.m[n][c], a.l[n][c], moved);
           a.l[n][c] *= even;
-          a.m[n][c] += moved;
           const float f = exp2_approx(0.5f * (ve[n][c] - moved));        // twice: the power itself may be out of FP32's range where the product is not
 #pragma unroll
           for (int i = 0; i < MT; ++i) { a.o[i][n][c] = a.o[i][n][c] * f * f; a.o[i][n][c + 2] = a.o[i][n][c + 2] * f * f; }

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from kv_reference import attention, check_attention
+from kv_reference import attention, check_attention, gathered
 from paper_2609_39223_b200 import api
 from test_gpu_kv import BF, fmts, gen, random_cache
 
@@ -123,3 +123,50 @@ def test_tensor_scales_at_the_ends_of_their_range():
         ref = attention(c, q, table, lens, 128 ** -0.5)[0]
         near = out.double() + (ref - out.double()).clamp(-2.0 ** -134, 2.0 ** -134)
         check_attention(c, q, table, lens, 128 ** -0.5, near, lse)
+
+
+def scored(c, q, table, n, scale):
+    """The form in FP32 for scores so far apart, or so large, that only their order matters: exact sums, scores rounded to FP32, their
+    differences taken from the rounded ones, in 64 bits from there."""
+    page, batch, q_len, q_heads, dim = c.page_size, *q.shape
+    out, lse = torch.empty(q.shape, dtype=torch.float64, device=q.device), torch.empty(q.shape[:3], dtype=torch.float64, device=q.device)
+    for b in range(batch):
+        k, v = gathered(c, table[b], n)
+        for i in range(q_len):
+            m = n - q_len + i + 1
+            s = (torch.einsum("hgd,hjd->hgj", q[b, i].double().view(c.kv_heads, -1, dim), k[:, :m]) * scale).float().double()
+            out[b, i] = torch.einsum("hgj,hjd->hgd", torch.softmax(s, -1), v[:, :m]).reshape(q_heads, dim)
+            lse[b, i] = torch.logsumexp(s, -1).reshape(-1)
+    return out, lse
+
+
+@fmts
+@CUTS
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_of_any_size(fmt, dim, sign, batch, heads, n):
+    """Equal keys, all of whose scores are +-2^20 to +-2^118: the mean of the values. Keys of two kinds that far apart: the mean over one."""
+    table, lens, pages = paged_in_order(batch, n, 32)
+    c = random_cache(fmt, pages, 32, heads, dim, 3)
+    c.k_codes.fill_(0x22)
+    for power in (20, 27, 31, 40, 80, 118):
+        k = power // 2 if fmt == api.FMT_MXFP4 else 2
+        c.k_scales.fill_(127 + k if fmt == api.FMT_MXFP4 else 0x38)          # keys of 2^k and of 1 times the tensor scale
+        if fmt == api.FMT_NVFP4:
+            c.k_tscale.fill_(2.0 ** k)
+        # queries of seven bits, so that no product is a power of two and sums are exact
+        q = torch.full((batch, 2, heads * 2, dim), sign * 1.3125 * 2.0 ** (power - k), dtype=BF, device="cuda")
+        q[:, 0] *= -1.171875
+        out, lse = api.qf_kv_attention(c, q, table, lens, softmax_scale=0.7 / dim, want_lse=True)
+        few = min(batch, 3)
+        ref, rlse = scored(c, q[:few], table, n, 0.7 / dim)
+        # weights of equal scores are equal but for their FP16 form, 2^-11; one rounding to BF16, 2^-8; their sums, 2^-19: of values of up to 6
+        assert torch.isfinite(out.float()).all()
+        assert ((out[:few].double() - ref).abs() <= ref.abs() * 2.0 ** -8 + 8 * 2.0 ** -11).all()
+        assert ((lse[:few].double() - rlse).abs() <= rlse.abs() * 2.0 ** -21 + 2.0 ** -10).all()
+    flip = (torch.arange(pages, device="cuda") % 3 == 1)[:, None, None, None]
+    c.k_codes.copy_(torch.where(flip, 0xAA, 0x22).to(torch.uint8).expand_as(c.k_codes))        # the other sign
+    out, lse = api.qf_kv_attention(c, q, table, lens, softmax_scale=0.7 / dim, want_lse=True)
+    ref, rlse = scored(c, q[:few], table, n, 0.7 / dim)
+    assert ((out[:few].double() - ref).abs() <= ref.abs() * 2.0 ** -8 + 8 * 2.0 ** -11).all()
+    assert ((lse[:few].double() - rlse).abs() <= rlse.abs() * 2.0 ** -21).all()
