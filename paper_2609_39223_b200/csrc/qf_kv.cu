@@ -763,7 +763,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, (Shape<FMT, D, NT>::CTAS)) kv
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         // not zero, so that a score of -infinity stays one
-        by[n][c] = fmaxf(__shfl_sync(0xFFFFFFFFu, down, (2 * t + c) * 4) * fabsf(kt), 0x1p-126f);
+        by[n][c] = fmaxf(__shfl_sync(0xFFFFFFFFu, down, (2 * t + c) * 4) * fabsf(kt), 0x1p-149f);
         const int tok = token_of(p, min(row0 + 8 * n + 2 * t + c, p.rows - 1));
         seen[n][c] = min(max(w.keys - p.q_len + tok + 1, 0), w.keys);
       }

@@ -170,3 +170,22 @@ def test_scores_of_any_size(fmt, dim, sign, batch, heads, n):
     ref, rlse = scored(c, q[:few], table, n, 0.7 / dim)
     assert ((out[:few].double() - ref).abs() <= ref.abs() * 2.0 ** -8 + 8 * 2.0 ** -11).all()
     assert ((lse[:few].double() - rlse).abs() <= rlse.abs() * 2.0 ** -21).all()
+
+
+@CUTS
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("power", [-105, -110, -113, -116, -120])
+def test_small_queries_of_large_keys(dim, power, batch, heads, n):
+    """MXFP4: block scales of the keys up to 2^102, the largest that no sum of products can take out of FP32's range, and queries so
+    small that scores are ordinary ones or close to 0."""
+    table, lens, pages = paged_in_order(batch, n, 16)
+    c = random_cache(api.FMT_MXFP4, pages, 16, heads, dim, 3)
+    c.k_scales.add_(102)                                            # 225 .. 229
+    q = (torch.randn((batch, 2, heads * 2, dim), generator=gen(1), device="cuda") * 2.0 ** power).to(BF)
+    q[:, 1] = 2.0 ** power                                          # all of one sign, as the keys below
+    out, lse = api.qf_kv_attention(c, q, table, lens, want_lse=True)
+    check_attention(c, q[:3], table[:3], lens[:3], dim ** -0.5, out[:3], lse[:3])
+    c.k_codes.copy_(torch.where((torch.arange(pages, device="cuda") % 3 == 0)[:, None, None, None], 0x77, 0xFF).to(torch.uint8).expand_as(c.k_codes))
+    c.k_scales.fill_(229)
+    out, lse = api.qf_kv_attention(c, q, table, lens, want_lse=True)
+    check_attention(c, q[:3], table[:3], lens[:3], dim ** -0.5, out[:3], lse[:3])
