@@ -386,7 +386,7 @@ qf_status_t qf_fq_grouped_matvec(qf_format_t fmt, const void* X, int64_t x_rows,
  * s / page_size. A page table row lists a sequence's pages in order: key j of the sequence is place j % page_size of page
  * page_table[b][j / page_size].
  *   fmt        QF_FMT_NVFP4 or QF_FMT_MXFP4
- *   head_dim   64, 128 or 256;  page_size a multiple of 16, at most 2^20;  kv_heads at most 65535
+ *   head_dim   64, 128 or 256;  page_size a multiple of 16, at most 2^20;  kv_heads at most 65535;  pages * page_size at most 2^36 slots
  * All four buffers are 16-byte aligned. The struct is host memory and read during the call only. The tables are device memory, so
  * the host cannot check them: slots outside [0, pages * page_size) are skipped, page numbers are forced into [0, pages) and lengths
  * into [0, max_pages * page_size], so that a table that breaks the contract gives meaningless results, never an access out of
@@ -410,7 +410,8 @@ typedef struct {
  *                        projection's output are taken as they are)
  *   slots        device [tokens], slots_dtype QF_DT_I32 or QF_DT_I64; a slot outside the cache (-1, say) skips the token. Slots of one
  *                call have to differ: what a slot that is named twice holds afterwards is not defined
- *   flags        QF_MXFP4_NO_CLIP */
+ *   flags        QF_MXFP4_NO_CLIP
+ * k and v are 16-byte aligned; strides and tokens below 2^31, at most 2^40 elements of each (as many as qf_kv_read returns of each). */
 qf_status_t qf_kv_append(const qf_kv_cache_t* cache, const void* k, int64_t k_stride, const void* v, int64_t v_stride, int64_t tokens,
                          const void* slots, qf_dtype_t slots_dtype, uint32_t flags, void* stream);
 
@@ -426,7 +427,8 @@ qf_status_t qf_kv_read(const qf_kv_cache_t* cache, const void* slots, qf_dtype_t
  * BF16 result's 2^-8, or, for weights below 2^-20 of the row's largest, by up to 2^-31 of that one) and the dequantized keys and values are
  * not rounded to BF16, as in qf_fq_matvec. MXFP4: key blocks of scale 2^-127 count as zeros, and so may value blocks whose scale is less
  * than 2^-36 of the largest of the same key and head; where the sizes of the values differ by more than 2^8, small weights of large values
- * are kept as well, and products p_j * v_j below 2^-31 of the largest may count as zeros. A row without
+ * are kept as well, and products p_j * v_j below 2^-31 of the largest may count as zeros; block scales of keys above 2^102 can take a
+ * row's sums of products out of FP32's range, which makes its out and lse NaN (below, no query and no other key can). A row without
  * keys (an empty place of a padded batch, a token of a sequence shorter than q_len) gives zeros. Results do not change from run to run;
  * how the keys are cut depends on the batch's lengths and on max_pages, so that the same row can have other last bits in another batch.
  *   q            BF16 [batch, q_len, q_heads, head_dim], q_stride elements from one token to the next (at least q_heads * head_dim, a
@@ -439,6 +441,8 @@ qf_status_t qf_kv_read(const qf_kv_cache_t* cache, const void* slots, qf_dtype_t
  *                lse NaN
  *   workspace    qf_workspace_bytes(QF_OP_KV_ATTENTION, batch * q_len, q_heads, head_dim, kv_heads) bytes, whatever they hold; calls
  *                that can overlap on the GPU (other streams, graphs) need one each
+ * q, out and the workspace are 16-byte aligned. At most 2^20 sequences and 2^20 query heads, max_pages * page_size below 2^31 - 1024, and
+ * (batch * q_len * q_heads / 8 + batch * kv_heads) * (max_pages * page_size / 32 + 1) at most 2^37.
  * Meant for a few tokens a sequence (a decode step, drafted tokens checked together): the cache is read and decoded once per 24 rows of
  * q_len * q_heads / kv_heads (32 for head_dim 64, 16 for 256; per 8 where there is little to read). For long prompts read the cache
  * back (qf_kv_read). A page table no wider than the sequences need gives short sequences the shorter way (no second kernel for up to
