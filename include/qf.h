@@ -504,6 +504,12 @@ qf_status_t qf_selftest_div(const float* xs, int64_t nx, const float* ys, int64_
  * that take turns at them. The cut is an estimate's choice, so that tests name the paths they want and see that they have them. */
 qf_status_t qf_selftest_matvec_cut(qf_format_t fmt, int64_t M, int64_t N, int64_t K, int G, int cut[9]);
 
+/* Self-test hook for how an attention call is cut (no GPU is touched, and no buffer of the cache looked at): cut (host) receives query
+ * rows of a tile in units of 8; CTAs that share a sequence and key head, 0 where each has a warp, -1 where all get equal shares of
+ * all sequences; CTAs in all; tasks of the second kernel, 0 without one; and whether these are numbered by sequence and key head (1)
+ * or by CTA (0). */
+qf_status_t qf_selftest_kv_attention_cut(const qf_kv_cache_t* cache, int64_t batch, int q_len, int q_heads, int64_t max_pages, int cut[5]);
+
 /* Self-test hook for the bounded device-side waits: launches one thread that waits, with the given limit
  * in SM clock cycles (at most 2^28), on a barrier nothing ever arrives at. The wait gives up, the kernel
  * returns normally, and the workspace then holds QF_ERR_TIMEOUT in its status word (qf_read_status)

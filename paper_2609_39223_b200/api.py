@@ -33,7 +33,7 @@ EXPORTS = [
     "qf_selftest_div", "qf_fq_linear_fwd_noalloc", "qf_selftest_mxfp4_bf16", "qf_selftest_timeout", "qf_pack_bytes", "qf_pack", "qf_unpack", "qf_nvfp4_tensor_scale", "qf_qdq_lora",
     "qf_fp4_matmul_native", "qf_qdq_batched", "qf_moe_rows_bound", "qf_moe_sort", "qf_moe_dispatch", "qf_moe_dispatch_bwd",
     "qf_moe_combine", "qf_moe_combine_bwd", "qf_fq_matvec", "qf_fq_grouped_matvec", "qf_selftest_matvec_cut",
-    "qf_kv_append", "qf_kv_read", "qf_kv_attention",
+    "qf_kv_append", "qf_kv_read", "qf_kv_attention", "qf_selftest_kv_attention_cut",
 ]
 NOALLOC_SCRATCH_BYTES = 32 << 20
 LAYOUT_GGUF_Q4_K, LAYOUT_FP4_SWIZZLED_SCALES = 1, 2
@@ -139,6 +139,8 @@ def lib() -> ctypes.CDLL:
         L.qf_kv_attention.restype = c_int
         L.qf_kv_attention.argtypes = [c_void_p, c_void_p, c_int64, c_int64, c_int, c_int, c_void_p, c_int64, c_void_p, c_float, c_void_p,
                                       c_void_p, c_void_p, c_size_t, c_void_p]
+        L.qf_selftest_kv_attention_cut.restype = c_int
+        L.qf_selftest_kv_attention_cut.argtypes = [c_void_p, c_int64, c_int, c_int, c_int64, c_void_p]
         _lib = L
     return _lib
 
@@ -769,6 +771,22 @@ def qf_kv_attention(cache: KvCache, q: torch.Tensor, page_table: torch.Tensor, s
     _check(lib().qf_kv_attention(cache._address, pq, q_stride, batch, q_len, q_heads, pt, max_pages, pl,
                                  dim ** -0.5 if softmax_scale is None else softmax_scale, po, pe, pw, ws.numel(), stream), "qf_kv_attention")
     return (out, lse) if want_lse else out
+
+
+class KvAttentionCut(NamedTuple):
+    """How an attention call is cut (see qf_selftest_kv_attention_cut in qf.h)."""
+    row_tiles: int
+    split: int
+    ctas: int
+    tasks: int
+    by_segment: int
+
+
+def qf_selftest_kv_attention_cut(fmt: int, batch: int, q_len: int, q_heads: int, kv_heads: int, head_dim: int, page_size: int,
+                                 max_pages: int) -> KvAttentionCut:
+    cache, out = _KvCacheStruct(fmt, kv_heads, head_dim, page_size, 1), (c_int * 5)()
+    _check(lib().qf_selftest_kv_attention_cut(ctypes.addressof(cache), batch, q_len, q_heads, max_pages, out), "qf_selftest_kv_attention_cut")
+    return KvAttentionCut(*out)
 
 
 def qf_fp4_matmul_native(fmt: int, a: dict, b: dict, K: int, *, flags: int = 0, ws=None) -> torch.Tensor:

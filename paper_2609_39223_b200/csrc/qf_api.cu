@@ -831,16 +831,36 @@ qf_status_t qf_kv_read(const qf_kv_cache_t* cache, const void* slots, qf_dtype_t
   return cu(launch_kv_read(*cache, slots, slots_dtype == QF_DT_I64, rows, k, v, static_cast<cudaStream_t>(stream)));
 }
 
+static qf_status_t check_kv_attention(const qf_kv_cache_t& c, int64_t q_stride, int64_t batch, int q_len, int q_heads, int64_t max_pages) {
+  if (batch < 0 || q_len < 0 || q_heads < 1 || q_heads % c.kv_heads) return QF_ERR_SHAPE;
+  if (batch > (1 << 20) || q_heads > (1 << 20) || batch * q_len > INT32_MAX || batch * q_len * q_heads > INT32_MAX) return QF_ERR_SHAPE;
+  if (max_pages < 0 || max_pages > INT32_MAX || max_pages * c.page_size > INT32_MAX - 1024) return QF_ERR_SHAPE;         // keys are numbered in 32 bits
+  if (!kv_stride_ok(q_stride, static_cast<int64_t>(q_heads) * c.head_dim)) return QF_ERR_SHAPE;
+  if ((batch * q_len * q_heads / 8 + batch * c.kv_heads) * (max_pages * c.page_size / 32 + 1) > (1ll << 37)) return QF_ERR_SHAPE;   // a CTA's share of the work is counted in 31 bits
+  return QF_OK;
+}
+
+qf_status_t qf_selftest_kv_attention_cut(const qf_kv_cache_t* cache, int64_t batch, int q_len, int q_heads, int64_t max_pages, int cut[5]) {
+  if (qf_status_t s = check_kv(cache)) return s;
+  if (!cut) return QF_ERR_NULL;
+  if (qf_status_t s = check_kv_attention(*cache, static_cast<int64_t>(q_heads) * cache->head_dim, batch, q_len, q_heads, max_pages)) return s;
+  if (batch == 0 || q_len == 0) return QF_ERR_SHAPE;
+  KvAttentionArgs a{};
+  a.cache = *cache;
+  a.batch = batch;
+  a.q_len = q_len;
+  a.q_heads = q_heads;
+  a.max_pages = cache->pages > 0 ? max_pages : 0;
+  kv_attention_cut(a, cut);
+  return QF_OK;
+}
+
 qf_status_t qf_kv_attention(const qf_kv_cache_t* cache, const void* q, int64_t q_stride, int64_t batch, int q_len, int q_heads,
                             const int32_t* page_table, int64_t max_pages, const int32_t* seq_lens, float softmax_scale, void* out,
                             float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   if (qf_status_t s = check_kv(cache)) return s;
-  if (batch < 0 || q_len < 0 || q_heads < 1 || q_heads % cache->kv_heads) return QF_ERR_SHAPE;
-  if (batch > (1 << 20) || q_heads > (1 << 20) || batch * q_len > INT32_MAX || batch * q_len * q_heads > INT32_MAX) return QF_ERR_SHAPE;
-  if (max_pages < 0 || max_pages > INT32_MAX || max_pages * cache->page_size > INT32_MAX - 1024) return QF_ERR_SHAPE;   // keys are numbered in 32 bits
-  if (!kv_stride_ok(q_stride, static_cast<int64_t>(q_heads) * cache->head_dim)) return QF_ERR_SHAPE;
+  if (qf_status_t s = check_kv_attention(*cache, q_stride, batch, q_len, q_heads, max_pages)) return s;
   const int64_t rows = batch * q_len;
-  if ((rows * q_heads / 8 + batch * cache->kv_heads) * (max_pages * cache->page_size / 32 + 1) > (1ll << 37)) return QF_ERR_SHAPE;   // a CTA's share of the work is counted in 31 bits
   if (!workspace || workspace_bytes < qf_workspace_bytes(QF_OP_KV_ATTENTION, rows, q_heads, cache->head_dim, cache->kv_heads)) return QF_ERR_WORKSPACE;
   const bool keys = max_pages > 0 && cache->pages > 0;
   if (rows > 0 && (!q || !out || !seq_lens || !kv_has_scales(cache) || (keys && (!page_table || !kv_has_buffers(cache))))) return QF_ERR_NULL;

@@ -417,6 +417,8 @@ struct KvAttentionArgs {
 };
 size_t kv_attention_ws_bytes(int64_t rows, int q_heads, int head_dim, int kv_heads);       // without the header
 cudaError_t launch_kv_attention(const KvAttentionArgs& a, cudaStream_t st);
+// How it would be cut (see qf_selftest_kv_attention_cut); no pointer of a is looked at.
+void kv_attention_cut(const KvAttentionArgs& a, int* cut);
 
 cudaError_t launch_selftest_timeout(uint32_t* status, long long limit_cycles, int* gave_up, cudaStream_t st);
 

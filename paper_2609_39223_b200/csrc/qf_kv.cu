@@ -1327,8 +1327,14 @@ cudaError_t launch_attention(const KvAttn& p, int64_t ctas, int cluster, cudaStr
   return launch_overlapping(kv_attention_kernel<FMT, D, NT, DIRECT>, dim3(static_cast<unsigned>(ctas)), kAttnWarps * 32, S::SMEM, st, cluster, p);
 }
 
+// How the work is cut: CTAs of the attention kernel; tasks of the second one, 0 without it. Sets p.split and p.by_segment.
+struct AttnCut {
+  bool direct;
+  int64_t ctas;
+  int tasks;
+};
 template <int FMT, int D, int NT>
-cudaError_t attend(KvAttn& p, cudaStream_t st) {
+AttnCut cut_attention(KvAttn& p) {
   using S = Shape<FMT, D, NT>;
   constexpr int64_t ROOM = kNumSMs * S::CTAS;
   const int64_t segments = static_cast<int64_t>(p.batch) * p.segs;
@@ -1339,22 +1345,34 @@ cudaError_t attend(KvAttn& p, cudaStream_t st) {
   // 11.3 with CTAs, 12.9 with warps, whose units then take longer than a second round). At most 64, for the one long sequence among short ones.
   if (segments > ROOM && units <= kAloneMost && units * ROOM <= kAloneUnits * segments && segments <= INT32_MAX) {
     p.split = 0;
-    return launch_attention<FMT, D, NT, true>(p, (segments + kAttnWarps - 1) / kAttnWarps, 1, st);
+    return {true, (segments + kAttnWarps - 1) / kAttnWarps, 0};
   }
   // Short sequences: CTAs of their own for each, so that nothing has to be counted, nor joined by a second
   // kernel. As many as there is room for and as have a unit for every warp.
   p.split = 1;
   while (p.split < 8 && p.split * kAttnWarps < units && 2 * p.split * segments <= ROOM) p.split *= 2;
-  if (p.split * kDirectUnits >= units && segments <= INT32_MAX) return launch_attention<FMT, D, NT, true>(p, segments * p.split, p.split, st);
+  if (p.split * kDirectUnits >= units && segments <= INT32_MAX) return {true, segments * p.split, 0};
   // no more CTAs than there can be work for
   const int64_t most = segments * (units + kPieceCost) / kAttnWarps + 1;
   const int grid = static_cast<int>(most < ROOM ? most : ROOM);
   p.by_segment = segments <= grid;
-  if (cudaError_t e = launch_attention<FMT, D, NT, false>(p, grid, 1, st)) return e;
+  return {false, grid, p.by_segment ? static_cast<int>(segments) : grid};
+}
+
+template <int FMT, int D, int NT>
+cudaError_t attend(KvAttn& p, cudaStream_t st, int* told) {
+  using S = Shape<FMT, D, NT>;
+  const AttnCut cut = cut_attention<FMT, D, NT>(p);
+  if (told) {
+    const int all[5] = {NT, cut.direct ? p.split : -1, static_cast<int>(cut.ctas), cut.tasks, p.by_segment};
+    for (int i = 0; i < 5; ++i) told[i] = all[i];
+    return cudaSuccess;
+  }
+  if (cut.direct) return launch_attention<FMT, D, NT, true>(p, cut.ctas, p.split > 1 ? p.split : 1, st);
+  if (cudaError_t e = launch_attention<FMT, D, NT, false>(p, cut.ctas, 1, st)) return e;
   // the fewer sequences, the more parts each may have: up to a CTA per value tile
-  const int tasks = p.by_segment ? static_cast<int>(segments) : grid;
-  const int share = 4 * kNumSMs / tasks, parts = grid / tasks, threads = parts < 32 ? 256 : parts < 128 ? 512 : 1024;
-  return launch_overlapping(kv_join_kernel<FMT, D, NT>, dim3(tasks, share < 1 ? 1 : share < S::MT * NT ? share : S::MT * NT), threads, threads * 16, st, 1, p, grid);
+  const int grid = static_cast<int>(cut.ctas), share = 4 * kNumSMs / cut.tasks, parts = grid / cut.tasks, threads = parts < 32 ? 256 : parts < 128 ? 512 : 1024;
+  return launch_overlapping(kv_join_kernel<FMT, D, NT>, dim3(cut.tasks, share < 1 ? 1 : share < S::MT * NT ? share : S::MT * NT), threads, threads * 16, st, 1, p, grid);
 }
 
 // Query rows of a tile, in units of 8, at most: what registers hold next to the decoded words. (Heads of 256 with 16 rows: only with the
@@ -1367,7 +1385,7 @@ constexpr int tile_most(int head_dim) { return head_dim == 64 ? 4 : head_dim == 
 // each: one sequence of 300 keys 6.1 us instead of 9.1, 7 of them 8.0 instead of 10.4; 7 of 2500 keys 17.4, with tiles of 8 rows 20.0).
 constexpr int64_t kTileUnits = 3 * 2 * kNumSMs * kAttnWarps;
 template <int FMT>
-cudaError_t attend_format(KvAttn& p, int head_dim, cudaStream_t st) {
+cudaError_t attend_format(KvAttn& p, int head_dim, cudaStream_t st, int* told) {
   const int eights = (p.rows + 7) / 8, most = tile_most(head_dim);
   const int64_t units = static_cast<int64_t>(p.batch) * p.kv_heads * ((p.max_keys + kUnitKeys - 1) / kUnitKeys);
   int nt = 1;
@@ -1375,9 +1393,9 @@ cudaError_t attend_format(KvAttn& p, int head_dim, cudaStream_t st) {
   p.tiles = (eights + nt - 1) / nt;
   nt = (eights + p.tiles - 1) / p.tiles;
   p.segs = p.tiles * p.kv_heads;
-  if (head_dim == 64) return nt == 1 ? attend<FMT, 64, 1>(p, st) : nt == 2 ? attend<FMT, 64, 2>(p, st) : nt == 3 ? attend<FMT, 64, 3>(p, st) : attend<FMT, 64, 4>(p, st);
-  if (head_dim == 128) return nt == 1 ? attend<FMT, 128, 1>(p, st) : nt == 2 ? attend<FMT, 128, 2>(p, st) : attend<FMT, 128, 3>(p, st);
-  return nt == 1 ? attend<FMT, 256, 1>(p, st) : attend<FMT, 256, 2>(p, st);
+  if (head_dim == 64) return nt == 1 ? attend<FMT, 64, 1>(p, st, told) : nt == 2 ? attend<FMT, 64, 2>(p, st, told) : nt == 3 ? attend<FMT, 64, 3>(p, st, told) : attend<FMT, 64, 4>(p, st, told);
+  if (head_dim == 128) return nt == 1 ? attend<FMT, 128, 1>(p, st, told) : nt == 2 ? attend<FMT, 128, 2>(p, st, told) : attend<FMT, 128, 3>(p, st, told);
+  return nt == 1 ? attend<FMT, 256, 1>(p, st, told) : attend<FMT, 256, 2>(p, st, told);
 }
 
 // Workspace: for the largest kernel of a head size, whatever the format and the tile, since how the rows are split over sequences is
@@ -1419,7 +1437,7 @@ size_t kv_attention_ws_bytes(int64_t, int, int head_dim, int) {
   return head_dim <= 64 ? ws_bytes<64, tile_most(64)>() : head_dim <= 128 ? ws_bytes<128, tile_most(128)>() : ws_bytes<256, tile_most(256)>();
 }
 
-cudaError_t launch_kv_attention(const KvAttentionArgs& a, cudaStream_t st) {
+static cudaError_t kv_attention(const KvAttentionArgs& a, cudaStream_t st, int* told) {
   KvAttn p{};
   p.q = static_cast<const __nv_bfloat16*>(a.q);
   p.q_stride = a.q_stride;
@@ -1446,7 +1464,11 @@ cudaError_t launch_kv_attention(const KvAttentionArgs& a, cudaStream_t st) {
   p.rows = a.q_len * p.group;
   p.scale = a.scale * 1.4426950408889634f;
   p.page_codes = static_cast<int64_t>(p.kv_heads) * p.page_size * (a.cache.head_dim / 2);
-  return a.cache.fmt == QF_FMT_NVFP4 ? attend_format<QF_FMT_NVFP4>(p, a.cache.head_dim, st) : attend_format<QF_FMT_MXFP4>(p, a.cache.head_dim, st);
+  return a.cache.fmt == QF_FMT_NVFP4 ? attend_format<QF_FMT_NVFP4>(p, a.cache.head_dim, st, told) : attend_format<QF_FMT_MXFP4>(p, a.cache.head_dim, st, told);
 }
+
+cudaError_t launch_kv_attention(const KvAttentionArgs& a, cudaStream_t st) { return kv_attention(a, st, nullptr); }
+
+void kv_attention_cut(const KvAttentionArgs& a, int* cut) { kv_attention(a, nullptr, cut); }
 
 }  // namespace qf

@@ -53,8 +53,11 @@ def test_values_that_grow_where_scores_fall(dim, q_len, group, batch, heads, n, 
     check_attention(c, q[:2], table[:2], [n] * min(batch, 2), 2 * scale, out[:2], lse[:2])
 
 
-# one sequence to a warp, a CTA, a cluster, and in shares that a second kernel joins
-CUTS = pytest.mark.parametrize("batch,heads,n", [(300, 2, 100), (20, 3, 600), (2, 2, 1000), (2, 2, 30000)], ids=["warps", "CTAs", "clusters", "shares"])
+# (batch, key heads, keys of each): a sequence and head to a warp, a CTA, a cluster; in equal shares, joined by sequence and head or by CTA.
+# What the sizes are there for is looked at in test_kv_cut.py.
+WAYS = {"warps": (300, 2, 100), "CTAs": (100, 3, 600), "small clusters": (30, 3, 600), "clusters": (2, 2, 1000), "shares": (2, 2, 30000),
+        "shares by CTA": (80, 8, 2000)}
+CUTS = pytest.mark.parametrize("batch,heads,n", WAYS.values(), ids=[w.replace(" ", "-") for w in WAYS])
 
 
 @fmts
