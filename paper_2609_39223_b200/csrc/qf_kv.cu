@@ -16,8 +16,9 @@ namespace {
 // 32-byte steps the L1's write path was 75% busy: 78 us for 16 contexts of up to 8192 tokens, 62 now, 0.91 of the copy rate). A CTA takes
 // a few tokens (slots): where their rows lie is found once per token, and a thread keeps its head and part while it goes through them, so
 // that little is left to do per row but the row itself (divisions for every part: 94 us). Writing 16384 tokens of 8 heads of 128 takes
-// 16.5 us in MXFP4 and 20.9 in NVFP4 (0.80 and 0.64 of the copy rate): half of the issue slots are the quantizer's arithmetic, the rest waits for
-// rows. One row of a thread on the way instead of two: 19.5 and 20.3; four: 21.1 and 26.1 (registers).
+// 16.2 us in MXFP4 and 20.5 in NVFP4 (0.81 and 0.65 of the copy rate), whose quantizer has 1.3 times the instructions: half of the issue slots
+// are used, warps wait for their CTA's slots (the barrier is the largest stall in MXFP4) and for the arithmetic's own results (in NVFP4). One
+// row of a thread on the way instead of two: 16.9 and 20.1; four: 20.6 and 26.1 (registers).
 
 constexpr int kRowsTokens = 64;      // tokens of a CTA at most
 constexpr int kAppendTurns = 4, kReadTurns = 16;              // rows of a thread, where there are enough
@@ -244,15 +245,17 @@ cudaError_t launch_rows(void (*kernel)(KvRows), KvRows& p, int parts, int kinds,
 //    the CTAs take equal runs of them, whatever the lengths (sequences of up to 384 keys are not cut). A CTA's warps
 //    share what it has of a sequence and meet in shared memory. Only a CTA's first and last pieces can be parts of longer sequences:
 //    those go to the workspace, and a second kernel joins them in order. Where the page table holds short sequences only, each gets a
-//    cluster of up to 8 CTAs instead, which meets in distributed shared memory: nothing to count, no second kernel (1 x 1000 keys: 8.6 us
+//    cluster of up to 8 CTAs instead, which meets in distributed shared memory: nothing to count, no second kernel (1 x 1000 keys: 8.8 us
 //    without, 5.5 with); or, where there are many, a warp: no meeting either.
 //
-// What bounds it: instructions. 8 heads of 128, up to 8 rows: 594 a unit in NVFP4 (164 for keys, 250 for values, 72 for copies; 637 in MXFP4),
-// of which the ALU's 260 run at half rate; a copy at the full rate leaves an SM's scheduler 806 cycles for a unit. 128 x 8192: 231 us NVFP4,
-// 241 MXFP4 (0.81 and 0.74 of the copy rate), heads of 256 215 and 227, of 64 (16 of them) 292 and 310. Three CTAs an SM with 168 registers: four with
-// 128 take 1.01 times as long, two with 64 keys a unit 0.98 (and 1.03 to 1.2 times at ragged and short ones). Around the keys a call
-// spends 3.7 us until the first data, up to 4 us on shares that the memory serves unevenly, 2 us where warps meet and 3.5 us in the
-// second kernel: 1 x 131072 keys take 38 us where 23.4 is the floor.
+// What bounds it: latency. A unit's products are one chain from shared memory through conversion, scale, product, exponential and transpose to
+// the second product, and an SM has 8 to 16 warps to run beside one another. 8 heads of 128, up to 8 rows: 613 instructions a unit in
+// NVFP4 (257 on the ALU, which takes one every other cycle, 238 on the FMA pipes), 633 in MXFP4; a copy at the full rate leaves an SM's scheduler
+// 806 cycles for a unit, and 56% of the issue slots are used. 128 x 8192: 230 us NVFP4, 234 MXFP4 (0.81 and 0.76 of the copy
+// rate), heads of 256 212 and 227, of 64 (16 of them) 288 and 307. Three CTAs an SM with 168 registers: four with 128 took 1.01 times as long, two
+// with 64 keys a unit 0.98 (and 1.03 to 1.2 times at ragged and short ones). Around the keys a call spends 3.7 us until the first data, up to
+// 4 us on shares that the memory serves unevenly, 2 us where warps meet and 3.5 us in the second kernel: 1 x 131072 keys take 38 us where
+// 23.4 is the floor.
 
 constexpr int kUnitKeys = 32;
 constexpr int kAttnWarpBits = 2, kAttnWarps = 1 << kAttnWarpBits;       // of a CTA
