@@ -426,9 +426,9 @@ qf_status_t qf_kv_read(const qf_kv_cache_t* cache, const void* slots, qf_dtype_t
  * FP32 scores, softmax and sums; the weights p_j enter the value product as FP16 numbers (off by 2^-11 of themselves at most, below the
  * BF16 result's 2^-8, or, for weights below 2^-20 of the row's largest, by up to 2^-31 of that one) and the dequantized keys and values are
  * not rounded to BF16, as in qf_fq_matvec. MXFP4: key blocks of scale 2^-127 count as zeros, and so may value blocks whose scale is less
- * than 2^-36 of the largest of the same key and head; where the sizes of the values differ by more than 2^8, small weights of large values
- * are kept as well, and products p_j * v_j below 2^-31 of the largest may count as zeros; block scales of keys above 2^102 can take a
- * row's sums of products out of FP32's range, which makes its out and lse NaN (below, no query and no other key can). A row without
+ * than 2^-36 of the largest of the same key and head; small weights of values more than 2^27 times as large as those of larger weights are
+ * kept as well, down to products p_j * v_j of 2^-31 of the largest; block scales of keys above 2^102 can take a row's sums of products
+ * out of FP32's range, which makes its out and lse NaN (below, no query and no other key can). A row without
  * keys (an empty place of a padded batch, a token of a sequence shorter than q_len) gives zeros. Results do not change from run to run;
  * how the keys are cut depends on the batch's lengths and on max_pages, so that the same row can have other last bits in another batch.
  *   q            BF16 [batch, q_len, q_heads, head_dim], q_stride elements from one token to the next (at least q_heads * head_dim, a
